@@ -9,7 +9,7 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libalexnet_b200.so")
 LIB_TIMELINE = os.path.join(HERE, "libalexnet_b200_timeline.so")      # the same sources with -DALEXNET_TIMELINE
 SOURCES = ["alexnet_api.cu", "loader.cpp"]
-HEADERS = ["tc_gemm.cuh", "kernels.cuh", os.path.join("..", "..", "include", "alexnet.h")]
+HEADERS = ["ptx.cuh", "tc_gemm.cuh", "kernels.cuh", os.path.join("..", "..", "include", "alexnet.h")]
 
 
 def _stale() -> bool:

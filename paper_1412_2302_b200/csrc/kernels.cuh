@@ -9,14 +9,9 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
-namespace kn {
+#include "ptx.cuh"
 
-// Programmatic dependent launch: every kernel of the step lets the next launch of its stream start its blocks early
-// (they become resident as the SMs drain) and itself waits here, before its first access to global memory, until the
-// kernels before it have completed and their writes are visible.  Without the launch attribute both are no-ops.
-__device__ __forceinline__ void pdl_trigger() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
-__device__ __forceinline__ void pdl_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
-__device__ __forceinline__ void pdl_sync() { pdl_trigger(); pdl_wait(); }
+namespace kn {
 
 // ---------------------------------------------------------------- counter hash
 // SplitMix64 finaliser over key + golden*(idx+1); key = finalise(seed ^ stream<<56 ^ replica<<48 ^ step).
@@ -341,14 +336,6 @@ __device__ __forceinline__ uint32_t prmt(uint32_t a, uint32_t b, uint32_t sel) {
 // neighbouring channels.  Measured at batch 128 (back to back), this form against one thread per pixel vector with the
 // pooling gradient scattered through shared memory: forward 40.4 -> 36.6 us (LRN1) and 27.6 -> 24.8 (LRN2), backward 79.1 ->
 // 53.5 and 48.9 -> 34; at batch 512 forward 141 -> 128 and 97 -> 83.  Same arithmetic in the same order as the single-operation kernels.
-typedef unsigned long long f2;
-__device__ __forceinline__ f2 mk2(float lo, float hi) { f2 r; asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi)); return r; }
-__device__ __forceinline__ void un2(f2 v, float& lo, float& hi) { asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(v)); }
-__device__ __forceinline__ f2 add2(f2 a, f2 b) { f2 r; asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b)); return r; }
-__device__ __forceinline__ f2 mul2(f2 a, f2 b) { f2 r; asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b)); return r; }
-__device__ __forceinline__ f2 fma2(f2 a, f2 b, f2 c) { f2 r; asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c)); return r; }
-__device__ __forceinline__ float bf_lo(uint32_t u) { return __uint_as_float(u << 16); }
-__device__ __forceinline__ float bf_hi(uint32_t u) { return __uint_as_float(u & 0xffff0000u); }
 // twelve channels c0-2 .. c0+9 of a pixel pair from six words each (two bf16 channels per word)
 __device__ __forceinline__ void unpack_pair(const uint32_t* w0, const uint32_t* w1, f2* x) {
     #pragma unroll
