@@ -431,6 +431,113 @@ int alexnet_debug_expire_wait(alexnet_t* h, long long budget_cycles);
 int alexnet_sync(alexnet_t* h);
 const char* alexnet_last_error(const alexnet_t* h);
 
+/* ---------------------------------------------------------------------------
+ * Operators on the caller's tensors (no handle; the paper has no counterpart of
+ * them).  They stand beside the step's own normalisation, activations and weight
+ * gradients for networks that are built from this library's layout: activations
+ * [n][h][w][channels] with adjacent channels, dense or inside a larger grid.
+ *
+ * Common to all: pointers are device pointers of the current device; work is
+ * queued on `stream`; nothing is allocated; every buffer, the workspace included,
+ * belongs to the caller and must stay until the stream has passed the call, so
+ * calls on different streams share nothing unless the caller gives them the same
+ * workspace.  Results repeat bit for bit.  A call may be captured into a graph.
+ * Outputs must not share memory with inputs.  n (rows) may be 0.  Errors: ARG
+ * (message in `err`, nothing launched), CUDA. */
+enum { ALEXNET_DTYPE_BF16 = 0, ALEXNET_DTYPE_F16 = 1, ALEXNET_DTYPE_F32 = 2 };
+enum { ALEXNET_ACT_NONE = 0, ALEXNET_ACT_RELU = 1, ALEXNET_ACT_SILU = 2 };
+enum { ALEXNET_CODES_INT8 = 1, ALEXNET_CODES_E4M3 = 2 };
+
+/* a tensor [n][h][w][channels]; strides in elements, channels adjacent; the
+ * stride of a dimension of size 1 is ignored; inputs may have strides of 0 */
+typedef struct alexnet_view {
+    void* data;
+    int64_t stride_n, stride_h, stride_w;
+} alexnet_view_t;
+
+/* 8-bit checkpoint of a tensor, dense: codes [n][h][w][channels], one byte each,
+ * and scales [n][h][w][ceil(channels / 32)], one exponent byte E per block of 32
+ * consecutive channels; value = code * 2^(E - 127), codes being int8 or float8
+ * e4m3.  E is the smallest exponent (at least 0) with which the block's largest
+ * magnitude is at most 127 (int8) or 448 (e4m3) in codes; codes are rounded to
+ * nearest even.  A block with an infinity or NaN has E = 255 and codes 0 and
+ * stands for NaN.  (Magnitudes within a code's half step of 2^128 round up to it,
+ * which is an infinity in fp32 and bf16; fp16 has them beyond 65504.) */
+typedef struct alexnet_checkpoint {
+    void* codes;
+    uint8_t* scales;
+    int32_t format;             /* ALEXNET_CODES_* */
+    int32_t reserved;
+} alexnet_checkpoint_t;
+
+typedef struct alexnet_checkpoint_args {
+    int64_t n;
+    int32_t h, w, channels, dtype;
+    alexnet_view_t x;           /* encode: read; decode: written, rounded to dtype */
+    alexnet_checkpoint_t checkpoint;
+} alexnet_checkpoint_args_t;
+int alexnet_checkpoint_encode(const alexnet_checkpoint_args_t* args, void* stream, char* err, size_t err_len);
+int alexnet_checkpoint_decode(const alexnet_checkpoint_args_t* args, void* stream, char* err, size_t err_len);
+
+/* Group normalisation with an activation.  Over the h * w positions and the
+ * channels / groups channels of a group of one sample: mean and (biased)
+ * variance, rstd = 1 / sqrt(var + eps); z = (x - mean) rstd weight + bias;
+ * y = act(z) with act the identity, max(z, 0) or z / (1 + e^-z).  Statistics and
+ * sums are fp32 or wider; squared deviations must stay within fp32's range. */
+typedef struct alexnet_group_norm {
+    int64_t n;
+    int32_t h, w, channels, groups;
+    int32_t dtype, activation;
+    float eps;
+    int32_t reserved;
+} alexnet_group_norm_t;
+/* bytes of workspace of one call (0: invalid shape) */
+size_t alexnet_group_norm_workspace_bytes(const alexnet_group_norm_t* shape, int backward);
+
+typedef struct alexnet_group_norm_forward_args {
+    alexnet_group_norm_t shape;
+    alexnet_view_t x, y;
+    const float *weight, *bias;         /* [channels]; NULL: 1 and 0 */
+    float *mean, *rstd;                 /* [n][groups], written */
+    alexnet_checkpoint_t keep_x;        /* codes NULL, or a checkpoint of x, written on the way */
+    alexnet_checkpoint_t keep_y;        /* codes NULL, or one of y as it is stored */
+    void* workspace;                    /* 16-byte aligned */
+    size_t workspace_bytes;
+} alexnet_group_norm_forward_t;
+int alexnet_group_norm_forward(const alexnet_group_norm_forward_t* args, void* stream, char* err, size_t err_len);
+
+/* Gradients of y = act(norm(x) weight + bias) for a given dy and the statistics
+ * that the forward pass wrote: dz = dy act'(z), dbias = sum dz, dweight = sum dz
+ * xhat, dx = rstd (dz weight - mean(dz weight) - xhat mean(dz weight xhat)), the
+ * means over a group.  x is a tensor (x.data) or a checkpoint of one (kept), whose
+ * values then stand for x throughout. */
+typedef struct alexnet_group_norm_backward_args {
+    alexnet_group_norm_t shape;         /* eps is not used, but must be positive */
+    alexnet_view_t dy, x, dx;
+    alexnet_checkpoint_t kept;
+    const float *mean, *rstd, *weight, *bias;
+    float *dweight, *dbias;             /* [channels], written; may be NULL */
+    void* workspace;
+    size_t workspace_bytes;
+} alexnet_group_norm_backward_t;
+int alexnet_group_norm_backward(const alexnet_group_norm_backward_t* args, void* stream, char* err, size_t err_len);
+
+/* Weight gradient of a linear layer (or of a 1 x 1 convolution, whose rows are the
+ * positions) whose input was kept as a checkpoint: dw[o][i] = sum over rows of
+ * dy[row][o] x[row][i], products of bf16 dy and decoded x, sums in fp32. */
+typedef struct alexnet_linear_weight_grad_args {
+    int64_t rows;
+    int32_t n_in, n_out;
+    const void* dy;                     /* bf16 [rows][n_out], rows dy_stride elements apart */
+    int64_t dy_stride;
+    alexnet_checkpoint_t x;             /* of [rows][n_in], dense */
+    float* dw;                          /* [n_out][n_in], written */
+    void* workspace;                    /* 16-byte aligned */
+    size_t workspace_bytes;
+} alexnet_linear_weight_grad_t;
+size_t alexnet_linear_weight_grad_workspace_bytes(int64_t rows, int32_t n_in, int32_t n_out);
+int alexnet_linear_weight_grad(const alexnet_linear_weight_grad_t* args, void* stream, char* err, size_t err_len);
+
 #ifdef __cplusplus
 }
 #endif

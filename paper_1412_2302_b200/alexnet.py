@@ -39,7 +39,9 @@ EXPORTS = ["alexnet_param_count", "alexnet_workspace_bytes", "alexnet_create", "
            "alexnet_loader_create", "alexnet_loader_next", "alexnet_loader_release", "alexnet_loader_destroy",
            "alexnet_forward_backward", "alexnet_apply_update", "alexnet_update_and_average", "alexnet_param_regions",
            "alexnet_scale_and_refresh", "alexnet_create_error", "alexnet_debug_expire_wait", "alexnet_set_color_augmentation", "alexnet_average_received", "alexnet_param_layout",
-           "alexnet_stream_wait_fc_gradients", "alexnet_timeline_read", "alexnet_profile_read_kinds"]
+           "alexnet_stream_wait_fc_gradients", "alexnet_timeline_read", "alexnet_profile_read_kinds",
+           "alexnet_checkpoint_encode", "alexnet_checkpoint_decode", "alexnet_group_norm_workspace_bytes", "alexnet_group_norm_forward",
+           "alexnet_group_norm_backward", "alexnet_linear_weight_grad_workspace_bytes", "alexnet_linear_weight_grad"]
 
 
 class Config(ctypes.Structure):
@@ -117,6 +119,13 @@ def load_library():
     L.alexnet_loader_release.argtypes = [vp]
     L.alexnet_loader_destroy.argtypes = [vp]
     L.alexnet_bias_grad_noalloc.argtypes = [vp, ctypes.c_int64, ctypes.c_int32, vp, vp, ctypes.c_char_p, sz]
+    # the operators take one packed argument block each (operators.py), an object of type bytes
+    for name in ("checkpoint_encode", "checkpoint_decode", "group_norm_forward", "group_norm_backward", "linear_weight_grad"):
+        getattr(L, "alexnet_" + name).argtypes = [ctypes.c_char_p, vp, ctypes.c_char_p, sz]
+    L.alexnet_group_norm_workspace_bytes.restype = sz
+    L.alexnet_group_norm_workspace_bytes.argtypes = [ctypes.c_char_p, i32]
+    L.alexnet_linear_weight_grad_workspace_bytes.restype = sz
+    L.alexnet_linear_weight_grad_workspace_bytes.argtypes = [ctypes.c_int64, ctypes.c_int32, ctypes.c_int32]
     _lib = L
     return L
 

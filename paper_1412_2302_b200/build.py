@@ -8,8 +8,8 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libalexnet_b200.so")
 LIB_TIMELINE = os.path.join(HERE, "libalexnet_b200_timeline.so")      # the same sources with -DALEXNET_TIMELINE
-SOURCES = ["alexnet_api.cu", "loader.cpp"]
-HEADERS = ["ptx.cuh", "tc_gemm.cuh", "kernels.cuh", os.path.join("..", "..", "include", "alexnet.h")]
+SOURCES = ["alexnet_api.cu", "operators.cu", "loader.cpp"]
+HEADERS = ["ptx.cuh", "tc_gemm.cuh", "kernels.cuh", "checkpoint.cuh", "group_norm.cuh", "linear_grad.cuh", os.path.join("..", "..", "include", "alexnet.h")]
 
 
 def _stale() -> bool:

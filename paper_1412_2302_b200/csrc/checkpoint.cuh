@@ -1,0 +1,364 @@
+// Activations as channels-last tensors [n][h][w][c] of three types, and their 8-bit checkpoints.
+//
+// A checkpoint holds blocks of 32 consecutive channels of one position (the last block of a row may be shorter): one byte per value
+// and one byte E per block, value = code * 2^(E - 127).  E is the smallest exponent with which the block's largest magnitude stays
+// within 127 (int8) or 448 (e4m3); the codes are rounded to nearest even.  The scale is a power of two, so dividing by it is exact, a code
+// follows from the values alone (no reciprocal whose last bit decides a tie), and a decoded value is exact in bf16 (both codes have at
+// most seven significant bits).  A block with an infinity or a NaN gets E = 255 and codes 0 and stands for NaN throughout.
+#pragma once
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+#include <type_traits>
+
+#include "ptx.cuh"
+
+namespace op {
+
+using kn::f2;
+using kn::add2; using kn::mul2; using kn::fma2; using kn::mk2; using kn::un2;
+enum { kSrcSame = 0, kSrcInt8 = 1, kSrcE4m3 = 2 };      // what a backward pass reads x from (and the two formats of codes)
+
+// ---------------------------------------------------------------- vectors of V elements
+template <int BYTES> struct RawOf;
+template <> struct RawOf<1> { using type = uint8_t; };
+template <> struct RawOf<2> { using type = uint16_t; };
+template <> struct RawOf<4> { using type = uint32_t; };
+template <> struct RawOf<8> { using type = uint2; };
+template <> struct RawOf<16> { using type = uint4; };
+struct alignas(16) Raw32 { uint4 a, b; };
+template <> struct RawOf<32> { using type = Raw32; };
+template <typename T, int V> using Raw = typename RawOf<sizeof(T) * V>::type;
+
+template <typename T> __device__ __forceinline__ float to_f(T v);
+template <> __device__ __forceinline__ float to_f(float v) { return v; }
+template <> __device__ __forceinline__ float to_f(__nv_bfloat16 v) { return __bfloat162float(v); }
+template <> __device__ __forceinline__ float to_f(__half v) { return __half2float(v); }
+template <typename T> __device__ __forceinline__ T from_f(float v);
+template <> __device__ __forceinline__ float from_f(float v) { return v; }
+template <> __device__ __forceinline__ __nv_bfloat16 from_f(float v) { return __float2bfloat16_rn(v); }
+template <> __device__ __forceinline__ __half from_f(float v) { return __float2half_rn(v); }
+
+template <typename T, int V>
+__device__ __forceinline__ void unpack(const Raw<T, V>& r, float* f) {
+    if constexpr (V > 1 && sizeof(T) == 2) {
+        const uint32_t* u = (const uint32_t*)&r;
+        #pragma unroll
+        for (int i = 0; i < V / 2; ++i) {
+            if constexpr (std::is_same<T, __nv_bfloat16>::value) { f[2 * i] = kn::bf_lo(u[i]); f[2 * i + 1] = kn::bf_hi(u[i]); }
+            else { const float2 t = __half22float2(*(const __half2*)&u[i]); f[2 * i] = t.x; f[2 * i + 1] = t.y; }
+        }
+    } else {
+        const T* e = (const T*)&r;
+        #pragma unroll
+        for (int i = 0; i < V; ++i) f[i] = to_f<T>(e[i]);
+    }
+}
+// rounds to nearest, as a cast does
+template <typename T, int V>
+__device__ __forceinline__ Raw<T, V> pack(const float* f) {
+    Raw<T, V> r;
+    if constexpr (V > 1 && sizeof(T) == 2) {
+        uint32_t* u = (uint32_t*)&r;
+        #pragma unroll
+        for (int i = 0; i < V / 2; ++i) {
+            if constexpr (std::is_same<T, __nv_bfloat16>::value) { const __nv_bfloat162 h = __floats2bfloat162_rn(f[2 * i], f[2 * i + 1]); u[i] = *(const uint32_t*)&h; }
+            else { const __half2 h = __floats2half2_rn(f[2 * i], f[2 * i + 1]); u[i] = *(const uint32_t*)&h; }
+        }
+    } else {
+        T* e = (T*)&r;
+        #pragma unroll
+        for (int i = 0; i < V; ++i) e[i] = from_f<T>(f[i]);
+    }
+    return r;
+}
+
+// ---------------------------------------------------------------- positions
+struct FastDiv {               // x / d for x < 2^31
+    uint32_t d, mul, shift;
+    __device__ __forceinline__ uint32_t div(uint32_t x) const { return (uint32_t)(((uint64_t)x * mul) >> shift); }
+};
+inline FastDiv fast_div(uint32_t d) {
+    // m = floor(2^(31 + s) / d) + 1 with 2^s >= d: x m / 2^(31 + s) is below x / d + x / 2^(31 + s) < x / d + 1 / d
+    uint32_t s = 0;
+    while ((1ull << s) < d) ++s;
+    return {d, (uint32_t)(((1ull << (31 + s)) / d) + 1), 31 + s};
+}
+// strides in elements; flat: position p of a sample lies at p * sw
+struct Geo {
+    long long sn, sh, sw;
+    FastDiv w;
+    int flat;
+    __device__ __forceinline__ long long at(uint32_t p) const {
+        if (flat) return (long long)p * sw;
+        const uint32_t h = w.div(p);
+        return (long long)h * sh + (long long)(p - h * w.d) * sw;
+    }
+};
+
+// ---------------------------------------------------------------- codes
+__device__ __forceinline__ float scale_of(uint32_t e) {         // 2^(e - 127); e = 0: a subnormal; 255: NaN
+    return e == 255u ? __uint_as_float(0x7fffffffu) : __uint_as_float(e ? e << 23 : 1u << 22);
+}
+// exponent byte of a block from the bits of its largest magnitude.  amax = m 2^k with m in [1, 2): amax / 2^(k - 6) = 64 m stays within 127 for
+// m up to 127/64, whose mantissa field is 0x7E0000: adding 0x1FFFF carries into the exponent exactly for larger ones.  e4m3: 256 m
+// within 448, 0x600000.
+template <int FMT>
+__device__ __forceinline__ uint32_t scale_byte(uint32_t amax_bits) {
+    if (amax_bits >= 0x7f800000u) return 255u;
+    const int e = FMT == kSrcInt8 ? (int)((amax_bits + 0x1ffffu) >> 23) - 6 : (int)((amax_bits + 0x1fffffu) >> 23) - 8;
+    return (uint32_t)max(e, 0);
+}
+__device__ __forceinline__ float inverse_scale(uint32_t e) { return e == 255u ? 0.f : __uint_as_float((254u - e) << 23); }      // 2^(127 - e), e <= 249
+
+// codes of V values.  int8: 1.5 * 2^23 + v has v, rounded to nearest even, in its low byte.  A block that stands for NaN has inv = 0;
+// its infinities and NaN give 0 * inf = NaN, so its codes are set to 0 by the caller's `nan`.
+template <int FMT, int V>
+__device__ __forceinline__ Raw<uint8_t, V> codes_of(const float* f, float inv, bool nan) {
+    Raw<uint8_t, V> r;
+    if constexpr (FMT == kSrcInt8) {
+        uint32_t b[V];
+        #pragma unroll
+        for (int i = 0; i < V; ++i) b[i] = __float_as_uint(fmaf(f[i], inv, 12582912.f));
+        if constexpr (V >= 4) {
+            uint32_t* u = (uint32_t*)&r;
+            #pragma unroll
+            for (int i = 0; i < V / 4; ++i) {
+                const uint32_t lo = __byte_perm(b[4 * i], b[4 * i + 1], 0x0040), hi = __byte_perm(b[4 * i + 2], b[4 * i + 3], 0x0040);
+                u[i] = nan ? 0u : __byte_perm(lo, hi, 0x5410);
+            }
+        } else {
+            uint8_t* u = (uint8_t*)&r;
+            #pragma unroll
+            for (int i = 0; i < V; ++i) u[i] = nan ? 0 : (uint8_t)b[i];
+        }
+    } else {
+        if constexpr (V >= 2) {
+            uint16_t* u = (uint16_t*)&r;
+            #pragma unroll
+            for (int i = 0; i < V / 2; ++i) {
+                uint16_t q;
+                asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(q) : "f"(f[2 * i + 1] * inv), "f"(f[2 * i] * inv));
+                u[i] = nan ? 0 : q;
+            }
+        } else {
+            uint16_t q;
+            asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(q) : "f"(0.f), "f"(f[0] * inv));
+            *(uint8_t*)&r = nan ? 0 : (uint8_t)q;
+        }
+    }
+    return r;
+}
+// the integers or e4m3 numbers that V codes are, without their scale
+template <int FMT, int V>
+__device__ __forceinline__ void code_values(const Raw<uint8_t, V>& r, float* f) {
+    if constexpr (FMT == kSrcInt8) {
+        if constexpr (V >= 4) {
+            const uint32_t* u = (const uint32_t*)&r;
+            #pragma unroll
+            for (int i = 0; i < V / 4; ++i) {
+                const uint32_t t = u[i] ^ 0x80808080u;       // code + 128 as an unsigned byte, then 2^23 + that as a float
+                #pragma unroll
+                for (int k = 0; k < 4; ++k) f[4 * i + k] = __uint_as_float(__byte_perm(t, 0x4b000000u, 0x7440u | k)) - 8388736.f;
+            }
+        } else {
+            const int8_t* u = (const int8_t*)&r;
+            #pragma unroll
+            for (int i = 0; i < V; ++i) f[i] = (float)u[i];
+        }
+    } else {
+        if constexpr (V >= 2) {
+            const uint16_t* u = (const uint16_t*)&r;
+            #pragma unroll
+            for (int i = 0; i < V / 2; ++i) {
+                uint32_t h;
+                asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h) : "h"(u[i]));
+                const float2 t = __half22float2(*(const __half2*)&h);
+                f[2 * i] = t.x; f[2 * i + 1] = t.y;
+            }
+        } else {
+            uint32_t h;
+            asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h) : "h"((uint16_t) * (const uint8_t*)&r));
+            f[0] = __half22float2(*(const __half2*)&h).x;
+        }
+    }
+}
+// the largest magnitude of eight values as the bits of a float: an unsigned comparison of magnitudes puts NaN above infinity above all others
+template <int V>
+__device__ __forceinline__ uint32_t amax_bits(const float* f) {
+    uint32_t m = 0;
+    #pragma unroll
+    for (int i = 0; i < V; ++i) m = max(m, __float_as_uint(f[i]) & 0x7fffffffu);
+    return m;
+}
+// Codes and exponents of one position's vector, called by the four lanes of a block together (the lanes of a row's last block that hold
+// no channels pass zeros and store nothing).  col: vector within the row; row: position within the tensor.
+template <int FMT>
+__device__ __forceinline__ void store_codes(const float* f, bool has, uint8_t* codes, uint8_t* scales, long long row, int col, int C, int blocks) {
+    const uint32_t quad = 0xfu << (threadIdx.x & 28);
+    uint32_t m = amax_bits<8>(f);
+    m = max(m, __shfl_xor_sync(quad, m, 1));
+    m = max(m, __shfl_xor_sync(quad, m, 2));
+    const uint32_t e = scale_byte<FMT>(m);
+    if (has) {
+        *(uint2*)(codes + row * C + 8 * col) = codes_of<FMT, 8>(f, inverse_scale(e), e == 255u);
+        if ((col & 3) == 0) scales[row * blocks + (col >> 2)] = (uint8_t)e;
+    }
+}
+__device__ __forceinline__ void store_codes(int fmt, const float* f, bool has, uint8_t* codes, uint8_t* scales, long long row, int col, int C, int blocks) {
+    if (fmt == kSrcInt8) store_codes<kSrcInt8>(f, has, codes, scales, row, col, C, blocks);
+    else store_codes<kSrcE4m3>(f, has, codes, scales, row, col, C, blocks);
+}
+
+// How a launch walks a tensor: a block takes the positions [chunk * ppc, + ppc) of a sample and `cols` vectors of V channels; thread
+// (row, col) takes every `rows`-th position of its vector.  With V = 8 the vectors of a row are counted up to a multiple of four, so that
+// the four lanes of a checkpoint block are neighbours in one warp.
+struct Walk {
+    int C, HW, vecs, cols, rows, colblocks, ppc;
+    long long chunks;           // per sample
+};
+struct Spot { int col, row, v, p0, p1; long long n, chunk; bool on, has; };
+__device__ __forceinline__ Spot spot(const Walk& w) {
+    Spot s;
+    const long long b = blockIdx.x;
+    const long long t = b / w.colblocks;
+    const int cb = (int)(b - t * w.colblocks);
+    s.n = t / w.chunks;
+    s.chunk = t - s.n * w.chunks;
+    s.row = threadIdx.x / w.cols;
+    s.col = threadIdx.x - s.row * w.cols;
+    s.v = cb * w.cols + s.col;
+    s.on = s.row < w.rows;
+    s.has = s.on && s.v < w.vecs;
+    s.p0 = (int)s.chunk * w.ppc;
+    s.p1 = min(w.HW, s.p0 + w.ppc);
+    return s;
+}
+
+// ---------------------------------------------------------------- encode, decode
+// Rows of a multiple of eight channels at 16-byte boundaries: four lanes per block.  HBM-bound: 2 bytes read and 1.03 written per bf16 value.
+template <typename T>
+__global__ void __launch_bounds__(256) checkpoint_encode_kernel(const T* __restrict__ x, const Geo g, const Walk w, int fmt, uint8_t* __restrict__ codes, uint8_t* __restrict__ scales) {
+    kn::pdl_sync();
+    const Spot s = spot(w);
+    if (!s.on) return;
+    const T* xp = x + s.n * g.sn + 8 * s.v;
+    const int blocks = (w.C + 31) / 32;
+    constexpr int U = 4;
+    for (int p = s.p0 + s.row; p < s.p1; p += U * w.rows) {
+        Raw<T, 8> r[U];
+        #pragma unroll
+        for (int u = 0; u < U; ++u)
+            if (s.has && p + u * w.rows < s.p1) r[u] = *(const Raw<T, 8>*)(xp + g.at(p + u * w.rows));
+        #pragma unroll
+        for (int u = 0; u < U; ++u)
+            if (p + u * w.rows < s.p1) {
+                float f[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+                if (s.has) unpack<T, 8>(r[u], f);
+                store_codes(fmt, f, s.has, codes, scales, s.n * w.HW + p + u * w.rows, s.v, w.C, blocks);
+            }
+    }
+}
+template <typename T>
+__global__ void __launch_bounds__(256) checkpoint_decode_kernel(const uint8_t* __restrict__ codes, const uint8_t* __restrict__ scales, int fmt, const Geo g, const Walk w, T* __restrict__ out) {
+    kn::pdl_sync();
+    const Spot s = spot(w);
+    if (!s.has) return;
+    T* op = out + s.n * g.sn + 8 * s.v;
+    const int blocks = (w.C + 31) / 32;
+    constexpr int U = 4;
+    for (int p = s.p0 + s.row; p < s.p1; p += U * w.rows) {
+        uint2 r[U];
+        uint8_t e[U];
+        #pragma unroll
+        for (int u = 0; u < U; ++u)
+            if (p + u * w.rows < s.p1) {
+                const long long row = s.n * w.HW + p + u * w.rows;
+                r[u] = *(const uint2*)(codes + row * w.C + 8 * s.v);
+                e[u] = scales[row * blocks + (s.v >> 2)];
+            }
+        #pragma unroll
+        for (int u = 0; u < U; ++u)
+            if (p + u * w.rows < s.p1) {
+                float f[8];
+                if (fmt == kSrcInt8) code_values<kSrcInt8, 8>(r[u], f);
+                else code_values<kSrcE4m3, 8>(r[u], f);
+                const float sc = scale_of(e[u]);
+                #pragma unroll
+                for (int i = 0; i < 8; ++i) f[i] *= sc;
+                *(Raw<T, 8>*)(op + g.at(p + u * w.rows)) = pack<T, 8>(f);
+            }
+    }
+}
+// Any other rows: a warp per block, a lane per value.
+template <typename T>
+__global__ void __launch_bounds__(256) checkpoint_encode_any_kernel(const T* __restrict__ x, const Geo g, const Walk w, FastDiv blocks, int fmt,
+                                                                    uint8_t* __restrict__ codes, uint8_t* __restrict__ scales) {
+    kn::pdl_sync();
+    const long long n = blockIdx.x / w.chunks, chunk = blockIdx.x - n * w.chunks;
+    const int p0 = (int)chunk * w.ppc, np = min(w.HW, p0 + w.ppc) - p0, lane = threadIdx.x & 31;
+    const T* xp = x + n * g.sn;
+    const int total = np * (int)blocks.d;
+    constexpr int U = 4;
+    for (int i = threadIdx.x >> 5; i < total; i += 8 * U) {
+        float f[U];
+        int pos[U], c[U];
+        #pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int j = i + 8 * u;
+            const int q = (int)blocks.div((uint32_t)j);
+            pos[u] = p0 + q;
+            c[u] = (j - q * (int)blocks.d) * 32 + lane;
+            f[u] = j < total && c[u] < w.C ? to_f<T>(xp[g.at(pos[u]) + c[u]]) : 0.f;
+        }
+        #pragma unroll
+        for (int u = 0; u < U; ++u) {
+            if (i + 8 * u >= total) break;
+            const uint32_t m = __reduce_max_sync(~0u, __float_as_uint(f[u]) & 0x7fffffffu);
+            const uint32_t e = fmt == kSrcInt8 ? scale_byte<kSrcInt8>(m) : scale_byte<kSrcE4m3>(m);
+            const float inv = inverse_scale(e);
+            const long long row = n * w.HW + pos[u];
+            if (c[u] < w.C)
+                codes[row * w.C + c[u]] = fmt == kSrcInt8 ? codes_of<kSrcInt8, 1>(f + u, inv, e == 255u) : codes_of<kSrcE4m3, 1>(f + u, inv, e == 255u);
+            if (lane == 0) scales[row * blocks.d + (c[u] >> 5)] = (uint8_t)e;
+        }
+    }
+}
+template <typename T>
+__global__ void __launch_bounds__(256) checkpoint_decode_any_kernel(const uint8_t* __restrict__ codes, const uint8_t* __restrict__ scales, int fmt, const Geo g, const Walk w,
+                                                                    FastDiv blocks, T* __restrict__ out) {
+    kn::pdl_sync();
+    const long long n = blockIdx.x / w.chunks, chunk = blockIdx.x - n * w.chunks;
+    const int p0 = (int)chunk * w.ppc, np = min(w.HW, p0 + w.ppc) - p0, lane = threadIdx.x & 31;
+    T* op = out + n * g.sn;
+    const int total = np * (int)blocks.d;
+    constexpr int U = 4;
+    for (int i = threadIdx.x >> 5; i < total; i += 8 * U) {
+        uint8_t q[U], e[U];
+        int pos[U], c[U];
+        #pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int j = i + 8 * u;
+            const int d = (int)blocks.div((uint32_t)j);
+            pos[u] = p0 + d;
+            c[u] = (j - d * (int)blocks.d) * 32 + lane;
+            if (j < total && c[u] < w.C) {
+                const long long row = n * w.HW + pos[u];
+                q[u] = codes[row * w.C + c[u]];
+                e[u] = scales[row * blocks.d + (c[u] >> 5)];
+            }
+        }
+        #pragma unroll
+        for (int u = 0; u < U; ++u)
+            if (i + 8 * u < total && c[u] < w.C) {
+                float f;
+                if (fmt == kSrcInt8) code_values<kSrcInt8, 1>(q[u], &f);
+                else code_values<kSrcE4m3, 1>(q[u], &f);
+                op[g.at(pos[u]) + c[u]] = from_f<T>(f * scale_of(e[u]));
+            }
+    }
+}
+
+}  // namespace op

@@ -1,0 +1,322 @@
+// Host side of the operators on caller-owned tensors declared at the end of include/alexnet.h: group normalisation with an activation, 8-bit
+// activation checkpoints, and the weight gradient of a linear layer from a checkpoint.  No handle and no device memory of their own: the
+// caller gives every buffer, the workspace included, so calls on different streams share nothing.
+#include "../../include/alexnet.h"
+
+#include <algorithm>
+#include <cstdio>
+#include <utility>
+
+#include "checkpoint.cuh"
+#include "group_norm.cuh"
+#include "linear_grad.cuh"
+
+namespace {
+using namespace op;
+using bf16 = __nv_bfloat16;
+constexpr int kSms = 148;
+
+struct Err {
+    char* buf; size_t len; const char* who;
+    int arg(const char* msg) const { if (buf && len) snprintf(buf, len, "%s: %s", who, msg); return ALEXNET_ERR_ARG; }
+    int cuda(cudaError_t e) const { cudaGetLastError(); if (buf && len) snprintf(buf, len, "%s: %s", who, cudaGetErrorString(e)); return ALEXNET_ERR_CUDA; }
+};
+
+// launches of one call, in order; the first refused launch ends it
+struct Launcher {
+    cudaStream_t st;
+    cudaError_t e = cudaSuccess;
+    template <typename... KArgs, typename... Args>
+    void operator()(void (*kernel)(KArgs...), long long grid, int block, Args&&... args) {
+        if (e != cudaSuccess) return;
+        cudaLaunchConfig_t lc{};
+        lc.gridDim = dim3((unsigned)grid); lc.blockDim = block; lc.stream = st;
+        cudaLaunchAttribute at{};
+        at.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+        at.val.programmaticStreamSerializationAllowed = 1;
+        lc.attrs = &at; lc.numAttrs = 1;
+        e = cudaLaunchKernelEx(&lc, kernel, std::forward<Args>(args)...);
+    }
+};
+
+long long ceil_div(long long a, long long b) { return (a + b - 1) / b; }
+bool is_fmt(int f) { return f == ALEXNET_CODES_INT8 || f == ALEXNET_CODES_E4M3; }
+int elem_bytes(int dtype) { return dtype == ALEXNET_DTYPE_F32 ? 4 : 2; }
+int src_of(int fmt) { return fmt == ALEXNET_CODES_INT8 ? kSrcInt8 : kSrcE4m3; }
+
+struct Dims { long long n; int h, w, C; };
+const char* check_dims(const Dims& d) {
+    if (d.n < 0) return "n must not be negative";
+    if (d.h < 1 || d.w < 1) return "h and w must be at least 1";
+    if (d.C < 1 || d.C > (1 << 20)) return "channels must be 1 to 1048576";
+    if ((long long)d.h * d.w > (1ll << 30)) return "h * w exceeds 2^30";
+    if (d.n > (1ll << 31) || (d.n > 0 && d.n * d.h * d.w > (1ll << 48) / d.C)) return "the tensor is too large";
+    return nullptr;
+}
+const char* check_view(const alexnet_view_t& v, const Dims& d, int dtype, bool output) {
+    if (d.n == 0) return nullptr;
+    if (!v.data) return "NULL pointer";
+    if ((uintptr_t)v.data % elem_bytes(dtype)) return "a tensor is not aligned to its elements";
+    long long size[3] = {d.n, d.h, d.w}, st[3] = {v.stride_n, v.stride_h, v.stride_w};
+    for (int i = 0; i < 3; ++i)
+        if (size[i] > 1 && (st[i] < 0 || st[i] > (1ll << 48))) return "a stride is negative or too large";
+    if (output) {      // positions must not share memory: by rising stride, each dimension steps over all of the ones below
+        for (int i = 0; i < 3; ++i)
+            for (int j = i + 1; j < 3; ++j)
+                if (st[j] < st[i]) { std::swap(st[i], st[j]); std::swap(size[i], size[j]); }
+        long long extent = d.C;
+        for (int i = 0; i < 3; ++i)
+            if (size[i] > 1) {
+                if (st[i] < extent) return "positions of an output overlap";
+                extent += (size[i] - 1) * st[i];
+            }
+    }
+    return nullptr;
+}
+Geo geo_of(const alexnet_view_t& v, const Dims& d) {
+    Geo g{};
+    g.sn = d.n > 1 ? v.stride_n : 0;
+    g.sh = d.h > 1 ? v.stride_h : 0;
+    g.sw = d.w > 1 ? v.stride_w : 0;
+    g.w = fast_div((uint32_t)d.w);
+    g.flat = d.h == 1 || d.w == 1 || g.sh == (long long)d.w * g.sw;
+    if (d.w == 1) g.sw = g.sh;
+    return g;
+}
+// vectors of eight channels at 16-byte boundaries everywhere
+bool vec_ok(const alexnet_view_t& v, const Dims& d, int dtype) {
+    const int step = 16 / elem_bytes(dtype);
+    return d.C % 8 == 0 && (uintptr_t)v.data % 16 == 0 && (d.n <= 1 || v.stride_n % step == 0) && (d.h <= 1 || v.stride_h % step == 0) && (d.w <= 1 || v.stride_w % step == 0);
+}
+bool vec_ok(const alexnet_checkpoint_t& k, const Dims& d) { return d.C % 8 == 0 && (uintptr_t)k.codes % 8 == 0; }
+
+// how a launch walks [n][h w][C] with vectors of V channels: about eight blocks per SM, of at least four positions per thread
+Walk walk_of(const Dims& d, int V) {
+    Walk w{};
+    w.C = d.C; w.HW = d.h * d.w; w.vecs = d.C / V;
+    const int q = V == 8 ? 4 : 1, padded = (int)ceil_div(w.vecs, q) * q;
+    w.colblocks = (int)ceil_div(padded, 256);
+    w.cols = (int)ceil_div(ceil_div(padded, w.colblocks), q) * q;
+    w.rows = 256 / w.cols;
+    long long chunks = ceil_div(8 * kSms, std::max<long long>(1, d.n * w.colblocks));
+    chunks = std::min(chunks, ceil_div(w.HW, 4 * w.rows));
+    chunks = std::max(chunks, ceil_div((long long)w.HW * ceil_div(d.C, 32), 1 << 30));      // indices of a chunk's blocks fit 31 bits
+    chunks = std::max<long long>(1, std::min<long long>(chunks, w.HW));
+    w.ppc = (int)ceil_div(w.HW, chunks);
+    w.chunks = ceil_div(w.HW, w.ppc);
+    return w;
+}
+long long grid_of(const Walk& w, const Dims& d) { return d.n * w.chunks * w.colblocks; }
+constexpr long long kMaxGrid = 0x7fffffffll;
+
+template <typename T>
+void encode(Launcher& go, const Dims& d, const alexnet_view_t& x, const alexnet_checkpoint_t& k, int dtype) {
+    const Geo g = geo_of(x, d);
+    const FastDiv blocks = fast_div((uint32_t)ceil_div(d.C, 32));
+    const bool vec = vec_ok(x, d, dtype) && vec_ok(k, d);
+    const Walk w = walk_of(d, vec ? 8 : 1);
+    if (vec) go(checkpoint_encode_kernel<T>, grid_of(w, d), 256, (const T*)x.data, g, w, src_of(k.format), (uint8_t*)k.codes, k.scales);
+    else go(checkpoint_encode_any_kernel<T>, d.n * w.chunks, 256, (const T*)x.data, g, w, blocks, src_of(k.format), (uint8_t*)k.codes, k.scales);
+}
+template <typename T>
+void decode(Launcher& go, const Dims& d, const alexnet_view_t& x, const alexnet_checkpoint_t& k, int dtype) {
+    const Geo g = geo_of(x, d);
+    const FastDiv blocks = fast_div((uint32_t)ceil_div(d.C, 32));
+    const bool vec = vec_ok(x, d, dtype) && vec_ok(k, d);
+    const Walk w = walk_of(d, vec ? 8 : 1);
+    if (vec) go(checkpoint_decode_kernel<T>, grid_of(w, d), 256, (const uint8_t*)k.codes, (const uint8_t*)k.scales, src_of(k.format), g, w, (T*)x.data);
+    else go(checkpoint_decode_any_kernel<T>, d.n * w.chunks, 256, (const uint8_t*)k.codes, (const uint8_t*)k.scales, src_of(k.format), g, w, blocks, (T*)x.data);
+}
+const char* check_codes(const alexnet_checkpoint_t& k, const Dims& d) {
+    if (!is_fmt(k.format)) return "unknown checkpoint format";
+    if (d.n > 0 && (!k.codes || !k.scales)) return "NULL pointer in a checkpoint";
+    return nullptr;
+}
+bool is_dtype(int t) { return t == ALEXNET_DTYPE_BF16 || t == ALEXNET_DTYPE_F16 || t == ALEXNET_DTYPE_F32; }
+
+int checkpoint_call(const alexnet_checkpoint_args_t* a, cudaStream_t st, const Err& err, bool enc) {
+    if (!a) return err.arg("NULL arguments");
+    const Dims d{a->n, a->h, a->w, a->channels};
+    if (const char* m = check_dims(d)) return err.arg(m);
+    if (!is_dtype(a->dtype)) return err.arg("unknown dtype");
+    if (const char* m = check_view(a->x, d, a->dtype, !enc)) return err.arg(m);
+    if (const char* m = check_codes(a->checkpoint, d)) return err.arg(m);
+    if (d.n == 0) return ALEXNET_OK;
+    if (grid_of(walk_of(d, 1), d) > kMaxGrid) return err.arg("the tensor is too large");
+    Launcher go{st};
+    switch (a->dtype) {
+    case ALEXNET_DTYPE_BF16: enc ? encode<bf16>(go, d, a->x, a->checkpoint, a->dtype) : decode<bf16>(go, d, a->x, a->checkpoint, a->dtype); break;
+    case ALEXNET_DTYPE_F16: enc ? encode<__half>(go, d, a->x, a->checkpoint, a->dtype) : decode<__half>(go, d, a->x, a->checkpoint, a->dtype); break;
+    default: enc ? encode<float>(go, d, a->x, a->checkpoint, a->dtype) : decode<float>(go, d, a->x, a->checkpoint, a->dtype); break;
+    }
+    return go.e == cudaSuccess ? ALEXNET_OK : err.cuda(go.e);
+}
+
+// ---------------------------------------------------------------- group norm
+const char* check_shape(const alexnet_group_norm_t& s) {
+    if (const char* m = check_dims({s.n, s.h, s.w, s.channels})) return m;
+    if (s.groups < 1 || s.channels % s.groups) return "groups must divide the channels";
+    if (!is_dtype(s.dtype)) return "unknown dtype";
+    if (s.activation < ALEXNET_ACT_NONE || s.activation > ALEXNET_ACT_SILU) return "unknown activation";
+    if (!(s.eps > 0.f)) return "eps must be positive";
+    if (s.n * s.groups > kMaxGrid / 2) return "the tensor is too large";
+    return nullptr;
+}
+NormShape norm_shape(const alexnet_group_norm_t& s) { return {s.channels, s.h * s.w, s.groups, s.channels / s.groups, s.eps, s.activation}; }
+size_t forward_ws(const Walk& w, const Dims& d) { return (size_t)(d.n * w.chunks) * d.C * sizeof(double2); }
+size_t backward_ws(const Walk& w, const Dims& d, int groups) { return (size_t)(d.n * groups) * sizeof(float2) + (size_t)(d.n * w.chunks) * 2 * d.C * sizeof(float); }
+
+template <typename T, int V>
+void forward(Launcher& go, const alexnet_group_norm_forward_t* a, const Dims& d) {
+    const Walk w = walk_of(d, V);
+    const NormShape s = norm_shape(a->shape);
+    const Geo gx = geo_of(a->x, d), gy = geo_of(a->y, d);
+    double2* partial = (double2*)a->workspace;
+    const T *x = (const T*)a->x.data;
+    Keep kx{}, ky{};
+    if (V == 8) {
+        if (a->keep_x.codes) kx = {(uint8_t*)a->keep_x.codes, a->keep_x.scales, src_of(a->keep_x.format)};
+        if (a->keep_y.codes) ky = {(uint8_t*)a->keep_y.codes, a->keep_y.scales, src_of(a->keep_y.format)};
+    }
+    go(gn_sums_kernel<T, V>, grid_of(w, d), 256, x, gx, w, partial);
+    go(gn_statistics_kernel, d.n * s.groups, 128, (const double2*)partial, s, w.chunks, a->mean, a->rstd);
+    go(gn_apply_kernel<T, V>, grid_of(w, d), 256, x, gx, w, s, a->weight, a->bias, (const float*)a->mean, (const float*)a->rstd, (T*)a->y.data, gy, kx, ky);
+    if (V != 8) {
+        if (a->keep_x.codes) encode<T>(go, d, a->x, a->keep_x, a->shape.dtype);
+        if (a->keep_y.codes) encode<T>(go, d, a->y, a->keep_y, a->shape.dtype);
+    }
+}
+template <typename T, int V, int SRC>
+void backward(Launcher& go, const alexnet_group_norm_backward_t* a, const Dims& d) {
+    const Walk w = walk_of(d, V);
+    const NormShape s = norm_shape(a->shape);
+    const Geo gdy = geo_of(a->dy, d), gx = geo_of(a->x, d), gdx = geo_of(a->dx, d);
+    float2* c12 = (float2*)a->workspace;
+    float* partial = (float*)(c12 + d.n * s.groups);
+    const Source src{a->x.data, (const uint8_t*)a->kept.codes, a->kept.scales};
+    const BackwardArgs A{a->mean, a->rstd, a->weight, a->bias};
+    const T* dy = (const T*)a->dy.data;
+    go(gn_backward_sums_kernel<T, V, SRC>, grid_of(w, d), 256, dy, gdy, src, gx, w, s, A, partial);
+    go(gn_backward_final_kernel, d.n * s.groups + (a->dweight || a->dbias ? ceil_div(d.C, 32) : 0), 256, (const float*)partial, s, d.n, w.chunks, A, c12, a->dweight, a->dbias);
+    go(gn_backward_apply_kernel<T, V, SRC>, grid_of(w, d), 256, dy, gdy, src, gx, w, s, A, (const float2*)c12, (T*)a->dx.data, gdx);
+}
+template <typename T, int V>
+void backward(Launcher& go, const alexnet_group_norm_backward_t* a, const Dims& d) {
+    if (a->x.data) backward<T, V, kSrcSame>(go, a, d);
+    else if (a->kept.format == ALEXNET_CODES_INT8) backward<T, V, kSrcInt8>(go, a, d);
+    else backward<T, V, kSrcE4m3>(go, a, d);
+}
+}  // namespace
+
+extern "C" {
+
+int alexnet_checkpoint_encode(const alexnet_checkpoint_args_t* args, void* stream, char* err, size_t err_len) {
+    return checkpoint_call(args, (cudaStream_t)stream, {err, err_len, "checkpoint_encode"}, true);
+}
+int alexnet_checkpoint_decode(const alexnet_checkpoint_args_t* args, void* stream, char* err, size_t err_len) {
+    return checkpoint_call(args, (cudaStream_t)stream, {err, err_len, "checkpoint_decode"}, false);
+}
+
+size_t alexnet_group_norm_workspace_bytes(const alexnet_group_norm_t* s, int backward) {
+    if (!s || check_shape(*s)) return 0;
+    const Dims d{s->n, s->h, s->w, s->channels};
+    size_t bytes = 0;
+    for (int V : {8, 1})
+        if (d.C % V == 0) {
+            const Walk w = walk_of(d, V);
+            bytes = std::max(bytes, backward ? backward_ws(w, d, s->groups) : forward_ws(w, d));
+        }
+    return (bytes + 256) / 256 * 256;
+}
+
+int alexnet_group_norm_forward(const alexnet_group_norm_forward_t* a, void* stream, char* err_buf, size_t err_len) {
+    const Err err{err_buf, err_len, "group_norm_forward"};
+    if (!a) return err.arg("NULL arguments");
+    const alexnet_group_norm_t& s = a->shape;
+    const Dims d{s.n, s.h, s.w, s.channels};
+    if (const char* m = check_shape(s)) return err.arg(m);
+    if (const char* m = check_view(a->x, d, s.dtype, false)) return err.arg(m);
+    if (const char* m = check_view(a->y, d, s.dtype, true)) return err.arg(m);
+    for (const alexnet_checkpoint_t* k : {&a->keep_x, &a->keep_y})
+        if (k->codes || k->scales)
+            if (const char* m = check_codes(*k, d)) return err.arg(m);
+    if (d.n == 0) return ALEXNET_OK;
+    if (!a->mean || !a->rstd || !a->workspace) return err.arg("NULL pointer");
+    if (a->x.data == a->y.data) return err.arg("y must not share memory with x");
+    if ((uintptr_t)a->workspace % 16 || a->workspace_bytes < alexnet_group_norm_workspace_bytes(&s, 0)) return err.arg("the workspace is too small or not 16-byte aligned");
+    if (grid_of(walk_of(d, 1), d) > kMaxGrid) return err.arg("the tensor is too large");
+    bool vec = vec_ok(a->x, d, s.dtype) && vec_ok(a->y, d, s.dtype);
+    if (a->keep_x.codes) vec = vec && vec_ok(a->keep_x, d);
+    if (a->keep_y.codes) vec = vec && vec_ok(a->keep_y, d);
+    Launcher go{(cudaStream_t)stream};
+    switch (s.dtype) {
+    case ALEXNET_DTYPE_BF16: vec ? forward<bf16, 8>(go, a, d) : forward<bf16, 1>(go, a, d); break;
+    case ALEXNET_DTYPE_F16: vec ? forward<__half, 8>(go, a, d) : forward<__half, 1>(go, a, d); break;
+    default: vec ? forward<float, 8>(go, a, d) : forward<float, 1>(go, a, d); break;
+    }
+    return go.e == cudaSuccess ? ALEXNET_OK : err.cuda(go.e);
+}
+
+int alexnet_group_norm_backward(const alexnet_group_norm_backward_t* a, void* stream, char* err_buf, size_t err_len) {
+    const Err err{err_buf, err_len, "group_norm_backward"};
+    if (!a) return err.arg("NULL arguments");
+    const alexnet_group_norm_t& s = a->shape;
+    const Dims d{s.n, s.h, s.w, s.channels};
+    if (const char* m = check_shape(s)) return err.arg(m);
+    const bool kept = a->kept.codes || a->kept.scales;
+    if (kept && a->x.data) return err.arg("x is given twice, as a tensor and as a checkpoint");
+    if (const char* m = kept ? check_codes(a->kept, d) : check_view(a->x, d, s.dtype, false)) return err.arg(m);
+    if (const char* m = check_view(a->dy, d, s.dtype, false)) return err.arg(m);
+    if (const char* m = check_view(a->dx, d, s.dtype, true)) return err.arg(m);
+    if (d.n == 0) {          // no samples: the parameters' gradients are empty sums
+        cudaError_t e = cudaSuccess;
+        for (float* p : {a->dweight, a->dbias})
+            if (p && e == cudaSuccess) e = cudaMemsetAsync(p, 0, (size_t)d.C * sizeof(float), (cudaStream_t)stream);
+        return e == cudaSuccess ? ALEXNET_OK : err.cuda(e);
+    }
+    if (!a->mean || !a->rstd || !a->workspace) return err.arg("NULL pointer");
+    if (a->dx.data == a->x.data || a->dx.data == a->dy.data) return err.arg("dx must not share memory with x or dy");
+    if ((uintptr_t)a->workspace % 16 || a->workspace_bytes < alexnet_group_norm_workspace_bytes(&s, 1)) return err.arg("the workspace is too small or not 16-byte aligned");
+    if (grid_of(walk_of(d, 1), d) > kMaxGrid) return err.arg("the tensor is too large");
+    const bool vec = vec_ok(a->dy, d, s.dtype) && vec_ok(a->dx, d, s.dtype) && (kept ? vec_ok(a->kept, d) : vec_ok(a->x, d, s.dtype));
+    Launcher go{(cudaStream_t)stream};
+    switch (s.dtype) {
+    case ALEXNET_DTYPE_BF16: vec ? backward<bf16, 8>(go, a, d) : backward<bf16, 1>(go, a, d); break;
+    case ALEXNET_DTYPE_F16: vec ? backward<__half, 8>(go, a, d) : backward<__half, 1>(go, a, d); break;
+    default: vec ? backward<float, 8>(go, a, d) : backward<float, 1>(go, a, d); break;
+    }
+    return go.e == cudaSuccess ? ALEXNET_OK : err.cuda(go.e);
+}
+
+size_t alexnet_linear_weight_grad_workspace_bytes(int64_t rows, int32_t n_in, int32_t n_out) {
+    if (rows < 0 || n_in < 1 || n_out < 1) return 0;
+    return 256;
+}
+
+int alexnet_linear_weight_grad(const alexnet_linear_weight_grad_t* a, void* stream, char* err_buf, size_t err_len) {
+    const Err err{err_buf, err_len, "linear_weight_grad"};
+    if (!a) return err.arg("NULL arguments");
+    if (a->rows < 0 || a->rows > (1ll << 30)) return err.arg("rows must be 0 to 2^30");
+    if (a->n_in < 1 || a->n_out < 1 || a->n_in > (1 << 20) || a->n_out > (1 << 20)) return err.arg("features must be 1 to 1048576");
+    if (!is_fmt(a->x.format)) return err.arg("unknown checkpoint format");
+    if (!a->dw || (uintptr_t)a->dw % 4) return err.arg("dw is NULL or not aligned");
+    if (a->rows > 0) {
+        if (!a->dy || !a->x.codes || !a->x.scales) return err.arg("NULL pointer");
+        if ((uintptr_t)a->dy % 2) return err.arg("dy is not aligned to its elements");
+        if (a->rows > 1 && (a->dy_stride < 0 || a->dy_stride > (1ll << 48))) return err.arg("the stride of dy is negative or too large");
+    }
+    if (!a->workspace || (uintptr_t)a->workspace % 16 || a->workspace_bytes < alexnet_linear_weight_grad_workspace_bytes(a->rows, a->n_in, a->n_out))
+        return err.arg("the workspace is too small or not 16-byte aligned");
+    cudaStream_t st = (cudaStream_t)stream;
+    if (a->rows == 0) {
+        const cudaError_t e = cudaMemsetAsync(a->dw, 0, (size_t)a->n_in * a->n_out * sizeof(float), st);
+        return e == cudaSuccess ? ALEXNET_OK : err.cuda(e);
+    }
+    const dim3 grid((unsigned)ceil_div(a->n_in, 64), (unsigned)ceil_div(a->n_out, 64));
+    auto* k = a->x.format == ALEXNET_CODES_INT8 ? linear_grad_simple_kernel<kSrcInt8> : linear_grad_simple_kernel<kSrcE4m3>;
+    k<<<grid, 256, 0, st>>>((const bf16*)a->dy, a->rows > 1 ? a->dy_stride : 0, (const uint8_t*)a->x.codes, a->x.scales, a->rows, a->n_in, a->n_out, a->dw);
+    const cudaError_t e = cudaGetLastError();
+    return e == cudaSuccess ? ALEXNET_OK : err.cuda(e);
+}
+
+}  // extern "C"

@@ -1,0 +1,314 @@
+"""Operators on the caller's CUDA tensors, next to those that run inside a handle: group normalisation with an activation, 8-bit
+activation checkpoints, and the weight gradient of a linear layer from such a checkpoint (include/alexnet.h, the last part).
+
+    r = group_norm(x, groups, weight, bias, activation="silu", keep_input="int8")      # r.y, r.mean, r.rstd, r.input
+    dx, dweight, dbias = group_norm_backward(dy, r.input, r.mean, r.rstd, weight, bias, activation="silu")
+    kept = checkpoint_encode(h, "e4m3")
+    dw = linear_weight_grad(dz, kept)
+
+Tensors are channels-last: [n, h, w, c], [n, l, c] or [n, c] (`checkpoint_*` and `linear_weight_grad`: any number of leading dimensions that
+form rows) with adjacent channels, dense or a view of a larger grid; bfloat16, float16 or float32.  Weights, biases, statistics and their
+gradients are float32.  Every call queues its work on `stream` (a torch.cuda.Stream; default: the current stream of the tensors' device)
+and returns without waiting.  Outputs and workspace come from torch's allocator on that stream unless `out` gives the output.  A wrong
+argument raises AlexNetError with code ERR_ARG before anything is launched.  There is no CPU fallback.
+"""
+from __future__ import annotations
+
+import ctypes
+import functools
+import struct
+import threading
+from typing import NamedTuple, Optional
+
+import torch
+
+from . import alexnet as _alexnet
+from .alexnet import ERR_ARG, OK, AlexNetError
+
+DTYPES = {torch.bfloat16: 0, torch.float16: 1, torch.float32: 2}
+ACTIVATIONS = {"none": 0, "relu": 1, "silu": 2}
+FORMATS = {"int8": 1, "e4m3": 2}
+CODE_DTYPES = {"int8": torch.int8, "e4m3": torch.float8_e4m3fn}
+_FORMAT_OF = {dtype: name for name, dtype in CODE_DTYPES.items()}
+
+# the argument blocks of include/alexnet.h (all fields naturally aligned)
+_NORM = "q4i2ifi"
+_VIEW = "P3q"
+_KEPT = "2P2i"
+_pack_shape = struct.Struct("=" + _NORM.replace("P", "Q")).pack
+_pack_checkpoint = struct.Struct(("=q4i" + _VIEW + _KEPT).replace("P", "Q")).pack
+_pack_forward = struct.Struct(("=" + _NORM + 2 * _VIEW + "4P" + 2 * _KEPT + "PQ").replace("P", "Q")).pack
+_pack_backward = struct.Struct(("=" + _NORM + 3 * _VIEW + _KEPT + "6PPQ").replace("P", "Q")).pack
+_pack_linear = struct.Struct(("=q2iPq" + _KEPT + "PPQ").replace("P", "Q")).pack
+
+_local = threading.local()
+
+
+class Checkpoint:
+    """codes (int8 or float8_e4m3fn, the shape of the tensor) and scales (uint8, one exponent byte per 32 channels, rounded up): both dense."""
+    __slots__ = ("codes", "scales")
+
+    def __init__(self, codes, scales):
+        if codes.dtype not in _FORMAT_OF or scales.dtype != torch.uint8:
+            raise AlexNetError(ERR_ARG, "a checkpoint's codes are int8 or float8_e4m3fn and its scales uint8")
+        if codes.dim() < 1 or scales.shape != (*codes.shape[:-1], (codes.shape[-1] + 31) // 32):
+            raise AlexNetError(ERR_ARG, f"scales {tuple(scales.shape)} do not fit codes {tuple(codes.shape)}: one per 32 channels, rounded up")
+        if codes.device != scales.device or not codes.is_contiguous() or not scales.is_contiguous():
+            raise AlexNetError(ERR_ARG, "a checkpoint's codes and scales are dense and on one device")
+        self.codes, self.scales = codes, scales
+
+    @property
+    def format(self):
+        return _FORMAT_OF[self.codes.dtype]
+
+    @property
+    def shape(self):
+        return self.codes.shape
+
+    @property
+    def nbytes(self):
+        return self.codes.numel() + self.scales.numel()
+
+
+class GroupNormResult(NamedTuple):
+    y: torch.Tensor
+    mean: torch.Tensor                      # [n, groups]
+    rstd: torch.Tensor
+    input: Optional[Checkpoint] = None      # of x, when keep_input was given
+    output: Optional[Checkpoint] = None     # of y, when keep_output was given
+
+
+def _refuse(message):
+    raise AlexNetError(ERR_ARG, message)
+
+
+def _name(table, key, what):
+    try:
+        return table[key]
+    except (KeyError, TypeError):
+        _refuse(f"unknown {what} {key!r}: one of {', '.join(map(str, table))}")
+
+
+class _Call:
+    """The device, the stream and the error buffer of one call."""
+    __slots__ = ("device", "stream", "_device_guard", "_stream_guard")
+
+    def __init__(self, tensor, stream):
+        self.device = tensor.device
+        if self.device.type != "cuda":
+            _refuse("the tensors must be on a CUDA device (there is no CPU fallback)")
+        self._device_guard = self._stream_guard = None
+        if stream is not None:
+            if stream.device != self.device:
+                _refuse(f"the stream belongs to {stream.device}, the tensors are on {self.device}")
+            self._stream_guard = torch.cuda.stream(stream)        # sets the device too
+            self.stream = stream.cuda_stream
+        else:
+            if torch.cuda.current_device() != self.device.index:
+                self._device_guard = torch.cuda.device(self.device)
+            self.stream = torch.cuda.current_stream(self.device).cuda_stream
+
+    def __enter__(self):
+        for guard in (self._device_guard, self._stream_guard):
+            if guard is not None:
+                guard.__enter__()
+        return self
+
+    def __exit__(self, *exc):
+        for guard in (self._stream_guard, self._device_guard):
+            if guard is not None:
+                guard.__exit__(*exc)
+
+    def run(self, function, block):
+        err = getattr(_local, "err", None)
+        if err is None:
+            err = _local.err = ctypes.create_string_buffer(256)
+        rc = function(block, self.stream, err, 256)
+        if rc != OK:
+            raise AlexNetError(rc, err.value.decode())
+
+
+def _same(call, *tensors):
+    for t in tensors:
+        if t is not None and t.device != call.device:
+            _refuse(f"tensors on {t.device} and {call.device}: all of a call are on one device")
+
+
+def _rows(t, what):
+    """(n, h, w, c) and the strides of n, h, w of a channels-last tensor of two to four dimensions."""
+    d, shape = t.dim(), t.shape
+    if d < 2 or d > 4:
+        _refuse(f"{what} has {d} dimensions: [n, h, w, c], [n, l, c] or [n, c] is wanted")
+    st = t.stride()
+    if st[-1] != 1 and shape[-1] > 1:
+        _refuse(f"the channels of {what} are not adjacent")
+    if d == 4:
+        return (shape[0], shape[1], shape[2], shape[3]), st[:3]
+    if d == 3:
+        return (shape[0], 1, shape[1], shape[2]), (st[0], 0, st[1])
+    return (shape[0], 1, 1, shape[1]), (st[0], 0, 0)
+
+
+def _rows_any(t, what):
+    """The same for a checkpoint: more leading dimensions, or none, are folded where they are dense."""
+    if t.dim() > 4:
+        if not t.is_contiguous():
+            _refuse(f"{what} has {t.dim()} dimensions and is not dense")
+        t = t.view(-1, t.shape[-1])
+    elif t.dim() == 1:
+        t = t.view(1, -1)
+    elif t.dim() == 0:
+        _refuse(f"{what} has no channels")
+    return _rows(t, what)
+
+
+def _vector(t, n, what):
+    if t is None:
+        return 0
+    if t.dtype != torch.float32 or t.shape != (n,) or not t.is_contiguous():
+        _refuse(f"{what} must be a dense float32 vector of {n}")
+    return t.data_ptr()
+
+
+def _output(out, like_shape, dtype, what, device):
+    if out is None:
+        return torch.empty(like_shape, dtype=dtype, device=device)
+    if out.dtype != dtype or out.shape != like_shape:
+        _refuse(f"{what} must be {dtype} {tuple(like_shape)}, not {out.dtype} {tuple(out.shape)}")
+    return out
+
+
+def _new_checkpoint(shape, fmt, device):
+    codes = torch.empty(shape, dtype=_name(CODE_DTYPES, fmt, "checkpoint format"), device=device)
+    return Checkpoint(codes, torch.empty((*shape[:-1], (shape[-1] + 31) // 32), dtype=torch.uint8, device=device))
+
+
+def _kept(k):
+    return (0, 0, 0, 0) if k is None else (k.codes.data_ptr(), k.scales.data_ptr(), FORMATS[_FORMAT_OF[k.codes.dtype]], 0)
+
+
+@functools.lru_cache(maxsize=1024)
+def _norm_workspace(shape, backward):
+    n = int(_alexnet.load_library().alexnet_group_norm_workspace_bytes(_pack_shape(*shape), backward))
+    if n == 0:
+        raise AlexNetError(ERR_ARG, f"invalid group norm: n, h, w, channels, groups = {shape[:5]}, eps = {shape[7]}")
+    return n
+
+
+def checkpoint_encode(x, format="int8", out=None, stream=None):
+    """The 8-bit checkpoint of x: 33 bytes for 32 values.  out: a Checkpoint to write instead of a new one."""
+    dtype = _name(DTYPES, x.dtype, "dtype")
+    lib = _alexnet.load_library()
+    with _Call(x, stream) as call:
+        (n, h, w, c), st = _rows_any(x, "x")
+        if out is None:
+            out = _new_checkpoint(x.shape, format, call.device)
+        elif out.shape != x.shape or out.codes.dtype != _name(CODE_DTYPES, format, "checkpoint format"):
+            _refuse("out is a checkpoint of another shape or format")
+        _same(call, out.codes)
+        call.run(lib.alexnet_checkpoint_encode, _pack_checkpoint(n, h, w, c, dtype, x.data_ptr(), *st, *_kept(out)))
+    return out
+
+
+def checkpoint_decode(checkpoint, dtype=torch.bfloat16, out=None, stream=None):
+    """The values that a checkpoint stands for, rounded to dtype (exact in bfloat16 and float32)."""
+    code = _name(DTYPES, dtype, "dtype")
+    lib = _alexnet.load_library()
+    with _Call(checkpoint.codes, stream) as call:
+        out = _output(out, checkpoint.shape, dtype, "out", call.device)
+        _same(call, out)
+        (n, h, w, c), st = _rows_any(out, "out")
+        call.run(lib.alexnet_checkpoint_decode, _pack_checkpoint(n, h, w, c, code, out.data_ptr(), *st, *_kept(checkpoint)))
+    return out
+
+
+def group_norm(x, groups, weight=None, bias=None, eps=1e-5, activation="none", keep_input=None, keep_output=None, out=None, stream=None):
+    """y = act((x - mean) rstd weight + bias) with the statistics of a group of channels over all positions of a sample.
+
+    x [n, h, w, c], [n, l, c] or [n, c]; activation "none", "relu" or "silu"; keep_input / keep_output: "int8" or "e4m3" writes a
+    checkpoint of x (what group_norm_backward needs) or of y (what the weight gradient of a layer behind needs) on the way."""
+    dtype, act = _name(DTYPES, x.dtype, "dtype"), _name(ACTIVATIONS, activation, "activation")
+    lib = _alexnet.load_library()
+    with _Call(x, stream) as call:
+        (n, h, w, c), xs = _rows(x, "x")
+        shape = (n, h, w, c, groups, dtype, act, eps, 0)
+        nbytes = _norm_workspace(shape, 0)
+        wp, bp = _vector(weight, c, "weight"), _vector(bias, c, "bias")
+        device = call.device
+        y = _output(out, x.shape, x.dtype, "out", device)
+        _, ys = _rows(y, "out")
+        stats = torch.empty((2, n, groups), dtype=torch.float32, device=device)
+        mean, rstd = stats.unbind(0)
+        kx = None if keep_input is None else _new_checkpoint(x.shape, keep_input, device)
+        ky = None if keep_output is None else _new_checkpoint(x.shape, keep_output, device)
+        ws = torch.empty(nbytes, dtype=torch.uint8, device=device)
+        _same(call, y, weight, bias)
+        sp = stats.data_ptr()
+        call.run(lib.alexnet_group_norm_forward,
+                 _pack_forward(*shape, x.data_ptr(), *xs, y.data_ptr(), *ys, wp, bp, sp, sp + 4 * n * groups, *_kept(kx), *_kept(ky), ws.data_ptr(), nbytes))
+    return GroupNormResult(y, mean, rstd, kx, ky)
+
+
+def group_norm_backward(dy, x, mean, rstd, weight=None, bias=None, activation="none", out=None, stream=None):
+    """(dx, dweight, dbias) of group_norm for the gradient dy of y.  x: the tensor that group_norm was given, or a Checkpoint of it; mean and
+    rstd [n, groups] as group_norm returned them.  out: the tensor that takes dx."""
+    dtype, act = _name(DTYPES, dy.dtype, "dtype"), _name(ACTIVATIONS, activation, "activation")
+    lib = _alexnet.load_library()
+    with _Call(dy, stream) as call:
+        (n, h, w, c), ds = _rows(dy, "dy")
+        if x.shape != dy.shape:
+            _refuse(f"x {tuple(x.shape)} and dy {tuple(dy.shape)} differ in shape")
+        if isinstance(x, Checkpoint):
+            kept, xv = _kept(x), (0, 0, 0, 0)
+            _same(call, x.codes)
+        else:
+            if x.dtype != dy.dtype:
+                _refuse(f"x is {x.dtype}, dy {dy.dtype}")
+            kept, xv = (0, 0, 0, 0), (x.data_ptr(), *_rows(x, "x")[1])
+            _same(call, x)
+        if mean.dim() != 2 or mean.shape[0] != n or mean.dtype != torch.float32 or rstd.shape != mean.shape or rstd.dtype != torch.float32 \
+                or not mean.is_contiguous() or not rstd.is_contiguous():
+            _refuse("mean and rstd must be dense float32 [n, groups]")
+        shape = (n, h, w, c, mean.shape[1], dtype, act, 1.0, 0)
+        nbytes = _norm_workspace(shape, 1)
+        wp, bp = _vector(weight, c, "weight"), _vector(bias, c, "bias")
+        device = call.device
+        dx = _output(out, dy.shape, dy.dtype, "out", device)
+        _, os = _rows(dx, "out")
+        grads = torch.empty((2, c), dtype=torch.float32, device=device)
+        ws = torch.empty(nbytes, dtype=torch.uint8, device=device)
+        _same(call, dx, mean, rstd, weight, bias)
+        gp = grads.data_ptr()
+        call.run(lib.alexnet_group_norm_backward,
+                 _pack_backward(*shape, dy.data_ptr(), *ds, *xv, dx.data_ptr(), *os, *kept, mean.data_ptr(), rstd.data_ptr(), wp, bp, gp, gp + 4 * c, ws.data_ptr(), nbytes))
+    dweight, dbias = grads.unbind(0)
+    return dx, dweight, dbias
+
+
+def linear_weight_grad(dy, x, out=None, stream=None):
+    """dw [out features, in features] = dy^T x, float32, for dy bfloat16 [..., out features] and a Checkpoint x of [..., in features]."""
+    if not isinstance(x, Checkpoint):
+        _refuse("x must be a Checkpoint")
+    if dy.dtype != torch.bfloat16:
+        _refuse(f"dy must be bfloat16, not {dy.dtype}")
+    if dy.dim() < 1 or dy.shape[:-1] != x.shape[:-1]:
+        _refuse(f"dy {tuple(dy.shape)} and x {tuple(x.shape)} differ in their rows")
+    lib = _alexnet.load_library()
+    with _Call(dy, stream) as call:
+        n_in, n_out = x.shape[-1], dy.shape[-1]
+        if dy.dim() != 2:
+            if not dy.is_contiguous():
+                _refuse("dy of other than two dimensions must be dense")
+            dy = dy.view(-1, n_out)
+        if dy.stride(1) != 1 and n_out > 1:
+            _refuse("the features of dy are not adjacent")
+        rows = dy.shape[0]
+        dw = _output(out, (n_out, n_in), torch.float32, "out", call.device)
+        if not dw.is_contiguous():
+            _refuse("out must be dense")
+        _same(call, x.codes, dw)
+        nbytes = int(lib.alexnet_linear_weight_grad_workspace_bytes(rows, n_in, n_out))
+        ws = torch.empty(max(nbytes, 16), dtype=torch.uint8, device=call.device)
+        call.run(lib.alexnet_linear_weight_grad,
+                 _pack_linear(rows, n_in, n_out, dy.data_ptr(), dy.stride(0), *_kept(x), dw.data_ptr(), ws.data_ptr(), nbytes))
+    return dw

@@ -1,0 +1,169 @@
+"""Refusals of the operators on caller-owned tensors, without a GPU: the binding's own checks and the library's, which come before any
+CUDA call.  And the argument blocks that the binding packs."""
+import ctypes
+import os
+import re
+import subprocess
+
+import pytest
+import torch
+
+from paper_1412_2302_b200 import alexnet as A
+from paper_1412_2302_b200 import build as B
+from paper_1412_2302_b200 import operators as ops
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+
+
+@pytest.fixture(scope="module")
+def lib():
+    B.build()
+    return A.load_library()
+
+
+def call(lib, name, block):
+    msg = ctypes.create_string_buffer(256)
+    return getattr(lib, "alexnet_" + name)(block, None, msg, 256), msg.value.decode()
+
+
+P = 1 << 20           # stands for a pointer: nothing is launched, nothing follows it
+VIEW = lambda h, w, c, p=P: (p, h * w * c, w * c, c)      # noqa: E731
+KEPT = (P, P, 1, 0)
+NONE = (0, 0, 0, 0)
+
+
+def test_argument_blocks_have_the_headers_sizes(tmp_path):
+    src = tmp_path / "sizes.c"
+    src.write_text('#include "%s"\n#include <stdio.h>\nint main(void) { printf("%%zu %%zu %%zu %%zu %%zu\\n", sizeof(alexnet_group_norm_t), '
+                   'sizeof(alexnet_checkpoint_args_t), sizeof(alexnet_group_norm_forward_t), sizeof(alexnet_group_norm_backward_t), '
+                   'sizeof(alexnet_linear_weight_grad_t)); return 0; }\n' % os.path.join(ROOT, "include", "alexnet.h"))
+    exe = str(tmp_path / "sizes")
+    subprocess.check_call(["gcc", "-o", exe, str(src)])
+    sizes = [int(v) for v in subprocess.check_output([exe], text=True).split()]
+    assert sizes == [p.__self__.size for p in (ops._pack_shape, ops._pack_checkpoint, ops._pack_forward, ops._pack_backward, ops._pack_linear)]
+
+
+def test_enums_match_the_header():
+    src = open(os.path.join(ROOT, "include", "alexnet.h")).read()
+    value = lambda name: int(re.search(r"\bALEXNET_%s = (\d+)" % name, src).group(1))      # noqa: E731
+    assert [value("DTYPE_" + n) for n in ("BF16", "F16", "F32")] == [ops.DTYPES[t] for t in (torch.bfloat16, torch.float16, torch.float32)]
+    assert {n: value("ACT_" + n.upper()) for n in ops.ACTIVATIONS} == ops.ACTIVATIONS
+    assert {n: value("CODES_" + n.upper()) for n in ops.FORMATS} == ops.FORMATS
+
+
+def shape(n=2, h=3, w=4, c=64, groups=8, dtype=0, act=0, eps=1e-5):
+    return (n, h, w, c, groups, dtype, act, eps, 0)
+
+
+BAD_SHAPES = [(dict(n=-1), "n must"), (dict(h=0), "at least 1"), (dict(w=0), "at least 1"), (dict(c=0, groups=1), "channels"), (dict(c=(1 << 20) + 8), "channels"),
+              (dict(groups=0), "groups"), (dict(groups=7), "groups"), (dict(groups=-8), "groups"), (dict(dtype=3), "dtype"), (dict(dtype=-1), "dtype"),
+              (dict(act=3), "activation"), (dict(act=-1), "activation"), (dict(eps=0.0), "eps"), (dict(eps=-1.0), "eps"), (dict(eps=float("nan")), "eps"),
+              (dict(h=1 << 16, w=1 << 16), "2^30"), (dict(n=1 << 40), "too large"), (dict(n=1 << 31, c=1 << 20, groups=1), "too large")]
+
+
+@pytest.mark.parametrize("bad,word", BAD_SHAPES)
+def test_group_norm_refuses_shapes(lib, bad, word):
+    s = shape(**bad)
+    for backward in (0, 1):
+        assert lib.alexnet_group_norm_workspace_bytes(ops._pack_shape(*s), backward) == 0
+    v = VIEW(3, 4, 64)
+    rc, msg = call(lib, "group_norm_forward", ops._pack_forward(*s, *v, *v[:1], *v[1:], P, P, P, P, *NONE, *NONE, P, 1 << 40))
+    assert rc == A.ERR_ARG and word in msg, msg
+    rc, msg = call(lib, "group_norm_backward", ops._pack_backward(*s, *v, *v, *v, *NONE, P, P, P, P, P, P, P, 1 << 40))
+    assert rc == A.ERR_ARG and word in msg, msg
+
+
+def forward_block(s=shape(), x=VIEW(3, 4, 64), y=VIEW(3, 4, 64, 2 * P), mean=P, rstd=P, kx=NONE, ky=NONE, ws=P, nbytes=1 << 40):
+    return ops._pack_forward(*s, *x, *y, P, P, mean, rstd, *kx, *ky, ws, nbytes)
+
+
+FORWARD = [(dict(x=VIEW(3, 4, 64, 0)), "NULL"), (dict(y=VIEW(3, 4, 64, 0)), "NULL"), (dict(mean=0), "NULL"), (dict(rstd=0), "NULL"), (dict(ws=0), "NULL"),
+           (dict(x=VIEW(3, 4, 64, P + 1)), "aligned"), (dict(s=shape(dtype=2), x=VIEW(3, 4, 64, P + 2)), "aligned"), (dict(ws=P + 8), "workspace"), (dict(nbytes=16), "workspace"),
+           (dict(y=VIEW(3, 4, 64)), "share"), (dict(x=(P, -768, 256, 64)), "stride"), (dict(x=(P, 768, 1 << 50, 64)), "stride"),
+           (dict(y=(2 * P, 768, 256, 63)), "overlap"), (dict(y=(2 * P, 768, 255, 64)), "overlap"), (dict(y=(2 * P, 0, 256, 64)), "overlap"),
+           (dict(y=(2 * P, 64, 256, 64)), "overlap"),
+           (dict(kx=(P, P, 0, 0)), "format"), (dict(ky=(P, P, 3, 0)), "format"), (dict(kx=(P, 0, 1, 0)), "NULL"), (dict(ky=(0, P, 2, 0)), "NULL")]
+
+
+@pytest.mark.parametrize("bad,word", FORWARD)
+def test_group_norm_forward_refuses(lib, bad, word):
+    rc, msg = call(lib, "group_norm_forward", forward_block(**bad))
+    assert rc == A.ERR_ARG and word in msg, msg
+
+
+def backward_block(s=shape(), dy=VIEW(3, 4, 64), x=VIEW(3, 4, 64, 2 * P), dx=VIEW(3, 4, 64, 3 * P), kept=NONE, mean=P, rstd=P, ws=P, nbytes=1 << 40):
+    return ops._pack_backward(*s, *dy, *x, *dx, *kept, mean, rstd, P, P, P, P, ws, nbytes)
+
+
+BACKWARD = [(dict(dy=VIEW(3, 4, 64, 0)), "NULL"), (dict(x=VIEW(3, 4, 64, 0)), "NULL"), (dict(dx=VIEW(3, 4, 64, 0)), "NULL"), (dict(mean=0), "NULL"), (dict(rstd=0), "NULL"),
+            (dict(kept=KEPT), "twice"), (dict(x=NONE, kept=(P, P, 9, 0)), "format"), (dict(x=NONE, kept=(P, 0, 1, 0)), "NULL"), (dict(dx=VIEW(3, 4, 64)), "share"),
+            (dict(dx=VIEW(3, 4, 64, 2 * P)), "share"), (dict(dx=(3 * P, 768, 0, 64)), "overlap"), (dict(ws=P + 4), "workspace"), (dict(nbytes=0), "workspace"), (dict(ws=0), "NULL")]
+
+
+@pytest.mark.parametrize("bad,word", BACKWARD)
+def test_group_norm_backward_refuses(lib, bad, word):
+    rc, msg = call(lib, "group_norm_backward", backward_block(**bad))
+    assert rc == A.ERR_ARG and word in msg, msg
+
+
+CHECKPOINT = [(dict(h=0), "at least 1"), (dict(c=0), "channels"), (dict(dtype=7), "dtype"), (dict(x=(0, 1, 1, 1)), "NULL"), (dict(kept=(0, P, 1, 0)), "NULL"), (dict(kept=(P, P, 4, 0)), "format"),
+              (dict(x=(P + 1, 768, 256, 64)), "aligned"), (dict(x=(P, 768, 256, -64)), "stride")]
+
+
+@pytest.mark.parametrize("bad,word", CHECKPOINT)
+def test_checkpoint_refuses(lib, bad, word):
+    a = dict(dict(n=2, h=3, w=4, c=64, dtype=0, x=VIEW(3, 4, 64), kept=KEPT), **bad)
+    block = ops._pack_checkpoint(a["n"], a["h"], a["w"], a["c"], a["dtype"], *a["x"], *a["kept"])
+    for name in ("checkpoint_encode", "checkpoint_decode"):
+        rc, msg = call(lib, name, block)
+        assert rc == A.ERR_ARG and word in msg and msg.startswith(name), msg
+    rc, msg = call(lib, "checkpoint_decode", ops._pack_checkpoint(2, 3, 4, 64, 0, P, 768, 0, 64, *KEPT))
+    assert rc == A.ERR_ARG and "overlap" in msg
+
+
+LINEAR = [(dict(rows=-1), "rows"), (dict(rows=1 << 31), "rows"), (dict(n_in=0), "features"), (dict(n_out=0), "features"), (dict(n_in=1 << 21), "features"), (dict(dy=0), "NULL"),
+          (dict(dy=P + 1), "aligned"), (dict(stride=-8), "stride"), (dict(kept=(P, 0, 1, 0)), "NULL"), (dict(kept=(0, P, 1, 0)), "NULL"), (dict(kept=(P, P, 0, 0)), "format"), (dict(dw=0), "dw"),
+          (dict(dw=P + 2), "dw"), (dict(ws=0), "workspace"), (dict(ws=P + 8), "workspace"), (dict(nbytes=0), "workspace")]
+
+
+@pytest.mark.parametrize("bad,word", LINEAR)
+def test_linear_weight_grad_refuses(lib, bad, word):
+    a = dict(dict(rows=64, n_in=64, n_out=64, dy=P, stride=64, kept=KEPT, dw=P, ws=P, nbytes=1 << 40), **bad)
+    rc, msg = call(lib, "linear_weight_grad", ops._pack_linear(a["rows"], a["n_in"], a["n_out"], a["dy"], a["stride"], *a["kept"], a["dw"], a["ws"], a["nbytes"]))
+    assert rc == A.ERR_ARG and word in msg, msg
+    assert lib.alexnet_linear_weight_grad_workspace_bytes(-1, 64, 64) == 0 and lib.alexnet_linear_weight_grad_workspace_bytes(4, 0, 64) == 0
+
+
+def test_null_blocks_and_no_samples(lib):
+    for name in ("checkpoint_encode", "checkpoint_decode", "group_norm_forward", "group_norm_backward", "linear_weight_grad"):
+        rc, msg = call(lib, name, None)
+        assert rc == A.ERR_ARG and "NULL" in msg
+    # no samples: nothing to read or write, so no pointer is needed and nothing is launched
+    s = shape(n=0)
+    assert lib.alexnet_group_norm_workspace_bytes(ops._pack_shape(*s), 0) > 0
+    assert call(lib, "group_norm_forward", ops._pack_forward(*s, *NONE, *NONE, 0, 0, 0, 0, *NONE, *NONE, 0, 0))[0] == A.OK
+    assert call(lib, "checkpoint_encode", ops._pack_checkpoint(0, 3, 4, 64, 0, *NONE, 0, 0, 1, 0))[0] == A.OK
+
+
+def test_binding_refuses(lib):
+    def refused(word, f, *args, **kw):
+        with pytest.raises(A.AlexNetError, match=word) as e:
+            f(*args, **kw)
+        assert e.value.code == A.ERR_ARG
+    x = torch.zeros(2, 3, 4, 64, dtype=torch.bfloat16)
+    codes, scales = torch.zeros(2, 64, dtype=torch.int8), torch.zeros(2, 2, dtype=torch.uint8)
+    refused("no CPU fallback", ops.group_norm, x, 8)
+    refused("no CPU fallback", ops.checkpoint_encode, x)
+    refused("no CPU fallback", ops.checkpoint_decode, ops.Checkpoint(codes, scales))
+    refused("no CPU fallback", ops.group_norm_backward, x, x, torch.zeros(2, 8), torch.zeros(2, 8))
+    refused("no CPU fallback", ops.linear_weight_grad, torch.zeros(2, 8, dtype=torch.bfloat16), ops.Checkpoint(codes, scales))
+    refused("dtype", ops.group_norm, x.double(), 8)
+    refused("activation", ops.group_norm, x, 8, activation="gelu")
+    refused("dtype", ops.checkpoint_decode, ops.Checkpoint(codes, scales), torch.int8)
+    refused("int8", ops.Checkpoint, codes.float(), scales)
+    refused("uint8", ops.Checkpoint, codes, scales.int())
+    refused("rounded up", ops.Checkpoint, codes, scales[:, :1])
+    refused("dense", ops.Checkpoint, torch.zeros(64, 2, dtype=torch.int8).t(), scales)
+    refused("Checkpoint", ops.linear_weight_grad, torch.zeros(2, 8, dtype=torch.bfloat16), codes)
+    refused("bfloat16", ops.linear_weight_grad, torch.zeros(2, 8), ops.Checkpoint(codes, scales))
+    refused("rows", ops.linear_weight_grad, torch.zeros(3, 8, dtype=torch.bfloat16), ops.Checkpoint(codes, scales))
