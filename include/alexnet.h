@@ -535,8 +535,15 @@ typedef struct alexnet_linear_weight_grad_args {
     void* workspace;                    /* 16-byte aligned */
     size_t workspace_bytes;
 } alexnet_linear_weight_grad_t;
-size_t alexnet_linear_weight_grad_workspace_bytes(int64_t rows, int32_t n_in, int32_t n_out);
+/* bytes of workspace of a call with these arguments (the workspace and dw need not be set; 0: invalid).  It is small where rows of dy and
+ * x start on 16-byte boundaries and there are many outputs; else it takes a copy of them, or partial sums. */
+size_t alexnet_linear_weight_grad_workspace_bytes(const alexnet_linear_weight_grad_t* args);
 int alexnet_linear_weight_grad(const alexnet_linear_weight_grad_t* args, void* stream, char* err, size_t err_len);
+
+/* Waits inside these operators' kernels are bounded like all others: if one ran
+ * out, the outputs it stood for are NaN and this call, which synchronises with the
+ * current device's default stream, returns DEVICE_TIMEOUT from then on; else OK. */
+int alexnet_operators_check(void);
 
 #ifdef __cplusplus
 }

@@ -1,46 +1,272 @@
 // Weight gradient of a linear layer whose input was kept as an 8-bit checkpoint: dw[o][i] = sum_r dy[r][o] x[r][i].
+//
+// A GEMM whose reduction runs over the rows of both operands, so both reach the tensor cores MN-major, 64 rows at a time.  dy comes by
+// TMA; the codes of x are read to registers, decoded there (exact in bf16: seven significant bits times a power of two) and written to
+// the same swizzled tile that TMA would write, so x is never in memory as bf16: its traffic is a byte per value.
+//
+// The tile is 128 input features (rows of the accumulator) by BN output features: the decoded side is the narrow one, as each CTA decodes
+// its own tile of x again for every BN outputs.  An accumulator column then is 32 consecutive inputs of one output for each warp, which
+// leaves as one full 128-byte line.
+//
+// Warps: 0 = TMA producer (dy), 1 = MMA issuer and TMEM owner, 2..5 = epilogue, 6..13 = decoders.  Persistent over tiles with two
+// accumulators, so a tile's stores overlap the next one's products.  Few tiles with many rows are split over the rows; the
+// partial sums are added in a fixed order by a second kernel.  Every wait is bounded; a CTA whose wait runs out writes NaN and raises g_expired.
 #pragma once
 #include "checkpoint.cuh"
 
 namespace op {
 
-// 64 x 64 outputs per block, 16 rows at a time
+constexpr int kLgRows = 64, kLgThreads = 32 * 14, kLgDecoders = 8;
+constexpr int kLgA = 128 * kLgRows * 2;            // bytes of the decoded tile of a stage: two boxes of 64 features x 64 rows
+constexpr int kLgMaxStages = 6;
+struct LinearGradParams {
+    CUtensorMap tmD;                               // dy [rows][n_out], boxes of 64 features x 64 rows
+    const uint8_t *codes, *scales;
+    long long code_pitch;                          // bytes; a multiple of 16
+    int blocks;                                    // scales per row
+    int rows, n_in, n_out;
+    int BN, m_tiles, n_tiles, splits, steps, per;  // steps of 64 rows: in all, and of one split
+    int stages;
+    float* out;                                    // dw, or partial sums [split][n_out][n_in]
+};
+__device__ int g_expired;
+
+struct LinearGradTile {                            // tiles: input tile fastest, then output tile, then split
+    int m, n, z, k0, k1;
+    __device__ __forceinline__ void set(const LinearGradParams& p, int tile) {
+        m = tile % p.m_tiles;
+        const int r = tile / p.m_tiles;
+        n = r % p.n_tiles;
+        z = r / p.n_tiles;
+        k0 = z * p.per;
+        k1 = min(p.steps, k0 + p.per);
+    }
+};
+// a decoder's share of a stage: 16 codes of each of two rows
+struct LinearGradCodes { uint4 c[2]; uint8_t e[2]; };
+
 template <int FMT>
-__global__ void __launch_bounds__(256) linear_grad_simple_kernel(const __nv_bfloat16* __restrict__ dy, long long ld_dy, const uint8_t* __restrict__ codes, const uint8_t* __restrict__ scales,
-                                                                 long long rows, int n_in, int n_out, float* __restrict__ dw) {
-    kn::pdl_sync();
-    __shared__ float sd[16][64], sx[16][64];
-    const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
-    const int i0 = blockIdx.x * 64, o0 = blockIdx.y * 64, blocks = (n_in + 31) / 32;
-    float acc[4][4] = {};
-    for (long long r0 = 0; r0 < rows; r0 += 16) {
-        for (int t = threadIdx.x; t < 16 * 64; t += 256) {
-            const int k = t >> 6, c = t & 63;
-            const long long r = r0 + k;
-            sd[k][c] = r < rows && o0 + c < n_out ? __bfloat162float(dy[r * ld_dy + o0 + c]) : 0.f;
-            float f = 0.f;
-            if (r < rows && i0 + c < n_in) {
-                code_values<FMT, 1>(codes[r * n_in + i0 + c], &f);
-                f *= scale_of(scales[r * blocks + (i0 + c) / 32]);
+__global__ void __launch_bounds__(kLgThreads, 1) linear_grad_kernel(const __grid_constant__ LinearGradParams p) {
+    kn::pdl_trigger();
+    extern __shared__ uint8_t smem_raw[];
+    const uint32_t raw = tc::smem_u32(smem_raw), base = (raw + 1023u) & ~1023u;
+    const int nb = (p.BN + 63) >> 6, stages = p.stages;
+    const uint32_t stage_bytes = kLgA + (uint32_t)nb * 8192u;
+    // barriers behind the stages: full[8] @0, empty[8] @64, acc_full[2] @128, acc_empty[2] @144, tmem slot @160, abort flag @168
+    const uint32_t bar = base + stages * stage_bytes;
+    uint8_t* gen = smem_raw + (bar - raw);
+    volatile int* abort_flag = (volatile int*)(gen + 168);
+    volatile uint32_t* tmem_slot = (volatile uint32_t*)(gen + 160);
+    const uint32_t full0 = bar, empty0 = bar + 64u, accf0 = bar + 128u, acce0 = bar + 144u;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int tiles = p.m_tiles * p.n_tiles * p.splits;
+    uint32_t ncols = 32;
+    while ((int)ncols < 2 * p.BN) ncols <<= 1;
+
+    if (threadIdx.x == 0) {
+        *abort_flag = 0;
+        for (int s = 0; s < stages; ++s) { tc::mbar_init(full0 + 8u * s, 1 + kLgDecoders); tc::mbar_init(empty0 + 8u * s, 1); }
+        for (int s = 0; s < 2; ++s) { tc::mbar_init(accf0 + 8u * s, 1); tc::mbar_init(acce0 + 8u * s, 4); }
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        tc::tma_prefetch_desc(&p.tmD);
+    }
+    if (warp == 1) tc::tmem_alloc(tc::smem_u32((const void*)tmem_slot), ncols);
+    tc::tc_fence_before();
+    __syncthreads();
+    tc::tc_fence_after();
+    const uint32_t tmem = *tmem_slot;
+    kn::pdl_wait();
+
+    if (warp == 0) {
+        if (lane == 0) {
+            int st = 0; uint32_t ph = 0;
+            bool ok = true;
+            LinearGradTile t;
+            for (int tile = blockIdx.x; tile < tiles && ok; tile += gridDim.x) {
+                t.set(p, tile);
+                for (int k = t.k0; k < t.k1; ++k) {
+                    if (!(ok = tc::mbar_wait(empty0 + 8u * st, ph ^ 1u, abort_flag))) break;
+                    const uint32_t sb = base + st * stage_bytes + kLgA, fb = full0 + 8u * st;
+                    tc::mbar_expect_tx(fb, (uint32_t)nb * 8192u);
+                    for (int j = 0; j < nb; ++j) tc::tma_load_2d(sb + j * 8192, &p.tmD, t.n * p.BN + 64 * j, k * kLgRows, fb);
+                    if (++st == stages) { st = 0; ph ^= 1u; }
+                }
             }
-            sx[k][c] = f;
         }
-        __syncthreads();
-        #pragma unroll
-        for (int k = 0; k < 16; ++k)
-            #pragma unroll
-            for (int a = 0; a < 4; ++a)
+    } else if (warp == 1) {
+        const uint32_t idesc = tc::instr_desc(p.BN, 1, 1);
+        int st = 0; uint32_t ph = 0;
+        int ab = 0; uint32_t aph = 0;
+        bool ok = true;
+        LinearGradTile t;
+        for (int tile = blockIdx.x; tile < tiles && ok; tile += gridDim.x) {
+            t.set(p, tile);
+            if (!(ok = tc::mbar_wait_warp(acce0 + 8u * ab, aph ^ 1u, abort_flag))) break;
+            tc::tc_fence_after();
+            const uint32_t d = tmem + (uint32_t)(ab * p.BN);
+            for (int k = t.k0; k < t.k1; ++k) {
+                if (!(ok = tc::mbar_wait_warp(full0 + 8u * st, ph, abort_flag))) break;
+                tc::tc_fence_after();
+                const uint32_t sa = base + st * stage_bytes, sb = sa + kLgA;
                 #pragma unroll
-                for (int b = 0; b < 4; ++b) acc[a][b] = fmaf(sd[k][ty + 16 * a], sx[k][tx + 16 * b], acc[a][b]);
+                for (int j = 0; j < 4; ++j)
+                    tc::umma(d, tc::smem_desc(sa + j * 2048, 8192, 1024), tc::smem_desc(sb + j * 2048, 8192, 1024), idesc, (k > t.k0 || j > 0) ? 1u : 0u);
+                tc::umma_commit(empty0 + 8u * st);
+                if (++st == stages) { st = 0; ph ^= 1u; }
+            }
+            if (!ok) break;
+            tc::umma_commit(accf0 + 8u * ab);
+            if (++ab == 2) { ab = 0; aph ^= 1u; }
+        }
+    } else if (warp < 6) {
+        const int quad = warp & 3;
+        int ab = 0; uint32_t aph = 0;
+        bool ok = true;
+        LinearGradTile t;
+        for (int tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
+            t.set(p, tile);
+            ok = ok && tc::mbar_wait_idle(accf0 + 8u * ab, aph, abort_flag);
+            tc::tc_fence_after();
+            const int i = t.m * 128 + quad * 32 + lane, o0 = t.n * p.BN, nv = min(p.BN, p.n_out - o0);
+            float* out = p.out + (long long)t.z * p.n_out * p.n_in + (long long)o0 * p.n_in + i;
+            const uint32_t ta = tmem + (uint32_t)(ab * p.BN) + ((uint32_t)(quad * 32) << 16);
+            for (int c = 0; c < nv; c += 32) {
+                uint32_t v[32];
+                if (ok) { tc::tmem_ld32(ta + (uint32_t)c, v); tc::tmem_ld_wait(); }
+                else {
+                    #pragma unroll
+                    for (int q = 0; q < 32; ++q) v[q] = 0x7fffffffu;
+                }
+                if (i < p.n_in) {
+                    #pragma unroll
+                    for (int q = 0; q < 32; ++q)
+                        if (c + q < nv) out[(long long)(c + q) * p.n_in] = __uint_as_float(v[q]);
+                }
+            }
+            tc::tc_fence_before();
+            __syncwarp();
+            if (lane == 0) tc::mbar_arrive(acce0 + 8u * ab);
+            if (++ab == 2) { ab = 0; aph ^= 1u; }
+        }
+    } else {
+        // thread: codes 16 cg .. 16 cg + 15 of the rows kr and kr + 32 of a stage.  With the 128-byte swizzle, 16-byte chunk j of row k
+        // lies at j ^ (k & 7): of eight neighbouring lanes the four of the second box take the neighbouring row, so that the eight write to
+        // eight different bank groups.
+        const int td = threadIdx.x - 192, cg = td & 7, kr = (td >> 3) ^ (cg >> 2);
+        constexpr int PF = 3;                  // stages whose codes are in flight
+        LinearGradCodes f[PF];
+        int total = 0;
+        LinearGradTile t;
+        for (int tile = blockIdx.x; tile < tiles; tile += gridDim.x) { t.set(p, tile); total += t.k1 - t.k0; }
+        int ltile = blockIdx.x, lk, loaded = 0;
+        t.set(p, ltile);
+        lk = t.k0;
+        auto load = [&](LinearGradCodes& r) {
+            const int col = t.m * 128 + cg * 16;
+            #pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const long long row = (long long)lk * kLgRows + kr + 32 * h;
+                r.c[h] = make_uint4(0u, 0u, 0u, 0u);
+                r.e[h] = 0;
+                if (row < p.rows && col < p.n_in) {
+                    r.c[h] = __ldg((const uint4*)(p.codes + row * p.code_pitch + col));
+                    r.e[h] = __ldg(p.scales + row * p.blocks + (col >> 5));
+                }
+            }
+            ++loaded;
+            if (++lk == t.k1) {
+                ltile += gridDim.x;
+                if (ltile < tiles) { t.set(p, ltile); lk = t.k0; }
+            }
+        };
+        #pragma unroll
+        for (int u = 0; u < PF; ++u)
+            if (loaded < total) load(f[u]);
+        int st = 0; uint32_t ph = 0;
+        bool ok = true;
+        for (int s = 0; s < total && ok; s += PF) {
+            #pragma unroll
+            for (int u = 0; u < PF; ++u) {
+                if (s + u >= total || !ok) break;
+                if (!(ok = tc::mbar_wait_warp(empty0 + 8u * st, ph ^ 1u, abort_flag))) break;
+                const uint32_t sa = base + st * stage_bytes + (uint32_t)(cg >> 2) * 8192u;
+                #pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    float v[16];
+                    code_values<FMT, 16>(f[u].c[h], v);
+                    const float sc = scale_of(f[u].e[h]);
+                    const f2 s2 = mk2(sc, sc);
+                    uint32_t w[8];
+                    #pragma unroll
+                    for (int q = 0; q < 8; ++q) {
+                        float lo, hi;
+                        un2(mul2(mk2(v[2 * q], v[2 * q + 1]), s2), lo, hi);
+                        asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(w[q]) : "f"(hi), "f"(lo));
+                    }
+                    const int k = kr + 32 * h, j = 2 * (cg & 3);
+                    const uint32_t row = sa + (uint32_t)k * 128u;
+                    tc::st_shared_v4(row + (uint32_t)((j ^ (k & 7)) << 4), w[0], w[1], w[2], w[3]);
+                    tc::st_shared_v4(row + (uint32_t)(((j + 1) ^ (k & 7)) << 4), w[4], w[5], w[6], w[7]);
+                }
+                tc::fence_async_smem();
+                __syncwarp();
+                if (lane == 0) tc::mbar_arrive(full0 + 8u * st);
+                if (++st == stages) { st = 0; ph ^= 1u; }
+                if (loaded < total) load(f[u]);
+            }
+        }
+    }
+    tc::tc_fence_before();
+    __syncthreads();
+    if (*abort_flag) {                              // copies in flight land before the shared memory is given back
+        if (threadIdx.x == 0) atomicExch(&g_expired, 1);
+        const long long t0 = clock64();
+        while (clock64() - t0 < 2000000LL) { }
         __syncthreads();
     }
-    #pragma unroll
-    for (int a = 0; a < 4; ++a)
-        #pragma unroll
-        for (int b = 0; b < 4; ++b) {
-            const int o = o0 + ty + 16 * a, i = i0 + tx + 16 * b;
-            if (o < n_out && i < n_in) dw[(long long)o * n_in + i] = acc[a][b];
+    if (warp == 1) {
+        tc::tc_fence_after();
+        tc::tmem_dealloc(tmem, ncols);
+    }
+}
+
+// out[i] = sum over splits of partial[split][i], in that order
+__global__ void __launch_bounds__(256) linear_grad_join_kernel(const float* __restrict__ partial, int splits, long long n, float* __restrict__ out) {
+    kn::pdl_sync();
+    const long long i = ((long long)blockIdx.x * 256 + threadIdx.x) * 4;
+    if (i + 4 <= n && n % 4 == 0) {
+        float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
+        #pragma unroll 8
+        for (int z = 0; z < splits; ++z) {
+            const float4 t = *(const float4*)(partial + z * n + i);
+            s.x += t.x; s.y += t.y; s.z += t.z; s.w += t.w;
         }
+        if (((uintptr_t)out & 15) == 0) *(float4*)(out + i) = s;
+        else { out[i] = s.x; out[i + 1] = s.y; out[i + 2] = s.z; out[i + 3] = s.w; }
+    } else
+        for (long long j = i; j < min(n, i + 4); ++j) {
+            float s = 0.f;
+            for (int z = 0; z < splits; ++z) s += partial[z * n + j];
+            out[j] = s;
+        }
+}
+
+// Rows of `bytes` bytes (a multiple of UNIT), `src_pitch` apart, to rows `pitch` apart that start on 16-byte boundaries, zeros behind them: for
+// operands whose rows the copies above cannot read in place.  One thread per 16 bytes.
+template <typename UNIT>
+__global__ void __launch_bounds__(256) repitch_kernel(const uint8_t* __restrict__ src, long long src_pitch, int bytes, long long pitch, long long rows, uint8_t* __restrict__ dst) {
+    kn::pdl_sync();
+    const int per_row = (int)(pitch / 16);
+    const long long total = rows * per_row;
+    for (long long t = (long long)blockIdx.x * 256 + threadIdx.x; t < total; t += (long long)gridDim.x * 256) {
+        const long long r = t / per_row;
+        const int b0 = (int)(t - r * per_row) * 16;
+        const UNIT* s = (const UNIT*)(src + r * src_pitch + b0);
+        UNIT v[16 / sizeof(UNIT)];
+        #pragma unroll
+        for (int i = 0; i < (int)(16 / sizeof(UNIT)); ++i) v[i] = b0 + i * (int)sizeof(UNIT) < bytes ? s[i] : UNIT(0);
+        *(uint4*)(dst + r * pitch + b0) = *(const uint4*)v;
+    }
 }
 
 }  // namespace op

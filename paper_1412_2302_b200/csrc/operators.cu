@@ -3,7 +3,10 @@
 // caller gives every buffer, the workspace included, so calls on different streams share nothing.
 #include "../../include/alexnet.h"
 
+#include <cudaTypedefs.h>
+
 #include <algorithm>
+#include <atomic>
 #include <cstdio>
 #include <utility>
 
@@ -26,11 +29,13 @@ struct Err {
 struct Launcher {
     cudaStream_t st;
     cudaError_t e = cudaSuccess;
+    size_t smem = 0;            // of the next launch
     template <typename... KArgs, typename... Args>
     void operator()(void (*kernel)(KArgs...), long long grid, int block, Args&&... args) {
         if (e != cudaSuccess) return;
         cudaLaunchConfig_t lc{};
-        lc.gridDim = dim3((unsigned)grid); lc.blockDim = block; lc.stream = st;
+        lc.gridDim = dim3((unsigned)grid); lc.blockDim = block; lc.dynamicSmemBytes = smem; lc.stream = st;
+        smem = 0;
         cudaLaunchAttribute at{};
         at.id = cudaLaunchAttributeProgrammaticStreamSerialization;
         at.val.programmaticStreamSerializationAllowed = 1;
@@ -206,6 +211,68 @@ void backward(Launcher& go, const alexnet_group_norm_backward_t* a, const Dims& 
     else if (a->kept.format == ALEXNET_CODES_INT8) backward<T, V, kSrcInt8>(go, a, d);
     else backward<T, V, kSrcE4m3>(go, a, d);
 }
+
+// ---------------------------------------------------------------- linear weight gradient
+const char* check_linear(const alexnet_linear_weight_grad_t& a) {
+    if (a.rows < 0 || a.rows > (1ll << 30)) return "rows must be 0 to 2^30";
+    if (a.n_in < 1 || a.n_out < 1 || a.n_in > (1 << 20) || a.n_out > (1 << 20)) return "features must be 1 to 1048576";
+    if (!is_fmt(a.x.format)) return "unknown checkpoint format";
+    if ((uintptr_t)a.dy % 2) return "dy is not aligned to its elements";
+    if (a.rows > 1 && (a.dy_stride < 0 || a.dy_stride > (1ll << 38))) return "the stride of dy is negative or too large";
+    return nullptr;
+}
+PFN_cuTensorMapEncodeTiled_v12000 tensor_map_encoder() {
+    static std::atomic<void*> cached{nullptr};
+    void* fn = cached.load();
+    if (!fn) {
+        cudaDriverEntryPointQueryResult q;
+        if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &fn, cudaEnableDefault, &q) != cudaSuccess || q != cudaDriverEntryPointSuccess) { cudaGetLastError(); return nullptr; }
+        cached.store(fn);
+    }
+    return (PFN_cuTensorMapEncodeTiled_v12000)fn;
+}
+struct LinearPlan {
+    int BN, m_tiles, n_tiles, splits, steps, per, stages;
+    bool move_dy, move_x;               // copies with rows on 16-byte boundaries, where the rows are not
+    long long dy_pitch, x_pitch;        // bytes
+    size_t dy_at, x_at, bytes, smem;    // places in the workspace, behind the partial sums
+};
+LinearPlan linear_plan(const alexnet_linear_weight_grad_t& a) {
+    LinearPlan b{};
+    b.steps = (int)ceil_div(a.rows, kLgRows);
+    b.m_tiles = (int)ceil_div(a.n_in, 128);
+    // The tile's width and the number of splits by a model of the launch in cycles: a step of 64 rows costs its operands' way through shared
+    // memory (written once, read once, 128 bytes a cycle), a tile some 1500 for its first loads and last stores, a second launch 4000 and
+    // its partial sums 2500 bytes a cycle.
+    double best = 1e30;
+    for (int BN = 256; BN >= 32; BN /= 2) {
+        if (BN > 32 && BN / 2 >= a.n_out) continue;
+        const long long tiles = (long long)b.m_tiles * ceil_div(a.n_out, BN);
+        const double step = 256 + 2 * BN;
+        for (int s = 1; s <= 64; ++s) {
+            const long long per = ceil_div(std::max(1, b.steps), s);
+            if (s > 1 && (per < 4 || tiles * (s - 1) >= kSms)) break;
+            const int splits = (int)ceil_div(std::max(1, b.steps), per);
+            const double waves = (double)ceil_div(tiles * splits, kSms);
+            double cost = waves * (per * step + 1500) + 3.0 * BN;
+            if (splits > 1) cost += 4000 + (double)splits * a.n_in * a.n_out * 8 / 2500;
+            if (cost < best) { best = cost; b.BN = BN; b.splits = splits; b.per = (int)per; }
+        }
+    }
+    b.n_tiles = (int)ceil_div(a.n_out, b.BN);
+    const int stage = kLgA + (b.BN + 63) / 64 * 8192;
+    b.stages = std::min(kLgMaxStages, (227 * 1024 - 1024 - 256) / stage);
+    b.smem = tc::own_sm(1024 + (size_t)b.stages * stage + 256);
+    b.dy_pitch = ceil_div(a.n_out, 8) * 16;
+    b.x_pitch = ceil_div(a.n_in, 16) * 16;
+    b.move_dy = (uintptr_t)a.dy % 16 != 0 || (a.rows > 1 && (a.dy_stride % 8 != 0 || a.dy_stride < a.n_out));
+    b.move_x = (uintptr_t)a.x.codes % 16 != 0 || a.n_in % 16 != 0;
+    b.dy_at = b.splits > 1 ? ((size_t)b.splits * a.n_in * a.n_out * sizeof(float) + 255) / 256 * 256 : 0;
+    b.x_at = b.dy_at + (b.move_dy ? ((size_t)a.rows * b.dy_pitch + 255) / 256 * 256 : 0);
+    b.bytes = b.x_at + (b.move_x ? (size_t)a.rows * b.x_pitch : 0) + 256;
+    return b;
+}
+long long repitch_grid(long long rows, long long pitch) { return std::min<long long>(16 * kSms, ceil_div(rows * (pitch / 16), 256)); }
 }  // namespace
 
 extern "C" {
@@ -288,35 +355,65 @@ int alexnet_group_norm_backward(const alexnet_group_norm_backward_t* a, void* st
     return go.e == cudaSuccess ? ALEXNET_OK : err.cuda(go.e);
 }
 
-size_t alexnet_linear_weight_grad_workspace_bytes(int64_t rows, int32_t n_in, int32_t n_out) {
-    if (rows < 0 || n_in < 1 || n_out < 1) return 0;
-    return 256;
+size_t alexnet_linear_weight_grad_workspace_bytes(const alexnet_linear_weight_grad_t* a) {
+    if (!a || check_linear(*a)) return 0;
+    return linear_plan(*a).bytes;
 }
 
 int alexnet_linear_weight_grad(const alexnet_linear_weight_grad_t* a, void* stream, char* err_buf, size_t err_len) {
     const Err err{err_buf, err_len, "linear_weight_grad"};
     if (!a) return err.arg("NULL arguments");
-    if (a->rows < 0 || a->rows > (1ll << 30)) return err.arg("rows must be 0 to 2^30");
-    if (a->n_in < 1 || a->n_out < 1 || a->n_in > (1 << 20) || a->n_out > (1 << 20)) return err.arg("features must be 1 to 1048576");
-    if (!is_fmt(a->x.format)) return err.arg("unknown checkpoint format");
+    if (const char* m = check_linear(*a)) return err.arg(m);
     if (!a->dw || (uintptr_t)a->dw % 4) return err.arg("dw is NULL or not aligned");
-    if (a->rows > 0) {
-        if (!a->dy || !a->x.codes || !a->x.scales) return err.arg("NULL pointer");
-        if ((uintptr_t)a->dy % 2) return err.arg("dy is not aligned to its elements");
-        if (a->rows > 1 && (a->dy_stride < 0 || a->dy_stride > (1ll << 48))) return err.arg("the stride of dy is negative or too large");
-    }
-    if (!a->workspace || (uintptr_t)a->workspace % 16 || a->workspace_bytes < alexnet_linear_weight_grad_workspace_bytes(a->rows, a->n_in, a->n_out))
-        return err.arg("the workspace is too small or not 16-byte aligned");
+    if (a->rows > 0 && (!a->dy || !a->x.codes || !a->x.scales)) return err.arg("NULL pointer");
+    const LinearPlan pl = linear_plan(*a);
+    if (!a->workspace || (uintptr_t)a->workspace % 16 || a->workspace_bytes < pl.bytes) return err.arg("the workspace is too small or not 16-byte aligned");
     cudaStream_t st = (cudaStream_t)stream;
     if (a->rows == 0) {
         const cudaError_t e = cudaMemsetAsync(a->dw, 0, (size_t)a->n_in * a->n_out * sizeof(float), st);
         return e == cudaSuccess ? ALEXNET_OK : err.cuda(e);
     }
-    const dim3 grid((unsigned)ceil_div(a->n_in, 64), (unsigned)ceil_div(a->n_out, 64));
-    auto* k = a->x.format == ALEXNET_CODES_INT8 ? linear_grad_simple_kernel<kSrcInt8> : linear_grad_simple_kernel<kSrcE4m3>;
-    k<<<grid, 256, 0, st>>>((const bf16*)a->dy, a->rows > 1 ? a->dy_stride : 0, (const uint8_t*)a->x.codes, a->x.scales, a->rows, a->n_in, a->n_out, a->dw);
-    const cudaError_t e = cudaGetLastError();
-    return e == cudaSuccess ? ALEXNET_OK : err.cuda(e);
+    LinearGradParams p{};
+    Launcher go{st};
+    const void* dy = a->dy;
+    long long dy_pitch = a->dy_stride * 2;
+    if (pl.move_dy) {
+        uint8_t* t = (uint8_t*)a->workspace + pl.dy_at;
+        go(repitch_kernel<uint16_t>, repitch_grid(a->rows, pl.dy_pitch), 256, (const uint8_t*)a->dy, a->rows > 1 ? a->dy_stride * 2 : 0ll, a->n_out * 2, pl.dy_pitch, a->rows, t);
+        dy = t; dy_pitch = pl.dy_pitch;
+    } else if (a->rows == 1) dy_pitch = ceil_div(a->n_out, 8) * 16;
+    p.codes = (const uint8_t*)a->x.codes;
+    p.code_pitch = a->n_in;
+    if (pl.move_x) {
+        uint8_t* t = (uint8_t*)a->workspace + pl.x_at;
+        go(repitch_kernel<uint8_t>, repitch_grid(a->rows, pl.x_pitch), 256, p.codes, (long long)a->n_in, a->n_in, pl.x_pitch, a->rows, t);
+        p.codes = t; p.code_pitch = pl.x_pitch;
+    }
+    PFN_cuTensorMapEncodeTiled_v12000 enc = tensor_map_encoder();
+    if (!enc) return err.cuda(cudaErrorNotSupported);
+    const cuuint64_t dims[2] = {(cuuint64_t)a->n_out, (cuuint64_t)a->rows}, strides[1] = {(cuuint64_t)dy_pitch};
+    const cuuint32_t box[2] = {64, kLgRows}, one[2] = {1, 1};
+    if (enc(&p.tmD, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(dy), dims, strides, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+            CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
+        return err.arg("the driver refused the tensor map of dy");
+    p.scales = a->x.scales;
+    p.blocks = (int)ceil_div(a->n_in, 32);
+    p.rows = (int)a->rows; p.n_in = a->n_in; p.n_out = a->n_out;
+    p.BN = pl.BN; p.m_tiles = pl.m_tiles; p.n_tiles = pl.n_tiles; p.splits = pl.splits; p.steps = pl.steps; p.per = pl.per; p.stages = pl.stages;
+    p.out = pl.splits > 1 ? (float*)a->workspace : a->dw;
+    auto* kernel = a->x.format == ALEXNET_CODES_INT8 ? linear_grad_kernel<kSrcInt8> : linear_grad_kernel<kSrcE4m3>;
+    if (go.e == cudaSuccess) go.e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 227 * 1024);
+    go.smem = pl.smem;
+    go(kernel, std::min<long long>(kSms, (long long)pl.m_tiles * pl.n_tiles * pl.splits), kLgThreads, p);
+    const long long n = (long long)a->n_in * a->n_out;
+    if (pl.splits > 1) go(linear_grad_join_kernel, ceil_div(n, 1024), 256, (const float*)a->workspace, pl.splits, n, a->dw);
+    return go.e == cudaSuccess ? ALEXNET_OK : err.cuda(go.e);
+}
+
+int alexnet_operators_check(void) {
+    int expired = 0;
+    if (cudaMemcpyFromSymbol(&expired, g_expired, sizeof(int)) != cudaSuccess) { cudaGetLastError(); return ALEXNET_ERR_CUDA; }
+    return expired ? ALEXNET_ERR_DEVICE_TIMEOUT : ALEXNET_OK;
 }
 
 }  // extern "C"

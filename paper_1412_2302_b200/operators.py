@@ -195,6 +195,23 @@ def _norm_workspace(shape, backward):
     return n
 
 
+@functools.lru_cache(maxsize=1024)
+def _linear_workspace(rows, n_in, n_out, stride, dy_offset, codes_offset, fmt):
+    """by sizes and alignment: the pointers are given modulo 16"""
+    n = int(_alexnet.load_library().alexnet_linear_weight_grad_workspace_bytes(
+        _pack_linear(rows, n_in, n_out, 16 + dy_offset, stride, 16 + codes_offset, 16, fmt, 0, 0, 0, 0)))
+    if n == 0:
+        raise AlexNetError(ERR_ARG, f"invalid linear weight gradient: rows, in, out = {rows, n_in, n_out}, stride {stride}")
+    return n
+
+
+def check():
+    """Wait for the current device's work and raise if a bounded wait inside an operator's kernel has ever run out (its outputs are NaN)."""
+    rc = _alexnet.load_library().alexnet_operators_check()
+    if rc != OK:
+        raise AlexNetError(rc, "a wait inside an operator's kernel ran out" if rc == _alexnet.ERR_DEVICE_TIMEOUT else "the device could not be read")
+
+
 def checkpoint_encode(x, format="int8", out=None, stream=None):
     """The 8-bit checkpoint of x: 33 bytes for 32 values.  out: a Checkpoint to write instead of a new one."""
     dtype = _name(DTYPES, x.dtype, "dtype")
@@ -307,8 +324,8 @@ def linear_weight_grad(dy, x, out=None, stream=None):
         if not dw.is_contiguous():
             _refuse("out must be dense")
         _same(call, x.codes, dw)
-        nbytes = int(lib.alexnet_linear_weight_grad_workspace_bytes(rows, n_in, n_out))
-        ws = torch.empty(max(nbytes, 16), dtype=torch.uint8, device=call.device)
+        nbytes = _linear_workspace(rows, n_in, n_out, dy.stride(0), dy.data_ptr() % 16, x.codes.data_ptr() % 16, FORMATS[x.format])
+        ws = torch.empty(nbytes, dtype=torch.uint8, device=call.device)
         call.run(lib.alexnet_linear_weight_grad,
                  _pack_linear(rows, n_in, n_out, dy.data_ptr(), dy.stride(0), *_kept(x), dw.data_ptr(), ws.data_ptr(), nbytes))
     return dw
