@@ -8,7 +8,7 @@
 // its own tile of x again for every BN outputs.  An accumulator column then is 32 consecutive inputs of one output for each warp, which
 // leaves as one full 128-byte line.
 //
-// Warps: 0 = TMA producer (dy), 1 = MMA issuer and TMEM owner, 2..5 = epilogue, 6..13 = decoders.  Persistent over tiles with two
+// Warps: 0 = TMA producer (dy), 1 = MMA issuer and TMEM owner, 2..9 = epilogue (two sets of four), 10..17 = decoders.  Persistent over tiles with two
 // accumulators, so a tile's stores overlap the next one's products.  Few tiles with many rows are split over the rows; the
 // partial sums are added in a fixed order by a second kernel.  Every wait is bounded; a CTA whose wait runs out writes NaN and raises g_expired.
 #pragma once
@@ -16,7 +16,7 @@
 
 namespace op {
 
-constexpr int kLgRows = 64, kLgThreads = 32 * 14, kLgDecoders = 8;
+constexpr int kLgRows = 64, kLgEpilogue = 8, kLgDecoders = 8, kLgThreads = 32 * (2 + kLgEpilogue + kLgDecoders);
 constexpr int kLgA = 128 * kLgRows * 2;            // bytes of the decoded tile of a stage: two boxes of 64 features x 64 rows
 constexpr int kLgMaxStages = 6;
 struct LinearGradParams {
@@ -45,6 +45,38 @@ struct LinearGradTile {                            // tiles: input tile fastest,
 // a decoder's share of a stage: 16 codes of each of two rows
 struct LinearGradCodes { uint4 c[2]; uint8_t e[2]; };
 
+// sixteen codes and their exponent to bf16 pairs.  The int8 code + 128 as the low byte of 2^23 + that, times the scale, less (2^23 + 128) times the
+// scale, in one multiply-add: exact, unless the product passes fp32's range (exponents that only magnitudes above 2^110 have).
+template <int FMT>
+__device__ __forceinline__ void decode16(const uint4& c, uint32_t e, uint32_t* w) {
+    const float sc = scale_of(e);
+    const f2 s2 = mk2(sc, sc);
+    if (FMT == kSrcInt8 && e < 230u) {
+        const float off = -8388736.f * sc;
+        const f2 o2 = mk2(off, off);
+        const uint32_t* u = (const uint32_t*)&c;
+        #pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const uint32_t t = u[i] ^ 0x80808080u;
+            #pragma unroll
+            for (int q = 0; q < 2; ++q) {
+                float lo, hi;
+                un2(fma2(mk2(__uint_as_float(__byte_perm(t, 0x4b000000u, 0x7440u | 2 * q)), __uint_as_float(__byte_perm(t, 0x4b000000u, 0x7441u | 2 * q))), s2, o2), lo, hi);
+                asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(w[2 * i + q]) : "f"(hi), "f"(lo));
+            }
+        }
+        return;
+    }
+    float v[16];
+    code_values<FMT, 16>(c, v);
+    #pragma unroll
+    for (int q = 0; q < 8; ++q) {
+        float lo, hi;
+        un2(mul2(mk2(v[2 * q], v[2 * q + 1]), s2), lo, hi);
+        asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(w[q]) : "f"(hi), "f"(lo));
+    }
+}
+
 template <int FMT>
 __global__ void __launch_bounds__(kLgThreads, 1) linear_grad_kernel(const __grid_constant__ LinearGradParams p) {
     kn::pdl_trigger();
@@ -66,7 +98,7 @@ __global__ void __launch_bounds__(kLgThreads, 1) linear_grad_kernel(const __grid
     if (threadIdx.x == 0) {
         *abort_flag = 0;
         for (int s = 0; s < stages; ++s) { tc::mbar_init(full0 + 8u * s, 1 + kLgDecoders); tc::mbar_init(empty0 + 8u * s, 1); }
-        for (int s = 0; s < 2; ++s) { tc::mbar_init(accf0 + 8u * s, 1); tc::mbar_init(acce0 + 8u * s, 4); }
+        for (int s = 0; s < 2; ++s) { tc::mbar_init(accf0 + 8u * s, 1); tc::mbar_init(acce0 + 8u * s, kLgEpilogue); }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         tc::tma_prefetch_desc(&p.tmD);
     }
@@ -118,8 +150,8 @@ __global__ void __launch_bounds__(kLgThreads, 1) linear_grad_kernel(const __grid
             tc::umma_commit(accf0 + 8u * ab);
             if (++ab == 2) { ab = 0; aph ^= 1u; }
         }
-    } else if (warp < 6) {
-        const int quad = warp & 3;
+    } else if (warp < 2 + kLgEpilogue) {
+        const int quad = warp & 3, set = (warp - 2) >> 2;
         int ab = 0; uint32_t aph = 0;
         bool ok = true;
         LinearGradTile t;
@@ -128,9 +160,10 @@ __global__ void __launch_bounds__(kLgThreads, 1) linear_grad_kernel(const __grid
             ok = ok && tc::mbar_wait_idle(accf0 + 8u * ab, aph, abort_flag);
             tc::tc_fence_after();
             const int i = t.m * 128 + quad * 32 + lane, o0 = t.n * p.BN, nv = min(p.BN, p.n_out - o0);
-            float* out = p.out + (long long)t.z * p.n_out * p.n_in + (long long)o0 * p.n_in + i;
+            float* out = p.out + (long long)t.z * p.n_out * p.n_in + (long long)(o0 + 32 * set) * p.n_in + i;
             const uint32_t ta = tmem + (uint32_t)(ab * p.BN) + ((uint32_t)(quad * 32) << 16);
-            for (int c = 0; c < nv; c += 32) {
+            #pragma unroll 1
+            for (int c = 32 * set; c < nv; c += 64, out += 64ll * p.n_in) {
                 uint32_t v[32];
                 if (ok) { tc::tmem_ld32(ta + (uint32_t)c, v); tc::tmem_ld_wait(); }
                 else {
@@ -138,9 +171,14 @@ __global__ void __launch_bounds__(kLgThreads, 1) linear_grad_kernel(const __grid
                     for (int q = 0; q < 32; ++q) v[q] = 0x7fffffffu;
                 }
                 if (i < p.n_in) {
-                    #pragma unroll
-                    for (int q = 0; q < 32; ++q)
-                        if (c + q < nv) out[(long long)(c + q) * p.n_in] = __uint_as_float(v[q]);
+                    float* o = out;
+                    if (c + 32 <= nv) {
+                        #pragma unroll
+                        for (int q = 0; q < 32; ++q) { *o = __uint_as_float(v[q]); o += p.n_in; }
+                    } else {
+                        #pragma unroll
+                        for (int q = 0; q < 32; ++q) { if (c + q < nv) *o = __uint_as_float(v[q]); o += p.n_in; }
+                    }
                 }
             }
             tc::tc_fence_before();
@@ -152,67 +190,67 @@ __global__ void __launch_bounds__(kLgThreads, 1) linear_grad_kernel(const __grid
         // thread: codes 16 cg .. 16 cg + 15 of the rows kr and kr + 32 of a stage.  With the 128-byte swizzle, 16-byte chunk j of row k
         // lies at j ^ (k & 7): of eight neighbouring lanes the four of the second box take the neighbouring row, so that the eight write to
         // eight different bank groups.
-        const int td = threadIdx.x - 192, cg = td & 7, kr = (td >> 3) ^ (cg >> 2);
+        const int td = threadIdx.x - 32 * (2 + kLgEpilogue), cg = td & 7, kr = (td >> 3) ^ (cg >> 2);
         constexpr int PF = 3;                  // stages whose codes are in flight
         LinearGradCodes f[PF];
-        int total = 0;
+        int total = 0, tile = blockIdx.x, left = 0, row = 0;
         LinearGradTile t;
-        for (int tile = blockIdx.x; tile < tiles; tile += gridDim.x) { t.set(p, tile); total += t.k1 - t.k0; }
-        int ltile = blockIdx.x, lk, loaded = 0;
-        t.set(p, ltile);
-        lk = t.k0;
-        auto load = [&](LinearGradCodes& r) {
+        for (int k = blockIdx.x; k < tiles; k += gridDim.x) { t.set(p, k); total += t.k1 - t.k0; }
+        const uint8_t *cp = nullptr, *ep = nullptr;
+        bool col_ok = false;
+        auto enter = [&] {                     // the next tile whose codes are to be loaded
+            t.set(p, tile);
+            tile += gridDim.x;
+            left = t.k1 - t.k0;
+            row = t.k0 * kLgRows + kr;
             const int col = t.m * 128 + cg * 16;
+            col_ok = col < p.n_in;
+            cp = p.codes + row * p.code_pitch + col;
+            ep = p.scales + (long long)row * p.blocks + (col >> 5);
+        };
+        enter();
+        const long long half_c = 32 * p.code_pitch, half_e = 32ll * p.blocks;
+        int to_load = total;
+        auto load = [&](LinearGradCodes& r) {
+            if (left == 0) enter();
             #pragma unroll
             for (int h = 0; h < 2; ++h) {
-                const long long row = (long long)lk * kLgRows + kr + 32 * h;
                 r.c[h] = make_uint4(0u, 0u, 0u, 0u);
                 r.e[h] = 0;
-                if (row < p.rows && col < p.n_in) {
-                    r.c[h] = __ldg((const uint4*)(p.codes + row * p.code_pitch + col));
-                    r.e[h] = __ldg(p.scales + row * p.blocks + (col >> 5));
-                }
+                if (col_ok && row < p.rows) { r.c[h] = __ldg((const uint4*)cp); r.e[h] = __ldg(ep); }
+                row += 32;
+                cp += half_c;
+                ep += half_e;
             }
-            ++loaded;
-            if (++lk == t.k1) {
-                ltile += gridDim.x;
-                if (ltile < tiles) { t.set(p, ltile); lk = t.k0; }
-            }
+            --left;
+            --to_load;
         };
         #pragma unroll
         for (int u = 0; u < PF; ++u)
-            if (loaded < total) load(f[u]);
+            if (to_load > 0) load(f[u]);
+        const int k = kr & 7, j = 2 * (cg & 3);      // of both rows
+        const uint32_t off0 = (uint32_t)(cg >> 2) * 8192u + (uint32_t)kr * 128u + (uint32_t)((j ^ k) << 4);
+        const uint32_t off1 = (uint32_t)(cg >> 2) * 8192u + (uint32_t)kr * 128u + (uint32_t)(((j + 1) ^ k) << 4);
         int st = 0; uint32_t ph = 0;
         bool ok = true;
         for (int s = 0; s < total && ok; s += PF) {
             #pragma unroll
             for (int u = 0; u < PF; ++u) {
                 if (s + u >= total || !ok) break;
-                if (!(ok = tc::mbar_wait_warp(empty0 + 8u * st, ph ^ 1u, abort_flag))) break;
-                const uint32_t sa = base + st * stage_bytes + (uint32_t)(cg >> 2) * 8192u;
+                if (!(ok = tc::mbar_wait_idle(empty0 + 8u * st, ph ^ 1u, abort_flag))) break;
+                const uint32_t sa = base + st * stage_bytes;
                 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
-                    float v[16];
-                    code_values<FMT, 16>(f[u].c[h], v);
-                    const float sc = scale_of(f[u].e[h]);
-                    const f2 s2 = mk2(sc, sc);
                     uint32_t w[8];
-                    #pragma unroll
-                    for (int q = 0; q < 8; ++q) {
-                        float lo, hi;
-                        un2(mul2(mk2(v[2 * q], v[2 * q + 1]), s2), lo, hi);
-                        asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(w[q]) : "f"(hi), "f"(lo));
-                    }
-                    const int k = kr + 32 * h, j = 2 * (cg & 3);
-                    const uint32_t row = sa + (uint32_t)k * 128u;
-                    tc::st_shared_v4(row + (uint32_t)((j ^ (k & 7)) << 4), w[0], w[1], w[2], w[3]);
-                    tc::st_shared_v4(row + (uint32_t)(((j + 1) ^ (k & 7)) << 4), w[4], w[5], w[6], w[7]);
+                    decode16<FMT>(f[u].c[h], f[u].e[h], w);
+                    tc::st_shared_v4(sa + off0 + 4096u * h, w[0], w[1], w[2], w[3]);
+                    tc::st_shared_v4(sa + off1 + 4096u * h, w[4], w[5], w[6], w[7]);
                 }
                 tc::fence_async_smem();
                 __syncwarp();
                 if (lane == 0) tc::mbar_arrive(full0 + 8u * st);
                 if (++st == stages) { st = 0; ph ^= 1u; }
-                if (loaded < total) load(f[u]);
+                if (to_load > 0) load(f[u]);
             }
         }
     }
