@@ -8,7 +8,8 @@
 // its own tile of x again for every BN outputs.  An accumulator column then is 32 consecutive inputs of one output for each warp, which
 // leaves as one full 128-byte line.
 //
-// Warps: 0 = TMA producer (dy), 1 = MMA issuer and TMEM owner, 2..9 = epilogue (two sets of four), 10..17 = decoders.  Persistent over tiles with two
+// Warps: 0 = TMA producer (dy), 1 = MMA issuer and TMEM owner, 2..9 = epilogue (two sets of four), 10..25 = decoders, two groups
+// that take the steps in turn (a step takes a warp some 1100 cycles from its wait to its arrival, and the tensor cores 512).  Persistent over tiles with two
 // accumulators, so a tile's stores overlap the next one's products.  Few tiles with many rows are split over the rows; the
 // partial sums are added in a fixed order by a second kernel.  Every wait is bounded; a CTA whose wait runs out writes NaN and raises g_expired.
 #pragma once
@@ -16,7 +17,8 @@
 
 namespace op {
 
-constexpr int kLgRows = 64, kLgEpilogue = 8, kLgDecoders = 8, kLgThreads = 32 * (2 + kLgEpilogue + kLgDecoders);
+constexpr int kLgRows = 64, kLgEpilogue = 8, kLgDecoders = 8, kLgGroups = 2;      // decoders of a step; groups of them
+constexpr int kLgThreads = 32 * (2 + kLgEpilogue + kLgGroups * kLgDecoders);
 constexpr int kLgA = 128 * kLgRows * 2;            // bytes of the decoded tile of a stage: two boxes of 64 features x 64 rows
 constexpr int kLgMaxStages = 6;
 struct LinearGradParams {
@@ -190,8 +192,9 @@ __global__ void __launch_bounds__(kLgThreads, 1) linear_grad_kernel(const __grid
         // thread: codes 16 cg .. 16 cg + 15 of the rows kr and kr + 32 of a stage.  With the 128-byte swizzle, 16-byte chunk j of row k
         // lies at j ^ (k & 7): of eight neighbouring lanes the four of the second box take the neighbouring row, so that the eight write to
         // eight different bank groups.
-        const int td = threadIdx.x - 32 * (2 + kLgEpilogue), cg = td & 7, kr = (td >> 3) ^ (cg >> 2);
-        constexpr int PF = 3;                  // stages whose codes are in flight
+        const int group = (warp - 2 - kLgEpilogue) / kLgDecoders, td = (threadIdx.x - 32 * (2 + kLgEpilogue)) % (32 * kLgDecoders);
+        const int cg = td & 7, kr = (td >> 3) ^ (cg >> 2);
+        constexpr int PF = 2;                  // steps of the group whose codes are in flight
         LinearGradCodes f[PF];
         int total = 0, tile = blockIdx.x, left = 0, row = 0;
         LinearGradTile t;
@@ -210,20 +213,25 @@ __global__ void __launch_bounds__(kLgThreads, 1) linear_grad_kernel(const __grid
         };
         enter();
         const long long half_c = 32 * p.code_pitch, half_e = 32ll * p.blocks;
-        int to_load = total;
+        int to_load = total - group;
+        auto skip = [&](int steps) {           // forward by that many steps
+            for (int q = 0; q < steps; ++q) {
+                row += kLgRows;
+                cp += 2 * half_c;
+                ep += 2 * half_e;
+                if (--left == 0 && tile < tiles) enter();
+            }
+        };
+        skip(group);
         auto load = [&](LinearGradCodes& r) {
-            if (left == 0) enter();
             #pragma unroll
             for (int h = 0; h < 2; ++h) {
                 r.c[h] = make_uint4(0u, 0u, 0u, 0u);
                 r.e[h] = 0;
-                if (col_ok && row < p.rows) { r.c[h] = __ldg((const uint4*)cp); r.e[h] = __ldg(ep); }
-                row += 32;
-                cp += half_c;
-                ep += half_e;
+                if (col_ok && row + 32 * h < p.rows) { r.c[h] = __ldg((const uint4*)(cp + h * half_c)); r.e[h] = __ldg(ep + h * half_e); }
             }
-            --left;
-            --to_load;
+            skip(kLgGroups);
+            to_load -= kLgGroups;
         };
         #pragma unroll
         for (int u = 0; u < PF; ++u)
@@ -231,12 +239,12 @@ __global__ void __launch_bounds__(kLgThreads, 1) linear_grad_kernel(const __grid
         const int k = kr & 7, j = 2 * (cg & 3);      // of both rows
         const uint32_t off0 = (uint32_t)(cg >> 2) * 8192u + (uint32_t)kr * 128u + (uint32_t)((j ^ k) << 4);
         const uint32_t off1 = (uint32_t)(cg >> 2) * 8192u + (uint32_t)kr * 128u + (uint32_t)(((j + 1) ^ k) << 4);
-        int st = 0; uint32_t ph = 0;
+        int st = group; uint32_t ph = 0;
         bool ok = true;
-        for (int s = 0; s < total && ok; s += PF) {
+        for (int s = group; s < total && ok; s += kLgGroups * PF) {
             #pragma unroll
             for (int u = 0; u < PF; ++u) {
-                if (s + u >= total || !ok) break;
+                if (s + kLgGroups * u >= total || !ok) break;
                 if (!(ok = tc::mbar_wait_idle(empty0 + 8u * st, ph ^ 1u, abort_flag))) break;
                 const uint32_t sa = base + st * stage_bytes;
                 #pragma unroll
@@ -249,7 +257,8 @@ __global__ void __launch_bounds__(kLgThreads, 1) linear_grad_kernel(const __grid
                 tc::fence_async_smem();
                 __syncwarp();
                 if (lane == 0) tc::mbar_arrive(full0 + 8u * st);
-                if (++st == stages) { st = 0; ph ^= 1u; }
+                st += kLgGroups;
+                if (st >= stages) { st -= stages; ph ^= 1u; }
                 if (to_load > 0) load(f[u]);
             }
         }
