@@ -44,18 +44,14 @@ struct LinearGradTile {                            // tiles: input tile fastest,
         k1 = min(p.steps, k0 + p.per);
     }
 };
-// a decoder's share of a stage: 16 codes of each of two rows
-struct LinearGradCodes { uint4 c[2]; uint8_t e[2]; };
+// a decoder's share of a stage: a checkpoint block of one row
+struct LinearGradCodes { uint4 c[2]; uint32_t e; };
 
-// sixteen codes and their exponent to bf16 pairs.  The int8 code + 128 as the low byte of 2^23 + that, times the scale, less (2^23 + 128) times the
-// scale, in one multiply-add: exact, unless the product passes fp32's range (exponents that only magnitudes above 2^110 have).
-template <int FMT>
-__device__ __forceinline__ void decode16(const uint4& c, uint32_t e, uint32_t* w) {
-    const float sc = scale_of(e);
-    const f2 s2 = mk2(sc, sc);
-    if (FMT == kSrcInt8 && e < 230u) {
-        const float off = -8388736.f * sc;
-        const f2 o2 = mk2(off, off);
+// Sixteen codes to bf16 pairs, s2 = the scale twice.  int8: the code + 128 as the low byte of 2^23 + that, times the scale, less (2^23 + 128)
+// times the scale, in one multiply-add: exact, unless the product passes fp32's range (exponents that only magnitudes above 2^109 have).
+template <int FMT, bool FUSED>
+__device__ __forceinline__ void decode16(const uint4& c, f2 s2, f2 o2, uint32_t* w) {
+    if constexpr (FUSED) {
         const uint32_t* u = (const uint32_t*)&c;
         #pragma unroll
         for (int i = 0; i < 4; ++i) {
@@ -67,15 +63,28 @@ __device__ __forceinline__ void decode16(const uint4& c, uint32_t e, uint32_t* w
                 asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(w[2 * i + q]) : "f"(hi), "f"(lo));
             }
         }
-        return;
+    } else {
+        float v[16];
+        code_values<FMT, 16>(c, v);
+        #pragma unroll
+        for (int q = 0; q < 8; ++q) {
+            float lo, hi;
+            un2(mul2(mk2(v[2 * q], v[2 * q + 1]), s2), lo, hi);
+            asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(w[q]) : "f"(hi), "f"(lo));
+        }
     }
-    float v[16];
-    code_values<FMT, 16>(c, v);
+}
+// a block of 32 codes into its place in the stage: addr = row k of a box, the block's chunks 4 b .. 4 b + 3 (b = 0, 1), swizzled by k
+template <int FMT, bool FUSED>
+__device__ __forceinline__ void decode_block(const LinearGradCodes& r, uint32_t addr, uint32_t swz) {
+    const float sc = scale_of(r.e), off = -8388736.f * sc;
+    const f2 s2 = mk2(sc, sc), o2 = mk2(off, off);
     #pragma unroll
-    for (int q = 0; q < 8; ++q) {
-        float lo, hi;
-        un2(mul2(mk2(v[2 * q], v[2 * q + 1]), s2), lo, hi);
-        asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(w[q]) : "f"(hi), "f"(lo));
+    for (int h = 0; h < 2; ++h) {
+        uint32_t w[8];
+        decode16<FMT, FUSED>(r.c[h], s2, o2, w);
+        tc::st_shared_v4(addr + (swz ^ (uint32_t)(32 * h)), w[0], w[1], w[2], w[3]);
+        tc::st_shared_v4(addr + (swz ^ (uint32_t)(32 * h + 16)), w[4], w[5], w[6], w[7]);
     }
 }
 
@@ -189,56 +198,51 @@ __global__ void __launch_bounds__(kLgThreads, 1) linear_grad_kernel(const __grid
             if (++ab == 2) { ab = 0; aph ^= 1u; }
         }
     } else {
-        // thread: codes 16 cg .. 16 cg + 15 of the rows kr and kr + 32 of a stage.  With the 128-byte swizzle, 16-byte chunk j of row k
-        // lies at j ^ (k & 7): of eight neighbouring lanes the four of the second box take the neighbouring row, so that the eight write to
-        // eight different bank groups.
+        // thread: checkpoint block cb (32 codes) of row kr of a step.  With the 128-byte swizzle, 16-byte chunk j of row k lies at j ^ (k & 7);
+        // the threads of the second box take rows two apart from those of the first, so that eight neighbouring lanes (four blocks, two
+        // rows) write to eight different bank groups.
         const int group = (warp - 2 - kLgEpilogue) / kLgDecoders, td = (threadIdx.x - 32 * (2 + kLgEpilogue)) % (32 * kLgDecoders);
-        const int cg = td & 7, kr = (td >> 3) ^ (cg >> 2);
+        const int cb = td & 3, kr = (td >> 2) ^ (cb & 2);
         constexpr int PF = 2;                  // steps of the group whose codes are in flight
         LinearGradCodes f[PF];
         int total = 0, tile = blockIdx.x, left = 0, row = 0;
         LinearGradTile t;
         for (int k = blockIdx.x; k < tiles; k += gridDim.x) { t.set(p, k); total += t.k1 - t.k0; }
         const uint8_t *cp = nullptr, *ep = nullptr;
-        bool col_ok = false;
+        int halves = 0;                        // of the block's two halves of 16 codes, how many there are in memory
         auto enter = [&] {                     // the next tile whose codes are to be loaded
             t.set(p, tile);
             tile += gridDim.x;
             left = t.k1 - t.k0;
             row = t.k0 * kLgRows + kr;
-            const int col = t.m * 128 + cg * 16;
-            col_ok = col < p.n_in;
+            const int col = t.m * 128 + cb * 32;
+            halves = col >= p.n_in ? 0 : col + 16 < p.n_in ? 2 : 1;
             cp = p.codes + row * p.code_pitch + col;
             ep = p.scales + (long long)row * p.blocks + (col >> 5);
         };
-        enter();
-        const long long half_c = 32 * p.code_pitch, half_e = 32ll * p.blocks;
-        int to_load = total - group;
-        auto skip = [&](int steps) {           // forward by that many steps
-            for (int q = 0; q < steps; ++q) {
-                row += kLgRows;
-                cp += 2 * half_c;
-                ep += 2 * half_e;
-                if (--left == 0 && tile < tiles) enter();
-            }
+        const long long step_c = kLgRows * p.code_pitch, step_e = (long long)kLgRows * p.blocks;
+        auto forward = [&](int steps) {
+            while (steps >= left && tile < tiles) { steps -= left; enter(); }
+            left -= steps;
+            row += steps * kLgRows;
+            cp += steps * step_c;
+            ep += steps * step_e;
         };
-        skip(group);
+        enter();
+        int to_load = total - group;
+        if (to_load > 0) forward(group);
         auto load = [&](LinearGradCodes& r) {
-            #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                r.c[h] = make_uint4(0u, 0u, 0u, 0u);
-                r.e[h] = 0;
-                if (col_ok && row + 32 * h < p.rows) { r.c[h] = __ldg((const uint4*)(cp + h * half_c)); r.e[h] = __ldg(ep + h * half_e); }
-            }
-            skip(kLgGroups);
+            const bool in = row < p.rows;
+            r.c[0] = in && halves > 0 ? __ldg((const uint4*)cp) : make_uint4(0u, 0u, 0u, 0u);
+            r.c[1] = in && halves > 1 ? __ldg((const uint4*)cp + 1) : make_uint4(0u, 0u, 0u, 0u);
+            r.e = in && halves > 0 ? __ldg(ep) : 0u;
             to_load -= kLgGroups;
+            if (to_load > 0) forward(kLgGroups);
         };
         #pragma unroll
         for (int u = 0; u < PF; ++u)
             if (to_load > 0) load(f[u]);
-        const int k = kr & 7, j = 2 * (cg & 3);      // of both rows
-        const uint32_t off0 = (uint32_t)(cg >> 2) * 8192u + (uint32_t)kr * 128u + (uint32_t)((j ^ k) << 4);
-        const uint32_t off1 = (uint32_t)(cg >> 2) * 8192u + (uint32_t)kr * 128u + (uint32_t)(((j + 1) ^ k) << 4);
+        const uint32_t off = (uint32_t)(cb >> 1) * 8192u + (uint32_t)kr * 128u, swz = (uint32_t)((4 * (cb & 1)) ^ (kr & 7)) << 4;
         int st = group; uint32_t ph = 0;
         bool ok = true;
         for (int s = group; s < total && ok; s += kLgGroups * PF) {
@@ -246,14 +250,9 @@ __global__ void __launch_bounds__(kLgThreads, 1) linear_grad_kernel(const __grid
             for (int u = 0; u < PF; ++u) {
                 if (s + kLgGroups * u >= total || !ok) break;
                 if (!(ok = tc::mbar_wait_idle(empty0 + 8u * st, ph ^ 1u, abort_flag))) break;
-                const uint32_t sa = base + st * stage_bytes;
-                #pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    uint32_t w[8];
-                    decode16<FMT>(f[u].c[h], f[u].e[h], w);
-                    tc::st_shared_v4(sa + off0 + 4096u * h, w[0], w[1], w[2], w[3]);
-                    tc::st_shared_v4(sa + off1 + 4096u * h, w[4], w[5], w[6], w[7]);
-                }
+                const uint32_t addr = base + st * stage_bytes + off;
+                if (FMT == kSrcInt8 && __all_sync(~0u, f[u].e < 230u)) decode_block<FMT, FMT == kSrcInt8>(f[u], addr, swz);
+                else decode_block<FMT, false>(f[u], addr, swz);
                 tc::fence_async_smem();
                 __syncwarp();
                 if (lane == 0) tc::mbar_arrive(full0 + 8u * st);
