@@ -88,12 +88,17 @@ __device__ __forceinline__ void decode_block(const LinearGradCodes& r, uint32_t 
     }
 }
 
-template <int FMT>
+// CG = 2: CTA pairs.  The two CTAs (cluster of two) share a tile of 256 inputs: each decodes its own 128 and loads half of the BN columns of dy;
+// the leader's instructions cover both, so a CTA's shared memory takes half the traffic of dy.
+template <int FMT, int CG>
 __global__ void __launch_bounds__(kLgThreads, 1) linear_grad_kernel(const __grid_constant__ LinearGradParams p) {
     kn::pdl_trigger();
+    if (CG == 2) tc::cluster_arrive();                 // (this CTA runs)
+    const int rank = CG == 2 ? (int)tc::cluster_ctarank() : 0;
+    const int tile0 = (int)blockIdx.x / CG, tile_step = (int)gridDim.x / CG;
     extern __shared__ uint8_t smem_raw[];
     const uint32_t raw = tc::smem_u32(smem_raw), base = (raw + 1023u) & ~1023u;
-    const int nb = (p.BN + 63) >> 6, stages = p.stages;
+    const int nb = (p.BN / CG + 63) >> 6, stages = p.stages;
     const uint32_t stage_bytes = kLgA + (uint32_t)nb * 8192u;
     // barriers behind the stages: full[8] @0, empty[8] @64, acc_full[2] @128, acc_empty[2] @144, tmem slot @160, abort flag @168
     const uint32_t bar = base + stages * stage_bytes;
@@ -108,43 +113,60 @@ __global__ void __launch_bounds__(kLgThreads, 1) linear_grad_kernel(const __grid
 
     if (threadIdx.x == 0) {
         *abort_flag = 0;
-        for (int s = 0; s < stages; ++s) { tc::mbar_init(full0 + 8u * s, 1 + kLgDecoders); tc::mbar_init(empty0 + 8u * s, 1); }
-        for (int s = 0; s < 2; ++s) { tc::mbar_init(accf0 + 8u * s, 1); tc::mbar_init(acce0 + 8u * s, kLgEpilogue); }
+        for (int s = 0; s < stages; ++s) { tc::mbar_init(full0 + 8u * s, 1 + CG * kLgDecoders); tc::mbar_init(empty0 + 8u * s, 1); }
+        for (int s = 0; s < 2; ++s) { tc::mbar_init(accf0 + 8u * s, 1); tc::mbar_init(acce0 + 8u * s, CG * kLgEpilogue); }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         tc::tma_prefetch_desc(&p.tmD);
     }
-    if (warp == 1) tc::tmem_alloc(tc::smem_u32((const void*)tmem_slot), ncols);
+    __syncwarp();
+    if (CG == 2) tc::cluster_wait();                   // the peer runs
+    if (warp == 1) {
+        if (CG == 2) tc::tmem_alloc_pair(tc::smem_u32((const void*)tmem_slot), ncols);
+        else tc::tmem_alloc(tc::smem_u32((const void*)tmem_slot), ncols);
+    }
     tc::tc_fence_before();
     __syncthreads();
+    __syncwarp();
+    if (CG == 2) tc::cluster_arrive();
+    kn::pdl_wait();
+    if (CG == 2) {
+        tc::cluster_wait();                            // the peer has its tensor memory, and its barriers exist before anything arrives on them
+        if (warp == 1) tc::tmem_relinquish_pair();
+    }
     tc::tc_fence_after();
     const uint32_t tmem = *tmem_slot;
-    kn::pdl_wait();
 
     if (warp == 0) {
         if (lane == 0) {
             int st = 0; uint32_t ph = 0;
             bool ok = true;
             LinearGradTile t;
-            for (int tile = blockIdx.x; tile < tiles && ok; tile += gridDim.x) {
+            for (int tile = tile0; tile < tiles && ok; tile += tile_step) {
                 t.set(p, tile);
                 for (int k = t.k0; k < t.k1; ++k) {
                     if (!(ok = tc::mbar_wait(empty0 + 8u * st, ph ^ 1u, abort_flag))) break;
                     const uint32_t sb = base + st * stage_bytes + kLgA, fb = full0 + 8u * st;
-                    tc::mbar_expect_tx(fb, (uint32_t)nb * 8192u);
-                    for (int j = 0; j < nb; ++j) tc::tma_load_2d(sb + j * 8192, &p.tmD, t.n * p.BN + 64 * j, k * kLgRows, fb);
+                    if (rank == 0) tc::mbar_expect_tx(fb, (uint32_t)(CG * nb) * 8192u);
+                    const int col = t.n * p.BN + rank * (p.BN / CG);
+                    for (int j = 0; j < nb; ++j) {
+                        if (CG == 2) tc::tma_load_2d_pair(sb + j * 8192, &p.tmD, col + 64 * j, k * kLgRows, tc::mapa_u32(fb, 0));
+                        else tc::tma_load_2d(sb + j * 8192, &p.tmD, col + 64 * j, k * kLgRows, fb);
+                    }
                     if (++st == stages) { st = 0; ph ^= 1u; }
                 }
             }
         }
     } else if (warp == 1) {
-        const uint32_t idesc = tc::instr_desc(p.BN, 1, 1);
+        if (rank == 0) {
+        const uint32_t idesc = tc::instr_desc(p.BN, 1, 1, 128 * CG);
         int st = 0; uint32_t ph = 0;
         int ab = 0; uint32_t aph = 0;
         bool ok = true;
         LinearGradTile t;
-        for (int tile = blockIdx.x; tile < tiles && ok; tile += gridDim.x) {
+        for (int tile = tile0; tile < tiles && ok; tile += tile_step) {
             t.set(p, tile);
             if (!(ok = tc::mbar_wait_warp(acce0 + 8u * ab, aph ^ 1u, abort_flag))) break;
+            if (CG == 2) tc::fence_acq_rel_cluster();  // the peer's epilogue arrived from the other CTA
             tc::tc_fence_after();
             const uint32_t d = tmem + (uint32_t)(ab * p.BN);
             for (int k = t.k0; k < t.k1; ++k) {
@@ -153,24 +175,25 @@ __global__ void __launch_bounds__(kLgThreads, 1) linear_grad_kernel(const __grid
                 const uint32_t sa = base + st * stage_bytes, sb = sa + kLgA;
                 #pragma unroll
                 for (int j = 0; j < 4; ++j)
-                    tc::umma(d, tc::smem_desc(sa + j * 2048, 8192, 1024), tc::smem_desc(sb + j * 2048, 8192, 1024), idesc, (k > t.k0 || j > 0) ? 1u : 0u);
-                tc::umma_commit(empty0 + 8u * st);
+                    tc::umma_cg<CG>(d, tc::smem_desc(sa + j * 2048, 8192, 1024), tc::smem_desc(sb + j * 2048, 8192, 1024), idesc, (k > t.k0 || j > 0) ? 1u : 0u);
+                tc::umma_commit_cg<CG>(empty0 + 8u * st);
                 if (++st == stages) { st = 0; ph ^= 1u; }
             }
             if (!ok) break;
-            tc::umma_commit(accf0 + 8u * ab);
+            tc::umma_commit_cg<CG>(accf0 + 8u * ab);
             if (++ab == 2) { ab = 0; aph ^= 1u; }
+        }
         }
     } else if (warp < 2 + kLgEpilogue) {
         const int quad = warp & 3, set = (warp - 2) >> 2;
         int ab = 0; uint32_t aph = 0;
         bool ok = true;
         LinearGradTile t;
-        for (int tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
+        for (int tile = tile0; tile < tiles; tile += tile_step) {
             t.set(p, tile);
             ok = ok && tc::mbar_wait_idle(accf0 + 8u * ab, aph, abort_flag);
             tc::tc_fence_after();
-            const int i = t.m * 128 + quad * 32 + lane, o0 = t.n * p.BN, nv = min(p.BN, p.n_out - o0);
+            const int i = (t.m * CG + rank) * 128 + quad * 32 + lane, o0 = t.n * p.BN, nv = min(p.BN, p.n_out - o0);
             float* out = p.out + (long long)t.z * p.n_out * p.n_in + (long long)(o0 + 32 * set) * p.n_in + i;
             const uint32_t ta = tmem + (uint32_t)(ab * p.BN) + ((uint32_t)(quad * 32) << 16);
             #pragma unroll 1
@@ -194,7 +217,10 @@ __global__ void __launch_bounds__(kLgThreads, 1) linear_grad_kernel(const __grid
             }
             tc::tc_fence_before();
             __syncwarp();
-            if (lane == 0) tc::mbar_arrive(acce0 + 8u * ab);
+            if (lane == 0) {
+                if (CG == 2) tc::mbar_arrive_cluster(tc::mapa_u32(acce0 + 8u * ab, 0));
+                else tc::mbar_arrive(acce0 + 8u * ab);
+            }
             if (++ab == 2) { ab = 0; aph ^= 1u; }
         }
     } else {
@@ -205,17 +231,17 @@ __global__ void __launch_bounds__(kLgThreads, 1) linear_grad_kernel(const __grid
         const int cb = td & 3, kr = (td >> 2) ^ (cb & 2);
         constexpr int PF = 2;                  // steps of the group whose codes are in flight
         LinearGradCodes f[PF];
-        int total = 0, tile = blockIdx.x, left = 0, row = 0;
+        int total = 0, tile = tile0, left = 0, row = 0;
         LinearGradTile t;
-        for (int k = blockIdx.x; k < tiles; k += gridDim.x) { t.set(p, k); total += t.k1 - t.k0; }
+        for (int k = tile0; k < tiles; k += tile_step) { t.set(p, k); total += t.k1 - t.k0; }
         const uint8_t *cp = nullptr, *ep = nullptr;
         int halves = 0;                        // of the block's two halves of 16 codes, how many there are in memory
         auto enter = [&] {                     // the next tile whose codes are to be loaded
             t.set(p, tile);
-            tile += gridDim.x;
+            tile += tile_step;
             left = t.k1 - t.k0;
             row = t.k0 * kLgRows + kr;
-            const int col = t.m * 128 + cb * 32;
+            const int col = (t.m * CG + rank) * 128 + cb * 32;
             halves = col >= p.n_in ? 0 : col + 16 < p.n_in ? 2 : 1;
             cp = p.codes + row * p.code_pitch + col;
             ep = p.scales + (long long)row * p.blocks + (col >> 5);
@@ -255,7 +281,10 @@ __global__ void __launch_bounds__(kLgThreads, 1) linear_grad_kernel(const __grid
                 else decode_block<FMT, false>(f[u], addr, swz);
                 tc::fence_async_smem();
                 __syncwarp();
-                if (lane == 0) tc::mbar_arrive(full0 + 8u * st);
+                if (lane == 0) {
+                    if (CG == 2) tc::mbar_arrive_remote(tc::mapa_u32(full0 + 8u * st, 0));
+                    else tc::mbar_arrive(full0 + 8u * st);
+                }
                 st += kLgGroups;
                 if (st >= stages) { st -= stages; ph ^= 1u; }
                 if (to_load > 0) load(f[u]);
@@ -270,10 +299,14 @@ __global__ void __launch_bounds__(kLgThreads, 1) linear_grad_kernel(const __grid
         while (clock64() - t0 < 2000000LL) { }
         __syncthreads();
     }
+    __syncwarp();
+    if (CG == 2) tc::cluster_sync_all();               // no CTA leaves while its peer may still arrive on its barriers
     if (warp == 1) {
         tc::tc_fence_after();
-        tc::tmem_dealloc(tmem, ncols);
+        if (CG == 2) tc::tmem_dealloc_pair(tmem, ncols);
+        else tc::tmem_dealloc(tmem, ncols);
     }
+    if (CG == 2) { __syncwarp(); tc::cluster_sync_all(); }      // nor before both have deallocated
 }
 
 // out[i] = sum over splits of partial[split][i], in that order

@@ -8,6 +8,7 @@
 #include <algorithm>
 #include <atomic>
 #include <cstdio>
+#include <cstdlib>
 #include <utility>
 
 #include "checkpoint.cuh"
@@ -30,16 +31,19 @@ struct Launcher {
     cudaStream_t st;
     cudaError_t e = cudaSuccess;
     size_t smem = 0;            // of the next launch
+    int cluster = 1;
     template <typename... KArgs, typename... Args>
     void operator()(void (*kernel)(KArgs...), long long grid, int block, Args&&... args) {
         if (e != cudaSuccess) return;
         cudaLaunchConfig_t lc{};
         lc.gridDim = dim3((unsigned)grid); lc.blockDim = block; lc.dynamicSmemBytes = smem; lc.stream = st;
-        smem = 0;
-        cudaLaunchAttribute at{};
-        at.id = cudaLaunchAttributeProgrammaticStreamSerialization;
-        at.val.programmaticStreamSerializationAllowed = 1;
-        lc.attrs = &at; lc.numAttrs = 1;
+        cudaLaunchAttribute at[2]{};
+        at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+        at[0].val.programmaticStreamSerializationAllowed = 1;
+        at[1].id = cudaLaunchAttributeClusterDimension;
+        at[1].val.clusterDim.x = cluster; at[1].val.clusterDim.y = 1; at[1].val.clusterDim.z = 1;
+        lc.attrs = at; lc.numAttrs = cluster > 1 ? 2 : 1;
+        smem = 0; cluster = 1;
         e = cudaLaunchKernelEx(&lc, kernel, std::forward<Args>(args)...);
     }
 };
@@ -232,7 +236,7 @@ PFN_cuTensorMapEncodeTiled_v12000 tensor_map_encoder() {
     return (PFN_cuTensorMapEncodeTiled_v12000)fn;
 }
 struct LinearPlan {
-    int BN, m_tiles, n_tiles, splits, steps, per, stages;
+    int cg, BN, m_tiles, n_tiles, splits, steps, per, stages;
     bool move_dy, move_x;               // copies with rows on 16-byte boundaries, where the rows are not
     long long dy_pitch, x_pitch;        // bytes
     size_t dy_at, x_at, bytes, smem;    // places in the workspace, behind the partial sums
@@ -240,27 +244,30 @@ struct LinearPlan {
 LinearPlan linear_plan(const alexnet_linear_weight_grad_t& a) {
     LinearPlan b{};
     b.steps = (int)ceil_div(a.rows, kLgRows);
-    b.m_tiles = (int)ceil_div(a.n_in, 128);
-    // The tile's width and the number of splits by a model of the launch in cycles: a step of 64 rows costs its operands' way through shared
-    // memory (written once, read once, 128 bytes a cycle), a tile some 1500 for its first loads and last stores, a second launch 4000 and
-    // its partial sums 2500 bytes a cycle.
+    // The tile's width, pairs or single CTAs and the number of splits by a model of the launch in cycles: a step of 64 rows costs its operands' way
+    // through shared memory (dy half of it in a pair) or its products, a tile some 1500 for its first loads and last stores, a second
+    // launch 4000 and its partial sums 2500 bytes a cycle.
     double best = 1e30;
-    for (int BN = 256; BN >= 32; BN /= 2) {
-        if (BN > 32 && BN / 2 >= a.n_out) continue;
-        const long long tiles = (long long)b.m_tiles * ceil_div(a.n_out, BN);
-        const double step = 256 + 2 * BN;
-        for (int s = 1; s <= 64; ++s) {
-            const long long per = ceil_div(std::max(1, b.steps), s);
-            if (s > 1 && (per < 4 || tiles * (s - 1) >= kSms)) break;
-            const int splits = (int)ceil_div(std::max(1, b.steps), per);
-            const double waves = (double)ceil_div(tiles * splits, kSms);
-            double cost = waves * (per * step + 1500) + 3.0 * BN;
-            if (splits > 1) cost += 4000 + (double)splits * a.n_in * a.n_out * 8 / 2500;
-            if (cost < best) { best = cost; b.BN = BN; b.splits = splits; b.per = (int)per; }
+    for (int cg = 1; cg <= 2; ++cg)
+        for (int BN = 256; BN >= 32; BN -= 32) {
+            if (BN > 32 && BN - 32 >= a.n_out) continue;
+            if (cg == 2 && (BN < 128 || a.n_in <= 128)) continue;
+            const long long tiles = ceil_div(a.n_in, 128 * cg) * ceil_div(a.n_out, BN), slots = kSms / cg;
+            const double step = cg == 2 ? std::max(384 + BN, 2 * BN) : 384 + 2 * BN;
+            for (int s = 1; s <= 64; ++s) {
+                const long long per = ceil_div(std::max(1, b.steps), s);
+                if (s > 1 && (per < 4 || tiles * (s - 1) >= slots)) break;
+                const int splits = (int)ceil_div(std::max(1, b.steps), per);
+                const double waves = (double)ceil_div(tiles * splits, slots);
+                double cost = waves * (per * step + 1500) + 3.0 * BN;
+                if (splits > 1) cost += 4000 + (double)splits * a.n_in * a.n_out * 8 / 2500;
+                if (cost < best) { best = cost; b.BN = BN; b.splits = splits; b.per = (int)per; b.cg = cg; }
+            }
         }
-    }
+    if (const char* f = getenv("LG_FORCE")) { sscanf(f, "%d,%d", &b.cg, &b.BN); b.splits = 1; b.per = b.steps; }
+    b.m_tiles = (int)ceil_div(a.n_in, 128 * b.cg);
     b.n_tiles = (int)ceil_div(a.n_out, b.BN);
-    const int stage = kLgA + (b.BN + 63) / 64 * 8192;
+    const int stage = kLgA + (b.BN / b.cg + 63) / 64 * 8192;
     b.stages = std::min(kLgMaxStages, (227 * 1024 - 1024 - 256) / stage);
     b.smem = tc::own_sm(1024 + (size_t)b.stages * stage + 256);
     b.dy_pitch = ceil_div(a.n_out, 8) * 16;
@@ -401,10 +408,12 @@ int alexnet_linear_weight_grad(const alexnet_linear_weight_grad_t* a, void* stre
     p.rows = (int)a->rows; p.n_in = a->n_in; p.n_out = a->n_out;
     p.BN = pl.BN; p.m_tiles = pl.m_tiles; p.n_tiles = pl.n_tiles; p.splits = pl.splits; p.steps = pl.steps; p.per = pl.per; p.stages = pl.stages;
     p.out = pl.splits > 1 ? (float*)a->workspace : a->dw;
-    auto* kernel = a->x.format == ALEXNET_CODES_INT8 ? linear_grad_kernel<kSrcInt8> : linear_grad_kernel<kSrcE4m3>;
+    auto* kernel = a->x.format == ALEXNET_CODES_INT8 ? (pl.cg == 2 ? linear_grad_kernel<kSrcInt8, 2> : linear_grad_kernel<kSrcInt8, 1>)
+                                                     : (pl.cg == 2 ? linear_grad_kernel<kSrcE4m3, 2> : linear_grad_kernel<kSrcE4m3, 1>);
     if (go.e == cudaSuccess) go.e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 227 * 1024);
     go.smem = pl.smem;
-    go(kernel, std::min<long long>(kSms, (long long)pl.m_tiles * pl.n_tiles * pl.splits), kLgThreads, p);
+    go.cluster = pl.cg;
+    go(kernel, pl.cg * std::min<long long>(kSms / pl.cg, (long long)pl.m_tiles * pl.n_tiles * pl.splits), kLgThreads, p);
     const long long n = (long long)a->n_in * a->n_out;
     if (pl.splits > 1) go(linear_grad_join_kernel, ceil_div(n, 1024), 256, (const float*)a->workspace, pl.splits, n, a->dw);
     return go.e == cudaSuccess ? ALEXNET_OK : err.cuda(go.e);
