@@ -8,8 +8,8 @@
 // its own tile of x again for every BN outputs.  An accumulator column then is 32 consecutive inputs of one output for each warp, which
 // leaves as one full 128-byte line.
 //
-// Warps: 0 = TMA producer (dy), 1 = MMA issuer and TMEM owner, 2..9 = epilogue (two sets of four), 10..25 = decoders, two groups
-// that take the steps in turn (a step takes a warp some 1100 cycles from its wait to its arrival, and the tensor cores 512).  Persistent over tiles with two
+// Warps: 0 = TMA producer (dy), 1 = MMA issuer and TMEM owner, 2..9 = epilogue (two sets of four), 10..25 = decoders, four groups
+// that take the steps in turn (a step takes a warp over 1000 cycles from its wait to its arrival, and the tensor cores 512).  Persistent over tiles with two
 // accumulators, so a tile's stores overlap the next one's products.  Few tiles with many rows are split over the rows; the
 // partial sums are added in a fixed order by a second kernel.  Every wait is bounded; a CTA whose wait runs out writes NaN and raises g_expired.
 #pragma once
@@ -17,8 +17,9 @@
 
 namespace op {
 
-constexpr int kLgRows = 64, kLgEpilogue = 8, kLgDecoders = 8, kLgGroups = 2;      // decoders of a step; groups of them
+constexpr int kLgRows = 64, kLgEpilogue = 8, kLgDecoders = 4, kLgGroups = 4;      // decoder warps of a step; groups of them
 constexpr int kLgThreads = 32 * (2 + kLgEpilogue + kLgGroups * kLgDecoders);
+constexpr int kLgShare = kLgRows * 4 / (32 * kLgDecoders);     // checkpoint blocks of a step that a decoder takes: rows 8 kLgDecoders apart
 constexpr int kLgA = 128 * kLgRows * 2;            // bytes of the decoded tile of a stage: two boxes of 64 features x 64 rows
 constexpr int kLgMaxStages = 6;
 struct LinearGradParams {
@@ -44,8 +45,7 @@ struct LinearGradTile {                            // tiles: input tile fastest,
         k1 = min(p.steps, k0 + p.per);
     }
 };
-// a decoder's share of a stage: a checkpoint block of one row
-struct LinearGradCodes { uint4 c[2]; uint32_t e; };
+struct LinearGradCodes { uint4 c[2]; uint32_t e; };      // a checkpoint block of one row
 
 // Sixteen codes to bf16 pairs, s2 = the scale twice.  int8: the code + 128 as the low byte of 2^23 + that, times the scale, less (2^23 + 128)
 // times the scale, in one multiply-add: exact, unless the product passes fp32's range (exponents that only magnitudes above 2^109 have).
@@ -229,8 +229,7 @@ __global__ void __launch_bounds__(kLgThreads, 1) linear_grad_kernel(const __grid
         // rows) write to eight different bank groups.
         const int group = (warp - 2 - kLgEpilogue) / kLgDecoders, td = (threadIdx.x - 32 * (2 + kLgEpilogue)) % (32 * kLgDecoders);
         const int cb = td & 3, kr = (td >> 2) ^ (cb & 2);
-        constexpr int PF = 2;                  // steps of the group whose codes are in flight
-        LinearGradCodes f[PF];
+        LinearGradCodes f[kLgShare];           // of the group's next step: in flight while the other groups decode theirs
         int total = 0, tile = tile0, left = 0, row = 0;
         LinearGradTile t;
         for (int k = tile0; k < tiles; k += tile_step) { t.set(p, k); total += t.k1 - t.k0; }
@@ -257,38 +256,44 @@ __global__ void __launch_bounds__(kLgThreads, 1) linear_grad_kernel(const __grid
         enter();
         int to_load = total - group;
         if (to_load > 0) forward(group);
-        auto load = [&](LinearGradCodes& r) {
-            const bool in = row < p.rows;
-            r.c[0] = in && halves > 0 ? __ldg((const uint4*)cp) : make_uint4(0u, 0u, 0u, 0u);
-            r.c[1] = in && halves > 1 ? __ldg((const uint4*)cp + 1) : make_uint4(0u, 0u, 0u, 0u);
-            r.e = in && halves > 0 ? __ldg(ep) : 0u;
+        auto load = [&] {
+            #pragma unroll
+            for (int u = 0; u < kLgShare; ++u) {
+                LinearGradCodes& r = f[u];
+                const bool in = row + 8 * kLgDecoders * u < p.rows;
+                const uint8_t *c = cp + u * (step_c / kLgShare), *e = ep + u * (step_e / kLgShare);
+                r.c[0] = in && halves > 0 ? __ldg((const uint4*)c) : make_uint4(0u, 0u, 0u, 0u);
+                r.c[1] = in && halves > 1 ? __ldg((const uint4*)c + 1) : make_uint4(0u, 0u, 0u, 0u);
+                r.e = in && halves > 0 ? __ldg(e) : 0u;
+            }
             to_load -= kLgGroups;
             if (to_load > 0) forward(kLgGroups);
         };
-        #pragma unroll
-        for (int u = 0; u < PF; ++u)
-            if (to_load > 0) load(f[u]);
+        if (to_load > 0) load();
         const uint32_t off = (uint32_t)(cb >> 1) * 8192u + (uint32_t)kr * 128u, swz = (uint32_t)((4 * (cb & 1)) ^ (kr & 7)) << 4;
         int st = group; uint32_t ph = 0;
-        bool ok = true;
-        for (int s = group; s < total && ok; s += kLgGroups * PF) {
+        for (int s = group; s < total; s += kLgGroups) {
+            while (st >= stages) { st -= stages; ph ^= 1u; }
+            if (!tc::mbar_wait_idle(empty0 + 8u * st, ph ^ 1u, abort_flag)) break;
+            const uint32_t addr = base + st * stage_bytes + off;
+            bool small = true;
             #pragma unroll
-            for (int u = 0; u < PF; ++u) {
-                if (s + kLgGroups * u >= total || !ok) break;
-                if (!(ok = tc::mbar_wait_idle(empty0 + 8u * st, ph ^ 1u, abort_flag))) break;
-                const uint32_t addr = base + st * stage_bytes + off;
-                if (FMT == kSrcInt8 && __all_sync(~0u, f[u].e < 230u)) decode_block<FMT, FMT == kSrcInt8>(f[u], addr, swz);
-                else decode_block<FMT, false>(f[u], addr, swz);
-                tc::fence_async_smem();
-                __syncwarp();
-                if (lane == 0) {
-                    if (CG == 2) tc::mbar_arrive_remote(tc::mapa_u32(full0 + 8u * st, 0));
-                    else tc::mbar_arrive(full0 + 8u * st);
-                }
-                st += kLgGroups;
-                if (st >= stages) { st -= stages; ph ^= 1u; }
-                if (to_load > 0) load(f[u]);
+            for (int u = 0; u < kLgShare; ++u) small = small && f[u].e < 230u;
+            if (FMT == kSrcInt8 && __all_sync(~0u, small)) {
+                #pragma unroll
+                for (int u = 0; u < kLgShare; ++u) decode_block<FMT, FMT == kSrcInt8>(f[u], addr + 1024u * kLgDecoders * u, swz);
+            } else {
+                #pragma unroll
+                for (int u = 0; u < kLgShare; ++u) decode_block<FMT, false>(f[u], addr + 1024u * kLgDecoders * u, swz);
             }
+            tc::fence_async_smem();
+            __syncwarp();
+            if (lane == 0) {
+                if (CG == 2) tc::mbar_arrive_remote(tc::mapa_u32(full0 + 8u * st, 0));
+                else tc::mbar_arrive(full0 + 8u * st);
+            }
+            st += kLgGroups;
+            if (to_load > 0) load();
         }
     }
     tc::tc_fence_before();
