@@ -10,8 +10,8 @@
 //
 // Warps: 0 = TMA producer (dy), 1 = MMA issuer and TMEM owner, 2..9 = epilogue (two sets of four), 10..25 = decoders, four groups
 // that take the steps in turn (a step takes a warp over 1000 cycles from its wait to its arrival, and the tensor cores 512).  Persistent over tiles with two
-// accumulators, so a tile's stores overlap the next one's products.  Few tiles with many rows are split over the rows; the
-// partial sums are added in a fixed order by a second kernel.  Every wait is bounded; a CTA whose wait runs out writes NaN and raises g_expired.
+// accumulators, so a tile's stores overlap the next one's products.  Where the tiles do not fill the last
+// round of CTAs (or any), those of that round are split over the rows; a second kernel adds their partial sums in a fixed order.  Every wait is bounded; a CTA whose wait runs out writes NaN and raises g_expired.
 #pragma once
 #include "checkpoint.cuh"
 
@@ -28,21 +28,30 @@ struct LinearGradParams {
     long long code_pitch;                          // bytes; a multiple of 16
     int blocks;                                    // scales per row
     int rows, n_in, n_out;
-    int BN, m_tiles, n_tiles, splits, steps, per;  // steps of 64 rows: in all, and of one split
+    int BN, m_tiles, tiles, steps;                 // steps of 64 rows
+    int whole, splits, per;                        // the first `whole` tiles take all rows; each of the others is `splits` units of `per` steps
     int stages;
-    float* out;                                    // dw, or partial sums [split][n_out][n_in]
+    float* out;
+    float* partial;                                // sums of the split tiles: [split][tile - whole][BN][128 CG]
 };
 __device__ int g_expired;
 
-struct LinearGradTile {                            // tiles: input tile fastest, then output tile, then split
-    int m, n, z, k0, k1;
-    __device__ __forceinline__ void set(const LinearGradParams& p, int tile) {
+// A unit of work, in the order in which the CTAs take them: the whole tiles (input tile fastest), then the split ones, split by split.
+struct LinearGradTile {
+    int m, n, k0, k1, part;                        // part: index of the unit's partial sums, or -1
+    __device__ __forceinline__ void set(const LinearGradParams& p, int unit) {
+        int tile = unit, z = 0;
+        part = -1;
+        if (unit >= p.whole) {
+            const int rest = p.tiles - p.whole;
+            z = (unit - p.whole) / rest;
+            tile = unit - z * rest;
+            if (p.splits > 1) part = unit - p.whole;
+        }
         m = tile % p.m_tiles;
-        const int r = tile / p.m_tiles;
-        n = r % p.n_tiles;
-        z = r / p.n_tiles;
+        n = tile / p.m_tiles;
         k0 = z * p.per;
-        k1 = min(p.steps, k0 + p.per);
+        k1 = part < 0 ? p.steps : min(p.steps, k0 + p.per);
     }
 };
 struct LinearGradCodes { uint4 c[2]; uint32_t e; };      // a checkpoint block of one row
@@ -107,7 +116,7 @@ __global__ void __launch_bounds__(kLgThreads, 1) linear_grad_kernel(const __grid
     volatile uint32_t* tmem_slot = (volatile uint32_t*)(gen + 160);
     const uint32_t full0 = bar, empty0 = bar + 64u, accf0 = bar + 128u, acce0 = bar + 144u;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int tiles = p.m_tiles * p.n_tiles * p.splits;
+    const int tiles = p.whole + (p.tiles - p.whole) * p.splits;      // units
     uint32_t ncols = 32;
     while ((int)ncols < 2 * p.BN) ncols <<= 1;
 
@@ -194,24 +203,27 @@ __global__ void __launch_bounds__(kLgThreads, 1) linear_grad_kernel(const __grid
             ok = ok && tc::mbar_wait_idle(accf0 + 8u * ab, aph, abort_flag);
             tc::tc_fence_after();
             const int i = (t.m * CG + rank) * 128 + quad * 32 + lane, o0 = t.n * p.BN, nv = min(p.BN, p.n_out - o0);
-            float* out = p.out + (long long)t.z * p.n_out * p.n_in + (long long)(o0 + 32 * set) * p.n_in + i;
+            // dw[o][i], or the unit's partial sums [column][input]
+            const bool part = t.part >= 0, mine = part || i < p.n_in;
+            const long long pitch = part ? 128 * CG : p.n_in;
+            float* out = part ? p.partial + ((long long)t.part * p.BN + 32 * set) * (128 * CG) + rank * 128 + quad * 32 + lane : p.out + (long long)(o0 + 32 * set) * p.n_in + i;
             const uint32_t ta = tmem + (uint32_t)(ab * p.BN) + ((uint32_t)(quad * 32) << 16);
             #pragma unroll 1
-            for (int c = 32 * set; c < nv; c += 64, out += 64ll * p.n_in) {
+            for (int c = 32 * set; c < nv; c += 64, out += 64 * pitch) {
                 uint32_t v[32];
                 if (ok) { tc::tmem_ld32(ta + (uint32_t)c, v); tc::tmem_ld_wait(); }
                 else {
                     #pragma unroll
                     for (int q = 0; q < 32; ++q) v[q] = 0x7fffffffu;
                 }
-                if (i < p.n_in) {
+                if (mine) {
                     float* o = out;
                     if (c + 32 <= nv) {
                         #pragma unroll
-                        for (int q = 0; q < 32; ++q) { *o = __uint_as_float(v[q]); o += p.n_in; }
+                        for (int q = 0; q < 32; ++q) { *o = __uint_as_float(v[q]); o += pitch; }
                     } else {
                         #pragma unroll
-                        for (int q = 0; q < 32; ++q) { if (c + q < nv) *o = __uint_as_float(v[q]); o += p.n_in; }
+                        for (int q = 0; q < 32; ++q) { if (c + q < nv) *o = __uint_as_float(v[q]); o += pitch; }
                     }
                 }
             }
@@ -314,25 +326,51 @@ __global__ void __launch_bounds__(kLgThreads, 1) linear_grad_kernel(const __grid
     if (CG == 2) { __syncwarp(); tc::cluster_sync_all(); }      // nor before both have deallocated
 }
 
-// out[i] = sum over splits of partial[split][i], in that order
-__global__ void __launch_bounds__(256) linear_grad_join_kernel(const float* __restrict__ partial, int splits, long long n, float* __restrict__ out) {
+// dw of the split tiles: the sums of their splits, added in that order.  A thread takes four inputs of a column and J columns in turn, with the loads of
+// eight partial sums in flight; bound by their way from L2.  (One value per thread: 36 us for the 18 MB of 34 tiles of 256 x 256 in two
+// splits, four times as long: the blocks' set-up.)
+template <int J>
+__global__ void __launch_bounds__(256) linear_grad_join_kernel(const float* __restrict__ partial, float* __restrict__ dw, int n_in, int n_out, int m_tiles, int whole, int rest, int splits, int BN,
+                                                               int rows /* 128 CG */) {
     kn::pdl_sync();
-    const long long i = ((long long)blockIdx.x * 256 + threadIdx.x) * 4;
-    if (i + 4 <= n && n % 4 == 0) {
-        float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
-        #pragma unroll 8
-        for (int z = 0; z < splits; ++z) {
-            const float4 t = *(const float4*)(partial + z * n + i);
-            s.x += t.x; s.y += t.y; s.z += t.z; s.w += t.w;
+    const int lanes = rows / 4, at_once = 256 / lanes, blocks = (BN + J * at_once - 1) / (J * at_once);
+    const int t = blockIdx.x / blocks, tile = whole + t, n = tile / m_tiles, m = tile - n * m_tiles;
+    const int c0 = (blockIdx.x - t * blocks) * J * at_once + threadIdx.x / lanes, r = threadIdx.x % lanes * 4, i = m * rows + r;
+    if (i >= n_in) return;
+    const long long stride = (long long)rest * BN * rows;
+    const float* src = partial + (long long)t * BN * rows + r;
+    constexpr int Z = 8 / J;                           // splits whose sums are in flight
+    float4 s[J];
+    #pragma unroll
+    for (int j = 0; j < J; ++j) s[j] = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int z0 = 0; z0 < splits; z0 += Z) {
+        float4 v[Z][J];
+        #pragma unroll
+        for (int q = 0; q < Z; ++q)
+            #pragma unroll
+            for (int j = 0; j < J; ++j) {
+                const int c = c0 + j * at_once;
+                v[q][j] = z0 + q < splits && c < BN ? __ldcg((const float4*)(src + (z0 + q) * stride + (long long)c * rows)) : make_float4(0.f, 0.f, 0.f, 0.f);
+            }
+        #pragma unroll
+        for (int q = 0; q < Z; ++q)
+            #pragma unroll
+            for (int j = 0; j < J; ++j) { s[j].x += v[q][j].x; s[j].y += v[q][j].y; s[j].z += v[q][j].z; s[j].w += v[q][j].w; }
+    }
+    const bool vec = n_in % 4 == 0 && ((uintptr_t)dw & 15) == 0;
+    #pragma unroll
+    for (int j = 0; j < J; ++j) {
+        const int c = c0 + j * at_once, o = n * BN + c;
+        if (c >= BN || o >= n_out) continue;
+        float* d = dw + (long long)o * n_in + i;
+        if (vec) *(float4*)d = s[j];
+        else {
+            d[0] = s[j].x;
+            if (i + 1 < n_in) d[1] = s[j].y;
+            if (i + 2 < n_in) d[2] = s[j].z;
+            if (i + 3 < n_in) d[3] = s[j].w;
         }
-        if (((uintptr_t)out & 15) == 0) *(float4*)(out + i) = s;
-        else { out[i] = s.x; out[i + 1] = s.y; out[i + 2] = s.z; out[i + 3] = s.w; }
-    } else
-        for (long long j = i; j < min(n, i + 4); ++j) {
-            float s = 0.f;
-            for (int z = 0; z < splits; ++z) s += partial[z * n + j];
-            out[j] = s;
-        }
+    }
 }
 
 // Rows of `bytes` bytes (a multiple of UNIT), `src_pitch` apart, to rows `pitch` apart that start on 16-byte boundaries, zeros behind them: for

@@ -8,7 +8,6 @@
 #include <algorithm>
 #include <atomic>
 #include <cstdio>
-#include <cstdlib>
 #include <utility>
 
 #include "checkpoint.cuh"
@@ -236,7 +235,7 @@ PFN_cuTensorMapEncodeTiled_v12000 tensor_map_encoder() {
     return (PFN_cuTensorMapEncodeTiled_v12000)fn;
 }
 struct LinearPlan {
-    int cg, BN, m_tiles, n_tiles, splits, steps, per, stages;
+    int cg, BN, m_tiles, tiles, steps, whole, splits, per, stages;
     bool move_dy, move_x;               // copies with rows on 16-byte boundaries, where the rows are not
     long long dy_pitch, x_pitch;        // bytes
     size_t dy_at, x_at, bytes, smem;    // places in the workspace, behind the partial sums
@@ -244,29 +243,28 @@ struct LinearPlan {
 LinearPlan linear_plan(const alexnet_linear_weight_grad_t& a) {
     LinearPlan b{};
     b.steps = (int)ceil_div(a.rows, kLgRows);
-    // The tile's width, pairs or single CTAs and the number of splits by a model of the launch in cycles: a step of 64 rows costs its operands' way
-    // through shared memory (dy half of it in a pair) or its products, a tile some 1500 for its first loads and last stores, a second
-    // launch 4000 and its partial sums 2500 bytes a cycle.
+    // The tile's width, pairs or single CTAs and the splits of the last round by a model of the launch in cycles, fitted to measurements (BN 128 to
+    // 256): a step of 64 rows costs 480 + 1.6 BN, in a pair 420 + 1.4 BN (half of dy's way through shared memory); a tile no less
+    // than its stores, and 1500 or 2500 around them; a second launch 4000, and its partial sums 2500 bytes a cycle.
     double best = 1e30;
     for (int cg = 1; cg <= 2; ++cg)
         for (int BN = 256; BN >= 32; BN -= 32) {
             if (BN > 32 && BN - 32 >= a.n_out) continue;
             if (cg == 2 && (BN < 128 || a.n_in <= 128)) continue;
             const long long tiles = ceil_div(a.n_in, 128 * cg) * ceil_div(a.n_out, BN), slots = kSms / cg;
-            const double step = cg == 2 ? std::max(384 + BN, 2 * BN) : 384 + 2 * BN;
+            const double step = cg == 2 ? 420 + 1.4 * BN : 480 + 1.6 * BN, around = cg == 2 ? 2500 : 1500;
+            auto round = [&](long long steps) { return std::max(steps * step, 22.0 * BN) + around; };
             for (int s = 1; s <= 64; ++s) {
                 const long long per = ceil_div(std::max(1, b.steps), s);
-                if (s > 1 && (per < 4 || tiles * (s - 1) >= slots)) break;
                 const int splits = (int)ceil_div(std::max(1, b.steps), per);
-                const double waves = (double)ceil_div(tiles * splits, slots);
-                double cost = waves * (per * step + 1500) + 3.0 * BN;
-                if (splits > 1) cost += 4000 + (double)splits * a.n_in * a.n_out * 8 / 2500;
-                if (cost < best) { best = cost; b.BN = BN; b.splits = splits; b.per = (int)per; b.cg = cg; }
+                const long long whole = splits > 1 ? tiles / slots * slots : tiles, rest = tiles - whole;
+                if (s > 1 && (per < 4 || rest * (s - 1) >= slots)) break;
+                double cost = (double)ceil_div(whole, slots) * round(b.steps);
+                if (rest) cost += (double)ceil_div(rest * splits, slots) * round(per) + 4000 + (double)splits * rest * 128 * cg * BN * 8 / 2500;
+                if (cost < best) { best = cost; b.cg = cg; b.BN = BN; b.tiles = (int)tiles; b.whole = (int)whole; b.splits = splits; b.per = (int)per; }
             }
         }
-    if (const char* f = getenv("LG_FORCE")) { sscanf(f, "%d,%d", &b.cg, &b.BN); b.splits = 1; b.per = b.steps; }
     b.m_tiles = (int)ceil_div(a.n_in, 128 * b.cg);
-    b.n_tiles = (int)ceil_div(a.n_out, b.BN);
     const int stage = kLgA + (b.BN / b.cg + 63) / 64 * 8192;
     b.stages = std::min(kLgMaxStages, (227 * 1024 - 1024 - 256) / stage);
     b.smem = tc::own_sm(1024 + (size_t)b.stages * stage + 256);
@@ -274,7 +272,7 @@ LinearPlan linear_plan(const alexnet_linear_weight_grad_t& a) {
     b.x_pitch = ceil_div(a.n_in, 16) * 16;
     b.move_dy = (uintptr_t)a.dy % 16 != 0 || (a.rows > 1 && (a.dy_stride % 8 != 0 || a.dy_stride < a.n_out));
     b.move_x = (uintptr_t)a.x.codes % 16 != 0 || a.n_in % 16 != 0;
-    b.dy_at = b.splits > 1 ? ((size_t)b.splits * a.n_in * a.n_out * sizeof(float) + 255) / 256 * 256 : 0;
+    b.dy_at = (size_t)b.splits * (b.tiles - b.whole) * b.BN * 128 * b.cg * sizeof(float);
     b.x_at = b.dy_at + (b.move_dy ? ((size_t)a.rows * b.dy_pitch + 255) / 256 * 256 : 0);
     b.bytes = b.x_at + (b.move_x ? (size_t)a.rows * b.x_pitch : 0) + 256;
     return b;
@@ -406,16 +404,22 @@ int alexnet_linear_weight_grad(const alexnet_linear_weight_grad_t* a, void* stre
     p.scales = a->x.scales;
     p.blocks = (int)ceil_div(a->n_in, 32);
     p.rows = (int)a->rows; p.n_in = a->n_in; p.n_out = a->n_out;
-    p.BN = pl.BN; p.m_tiles = pl.m_tiles; p.n_tiles = pl.n_tiles; p.splits = pl.splits; p.steps = pl.steps; p.per = pl.per; p.stages = pl.stages;
-    p.out = pl.splits > 1 ? (float*)a->workspace : a->dw;
+    p.BN = pl.BN; p.m_tiles = pl.m_tiles; p.tiles = pl.tiles; p.steps = pl.steps; p.whole = pl.whole; p.splits = pl.splits; p.per = pl.per; p.stages = pl.stages;
+    p.out = a->dw;
+    p.partial = (float*)a->workspace;
     auto* kernel = a->x.format == ALEXNET_CODES_INT8 ? (pl.cg == 2 ? linear_grad_kernel<kSrcInt8, 2> : linear_grad_kernel<kSrcInt8, 1>)
                                                      : (pl.cg == 2 ? linear_grad_kernel<kSrcE4m3, 2> : linear_grad_kernel<kSrcE4m3, 1>);
     if (go.e == cudaSuccess) go.e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 227 * 1024);
     go.smem = pl.smem;
     go.cluster = pl.cg;
-    go(kernel, pl.cg * std::min<long long>(kSms / pl.cg, (long long)pl.m_tiles * pl.n_tiles * pl.splits), kLgThreads, p);
-    const long long n = (long long)a->n_in * a->n_out;
-    if (pl.splits > 1) go(linear_grad_join_kernel, ceil_div(n, 1024), 256, (const float*)a->workspace, pl.splits, n, a->dw);
+    const long long rest = pl.tiles - pl.whole;
+    go(kernel, pl.cg * std::min<long long>(kSms / pl.cg, pl.whole + rest * pl.splits), kLgThreads, p);
+    if (rest) {      // four columns at a time where there are enough tiles to fill the device so
+        const int rows = 128 * pl.cg, at_once = 1024 / rows;
+        const bool four = rest * (pl.BN / (4 * at_once)) >= kSms;
+        go(four ? linear_grad_join_kernel<4> : linear_grad_join_kernel<1>, rest * ceil_div(pl.BN, (four ? 4 : 1) * at_once), 256, (const float*)p.partial, p.out, p.n_in, p.n_out, p.m_tiles, p.whole,
+           (int)rest, p.splits, p.BN, rows);
+    }
     return go.e == cudaSuccess ? ALEXNET_OK : err.cuda(go.e);
 }
 
