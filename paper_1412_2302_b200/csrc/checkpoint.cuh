@@ -98,6 +98,17 @@ struct Geo {
     }
 };
 
+// A thread's walk over positions that lie `step` apart: its offset in a tensor, by one addition where the tensor is flat.
+struct Cursor {
+    long long off;
+    uint32_t p;
+    __device__ __forceinline__ Cursor(const Geo& g, uint32_t p0) : off(g.at(p0)), p(p0) {}
+    __device__ __forceinline__ void next(const Geo& g, int step) {
+        if (g.flat) off += (long long)step * g.sw;
+        else { p += step; off = g.at(p); }
+    }
+};
+
 // ---------------------------------------------------------------- codes
 __device__ __forceinline__ float scale_of(uint32_t e) {         // 2^(e - 127); e = 0: a subnormal; 255: NaN
     return e == 255u ? __uint_as_float(0x7fffffffu) : __uint_as_float(e ? e << 23 : 1u << 22);
@@ -120,8 +131,15 @@ __device__ __forceinline__ Raw<uint8_t, V> codes_of(const float* f, float inv, b
     Raw<uint8_t, V> r;
     if constexpr (FMT == kSrcInt8) {
         uint32_t b[V];
-        #pragma unroll
-        for (int i = 0; i < V; ++i) b[i] = __float_as_uint(fmaf(f[i], inv, 12582912.f));
+        if constexpr (V >= 2) {
+            const f2 i2 = mk2(inv, inv), m2 = mk2(12582912.f, 12582912.f);
+            #pragma unroll
+            for (int i = 0; i < V; i += 2) {
+                float lo, hi;
+                un2(fma2(mk2(f[i], f[i + 1]), i2, m2), lo, hi);
+                b[i] = __float_as_uint(lo); b[i + 1] = __float_as_uint(hi);
+            }
+        } else b[0] = __float_as_uint(fmaf(f[0], inv, 12582912.f));
         if constexpr (V >= 4) {
             uint32_t* u = (uint32_t*)&r;
             #pragma unroll
@@ -161,7 +179,9 @@ __device__ __forceinline__ void code_values(const Raw<uint8_t, V>& r, float* f) 
             for (int i = 0; i < V / 4; ++i) {
                 const uint32_t t = u[i] ^ 0x80808080u;       // code + 128 as an unsigned byte, then 2^23 + that as a float
                 #pragma unroll
-                for (int k = 0; k < 4; ++k) f[4 * i + k] = __uint_as_float(__byte_perm(t, 0x4b000000u, 0x7440u | k)) - 8388736.f;
+                for (int k = 0; k < 4; k += 2)
+                    un2(add2(mk2(__uint_as_float(__byte_perm(t, 0x4b000000u, 0x7440u | k)), __uint_as_float(__byte_perm(t, 0x4b000000u, 0x7441u | k))), mk2(-8388736.f, -8388736.f)),
+                        f[4 * i + k], f[4 * i + k + 1]);
             }
         } else {
             const int8_t* u = (const int8_t*)&r;
@@ -185,32 +205,48 @@ __device__ __forceinline__ void code_values(const Raw<uint8_t, V>& r, float* f) 
         }
     }
 }
-// the largest magnitude of eight values as the bits of a float: an unsigned comparison of magnitudes puts NaN above infinity above all others
-template <int V>
-__device__ __forceinline__ uint32_t amax_bits(const float* f) {
-    uint32_t m = 0;
-    #pragma unroll
-    for (int i = 0; i < V; ++i) m = max(m, __float_as_uint(f[i]) & 0x7fffffffu);
-    return m;
+// The largest magnitude of eight values as the bits of a float.  Magnitudes compare as unsigned integers, NaN above infinity above all others; 16-bit
+// types are compared in pairs (a NaN stays one).
+template <typename T>
+__device__ __forceinline__ uint32_t amax_bits(const Raw<T, 8>& r) {
+    const uint32_t* u = (const uint32_t*)&r;
+    if constexpr (sizeof(T) == 2) {
+        uint32_t m = u[0] & 0x7fff7fffu;
+        #pragma unroll
+        for (int i = 1; i < 4; ++i) {
+            if constexpr (std::is_same<T, __nv_bfloat16>::value) asm("max.NaN.bf16x2 %0, %0, %1;" : "+r"(m) : "r"(u[i] & 0x7fff7fffu));
+            else asm("max.NaN.f16x2 %0, %0, %1;" : "+r"(m) : "r"(u[i] & 0x7fff7fffu));
+        }
+        const uint32_t top = max(m >> 16, m & 0xffffu);
+        if constexpr (std::is_same<T, __nv_bfloat16>::value) return top << 16;
+        else return __float_as_uint(__half2float(__ushort_as_half((unsigned short)top)));
+    } else {
+        uint32_t m = 0;
+        #pragma unroll
+        for (int i = 0; i < 8; ++i) m = max(m, u[i] & 0x7fffffffu);
+        return m;
+    }
 }
-// Codes and exponents of one position's vector, called by the four lanes of a block together (the lanes of a row's last block that hold
-// no channels pass zeros and store nothing).  col: vector within the row; row: position within the tensor.
-template <int FMT>
-__device__ __forceinline__ void store_codes(const float* f, bool has, uint8_t* codes, uint8_t* scales, long long row, int col, int C, int blocks) {
+// Codes and exponent of a vector, called by the four lanes of a block together (the lanes of a row's last block that hold no channels pass zeros and
+// store nothing).  r, f: the vector as it is stored, and its values; codes, scales: where its codes and its block's exponent go.
+template <typename T, int FMT>
+__device__ __forceinline__ void store_codes(const Raw<T, 8>& r, const float* f, bool has, uint8_t* codes, uint8_t* scales) {
     const uint32_t quad = 0xfu << (threadIdx.x & 28);
-    uint32_t m = amax_bits<8>(f);
+    uint32_t m = amax_bits<T>(r);
     m = max(m, __shfl_xor_sync(quad, m, 1));
     m = max(m, __shfl_xor_sync(quad, m, 2));
     const uint32_t e = scale_byte<FMT>(m);
     if (has) {
-        *(uint2*)(codes + row * C + 8 * col) = codes_of<FMT, 8>(f, inverse_scale(e), e == 255u);
-        if ((col & 3) == 0) scales[row * blocks + (col >> 2)] = (uint8_t)e;
+        *(uint2*)codes = codes_of<FMT, 8>(f, inverse_scale(e), e == 255u);
+        if ((threadIdx.x & 3) == 0) *scales = (uint8_t)e;
     }
 }
-__device__ __forceinline__ void store_codes(int fmt, const float* f, bool has, uint8_t* codes, uint8_t* scales, long long row, int col, int C, int blocks) {
-    if (fmt == kSrcInt8) store_codes<kSrcInt8>(f, has, codes, scales, row, col, C, blocks);
-    else store_codes<kSrcE4m3>(f, has, codes, scales, row, col, C, blocks);
-}
+// where a thread's codes go, position by position
+struct CodesCursor {
+    uint8_t *codes, *scales;
+    __device__ __forceinline__ CodesCursor(uint8_t* c, uint8_t* s, long long row, int vec, int C) : codes(c + row * C + 8 * vec), scales(s + row * ((C + 31) / 32) + (vec >> 2)) {}
+    __device__ __forceinline__ void next(int step, int C) { codes += (long long)step * C; scales += (long long)step * ((C + 31) / 32); }
+};
 
 // How a launch walks a tensor: a block takes the positions [chunk * ppc, + ppc) of a sample and `cols` vectors of V channels; thread
 // (row, col) takes every `rows`-th position of its vector.  With V = 8 the vectors of a row are counted up to a multiple of four, so that
@@ -239,57 +275,62 @@ __device__ __forceinline__ Spot spot(const Walk& w) {
 
 // ---------------------------------------------------------------- encode, decode
 // Rows of a multiple of eight channels at 16-byte boundaries: four lanes per block.  HBM-bound: 2 bytes read and 1.03 written per bf16 value.
-template <typename T>
-__global__ void __launch_bounds__(256) checkpoint_encode_kernel(const T* __restrict__ x, const Geo g, const Walk w, int fmt, uint8_t* __restrict__ codes, uint8_t* __restrict__ scales) {
+template <typename T, int FMT>
+__global__ void __launch_bounds__(256) checkpoint_encode_kernel(const T* __restrict__ x, const Geo g, const Walk w, uint8_t* __restrict__ codes, uint8_t* __restrict__ scales) {
     kn::pdl_sync();
     const Spot s = spot(w);
     if (!s.on) return;
     const T* xp = x + s.n * g.sn + 8 * s.v;
-    const int blocks = (w.C + 31) / 32;
     constexpr int U = 4;
+    Cursor c(g, s.p0 + s.row);
+    CodesCursor k(codes, scales, s.n * w.HW + s.p0 + s.row, s.v, w.C);
     for (int p = s.p0 + s.row; p < s.p1; p += U * w.rows) {
-        Raw<T, 8> r[U];
+        Raw<T, 8> r[U] = {};
         #pragma unroll
-        for (int u = 0; u < U; ++u)
-            if (s.has && p + u * w.rows < s.p1) r[u] = *(const Raw<T, 8>*)(xp + g.at(p + u * w.rows));
+        for (int u = 0; u < U; ++u) {
+            if (s.has && p + u * w.rows < s.p1) r[u] = *(const Raw<T, 8>*)(xp + c.off);
+            c.next(g, w.rows);
+        }
         #pragma unroll
-        for (int u = 0; u < U; ++u)
+        for (int u = 0; u < U; ++u) {
             if (p + u * w.rows < s.p1) {
-                float f[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-                if (s.has) unpack<T, 8>(r[u], f);
-                store_codes(fmt, f, s.has, codes, scales, s.n * w.HW + p + u * w.rows, s.v, w.C, blocks);
+                float f[8];
+                unpack<T, 8>(r[u], f);
+                store_codes<T, FMT>(r[u], f, s.has, k.codes, k.scales);
             }
+            k.next(w.rows, w.C);
+        }
     }
 }
-template <typename T>
-__global__ void __launch_bounds__(256) checkpoint_decode_kernel(const uint8_t* __restrict__ codes, const uint8_t* __restrict__ scales, int fmt, const Geo g, const Walk w, T* __restrict__ out) {
+template <typename T, int FMT>
+__global__ void __launch_bounds__(256) checkpoint_decode_kernel(const uint8_t* __restrict__ codes, const uint8_t* __restrict__ scales, const Geo g, const Walk w, T* __restrict__ out) {
     kn::pdl_sync();
     const Spot s = spot(w);
     if (!s.has) return;
     T* op = out + s.n * g.sn + 8 * s.v;
-    const int blocks = (w.C + 31) / 32;
     constexpr int U = 4;
+    Cursor c(g, s.p0 + s.row);
+    CodesCursor k(const_cast<uint8_t*>(codes), const_cast<uint8_t*>(scales), s.n * w.HW + s.p0 + s.row, s.v, w.C);
     for (int p = s.p0 + s.row; p < s.p1; p += U * w.rows) {
         uint2 r[U];
         uint8_t e[U];
         #pragma unroll
-        for (int u = 0; u < U; ++u)
-            if (p + u * w.rows < s.p1) {
-                const long long row = s.n * w.HW + p + u * w.rows;
-                r[u] = *(const uint2*)(codes + row * w.C + 8 * s.v);
-                e[u] = scales[row * blocks + (s.v >> 2)];
-            }
+        for (int u = 0; u < U; ++u) {
+            if (p + u * w.rows < s.p1) { r[u] = *(const uint2*)k.codes; e[u] = *k.scales; }
+            k.next(w.rows, w.C);
+        }
         #pragma unroll
-        for (int u = 0; u < U; ++u)
+        for (int u = 0; u < U; ++u) {
             if (p + u * w.rows < s.p1) {
                 float f[8];
-                if (fmt == kSrcInt8) code_values<kSrcInt8, 8>(r[u], f);
-                else code_values<kSrcE4m3, 8>(r[u], f);
+                code_values<FMT, 8>(r[u], f);
                 const float sc = scale_of(e[u]);
                 #pragma unroll
-                for (int i = 0; i < 8; ++i) f[i] *= sc;
-                *(Raw<T, 8>*)(op + g.at(p + u * w.rows)) = pack<T, 8>(f);
+                for (int i = 0; i < 8; i += 2) un2(mul2(mk2(f[i], f[i + 1]), mk2(sc, sc)), f[i], f[i + 1]);
+                *(Raw<T, 8>*)(op + c.off) = pack<T, 8>(f);
             }
+            c.next(g, w.rows);
+        }
     }
 }
 // Any other rows: a warp per block, a lane per value.

@@ -7,6 +7,7 @@
 
 #include <algorithm>
 #include <atomic>
+#include <cmath>
 #include <cstdio>
 #include <utility>
 
@@ -123,7 +124,7 @@ void encode(Launcher& go, const Dims& d, const alexnet_view_t& x, const alexnet_
     const FastDiv blocks = fast_div((uint32_t)ceil_div(d.C, 32));
     const bool vec = vec_ok(x, d, dtype) && vec_ok(k, d);
     const Walk w = walk_of(d, vec ? 8 : 1);
-    if (vec) go(checkpoint_encode_kernel<T>, grid_of(w, d), 256, (const T*)x.data, g, w, src_of(k.format), (uint8_t*)k.codes, k.scales);
+    if (vec) go(k.format == ALEXNET_CODES_INT8 ? checkpoint_encode_kernel<T, kSrcInt8> : checkpoint_encode_kernel<T, kSrcE4m3>, grid_of(w, d), 256, (const T*)x.data, g, w, (uint8_t*)k.codes, k.scales);
     else go(checkpoint_encode_any_kernel<T>, d.n * w.chunks, 256, (const T*)x.data, g, w, blocks, src_of(k.format), (uint8_t*)k.codes, k.scales);
 }
 template <typename T>
@@ -132,7 +133,8 @@ void decode(Launcher& go, const Dims& d, const alexnet_view_t& x, const alexnet_
     const FastDiv blocks = fast_div((uint32_t)ceil_div(d.C, 32));
     const bool vec = vec_ok(x, d, dtype) && vec_ok(k, d);
     const Walk w = walk_of(d, vec ? 8 : 1);
-    if (vec) go(checkpoint_decode_kernel<T>, grid_of(w, d), 256, (const uint8_t*)k.codes, (const uint8_t*)k.scales, src_of(k.format), g, w, (T*)x.data);
+    if (vec) go(k.format == ALEXNET_CODES_INT8 ? checkpoint_decode_kernel<T, kSrcInt8> : checkpoint_decode_kernel<T, kSrcE4m3>, grid_of(w, d), 256, (const uint8_t*)k.codes, (const uint8_t*)k.scales, g, w,
+                (T*)x.data);
     else go(checkpoint_decode_any_kernel<T>, d.n * w.chunks, 256, (const uint8_t*)k.codes, (const uint8_t*)k.scales, src_of(k.format), g, w, blocks, (T*)x.data);
 }
 const char* check_codes(const alexnet_checkpoint_t& k, const Dims& d) {
@@ -174,10 +176,65 @@ NormShape norm_shape(const alexnet_group_norm_t& s) { return {s.channels, s.h * 
 size_t forward_ws(const Walk& w, const Dims& d) { return (size_t)(d.n * w.chunks) * d.C * sizeof(double2); }
 size_t backward_ws(const Walk& w, const Dims& d, int groups) { return (size_t)(d.n * groups) * sizeof(float2) + (size_t)(d.n * w.chunks) * 2 * d.C * sizeof(float); }
 
+constexpr size_t kSmSmem = 228 * 1024, kCtaSmem = 227 * 1024;
+// How clusters walk a tensor, `slot` bytes kept per vector of V channels and `moved` bytes to and from memory; k = 0: not at all (rows wider than a
+// block, or too few samples to fill the device with their clusters).  By a model in cycles: an SM moves 22 bytes per cycle, a round of CTAs
+// costs 5000 more for its first loads and the sums' way around, and vectors that do not stay on chip are read again at 40 bytes.
+template <int V>
+ClusterWalk cluster_walk(const Dims& d, int groups, int slot, int moved) {
+    ClusterWalk best{};
+    ClusterWalk w{};
+    w.C = d.C; w.HW = d.h * d.w; w.vecs = d.C / V;
+    w.cols = (int)ceil_div(w.vecs, V == 8 ? 4 : 1) * (V == 8 ? 4 : 1);
+    if (w.cols > kClThreads || groups > 1024 || d.n > kMaxGrid / 8) return best;
+    double cost = 1e30;
+    for (w.k = 1; w.k <= 8; w.k *= 2) {
+        if (w.k > w.HW) break;
+        w.ppc = (int)ceil_div(w.HW, w.k);
+        for (w.threads = 128; w.threads <= kClThreads; w.threads += 32) {
+            if (w.threads < w.cols) continue;
+            w.rows = w.threads / w.cols;
+            w.its = (int)ceil_div(w.ppc, w.rows);
+            const size_t scratch = cluster_scratch<V>(w, groups) + 64, per_it = (size_t)w.threads * slot;
+            if (scratch + 1024 > kCtaSmem) continue;
+            for (int occ = 1; occ <= 4 && occ * w.threads <= 2 * kClThreads; ++occ) {
+                const size_t room = std::min(kCtaSmem, kSmSmem / occ - 1024);
+                if (room < scratch) break;
+                w.keep = (int)std::min<size_t>(w.its, (room - scratch) / per_it);
+                const double work = (double)w.its * w.threads * moved / 22 + (double)(w.its - w.keep) * w.threads * moved / 40;
+                const double per_sm = (double)ceil_div(d.n * w.k, kSms), c = per_sm * work + 5000 * std::ceil(per_sm / occ);
+                if (c < cost) { cost = c; best = w; }
+            }
+        }
+    }
+    // a sample's cluster is at most eight SMs: a few large samples go faster through the kernels that spread over all of them
+    if (best.k && (double)d.n * best.k < kSms / 2 && (double)best.its * best.threads * moved > 2.0e5) best.k = 0;
+    return best;
+}
+template <typename K>
+cudaError_t allow_smem(K* kernel) { return cudaFuncSetAttribute((const void*)kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kCtaSmem); }
+
 template <typename T, int V>
 void forward(Launcher& go, const alexnet_group_norm_forward_t* a, const Dims& d) {
     const Walk w = walk_of(d, V);
     const NormShape s = norm_shape(a->shape);
+    const ClusterWalk cw = cluster_walk<V>(d, s.groups, sizeof(T) * V, 2 * sizeof(T) * V);
+    if (cw.k) {
+        Keep kx{}, ky{};
+        if (V == 8) {
+            if (a->keep_x.codes) kx = {(uint8_t*)a->keep_x.codes, a->keep_x.scales, src_of(a->keep_x.format)};
+            if (a->keep_y.codes) ky = {(uint8_t*)a->keep_y.codes, a->keep_y.scales, src_of(a->keep_y.format)};
+        }
+        if (go.e == cudaSuccess) go.e = allow_smem(gn_cluster_forward_kernel<T, V>);
+        go.smem = (size_t)cw.keep * cw.threads * sizeof(T) * V + cluster_scratch<V>(cw, s.groups);
+        go.cluster = cw.k;
+        go(gn_cluster_forward_kernel<T, V>, d.n * cw.k, cw.threads, (const T*)a->x.data, geo_of(a->x, d), cw, s, a->weight, a->bias, (T*)a->y.data, geo_of(a->y, d), a->mean, a->rstd, kx, ky);
+        if (V != 8) {
+            if (a->keep_x.codes) encode<T>(go, d, a->x, a->keep_x, a->shape.dtype);
+            if (a->keep_y.codes) encode<T>(go, d, a->y, a->keep_y, a->shape.dtype);
+        }
+        return;
+    }
     const Geo gx = geo_of(a->x, d), gy = geo_of(a->y, d);
     double2* partial = (double2*)a->workspace;
     const T *x = (const T*)a->x.data;
@@ -204,6 +261,19 @@ void backward(Launcher& go, const alexnet_group_norm_backward_t* a, const Dims& 
     const Source src{a->x.data, (const uint8_t*)a->kept.codes, a->kept.scales};
     const BackwardArgs A{a->mean, a->rstd, a->weight, a->bias};
     const T* dy = (const T*)a->dy.data;
+    constexpr int kX = SRC == kSrcSame ? (int)sizeof(T) * V : V, kSlot = (int)sizeof(T) * V + kX + (SRC == kSrcSame ? 0 : 1);
+    const ClusterWalk cw = cluster_walk<V>(d, s.groups, kSlot, 2 * (int)sizeof(T) * V + kX);
+    if (cw.k) {
+        partial = (float*)a->workspace;
+        auto* kernel = gn_cluster_backward_kernel<T, V, SRC>;
+        if (go.e == cudaSuccess) go.e = allow_smem(kernel);
+        const size_t slab = (size_t)cw.keep * cw.threads;
+        go.smem = slab * (kSlot - (SRC == kSrcSame ? 0 : 1)) + (SRC == kSrcSame ? 0 : (slab + 15) / 16 * 16) + cluster_scratch<V>(cw, s.groups);
+        go.cluster = cw.k;
+        go(kernel, d.n * cw.k, cw.threads, dy, gdy, src, gx, cw, s, A, (T*)a->dx.data, gdx, partial);
+        if (a->dweight || a->dbias) go(gn_parameter_gradient_kernel, ceil_div(d.C, 32), 1024, (const float*)partial, d.C, d.n, a->dweight, a->dbias);
+        return;
+    }
     go(gn_backward_sums_kernel<T, V, SRC>, grid_of(w, d), 256, dy, gdy, src, gx, w, s, A, partial);
     go(gn_backward_final_kernel, d.n * s.groups + (a->dweight || a->dbias ? ceil_div(d.C, 32) : 0), 256, (const float*)partial, s, d.n, w.chunks, A, c12, a->dweight, a->dbias);
     go(gn_backward_apply_kernel<T, V, SRC>, grid_of(w, d), 256, dy, gdy, src, gx, w, s, A, (const float2*)c12, (T*)a->dx.data, gdx);
