@@ -10,13 +10,15 @@
 //
 // Sums.  A thread sums, for each of its channels, the differences from the first value it reads and their squares, in fp32.  That value
 // is one of the summed, so the sum of squares is at most (1 + n) times the true one about the mean, however far the mean is from zero: nothing
-// cancels as it would in E[x^2] - mean^2.  Between threads sums are joined in fp64 with a fixed order, so results repeat bit for bit.
+// cancels as it would in E[x^2] - mean^2.  From there on parts of n values are joined by their means, each held as hi + lo, and their squared
+// deviations M2 from them (Part below): means as differences from one of them, M2 = sum M2_i + n_i (mean_i - mean)^2, all of one sign.  The order is
+// fixed, so results repeat bit for bit.  (fp64 sums of values and squares do as well but took 3 to 8 us of a call: conversions, divisions, roots.)
 #pragma once
 #include "checkpoint.cuh"
 
 namespace op {
 
-enum { kActNone = 0, kActRelu = 1, kActSilu = 2 };
+enum { kActNone = 0, kActRelu = 1, kActSilu = 2, kActAny = 3 };
 
 template <int V> __device__ __forceinline__ void v_add(const float* a, const float* b, float* o) {
     if constexpr (V == 1) o[0] = a[0] + b[0];
@@ -58,7 +60,9 @@ template <typename T, int V> __device__ __forceinline__ void sigmoid(const float
         for (int i = 0; i < V; ++i) asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(s[i]) : "f"(t[i]));
     }
 }
-template <typename T, int V> __device__ __forceinline__ void activate(int act, float* z) {
+// ACT: the activation, or kActAny to take it from `act`
+template <typename T, int V, int ACT> __device__ __forceinline__ void activate(int act, float* z) {
+    if (ACT != kActAny) act = ACT;
     if (act == kActRelu) {
         #pragma unroll
         for (int i = 0; i < V; ++i) z[i] = z[i] < 0.f ? 0.f : z[i];          // keeps NaN
@@ -69,7 +73,13 @@ template <typename T, int V> __device__ __forceinline__ void activate(int act, f
     }
 }
 
-struct NormShape { int C, HW, groups, cg; float eps; int act; };
+struct NormShape {
+    int C, HW, groups, cg;
+    FastDiv by_cg;
+    float eps;
+    int act;
+    __device__ __forceinline__ int group(int c) const { return (int)by_cg.div((uint32_t)c); }
+};
 
 // per-channel constants of a thread's vector
 template <int V> struct Chan { float nm[V], a[V], b[V]; };
@@ -77,7 +87,7 @@ template <int V>
 __device__ __forceinline__ void load_chan(Chan<V>& k, const NormShape& s, const float* mean, const float* rstd, const float* weight, const float* bias, long long n, int c0) {
     #pragma unroll
     for (int i = 0; i < V; ++i) {
-        const long long g = n * s.groups + (c0 + i) / s.cg;
+        const long long g = n * s.groups + s.group(c0 + i);
         k.nm[i] = -mean[g];
         k.a[i] = rstd[g] * (weight ? weight[c0 + i] : 1.f);
         k.b[i] = bias ? bias[c0 + i] : 0.f;
@@ -85,82 +95,145 @@ __device__ __forceinline__ void load_chan(Chan<V>& k, const NormShape& s, const 
 }
 
 // ---------------------------------------------------------------- forward, any size: sums, statistics, result
-// The sums of one thread for one channel, as sums of all values and of their squares (fp64: the squares' cancellation is harmless there
-// up to |mean| / std of 10^6).
-__device__ __forceinline__ double2 raw_moments(int n, float K, float S, float Q) {
-    if (n == 0) return make_double2(0., 0.);
-    const double s1 = (double)n * K + S, m2 = (double)Q - (double)S * S / n;
-    return make_double2(s1, m2 + s1 * s1 / n);
+// n values by their mean hi + lo and their squared deviations from it
+struct Part { float hi, lo, m2; };
+// a thread's values of a channel: n of them, shifted by -nK (one of them), S their sum, Q their sum of squares
+__device__ __forceinline__ Part moments(int n, float nK, float S, float Q) {
+    const float d = n ? __fdividef(S, (float)n) : 0.f, hi = d - nK;
+    return {hi, (-nK - hi) + d, fmaf(-S, d, Q)};
 }
+// The parts get(0) .. get(count - 1) of n(i) values each, joined; inv = 1 / all their values.  The mean is first taken to fp32, then what is left over:
+// the second pass sums small differences whatever the first part was.
+template <int UNROLL, typename G, typename N> __device__ __forceinline__ Part join(int count, float inv, G get, N n) {
+    const float ref = get(0).hi;
+    float m = 0.f, e = 0.f, q = 0.f;
+    #pragma unroll UNROLL
+    for (int i = 0; i < count; ++i) m = fmaf(n(i), get(i).hi - ref, m);
+    const float hi = fmaf(m, inv, ref);
+    #pragma unroll UNROLL
+    for (int i = 0; i < count; ++i) {
+        const Part t = get(i);
+        const float d = (t.hi - hi) + t.lo, w = n(i) * d;
+        e += w;
+        q += fmaf(w, d, t.m2);
+    }
+    const float lo = e * inv;
+    return {hi, lo, fmaf(-e, lo, q)};
+}
+// Per-thread sums of a block in shared memory, by vector element and thread: pitch = threads + 4, so that neighbouring threads' stores and the
+// reads of neighbouring channels (elements of neighbouring threads) each fall into different banks.
+template <int V> struct Table {
+    float* p;
+    int pitch;
+    __device__ __forceinline__ float& at(int k, int i, int t) const { return p[(k * V + i) * pitch + t]; }
+};
+__device__ __forceinline__ float warp_sum(float t) {
+    #pragma unroll
+    for (int o = 16; o; o >>= 1) t += __shfl_xor_sync(~0u, t, o);
+    return t;
+}
+__device__ __forceinline__ float2 warp_sum(float2 t) {
+    #pragma unroll
+    for (int o = 16; o; o >>= 1) { t.x += __shfl_xor_sync(~0u, t.x, o); t.y += __shfl_xor_sync(~0u, t.y, o); }
+    return t;
+}
+// the threads' parts of channel c (element c % V of column c / V), joined: the first `more` rows of threads have n_lo + 1 values, the others n_lo
+template <int V> __device__ __forceinline__ Part join_rows(const Table<V>& s, int c, int rows, int cols, int more, float n_lo, float inv) {
+    const int i = c % V, t = c / V;
+    return join<4>(rows, inv, [&](int r) { return Part{s.at(0, i, r * cols + t), s.at(1, i, r * cols + t), s.at(2, i, r * cols + t)}; }, [&](int r) { return r < more ? n_lo + 1.f : n_lo; });
+}
+__device__ __forceinline__ float2 statistics(const Part& t, const NormShape& s) {
+    return make_float2(t.hi + t.lo, __frsqrt_rn(__fdiv_rn(t.m2, (float)s.HW * (float)s.cg) + s.eps));
+}
+
 template <typename T, int V>
-__global__ void __launch_bounds__(256) gn_sums_kernel(const T* __restrict__ x, const Geo g, const Walk w, double2* __restrict__ partial) {
+__global__ void __launch_bounds__(256) gn_sums_kernel(const T* __restrict__ x, const Geo g, const Walk w, float4* __restrict__ partial) {
     kn::pdl_sync();
-    __shared__ double2 sums[256 * V];
+    __shared__ float sums[3 * V * 260];
+    const Table<V> table{sums, 260};
     const Spot s = spot(w);
     constexpr int U = V == 8 ? 4 : 8;
     float nK[V], S[V], Q[V];
     #pragma unroll
     for (int i = 0; i < V; ++i) nK[i] = S[i] = Q[i] = 0.f;
     int cnt = 0;
-    if (s.has) {
+    if (s.has && s.p0 + s.row < s.p1) {
         const T* xp = x + s.n * g.sn + V * s.v;
-        for (int p = s.p0 + s.row; p < s.p1; p += U * w.rows) {
+        Cursor c(g, s.p0 + s.row);
+        unpack<T, V>(*(const Raw<T, V>*)(xp + c.off), nK);
+        #pragma unroll
+        for (int i = 0; i < V; ++i) nK[i] = -nK[i];
+        cnt = (s.p1 - s.p0 - s.row + w.rows - 1) / w.rows;
+        for (int it = 0; it < cnt; it += U) {
             Raw<T, V> r[U];
             #pragma unroll
-            for (int u = 0; u < U; ++u)
-                if (p + u * w.rows < s.p1) r[u] = *(const Raw<T, V>*)(xp + g.at(p + u * w.rows));
+            for (int u = 0; u < U; ++u) {
+                if (it + u < cnt) r[u] = *(const Raw<T, V>*)(xp + c.off);
+                c.next(g, w.rows);
+            }
             #pragma unroll
             for (int u = 0; u < U; ++u)
-                if (p + u * w.rows < s.p1) {
+                if (it + u < cnt) {
                     float f[V];
                     unpack<T, V>(r[u], f);
-                    if (cnt == 0) {
-                        #pragma unroll
-                        for (int i = 0; i < V; ++i) nK[i] = -f[i];
-                    }
                     v_add<V>(f, nK, f);
                     v_add<V>(S, f, S);
                     v_fma<V>(f, f, Q, Q);
-                    ++cnt;
                 }
         }
     }
     #pragma unroll
-    for (int i = 0; i < V; ++i) sums[threadIdx.x * V + i] = raw_moments(cnt, -nK[i], S[i], Q[i]);
+    for (int i = 0; i < V; ++i) {
+        const Part t = moments(cnt, nK[i], S[i], Q[i]);
+        table.at(0, i, threadIdx.x) = t.hi; table.at(1, i, threadIdx.x) = t.lo; table.at(2, i, threadIdx.x) = t.m2;
+    }
     __syncthreads();
-    const int nch = w.cols * V, c0 = (s.v - s.col) * V;
-    for (int j = threadIdx.x; j < nch; j += 256) {
-        if (c0 + j >= w.C) break;
-        double2 t = make_double2(0., 0.);
-        for (int r = 0; r < w.rows; ++r) { const double2 q = sums[r * nch + j]; t.x += q.x; t.y += q.y; }
-        partial[(s.n * w.chunks + s.chunk) * w.C + c0 + j] = t;
+    const int nch = w.cols * V, c0 = (s.v - s.col) * V, np = s.p1 - s.p0;
+    for (int j = threadIdx.x; j < nch && c0 + j < w.C; j += 256) {
+        const Part t = join_rows<V>(table, j, min(w.rows, np), w.cols, np % w.rows, (float)(np / w.rows), __fdividef(1.f, (float)np));
+        partial[(s.n * w.chunks + s.chunk) * w.C + c0 + j] = make_float4(t.hi, t.lo, t.m2, 0.f);
     }
 }
-// a block per group
-__global__ void __launch_bounds__(128) gn_statistics_kernel(const double2* __restrict__ partial, const NormShape s, long long chunks, float* __restrict__ mean, float* __restrict__ rstd) {
-    kn::pdl_sync();
-    const long long n = blockIdx.x / s.groups;
-    const int g = (int)(blockIdx.x - n * s.groups);
-    const double2* p = partial + n * chunks * s.C + (long long)g * s.cg;
-    double2 t = make_double2(0., 0.);
-    const long long total = chunks * s.cg;
-    for (long long i = threadIdx.x; i < total; i += 128) {
-        const long long k = i / s.cg;
-        const double2 q = p[k * s.C + (i - k * s.cg)];
-        t.x += q.x; t.y += q.y;
-    }
-    #pragma unroll
-    for (int o = 16; o; o >>= 1) { t.x += __shfl_xor_sync(~0u, t.x, o); t.y += __shfl_xor_sync(~0u, t.y, o); }
-    __shared__ double2 ws[4];
-    if ((threadIdx.x & 31) == 0) ws[threadIdx.x >> 5] = t;
+__device__ __forceinline__ float2 block_sum(float2 t, float2* red) {        // of all 256 threads
+    t = warp_sum(t);
     __syncthreads();
+    if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5] = t;
+    __syncthreads();
+    t = red[0];
+    #pragma unroll
+    for (int k = 1; k < 8; ++k) { t.x += red[k].x; t.y += red[k].y; }
+    return t;
+}
+// a block per group: the chunks' parts [chunks][C] of its channels
+__global__ void __launch_bounds__(256) gn_statistics_kernel(const float4* __restrict__ partial, const NormShape s, int chunks, int ppc, float* __restrict__ mean, float* __restrict__ rstd) {
+    kn::pdl_sync();
+    __shared__ float2 red[8];
+    const long long n = blockIdx.x / s.groups;
+    const int g = (int)(blockIdx.x - n * s.groups), total = chunks * s.cg;
+    const float4* p = partial + n * chunks * s.C + (long long)g * s.cg;
+    const float ref = p[0].x, lo = (float)ppc, last = (float)(s.HW - (chunks - 1) * ppc), count = (float)s.HW * (float)s.cg;
+    float2 t = make_float2(0.f, 0.f);
+    #pragma unroll 4
+    for (int i = threadIdx.x; i < total; i += 256) {
+        const int k = s.group(i);
+        t.x = fmaf(k == chunks - 1 ? last : lo, p[(long long)k * s.C + (i - k * s.cg)].x - ref, t.x);
+    }
+    const float hi = ref + __fdiv_rn(block_sum(t, red).x, count);
+    t.x = 0.f;
+    #pragma unroll 4
+    for (int i = threadIdx.x; i < total; i += 256) {
+        const int k = s.group(i);
+        const float4 q = p[(long long)k * s.C + (i - k * s.cg)];
+        const float d = (q.x - hi) + q.y, w = (k == chunks - 1 ? last : lo) * d;
+        t.x += w;
+        t.y += fmaf(w, d, q.z);
+    }
+    t = block_sum(t, red);
     if (threadIdx.x == 0) {
-        t = make_double2(ws[0].x + ws[1].x + ws[2].x + ws[3].x, ws[0].y + ws[1].y + ws[2].y + ws[3].y);
-        const double m = (double)s.HW * s.cg, mu = t.x / m;
-        double var = t.y / m - mu * mu;
-        if (var < 0.) var = 0.;
-        mean[blockIdx.x] = (float)mu;
-        rstd[blockIdx.x] = (float)(1. / sqrt(var + (double)s.eps));
+        const float l = __fdiv_rn(t.x, count);
+        const float2 r = statistics(Part{hi, l, fmaf(-t.x, l, t.y)}, s);
+        mean[blockIdx.x] = r.x;
+        rstd[blockIdx.x] = r.y;
     }
 }
 struct Keep { uint8_t *codes, *scales; int fmt; };        // codes == nullptr: nothing kept
@@ -170,7 +243,7 @@ __device__ __forceinline__ void keep_codes(const Keep& k, const Raw<T, 8>& r, co
     else store_codes<T, kSrcE4m3>(r, f, has, c.codes, c.scales);
 }
 // A thread's positions from p on, `rows` apart, `cnt` of them: results (and checkpoints) of the vectors that fetch(it) gives.
-template <typename T, int V, typename F>
+template <typename T, int V, int ACT, typename F>
 __device__ __forceinline__ void apply_positions(const Chan<V>& k, const NormShape& sh, int p, int rows, int it0, int cnt, long long row0, int v, bool has, T* y, const Geo& gy, const Keep& kx, const Keep& ky,
                                                 F fetch) {
     Cursor c(gy, p + it0 * rows);
@@ -184,7 +257,7 @@ __device__ __forceinline__ void apply_positions(const Chan<V>& k, const NormShap
             if (kx.codes) { keep_codes<T>(kx, r, f, has, cx); cx.next(rows, sh.C); }
         v_add<V>(f, k.nm, f);
         v_fma<V>(f, k.a, k.b, z);
-        activate<T, V>(sh.act, z);
+        activate<T, V, ACT>(sh.act, z);
         Raw<T, V> out = pack<T, V>(z);
         if (has) *(Raw<T, V>*)(y + c.off) = out;
         c.next(gy, rows);
@@ -197,7 +270,7 @@ __device__ __forceinline__ void apply_positions(const Chan<V>& k, const NormShap
             }
     }
 }
-template <typename T, int V>
+template <typename T, int V, int ACT>
 __global__ void __launch_bounds__(256) gn_apply_kernel(const T* __restrict__ x, const Geo gx, const Walk w, const NormShape sh, const float* __restrict__ weight,
                                                        const float* __restrict__ bias, const float* __restrict__ mean, const float* __restrict__ rstd,
                                                        T* __restrict__ y, const Geo gy, const Keep kx, const Keep ky) {
@@ -209,7 +282,7 @@ __global__ void __launch_bounds__(256) gn_apply_kernel(const T* __restrict__ x, 
     if (s.has) load_chan<V>(k, sh, mean, rstd, weight, bias, s.n, V * s.v);
     const T* xp = x + s.n * gx.sn + V * s.v;
     Cursor c(gx, p);
-    apply_positions<T, V>(k, sh, p, w.rows, 0, (s.p1 - p + w.rows - 1) / w.rows, s.n * w.HW, s.v, s.has, y + s.n * gy.sn + V * s.v, gy, kx, ky, [&](int) {
+    apply_positions<T, V, ACT>(k, sh, p, w.rows, 0, (s.p1 - p + w.rows - 1) / w.rows, s.n * w.HW, s.v, s.has, y + s.n * gy.sn + V * s.v, gy, kx, ky, [&](int) {
         Raw<T, V> r = {};
         if (s.has) r = *(const Raw<T, V>*)(xp + c.off);
         c.next(gx, w.rows);
@@ -251,29 +324,36 @@ template <typename T, int V, int SRC> struct Fetch {
         }
     }
 };
-// The side of ReLU's kink that a value is on, where fp32 cannot tell: d and a carry a rounding each, so z = d a + b is off by up to
-// 2^-23 |b| or so when it is near zero.  Such values (a few in a million) are taken again in fp64 from x itself.
+// The side of ReLU's kink that a value is on, where fp32 cannot tell: d and a carry a rounding each, so z = d a + b is off by up to 2^-23 |b| or so when it
+// is near zero.  Such values (a few in a million) are taken again with the roundings of x + nm, rstd w, d a and the last sum carried along (Knuth's
+// and the fused multiply-add's exact errors): off by 2^-45 of b.
+__device__ __forceinline__ float relu_side(float x, float nm, float b, float rstd, float w) {
+    const float d = x + nm, u = d - x, de = (x - (d - u)) + (nm - u);
+    const float a = rstd * w, ae = fmaf(rstd, w, -a);
+    const float p = d * a, pe = fmaf(d, a, -p);
+    const float s = p + b, t = s - p, se = (p - (s - t)) + (b - t);
+    return s + (se + (pe + fmaf(d, ae, de * a)));
+}
 struct BackwardArgs {
     const float *mean, *rstd, *weight, *bias;
 };
 // d = x - mean, and dz in the place of dy
-template <typename T, int V, int SRC>
+template <typename T, int V, int SRC, int ACT>
 __device__ __forceinline__ void activation_gradient(const NormShape& sh, const Chan<V>& k, const BackwardArgs& A, long long n, int c0, const Fetch<T, V, SRC>& fx, float* d, float* dy) {
     float x[V];
     fx.value(k.nm, x, d);
-    if (sh.act == kActNone) return;
+    const int act = ACT == kActAny ? sh.act : ACT;
+    if (act == kActNone) return;
     float z[V];
     v_fma<V>(d, k.a, k.b, z);
-    if (sh.act == kActRelu) {
+    if (act == kActRelu) {
         bool near = false;
         #pragma unroll
         for (int i = 0; i < V; ++i) near = near || fabsf(z[i]) < fabsf(1e-6f * k.b[i]);
         if (near) {
             #pragma unroll
-            for (int i = 0; i < V; ++i) {
-                const double side = ((double)(x[i] * fx.scale()) + (double)k.nm[i]) * (double)A.rstd[n * sh.groups + (c0 + i) / sh.cg] * (A.weight ? (double)A.weight[c0 + i] : 1.) + (double)k.b[i];
-                if (fabsf(z[i]) < fabsf(1e-6f * k.b[i])) z[i] = side > 0. ? 1.f : -1.f;
-            }
+            for (int i = 0; i < V; ++i)
+                if (fabsf(z[i]) < fabsf(1e-6f * k.b[i])) z[i] = relu_side(x[i] * fx.scale(), k.nm[i], k.b[i], A.rstd[n * sh.groups + sh.group(c0 + i)], A.weight ? A.weight[c0 + i] : 1.f);
         }
         #pragma unroll
         for (int i = 0; i < V; ++i) dy[i] = z[i] <= 0.f ? 0.f : dy[i];
@@ -288,11 +368,12 @@ __device__ __forceinline__ void activation_gradient(const NormShape& sh, const C
         v_mul<V>(dy, u, dy);
     }
 }
-template <typename T, int V, int SRC>
+template <typename T, int V, int SRC, int ACT>
 __global__ void __launch_bounds__(256) gn_backward_sums_kernel(const T* __restrict__ dy, const Geo gdy, const Source src, const Geo gx, const Walk w, const NormShape sh,
                                                                const BackwardArgs A, float* __restrict__ partial) {
     kn::pdl_sync();
-    __shared__ float sums[2][256 * V];
+    __shared__ float sums[2 * V * 260];
+    const Table<V> table{sums, 260};
     const Spot s = spot(w);
     constexpr int U = V == 8 ? 2 : 4;
     float S1[V], S2[V];
@@ -316,67 +397,66 @@ __global__ void __launch_bounds__(256) gn_backward_sums_kernel(const T* __restri
                 if (p + u * w.rows < s.p1) {
                     float f[V], q[V];
                     unpack<T, V>(r[u], q);
-                    activation_gradient<T, V, SRC>(sh, k, A, s.n, V * s.v, fx[u], f, q);
+                    activation_gradient<T, V, SRC, ACT>(sh, k, A, s.n, V * s.v, fx[u], f, q);
                     v_add<V>(S1, q, S1);
                     v_fma<V>(f, q, S2, S2);
                 }
         }
     }
     #pragma unroll
-    for (int i = 0; i < V; ++i) { sums[0][threadIdx.x * V + i] = S1[i]; sums[1][threadIdx.x * V + i] = S2[i]; }
+    for (int i = 0; i < V; ++i) { table.at(0, i, threadIdx.x) = S1[i]; table.at(1, i, threadIdx.x) = S2[i]; }
     __syncthreads();
     const int nch = w.cols * V, c0 = (s.v - s.col) * V;
     for (int j = threadIdx.x; j < nch; j += 256) {
         if (c0 + j >= w.C) break;
         float t1 = 0.f, t2 = 0.f;
-        for (int r = 0; r < w.rows; ++r) { t1 += sums[0][r * nch + j]; t2 += sums[1][r * nch + j]; }
+        for (int r = 0; r < w.rows; ++r) { t1 += table.at(0, j % V, r * w.cols + j / V); t2 += table.at(1, j % V, r * w.cols + j / V); }
         float* o = partial + (s.n * w.chunks + s.chunk) * 2 * w.C + c0 + j;
         o[0] = t1;
-        o[w.C] = t2 * A.rstd[s.n * sh.groups + (c0 + j) / sh.cg];       // of xhat
+        o[w.C] = t2 * A.rstd[s.n * sh.groups + sh.group(c0 + j)];       // of xhat
     }
 }
-// Blocks below n * groups: c1 and c2 of a group.  The others: dweight and dbias of 32 channels, over samples and chunks.
-__global__ void __launch_bounds__(256) gn_backward_final_kernel(const float* __restrict__ partial, const NormShape sh, long long n_total, long long chunks, const BackwardArgs A,
-                                                                float2* __restrict__ c12, float* __restrict__ dweight, float* __restrict__ dbias) {
+// c1 and c2 of a group per block, from the chunks' sums [chunks][2][C]
+__global__ void __launch_bounds__(256) gn_backward_group_kernel(const float* __restrict__ partial, const NormShape sh, int chunks, const BackwardArgs A, float2* __restrict__ c12) {
     kn::pdl_sync();
-    __shared__ double2 red[8][32];
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const long long nblk = n_total * sh.groups;
-    double2 t = make_double2(0., 0.);
-    if (blockIdx.x < nblk) {
-        const long long n = blockIdx.x / sh.groups;
-        const int g = (int)(blockIdx.x - n * sh.groups);
-        const float* p = partial + n * chunks * 2 * sh.C + (long long)g * sh.cg;
-        for (long long i = threadIdx.x; i < chunks * sh.cg; i += 256) {
-            const long long k = i / sh.cg;
-            const int c = (int)(i - k * sh.cg);
-            const double wt = A.weight ? A.weight[g * sh.cg + c] : 1.f;
-            t.x += wt * p[k * 2 * sh.C + c];
-            t.y += wt * p[k * 2 * sh.C + sh.C + c];
-        }
-        #pragma unroll
-        for (int o = 16; o; o >>= 1) { t.x += __shfl_xor_sync(~0u, t.x, o); t.y += __shfl_xor_sync(~0u, t.y, o); }
-        if (lane == 0) red[warp][0] = t;
-        __syncthreads();
-        if (threadIdx.x == 0) {
-            for (int k = 1; k < 8; ++k) { t.x += red[k][0].x; t.y += red[k][0].y; }
-            const double m = (double)sh.HW * sh.cg;
-            c12[blockIdx.x] = make_float2((float)(t.x / m), (float)(t.y / m));
-        }
-        return;
+    __shared__ float2 red[8];
+    const long long n = blockIdx.x / sh.groups;
+    const int g = (int)(blockIdx.x - n * sh.groups), total = chunks * sh.cg;
+    const float* p = partial + n * chunks * 2 * sh.C + (long long)g * sh.cg;
+    float2 t = make_float2(0.f, 0.f);
+    #pragma unroll 4
+    for (int i = threadIdx.x; i < total; i += 256) {
+        const int k = sh.group(i), c = i - k * sh.cg;
+        const float wt = A.weight ? A.weight[g * sh.cg + c] : 1.f;
+        const float* q = p + (long long)k * 2 * sh.C + c;
+        t.x = fmaf(wt, q[0], t.x);
+        t.y = fmaf(wt, q[sh.C], t.y);
     }
-    const int c = (int)(blockIdx.x - nblk) * 32 + lane;
-    if (c < sh.C)
-        for (long long i = warp; i < n_total * chunks; i += 8) { t.x += partial[i * 2 * sh.C + c]; t.y += partial[i * 2 * sh.C + sh.C + c]; }
+    t = block_sum(t, red);
+    const float m = (float)sh.HW * (float)sh.cg;
+    if (threadIdx.x == 0) c12[blockIdx.x] = make_float2(__fdiv_rn(t.x, m), __fdiv_rn(t.y, m));
+}
+// dweight and dbias: the sums [n][2][C] of the samples (or of their chunks).  A block takes 32 channels, its warps every 32nd row.
+__global__ void __launch_bounds__(1024) gn_parameter_gradient_kernel(const float* __restrict__ partial, int C, long long n, float* __restrict__ dweight, float* __restrict__ dbias) {
+    kn::pdl_sync();
+    __shared__ float2 red[32][33];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, c = blockIdx.x * 32 + lane;
+    float2 t = make_float2(0.f, 0.f);
+    if (c < C) {
+        const float* p = partial + c;
+        #pragma unroll 8
+        for (long long i = warp; i < n; i += 32) { t.x += p[i * 2 * C]; t.y += p[i * 2 * C + C]; }
+    }
     red[warp][lane] = t;
     __syncthreads();
-    if (warp == 0 && c < sh.C) {
-        for (int k = 1; k < 8; ++k) { t.x += red[k][lane].x; t.y += red[k][lane].y; }
-        if (dbias) dbias[c] = (float)t.x;
-        if (dweight) dweight[c] = (float)t.y;
+    t = warp_sum(red[lane][warp]);               // lane: part, warp: channel
+    const int cw = blockIdx.x * 32 + warp;
+    if (lane == 0 && cw < C) {
+        if (dbias) dbias[cw] = t.x;
+        if (dweight) dweight[cw] = t.y;
     }
 }
-template <typename T, int V, int SRC>
+template <typename T, int V, int SRC, int ACT>
 __global__ void __launch_bounds__(256) gn_backward_apply_kernel(const T* __restrict__ dy, const Geo gdy, const Source src, const Geo gx, const Walk w, const NormShape sh,
                                                                 const BackwardArgs A, const float2* __restrict__ c12, T* __restrict__ dx, const Geo gdx) {
     kn::pdl_sync();
@@ -387,7 +467,7 @@ __global__ void __launch_bounds__(256) gn_backward_apply_kernel(const T* __restr
     float B[V], D[V];
     #pragma unroll
     for (int i = 0; i < V; ++i) {
-        const long long g = s.n * sh.groups + (V * s.v + i) / sh.cg;
+        const long long g = s.n * sh.groups + sh.group(V * s.v + i);
         const float2 c = c12[g];
         const float r = A.rstd[g];
         B[i] = -r * r * c.y;
@@ -410,7 +490,7 @@ __global__ void __launch_bounds__(256) gn_backward_apply_kernel(const T* __restr
             if (p + u * w.rows < s.p1) {
                 float f[V], q[V];
                 unpack<T, V>(r[u], q);
-                activation_gradient<T, V, SRC>(sh, k, A, s.n, V * s.v, fx[u], f, q);
+                activation_gradient<T, V, SRC, ACT>(sh, k, A, s.n, V * s.v, fx[u], f, q);
                 v_fma<V>(f, B, D, f);
                 v_fma<V>(q, k.a, f, q);
                 *(Raw<T, V>*)(op + gdx.at(p + u * w.rows)) = pack<T, V>(q);
@@ -451,29 +531,26 @@ __device__ __forceinline__ void copies_wait(int pending) {
 }
 constexpr int kClBatches = 4;                 // groups of copies
 
-__device__ __forceinline__ double2 ld_cluster_d2(uint32_t addr, uint32_t rank) {
-    double2 v;
-    asm volatile("ld.shared::cluster.v2.f64 {%0, %1}, [%2];" : "=d"(v.x), "=d"(v.y) : "r"(tc::mapa_u32(addr, rank)) : "memory");
+__device__ __forceinline__ float ld_cluster(const float* p, uint32_t rank) {
+    float v;
+    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(tc::mapa_u32(tc::smem_u32(p), rank)) : "memory");
     return v;
 }
-__device__ __forceinline__ double2 warp_sum(double2 t) {
-    #pragma unroll
-    for (int o = 16; o; o >>= 1) { t.x += __shfl_xor_sync(~0u, t.x, o); t.y += __shfl_xor_sync(~0u, t.y, o); }
-    return t;
-}
-// shared memory behind the slots: per-thread sums, per-channel sums, per-group sums of this CTA, per-group results
-struct ClusterSmem { float2* part; double2 *chan, *grp; float2* res; };
-template <int V> __device__ __forceinline__ ClusterSmem cluster_smem(uint8_t* p, const ClusterWalk& w, int groups) {
-    ClusterSmem s;
-    s.chan = (double2*)p;
-    s.grp = s.chan + w.C;
-    s.part = (float2*)(s.grp + groups);
-    s.res = s.part + w.threads * V;
-    return s;
-}
-template <int V> inline size_t cluster_scratch(const ClusterWalk& w, int groups) { return (size_t)(w.C + groups) * 16 + ((size_t)w.threads * V + groups) * 8; }
+// shared memory behind the slots: K sums per thread and vector element, K per channel, K per group of this CTA, and the groups' results
+template <int V> struct ClusterSmem {
+    Table<V> part;
+    float *chan, *grp;       // [K][C], [K][groups]
+    float2* res;
+    __device__ __forceinline__ ClusterSmem(uint8_t* p, const ClusterWalk& w, int groups, int K) {
+        res = (float2*)p;
+        part = {(float*)(res + groups), w.threads + 4};
+        chan = part.p + K * V * part.pitch;
+        grp = chan + K * w.C;
+    }
+};
+template <int V> inline size_t cluster_scratch(const ClusterWalk& w, int groups, int K) { return ((size_t)K * V * (w.threads + 4) + K * w.C + K * groups) * sizeof(float) + groups * sizeof(float2); }
 
-template <typename T, int V>
+template <typename T, int V, int ACT>
 __global__ void __launch_bounds__(kClThreads, 2) gn_cluster_forward_kernel(const T* __restrict__ x, const Geo gx, const ClusterWalk w, const NormShape sh, const float* __restrict__ weight,
                                                                            const float* __restrict__ bias, T* __restrict__ y, const Geo gy, float* __restrict__ mean,
                                                                            float* __restrict__ rstd, const Keep kx, const Keep ky) {
@@ -482,7 +559,7 @@ __global__ void __launch_bounds__(kClThreads, 2) gn_cluster_forward_kernel(const
     using R = Raw<T, V>;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, warps = w.threads >> 5;
     R* slots = (R*)smem + tid;
-    const ClusterSmem m = cluster_smem<V>(smem + (size_t)w.keep * w.threads * sizeof(R), w, sh.groups);
+    const ClusterSmem<V> m(smem + (size_t)w.keep * w.threads * sizeof(R), w, sh.groups, 3);
     const int rank = w.k > 1 ? (int)tc::cluster_ctarank() : 0;
     const long long n = blockIdx.x / w.k;
     const int row = tid / w.cols, v = tid - row * w.cols;
@@ -542,52 +619,49 @@ __global__ void __launch_bounds__(kClThreads, 2) gn_cluster_forward_kernel(const
                 if (it + u < cnt) add(r[u]);
         }
     }
-    {
-        const float nf = (float)cnt, inv = cnt ? __fdividef(1.f, nf) : 0.f;
-        #pragma unroll
-        for (int i = 0; i < V; ++i) {         // the mean of this thread's values and their squared deviations from it
-            const float d = S[i] * inv;
-            m.part[tid * V + i] = make_float2(d - nK[i], fmaf(-S[i], d, Q[i]));
-        }
+    #pragma unroll
+    for (int i = 0; i < V; ++i) {
+        const Part t = moments(cnt, nK[i], S[i], Q[i]);
+        m.part.at(0, i, tid) = t.hi; m.part.at(1, i, tid) = t.lo; m.part.at(2, i, tid) = t.m2;
     }
     __syncthreads();
-    const int more = np % w.rows;
-    const double n_lo = (double)(np / w.rows);
+    const float inv = np ? __fdividef(1.f, (float)np) : 0.f;
     for (int c = tid; c < w.C; c += w.threads) {
-        double2 t = make_double2(0., 0.);
-        for (int r = 0; r < w.rows; ++r) {          // the first `more` rows of threads have one position more than the others
-            const float2 q = m.part[r * w.cols * V + c];
-            const double nr = r < more ? n_lo + 1. : n_lo, mu = q.x;
-            t.x += nr * mu;
-            t.y += (double)q.y + nr * mu * mu;
-        }
-        m.chan[c] = t;
+        const Part t = join_rows<V>(m.part, c, min(w.rows, max(np, 1)), w.cols, np % w.rows, (float)(np / w.rows), inv);
+        m.chan[c] = t.hi; m.chan[w.C + c] = t.lo; m.chan[2 * w.C + c] = t.m2;
     }
     __syncthreads();
-    for (int g = warp; g < sh.groups; g += warps) {
-        double2 t = make_double2(0., 0.);
-        for (int c = lane; c < sh.cg; c += 32) { const double2 q = m.chan[g * sh.cg + c]; t.x += q.x; t.y += q.y; }
-        t = warp_sum(t);
-        if (lane == 0) m.grp[g] = t;
+    for (int g = warp; g < sh.groups; g += warps) {          // the channels of a group: parts of np values
+        const float* q = m.chan + g * sh.cg;
+        const float ref = q[0], per = __fdividef(1.f, (float)sh.cg);
+        float2 s = make_float2(0.f, 0.f);
+        for (int c = lane; c < sh.cg; c += 32) s.x += q[c] - ref;
+        const float hi = fmaf(warp_sum(s.x), per, ref);
+        s.x = 0.f;
+        for (int c = lane; c < sh.cg; c += 32) {
+            const float d = (q[c] - hi) + q[w.C + c];
+            s.x += d;
+            s.y += fmaf((float)np * d, d, q[2 * w.C + c]);
+        }
+        s = warp_sum(s);
+        if (lane == 0) { m.grp[g] = hi; m.grp[sh.groups + g] = s.x * per; m.grp[2 * sh.groups + g] = fmaf(-(float)np * s.x, s.x * per, s.y); }
     }
     __syncwarp();
     if (w.k > 1) tc::cluster_sync_all();
     else __syncthreads();
-    for (int g = warp; g < sh.groups; g += warps) {
-        double2 t = make_double2(0., 0.);
-        if (w.k == 1) t = m.grp[g];
-        else {
-            if (lane < w.k) t = ld_cluster_d2(tc::smem_u32(m.grp + g), lane);
-            t = warp_sum(t);
+    for (int g = tid; g < sh.groups; g += w.threads) {       // the CTAs of the cluster
+        Part t = {m.grp[g], m.grp[sh.groups + g], m.grp[2 * sh.groups + g]};
+        if (w.k > 1) {
+            Part q[8];
+            #pragma unroll
+            for (int i = 0; i < 8; ++i)
+                q[i] = i < w.k ? Part{ld_cluster(m.grp + g, i), ld_cluster(m.grp + sh.groups + g, i), ld_cluster(m.grp + 2 * sh.groups + g, i)} : Part{0.f, 0.f, 0.f};
+            // (CTAs beyond the cluster, and those without positions, count for nothing)
+            t = join<8>(8, __fdividef(1.f, (float)w.HW * (float)sh.cg), [&](int i) { return q[i]; }, [&](int i) { return i < w.k ? (float)max(0, min(w.HW - i * w.ppc, w.ppc)) * (float)sh.cg : 0.f; });
         }
-        const double count = (double)sh.HW * sh.cg, mu = t.x / count;
-        double var = t.y / count - mu * mu;
-        if (var < 0.) var = 0.;
-        const float2 r = make_float2((float)mu, (float)(1. / sqrt(var + (double)sh.eps)));
-        if (lane == 0) {
-            m.res[g] = r;
-            if (rank == 0) { mean[n * sh.groups + g] = r.x; rstd[n * sh.groups + g] = r.y; }
-        }
+        const float2 r = statistics(t, sh);
+        m.res[g] = r;
+        if (rank == 0) { mean[n * sh.groups + g] = r.x; rstd[n * sh.groups + g] = r.y; }
     }
     if (w.k > 1) { __syncwarp(); tc::cluster_arrive(); }        // this CTA has read the others' sums
     __syncthreads();
@@ -598,17 +672,17 @@ __global__ void __launch_bounds__(kClThreads, 2) gn_cluster_forward_kernel(const
         #pragma unroll
         for (int i = 0; i < V; ++i) {
             const int c = min(V * v + i, w.C - 1);
-            const float2 r = m.res[c / sh.cg];
+            const float2 r = m.res[sh.group(c)];
             k.nm[i] = -r.x;
             k.a[i] = r.y * (weight ? weight[c] : 1.f);
             k.b[i] = bias ? bias[c] : 0.f;
         }
         T* yp = y + n * gy.sn + V * v;
         const int split = min(cnt, w.keep);
-        apply_positions<T, V>(k, sh, p0 + row, w.rows, 0, split, n * w.HW, v, has, yp, gy, kx, ky, [&](int it) { return has ? slots[it * w.threads] : R{}; });
+        apply_positions<T, V, ACT>(k, sh, p0 + row, w.rows, 0, split, n * w.HW, v, has, yp, gy, kx, ky, [&](int it) { return has ? slots[it * w.threads] : R{}; });
         if (split < cnt) {
             Cursor c(gx, p0 + row + split * w.rows);
-            apply_positions<T, V>(k, sh, p0 + row, w.rows, split, cnt, n * w.HW, v, has, yp, gy, kx, ky, [&](int) {
+            apply_positions<T, V, ACT>(k, sh, p0 + row, w.rows, split, cnt, n * w.HW, v, has, yp, gy, kx, ky, [&](int) {
                 R r = {};
                 if (has) r = *(const R*)(xp + c.off);
                 c.next(gx, w.rows);
@@ -621,7 +695,7 @@ __global__ void __launch_bounds__(kClThreads, 2) gn_cluster_forward_kernel(const
 
 // The same for the backward pass: sums of dz and dz d per channel, around the cluster for c1 and c2, then dx.  The samples' sums for dweight and
 // dbias go to partial [n][2][C] (a CTA joins the channels rank, rank + k, ... of its cluster) and are added over the samples by a second launch.
-template <typename T, int V, int SRC>
+template <typename T, int V, int SRC, int ACT>
 __global__ void __launch_bounds__(kClThreads, 2) gn_cluster_backward_kernel(const T* __restrict__ dy, const Geo gdy, const Source src, const Geo gx, const ClusterWalk w, const NormShape sh,
                                                                             const BackwardArgs A, T* __restrict__ dx, const Geo gdx, float* __restrict__ partial) {
     kn::pdl_sync();
@@ -633,7 +707,7 @@ __global__ void __launch_bounds__(kClThreads, 2) gn_cluster_backward_kernel(cons
     R* slots = (R*)smem + tid;
     X* xslots = (X*)(smem + slab * sizeof(R)) + tid;
     uint8_t* eslots = smem + slab * (sizeof(R) + sizeof(X)) + tid;
-    const ClusterSmem m = cluster_smem<V>(smem + slab * (sizeof(R) + sizeof(X)) + (SRC == kSrcSame ? 0 : (slab + 15) / 16 * 16), w, sh.groups);
+    const ClusterSmem<V> m(smem + slab * (sizeof(R) + sizeof(X)) + (SRC == kSrcSame ? 0 : (slab + 15) / 16 * 16), w, sh.groups, 2);
     const int rank = w.k > 1 ? (int)tc::cluster_ctarank() : 0;
     const long long n = blockIdx.x / w.k;
     const int row = tid / w.cols, v = tid - row * w.cols;
@@ -686,7 +760,7 @@ __global__ void __launch_bounds__(kClThreads, 2) gn_cluster_backward_kernel(cons
             fx.load(src, gx, Walk{w.C, w.HW}, n, p, v);
         }
         unpack<T, V>(r, q);
-        activation_gradient<T, V, SRC>(sh, k, A, n, V * v, fx, f, q);
+        activation_gradient<T, V, SRC, ACT>(sh, k, A, n, V * v, fx, f, q);
     };
     auto add = [&](int it) {
         float f[V], q[V];
@@ -704,47 +778,42 @@ __global__ void __launch_bounds__(kClThreads, 2) gn_cluster_backward_kernel(cons
     #pragma unroll 2
     for (int it = kept; it < cnt; ++it) add(it);
     #pragma unroll
-    for (int i = 0; i < V; ++i) m.part[tid * V + i] = make_float2(S1[i], S2[i]);
+    for (int i = 0; i < V; ++i) { m.part.at(0, i, tid) = S1[i]; m.part.at(1, i, tid) = S2[i]; }
     __syncthreads();
     for (int c = tid; c < w.C; c += w.threads) {
-        double2 t = make_double2(0., 0.);
-        for (int r = 0; r < w.rows; ++r) { const float2 q = m.part[r * w.cols * V + c]; t.x += q.x; t.y += q.y; }
-        t.y *= A.rstd[n * sh.groups + c / sh.cg];              // of xhat
-        m.chan[c] = t;
+        float2 t = make_float2(0.f, 0.f);
+        #pragma unroll 4
+        for (int r = 0; r < w.rows; ++r) { t.x += m.part.at(0, c % V, r * w.cols + c / V); t.y += m.part.at(1, c % V, r * w.cols + c / V); }
+        m.chan[c] = t.x;
+        m.chan[w.C + c] = t.y * A.rstd[n * sh.groups + sh.group(c)];            // of xhat
     }
     __syncthreads();
     for (int g = warp; g < sh.groups; g += warps) {
-        double2 t = make_double2(0., 0.);
-        for (int c = lane; c < sh.cg; c += 32) {
-            const double2 q = m.chan[g * sh.cg + c];
-            const double wt = A.weight ? A.weight[g * sh.cg + c] : 1.f;
-            t.x += wt * q.x;
-            t.y += wt * q.y;
+        float2 t = make_float2(0.f, 0.f);
+        for (int c = g * sh.cg + lane; c < (g + 1) * sh.cg; c += 32) {
+            const float wt = A.weight ? A.weight[c] : 1.f;
+            t.x = fmaf(wt, m.chan[c], t.x);
+            t.y = fmaf(wt, m.chan[w.C + c], t.y);
         }
         t = warp_sum(t);
-        if (lane == 0) m.grp[g] = t;
+        if (lane == 0) { m.grp[g] = t.x; m.grp[sh.groups + g] = t.y; }
     }
     __syncwarp();
     if (w.k > 1) tc::cluster_sync_all();
     else __syncthreads();
-    for (int g = warp; g < sh.groups; g += warps) {
-        double2 t = make_double2(0., 0.);
-        if (w.k == 1) t = m.grp[g];
-        else {
-            if (lane < w.k) t = ld_cluster_d2(tc::smem_u32(m.grp + g), lane);
-            t = warp_sum(t);
-        }
-        const double count = (double)sh.HW * sh.cg;
-        if (lane == 0) m.res[g] = make_float2((float)(t.x / count), (float)(t.y / count));
-    }
+    auto over_cluster = [&](const float* p) {
+        if (w.k == 1) return *p;
+        float t = 0.f;
+        #pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (i < w.k) t += ld_cluster(p, i);
+        return t;
+    };
+    const float count = (float)sh.HW * (float)sh.cg;
+    for (int g = tid; g < sh.groups; g += w.threads) m.res[g] = make_float2(__fdiv_rn(over_cluster(m.grp + g), count), __fdiv_rn(over_cluster(m.grp + sh.groups + g), count));
     for (int c = rank + w.k * tid; c < w.C; c += w.k * w.threads) {
-        double2 t = m.chan[c];
-        if (w.k > 1) {
-            t = make_double2(0., 0.);
-            for (int r = 0; r < w.k; ++r) { const double2 q = ld_cluster_d2(tc::smem_u32(m.chan + c), r); t.x += q.x; t.y += q.y; }
-        }
-        partial[n * 2 * w.C + c] = (float)t.x;
-        partial[n * 2 * w.C + w.C + c] = (float)t.y;
+        partial[n * 2 * w.C + c] = over_cluster(m.chan + c);
+        partial[n * 2 * w.C + w.C + c] = over_cluster(m.chan + w.C + c);
     }
     if (w.k > 1) { __syncwarp(); tc::cluster_arrive(); }
     __syncthreads();
@@ -752,7 +821,7 @@ __global__ void __launch_bounds__(kClThreads, 2) gn_cluster_backward_kernel(cons
         float B[V], D[V];
         #pragma unroll
         for (int i = 0; i < V; ++i) {
-            const int g = (V * v + i) / sh.cg;
+            const int g = sh.group(V * v + i);
             const float2 c = m.res[g];
             const float r = A.rstd[n * sh.groups + g];
             B[i] = -r * r * c.y;
@@ -772,26 +841,4 @@ __global__ void __launch_bounds__(kClThreads, 2) gn_cluster_backward_kernel(cons
     }
     if (w.k > 1) { __syncwarp(); tc::cluster_wait(); }
 }
-// dweight and dbias: the samples' sums, added in fp64.  A block takes 32 channels, its warps every 32nd sample.
-__global__ void __launch_bounds__(1024) gn_parameter_gradient_kernel(const float* __restrict__ partial, int C, long long n, float* __restrict__ dweight, float* __restrict__ dbias) {
-    kn::pdl_sync();
-    __shared__ double2 red[32][33];
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, c = blockIdx.x * 32 + lane;
-    double2 t = make_double2(0., 0.);
-    if (c < C) {
-        const float* p = partial + c;
-        #pragma unroll 8
-        for (long long i = warp; i < n; i += 32) { t.x += p[i * 2 * C]; t.y += p[i * 2 * C + C]; }
-    }
-    red[warp][lane] = t;
-    __syncthreads();
-    t = red[lane][warp];               // lane: part, warp: channel
-    t = warp_sum(t);
-    const int cw = blockIdx.x * 32 + warp;
-    if (lane == 0 && cw < C) {
-        if (dbias) dbias[cw] = (float)t.x;
-        if (dweight) dweight[cw] = (float)t.y;
-    }
-}
-
 }  // namespace op

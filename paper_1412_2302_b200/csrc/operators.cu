@@ -172,8 +172,8 @@ const char* check_shape(const alexnet_group_norm_t& s) {
     if (s.n * s.groups > kMaxGrid / 2) return "the tensor is too large";
     return nullptr;
 }
-NormShape norm_shape(const alexnet_group_norm_t& s) { return {s.channels, s.h * s.w, s.groups, s.channels / s.groups, s.eps, s.activation}; }
-size_t forward_ws(const Walk& w, const Dims& d) { return (size_t)(d.n * w.chunks) * d.C * sizeof(double2); }
+NormShape norm_shape(const alexnet_group_norm_t& s) { return {s.channels, s.h * s.w, s.groups, s.channels / s.groups, fast_div((uint32_t)(s.channels / s.groups)), s.eps, s.activation}; }
+size_t forward_ws(const Walk& w, const Dims& d) { return (size_t)(d.n * w.chunks) * d.C * sizeof(float4); }
 size_t backward_ws(const Walk& w, const Dims& d, int groups) { return (size_t)(d.n * groups) * sizeof(float2) + (size_t)(d.n * w.chunks) * 2 * d.C * sizeof(float); }
 
 constexpr size_t kSmSmem = 228 * 1024, kCtaSmem = 227 * 1024;
@@ -181,7 +181,7 @@ constexpr size_t kSmSmem = 228 * 1024, kCtaSmem = 227 * 1024;
 // block, or too few samples to fill the device with their clusters).  By a model in cycles: an SM moves 22 bytes per cycle, a round of CTAs
 // costs 5000 more for its first loads and the sums' way around, and vectors that do not stay on chip are read again at 40 bytes.
 template <int V>
-ClusterWalk cluster_walk(const Dims& d, int groups, int slot, int moved) {
+ClusterWalk cluster_walk(const Dims& d, int groups, int slot, int moved, int K) {
     ClusterWalk best{};
     ClusterWalk w{};
     w.C = d.C; w.HW = d.h * d.w; w.vecs = d.C / V;
@@ -195,7 +195,7 @@ ClusterWalk cluster_walk(const Dims& d, int groups, int slot, int moved) {
             if (w.threads < w.cols) continue;
             w.rows = w.threads / w.cols;
             w.its = (int)ceil_div(w.ppc, w.rows);
-            const size_t scratch = cluster_scratch<V>(w, groups) + 64, per_it = (size_t)w.threads * slot;
+            const size_t scratch = cluster_scratch<V>(w, groups, K) + 64, per_it = (size_t)w.threads * slot;
             if (scratch + 1024 > kCtaSmem) continue;
             for (int occ = 1; occ <= 4 && occ * w.threads <= 2 * kClThreads; ++occ) {
                 const size_t room = std::min(kCtaSmem, kSmSmem / occ - 1024);
@@ -214,21 +214,21 @@ ClusterWalk cluster_walk(const Dims& d, int groups, int slot, int moved) {
 template <typename K>
 cudaError_t allow_smem(K* kernel) { return cudaFuncSetAttribute((const void*)kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kCtaSmem); }
 
-template <typename T, int V>
+template <typename T, int V, int ACT>
 void forward(Launcher& go, const alexnet_group_norm_forward_t* a, const Dims& d) {
     const Walk w = walk_of(d, V);
     const NormShape s = norm_shape(a->shape);
-    const ClusterWalk cw = cluster_walk<V>(d, s.groups, sizeof(T) * V, 2 * sizeof(T) * V);
+    const ClusterWalk cw = cluster_walk<V>(d, s.groups, sizeof(T) * V, 2 * sizeof(T) * V, 3);
     if (cw.k) {
         Keep kx{}, ky{};
         if (V == 8) {
             if (a->keep_x.codes) kx = {(uint8_t*)a->keep_x.codes, a->keep_x.scales, src_of(a->keep_x.format)};
             if (a->keep_y.codes) ky = {(uint8_t*)a->keep_y.codes, a->keep_y.scales, src_of(a->keep_y.format)};
         }
-        if (go.e == cudaSuccess) go.e = allow_smem(gn_cluster_forward_kernel<T, V>);
-        go.smem = (size_t)cw.keep * cw.threads * sizeof(T) * V + cluster_scratch<V>(cw, s.groups);
+        if (go.e == cudaSuccess) go.e = allow_smem(gn_cluster_forward_kernel<T, V, ACT>);
+        go.smem = (size_t)cw.keep * cw.threads * sizeof(T) * V + cluster_scratch<V>(cw, s.groups, 3);
         go.cluster = cw.k;
-        go(gn_cluster_forward_kernel<T, V>, d.n * cw.k, cw.threads, (const T*)a->x.data, geo_of(a->x, d), cw, s, a->weight, a->bias, (T*)a->y.data, geo_of(a->y, d), a->mean, a->rstd, kx, ky);
+        go(gn_cluster_forward_kernel<T, V, ACT>, d.n * cw.k, cw.threads, (const T*)a->x.data, geo_of(a->x, d), cw, s, a->weight, a->bias, (T*)a->y.data, geo_of(a->y, d), a->mean, a->rstd, kx, ky);
         if (V != 8) {
             if (a->keep_x.codes) encode<T>(go, d, a->x, a->keep_x, a->shape.dtype);
             if (a->keep_y.codes) encode<T>(go, d, a->y, a->keep_y, a->shape.dtype);
@@ -236,7 +236,7 @@ void forward(Launcher& go, const alexnet_group_norm_forward_t* a, const Dims& d)
         return;
     }
     const Geo gx = geo_of(a->x, d), gy = geo_of(a->y, d);
-    double2* partial = (double2*)a->workspace;
+    float4* partial = (float4*)a->workspace;
     const T *x = (const T*)a->x.data;
     Keep kx{}, ky{};
     if (V == 8) {
@@ -244,14 +244,14 @@ void forward(Launcher& go, const alexnet_group_norm_forward_t* a, const Dims& d)
         if (a->keep_y.codes) ky = {(uint8_t*)a->keep_y.codes, a->keep_y.scales, src_of(a->keep_y.format)};
     }
     go(gn_sums_kernel<T, V>, grid_of(w, d), 256, x, gx, w, partial);
-    go(gn_statistics_kernel, d.n * s.groups, 128, (const double2*)partial, s, w.chunks, a->mean, a->rstd);
-    go(gn_apply_kernel<T, V>, grid_of(w, d), 256, x, gx, w, s, a->weight, a->bias, (const float*)a->mean, (const float*)a->rstd, (T*)a->y.data, gy, kx, ky);
+    go(gn_statistics_kernel, d.n * s.groups, 256, (const float4*)partial, s, (int)w.chunks, w.ppc, a->mean, a->rstd);
+    go(gn_apply_kernel<T, V, ACT>, grid_of(w, d), 256, x, gx, w, s, a->weight, a->bias, (const float*)a->mean, (const float*)a->rstd, (T*)a->y.data, gy, kx, ky);
     if (V != 8) {
         if (a->keep_x.codes) encode<T>(go, d, a->x, a->keep_x, a->shape.dtype);
         if (a->keep_y.codes) encode<T>(go, d, a->y, a->keep_y, a->shape.dtype);
     }
 }
-template <typename T, int V, int SRC>
+template <typename T, int V, int SRC, int ACT>
 void backward(Launcher& go, const alexnet_group_norm_backward_t* a, const Dims& d) {
     const Walk w = walk_of(d, V);
     const NormShape s = norm_shape(a->shape);
@@ -262,27 +262,42 @@ void backward(Launcher& go, const alexnet_group_norm_backward_t* a, const Dims& 
     const BackwardArgs A{a->mean, a->rstd, a->weight, a->bias};
     const T* dy = (const T*)a->dy.data;
     constexpr int kX = SRC == kSrcSame ? (int)sizeof(T) * V : V, kSlot = (int)sizeof(T) * V + kX + (SRC == kSrcSame ? 0 : 1);
-    const ClusterWalk cw = cluster_walk<V>(d, s.groups, kSlot, 2 * (int)sizeof(T) * V + kX);
+    const ClusterWalk cw = cluster_walk<V>(d, s.groups, kSlot, 2 * (int)sizeof(T) * V + kX, 2);
     if (cw.k) {
         partial = (float*)a->workspace;
-        auto* kernel = gn_cluster_backward_kernel<T, V, SRC>;
+        auto* kernel = gn_cluster_backward_kernel<T, V, SRC, ACT>;
         if (go.e == cudaSuccess) go.e = allow_smem(kernel);
         const size_t slab = (size_t)cw.keep * cw.threads;
-        go.smem = slab * (kSlot - (SRC == kSrcSame ? 0 : 1)) + (SRC == kSrcSame ? 0 : (slab + 15) / 16 * 16) + cluster_scratch<V>(cw, s.groups);
+        go.smem = slab * (kSlot - (SRC == kSrcSame ? 0 : 1)) + (SRC == kSrcSame ? 0 : (slab + 15) / 16 * 16) + cluster_scratch<V>(cw, s.groups, 2);
         go.cluster = cw.k;
         go(kernel, d.n * cw.k, cw.threads, dy, gdy, src, gx, cw, s, A, (T*)a->dx.data, gdx, partial);
         if (a->dweight || a->dbias) go(gn_parameter_gradient_kernel, ceil_div(d.C, 32), 1024, (const float*)partial, d.C, d.n, a->dweight, a->dbias);
         return;
     }
-    go(gn_backward_sums_kernel<T, V, SRC>, grid_of(w, d), 256, dy, gdy, src, gx, w, s, A, partial);
-    go(gn_backward_final_kernel, d.n * s.groups + (a->dweight || a->dbias ? ceil_div(d.C, 32) : 0), 256, (const float*)partial, s, d.n, w.chunks, A, c12, a->dweight, a->dbias);
-    go(gn_backward_apply_kernel<T, V, SRC>, grid_of(w, d), 256, dy, gdy, src, gx, w, s, A, (const float2*)c12, (T*)a->dx.data, gdx);
+    go(gn_backward_sums_kernel<T, V, SRC, ACT>, grid_of(w, d), 256, dy, gdy, src, gx, w, s, A, partial);
+    go(gn_backward_group_kernel, d.n * s.groups, 256, (const float*)partial, s, (int)w.chunks, A, c12);
+    if (a->dweight || a->dbias) go(gn_parameter_gradient_kernel, ceil_div(d.C, 32), 1024, (const float*)partial, d.C, d.n * w.chunks, a->dweight, a->dbias);
+    go(gn_backward_apply_kernel<T, V, SRC, ACT>, grid_of(w, d), 256, dy, gdy, src, gx, w, s, A, (const float2*)c12, (T*)a->dx.data, gdx);
+}
+template <typename T, int V, int SRC>
+void backward(Launcher& go, const alexnet_group_norm_backward_t* a, const Dims& d) {
+    if constexpr (V == 1) backward<T, V, SRC, kActAny>(go, a, d);
+    else if (a->shape.activation == ALEXNET_ACT_NONE) backward<T, V, SRC, kActNone>(go, a, d);
+    else if (a->shape.activation == ALEXNET_ACT_RELU) backward<T, V, SRC, kActRelu>(go, a, d);
+    else backward<T, V, SRC, kActSilu>(go, a, d);
 }
 template <typename T, int V>
 void backward(Launcher& go, const alexnet_group_norm_backward_t* a, const Dims& d) {
     if (a->x.data) backward<T, V, kSrcSame>(go, a, d);
     else if (a->kept.format == ALEXNET_CODES_INT8) backward<T, V, kSrcInt8>(go, a, d);
     else backward<T, V, kSrcE4m3>(go, a, d);
+}
+template <typename T, int V>
+void forward(Launcher& go, const alexnet_group_norm_forward_t* a, const Dims& d) {
+    if constexpr (V == 1) forward<T, V, kActAny>(go, a, d);
+    else if (a->shape.activation == ALEXNET_ACT_NONE) forward<T, V, kActNone>(go, a, d);
+    else if (a->shape.activation == ALEXNET_ACT_RELU) forward<T, V, kActRelu>(go, a, d);
+    else forward<T, V, kActSilu>(go, a, d);
 }
 
 // ---------------------------------------------------------------- linear weight gradient
