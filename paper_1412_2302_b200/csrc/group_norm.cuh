@@ -41,23 +41,30 @@ template <int V> __device__ __forceinline__ void v_fma(const float* a, const flo
         for (int i = 0; i < V; i += 2) un2(fma2(mk2(a[i], a[i + 1]), mk2(b[i], b[i + 1]), mk2(c[i], c[i + 1])), o[i], o[i + 1]);
     }
 }
-// s = 1 / (1 + e^-z).  fp32 tensors take the accurate functions; 16-bit ones the hardware's approximate ones, without their care for subnormal
-// numbers (relative error below 2^-20 for |z| < 16, next to a rounding of 2^-9 or 2^-12; below z = -87 the result is 0).
+// s = 1 / (1 + e^-z).  fp32 tensors take the accurate functions; 16-bit ones the hardware's approximate ones (relative error below 2^-20 for |z| < 16, next to
+// a rounding of 2^-9 or 2^-12).  The special-function unit takes 16 values per SM and cycle and bounds SiLU's passes, so two values share
+// one reciprocal: 1 / a = b / (a b).  For that e^-z stops at 2^63: below z = -43 s is 2^-63, which is off by less than 2^-57 in any result.
 template <typename T, int V> __device__ __forceinline__ void sigmoid(const float* z, float* s) {
     if constexpr (sizeof(T) == 4) {
         #pragma unroll
         for (int i = 0; i < V; ++i) s[i] = __fdiv_rn(1.f, 1.f + expf(-z[i]));
     } else {
-        const float l = -1.44269504f;
         float t[V], one[V], ls[V];
         #pragma unroll
-        for (int i = 0; i < V; ++i) { one[i] = 1.f; ls[i] = l; }
+        for (int i = 0; i < V; ++i) { one[i] = 1.f; ls[i] = -1.44269504f; }
         v_mul<V>(z, ls, t);
         #pragma unroll
-        for (int i = 0; i < V; ++i) asm("ex2.approx.ftz.f32 %0, %0;" : "+f"(t[i]));
+        for (int i = 0; i < V; ++i) asm("min.NaN.f32 %0, %0, %1;\n\tex2.approx.ftz.f32 %0, %0;" : "+f"(t[i]) : "f"(63.f));
         v_add<V>(t, one, t);
-        #pragma unroll
-        for (int i = 0; i < V; ++i) asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(s[i]) : "f"(t[i]));
+        if constexpr (V == 1) asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(s[0]) : "f"(t[0]));
+        else {
+            #pragma unroll
+            for (int i = 0; i < V; i += 2) {
+                float r;
+                asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(t[i] * t[i + 1]));
+                un2(mul2(mk2(t[i + 1], t[i]), mk2(r, r)), s[i], s[i + 1]);
+            }
+        }
     }
 }
 // ACT: the activation, or kActAny to take it from `act`
@@ -117,6 +124,31 @@ template <int UNROLL, typename G, typename N> __device__ __forceinline__ Part jo
         e += w;
         q += fmaf(w, d, t.m2);
     }
+    const float lo = e * inv;
+    return {hi, lo, fmaf(-e, lo, q)};
+}
+// The same by `lanes` neighbouring lanes (a power of two): each takes every lanes-th part; the result is the same in all of them.  All 32 lanes of the warp
+// call it; inactive ones have count = 0.
+__device__ __forceinline__ float lanes_sum(float t, int lanes) {
+    for (int o = lanes >> 1; o; o >>= 1) t += __shfl_xor_sync(~0u, t, o);
+    return t;
+}
+template <typename G, typename N> __device__ __forceinline__ Part join_lanes(int count, int lanes, float inv, G get, N n) {
+    const int first = threadIdx.x & (lanes - 1);
+    const float ref = count ? get(0).hi : 0.f;
+    float m = 0.f, e = 0.f, q = 0.f;
+    #pragma unroll 4
+    for (int i = first; i < count; i += lanes) m = fmaf(n(i), get(i).hi - ref, m);
+    const float hi = fmaf(lanes_sum(m, lanes), inv, ref);
+    #pragma unroll 4
+    for (int i = first; i < count; i += lanes) {
+        const Part t = get(i);
+        const float d = (t.hi - hi) + t.lo, w = n(i) * d;
+        e += w;
+        q += fmaf(w, d, t.m2);
+    }
+    e = lanes_sum(e, lanes);
+    q = lanes_sum(q, lanes);
     const float lo = e * inv;
     return {hi, lo, fmaf(-e, lo, q)};
 }
@@ -505,9 +537,13 @@ __global__ void __launch_bounds__(256) gn_backward_apply_kernel(const T* __restr
 // asynchronous copies) while the sums go around the cluster through distributed shared memory, then turns them into the result:
 // every value is read from memory once.  Slots are private to a thread, so no barrier stands between its copies and its reads.
 // Iterations beyond `keep` (samples too large for the cluster's shared memory) are read again, from L2.
+// A block may also take a slice of the channels, of whole groups (and whole checkpoint blocks): slices have nothing to do with one another.
 struct ClusterWalk {
-    int C, HW, vecs, cols, rows, threads;     // rows = threads / cols
+    int C, HW;                                // of the tensor
+    int slices, Cs, groups;                   // channel slices; channels and groups of one
+    int vecs, cols, rows, threads;            // vectors of a slice's row; rows = threads / cols
     int k, ppc, its, keep;                    // CTAs of the cluster; positions of a CTA, at most; iterations of a thread, and those whose vectors stay
+    int lanes;                                // a power of two: lanes that join a group's sums
 };
 constexpr int kClThreads = 384;               // at most; two CTAs per SM with 80 registers
 
@@ -541,14 +577,37 @@ template <int V> struct ClusterSmem {
     Table<V> part;
     float *chan, *grp;       // [K][C], [K][groups]
     float2* res;
-    __device__ __forceinline__ ClusterSmem(uint8_t* p, const ClusterWalk& w, int groups, int K) {
+    __device__ __forceinline__ ClusterSmem(uint8_t* p, const ClusterWalk& w, int K) {
         res = (float2*)p;
-        part = {(float*)(res + groups), w.threads + 4};
+        part = {(float*)(res + w.groups), w.threads + 4};
         chan = part.p + K * V * part.pitch;
-        grp = chan + K * w.C;
+        grp = chan + K * w.Cs;
     }
 };
-template <int V> inline size_t cluster_scratch(const ClusterWalk& w, int groups, int K) { return ((size_t)K * V * (w.threads + 4) + K * w.C + K * groups) * sizeof(float) + groups * sizeof(float2); }
+template <int V> inline size_t cluster_scratch(const ClusterWalk& w, int K) { return ((size_t)K * V * (w.threads + 4) + K * w.Cs + K * w.groups) * sizeof(float) + w.groups * sizeof(float2); }
+// a block's place: sample, first channel, first group (within the sample), rank in its cluster
+struct ClusterSpot {
+    long long n;
+    int c0, g0, rank;
+    __device__ __forceinline__ ClusterSpot(const ClusterWalk& w) {
+        const long long b = blockIdx.x / w.k;
+        n = b / w.slices;
+        const int slice = (int)(b - n * w.slices);
+        c0 = slice * w.Cs;
+        g0 = slice * w.groups;
+        rank = w.k > 1 ? (int)tc::cluster_ctarank() : 0;
+    }
+};
+// V channels' parameters, or `other` where there are none
+template <int V> __device__ __forceinline__ void load_parameters(const float* p, int c, float other, float* out) {
+    if (V == 8 && p && ((uintptr_t)p & 15) == 0) {
+        *(float4*)out = *(const float4*)(p + c);
+        *(float4*)(out + 4) = *(const float4*)(p + c + 4);
+    } else {
+        #pragma unroll
+        for (int i = 0; i < V; ++i) out[i] = p ? p[c + i] : other;
+    }
+}
 
 template <typename T, int V, int ACT>
 __global__ void __launch_bounds__(kClThreads, 2) gn_cluster_forward_kernel(const T* __restrict__ x, const Geo gx, const ClusterWalk w, const NormShape sh, const float* __restrict__ weight,
@@ -559,14 +618,19 @@ __global__ void __launch_bounds__(kClThreads, 2) gn_cluster_forward_kernel(const
     using R = Raw<T, V>;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, warps = w.threads >> 5;
     R* slots = (R*)smem + tid;
-    const ClusterSmem<V> m(smem + (size_t)w.keep * w.threads * sizeof(R), w, sh.groups, 3);
-    const int rank = w.k > 1 ? (int)tc::cluster_ctarank() : 0;
-    const long long n = blockIdx.x / w.k;
+    const ClusterSmem<V> m(smem + (size_t)w.keep * w.threads * sizeof(R), w, 3);
+    const ClusterSpot b(w);
+    const long long n = b.n;
     const int row = tid / w.cols, v = tid - row * w.cols;
     const bool on = row < w.rows, has = on && v < w.vecs;
-    const int p0 = rank * w.ppc, np = max(0, min(w.HW - p0, w.ppc));
+    const int p0 = b.rank * w.ppc, np = max(0, min(w.HW - p0, w.ppc));
     const int cnt = on && row < np ? (np - row + w.rows - 1) / w.rows : 0;      // iterations of this thread
-    const T* xp = x + n * gx.sn + V * v;
+    const T* xp = x + n * gx.sn + b.c0 + V * v;
+    Chan<V> k = {};                             // (weight and bias; the statistics join them)
+    if (has) {
+        load_parameters<V>(weight, b.c0 + V * v, 1.f, k.a);
+        load_parameters<V>(bias, b.c0 + V * v, 0.f, k.b);
+    }
 
     // sums
     float nK[V], S[V], Q[V];
@@ -575,10 +639,10 @@ __global__ void __launch_bounds__(kClThreads, 2) gn_cluster_forward_kernel(const
     const int kept = has ? min(cnt, w.keep) : 0, batch = (w.keep + kClBatches - 1) / kClBatches;
     Cursor cur(gx, p0 + row);
     #pragma unroll 1
-    for (int b = 0; b < kClBatches; ++b) {
-        const int e = min(kept, (b + 1) * batch);
+    for (int bt = 0; bt < kClBatches; ++bt) {
+        const int e = min(kept, (bt + 1) * batch);
         #pragma unroll 4
-        for (int it = b * batch; it < e; ++it) {
+        for (int it = bt * batch; it < e; ++it) {
             fill_slot(slots + it * w.threads, xp + cur.off);
             cur.next(gx, w.rows);
         }
@@ -597,12 +661,12 @@ __global__ void __launch_bounds__(kClThreads, 2) gn_cluster_forward_kernel(const
         v_fma<V>(f, f, Q, Q);
     };
     #pragma unroll 1
-    for (int b = 0; b < kClBatches; ++b) {
-        copies_wait(kClBatches - 1 - b);
-        const int e = min(kept, (b + 1) * batch);
-        if (b == 0 && kept > 0) shift(slots[0]);
+    for (int bt = 0; bt < kClBatches; ++bt) {
+        copies_wait(kClBatches - 1 - bt);
+        const int e = min(kept, (bt + 1) * batch);
+        if (bt == 0 && kept > 0) shift(slots[0]);
         #pragma unroll 2
-        for (int it = b * batch; it < e; ++it) add(slots[it * w.threads]);
+        for (int it = bt * batch; it < e; ++it) add(slots[it * w.threads]);
     }
     if (has) {
         if (kept == 0 && cnt > 0) shift(*(const R*)(xp + cur.off));
@@ -625,64 +689,55 @@ __global__ void __launch_bounds__(kClThreads, 2) gn_cluster_forward_kernel(const
         m.part.at(0, i, tid) = t.hi; m.part.at(1, i, tid) = t.lo; m.part.at(2, i, tid) = t.m2;
     }
     __syncthreads();
-    const float inv = np ? __fdividef(1.f, (float)np) : 0.f;
-    for (int c = tid; c < w.C; c += w.threads) {
-        const Part t = join_rows<V>(m.part, c, min(w.rows, max(np, 1)), w.cols, np % w.rows, (float)(np / w.rows), inv);
-        m.chan[c] = t.hi; m.chan[w.C + c] = t.lo; m.chan[2 * w.C + c] = t.m2;
-    }
-    __syncthreads();
-    for (int g = warp; g < sh.groups; g += warps) {          // the channels of a group: parts of np values
-        const float* q = m.chan + g * sh.cg;
-        const float ref = q[0], per = __fdividef(1.f, (float)sh.cg);
-        float2 s = make_float2(0.f, 0.f);
-        for (int c = lane; c < sh.cg; c += 32) s.x += q[c] - ref;
-        const float hi = fmaf(warp_sum(s.x), per, ref);
-        s.x = 0.f;
-        for (int c = lane; c < sh.cg; c += 32) {
-            const float d = (q[c] - hi) + q[w.C + c];
-            s.x += d;
-            s.y += fmaf((float)np * d, d, q[2 * w.C + c]);
+    {
+        // of this CTA: the parts of the group's channels and of the rows of threads that have positions, the first `more` rows one more than the others
+        const int rows = min(w.rows, np), more = np % w.rows;
+        const float n_lo = (float)(np / w.rows), inv = np ? __fdividef(1.f, (float)np * (float)sh.cg) : 0.f;
+        const int at_once = 32 / w.lanes;
+        for (int g0 = warp * at_once; g0 < w.groups; g0 += warps * at_once) {
+            const int g = g0 + lane / w.lanes, c0 = g * sh.cg;
+            const Part t = join_lanes(g < w.groups ? rows * sh.cg : 0, w.lanes, inv, [&](int i) {
+                const int r = sh.group(i), c = c0 + i - r * sh.cg, at = r * w.cols + c / V;
+                return Part{m.part.at(0, c % V, at), m.part.at(1, c % V, at), m.part.at(2, c % V, at)};
+            }, [&](int i) { return sh.group(i) < more ? n_lo + 1.f : n_lo; });
+            if (g < w.groups && lane % w.lanes == 0) { m.grp[g] = t.hi; m.grp[w.groups + g] = t.lo; m.grp[2 * w.groups + g] = t.m2; }
         }
-        s = warp_sum(s);
-        if (lane == 0) { m.grp[g] = hi; m.grp[sh.groups + g] = s.x * per; m.grp[2 * sh.groups + g] = fmaf(-(float)np * s.x, s.x * per, s.y); }
     }
     __syncwarp();
     if (w.k > 1) tc::cluster_sync_all();
     else __syncthreads();
-    for (int g = tid; g < sh.groups; g += w.threads) {       // the CTAs of the cluster
-        Part t = {m.grp[g], m.grp[sh.groups + g], m.grp[2 * sh.groups + g]};
+    for (int g = tid; g < w.groups; g += w.threads) {        // the CTAs of the cluster
+        Part t = {m.grp[g], m.grp[w.groups + g], m.grp[2 * w.groups + g]};
         if (w.k > 1) {
             Part q[8];
             #pragma unroll
             for (int i = 0; i < 8; ++i)
-                q[i] = i < w.k ? Part{ld_cluster(m.grp + g, i), ld_cluster(m.grp + sh.groups + g, i), ld_cluster(m.grp + 2 * sh.groups + g, i)} : Part{0.f, 0.f, 0.f};
+                q[i] = i < w.k ? Part{ld_cluster(m.grp + g, i), ld_cluster(m.grp + w.groups + g, i), ld_cluster(m.grp + 2 * w.groups + g, i)} : Part{0.f, 0.f, 0.f};
             // (CTAs beyond the cluster, and those without positions, count for nothing)
             t = join<8>(8, __fdividef(1.f, (float)w.HW * (float)sh.cg), [&](int i) { return q[i]; }, [&](int i) { return i < w.k ? (float)max(0, min(w.HW - i * w.ppc, w.ppc)) * (float)sh.cg : 0.f; });
         }
         const float2 r = statistics(t, sh);
         m.res[g] = r;
-        if (rank == 0) { mean[n * sh.groups + g] = r.x; rstd[n * sh.groups + g] = r.y; }
+        if (b.rank == 0) { mean[n * sh.groups + b.g0 + g] = r.x; rstd[n * sh.groups + b.g0 + g] = r.y; }
     }
     if (w.k > 1) { __syncwarp(); tc::cluster_arrive(); }        // this CTA has read the others' sums
     __syncthreads();
 
     // result
     if (cnt > 0) {
-        Chan<V> k;
         #pragma unroll
         for (int i = 0; i < V; ++i) {
-            const int c = min(V * v + i, w.C - 1);
-            const float2 r = m.res[sh.group(c)];
+            const float2 r = m.res[sh.group(min(V * v + i, w.Cs - 1))];
             k.nm[i] = -r.x;
-            k.a[i] = r.y * (weight ? weight[c] : 1.f);
-            k.b[i] = bias ? bias[c] : 0.f;
+            k.a[i] *= r.y;
         }
-        T* yp = y + n * gy.sn + V * v;
+        T* yp = y + n * gy.sn + b.c0 + V * v;
+        const int cv = b.c0 / V + v;                // vector within the tensor's row
         const int split = min(cnt, w.keep);
-        apply_positions<T, V, ACT>(k, sh, p0 + row, w.rows, 0, split, n * w.HW, v, has, yp, gy, kx, ky, [&](int it) { return has ? slots[it * w.threads] : R{}; });
+        apply_positions<T, V, ACT>(k, sh, p0 + row, w.rows, 0, split, n * w.HW, cv, has, yp, gy, kx, ky, [&](int it) { return has ? slots[it * w.threads] : R{}; });
         if (split < cnt) {
             Cursor c(gx, p0 + row + split * w.rows);
-            apply_positions<T, V, ACT>(k, sh, p0 + row, w.rows, split, cnt, n * w.HW, v, has, yp, gy, kx, ky, [&](int) {
+            apply_positions<T, V, ACT>(k, sh, p0 + row, w.rows, split, cnt, n * w.HW, cv, has, yp, gy, kx, ky, [&](int) {
                 R r = {};
                 if (has) r = *(const R*)(xp + c.off);
                 c.next(gx, w.rows);
@@ -707,23 +762,23 @@ __global__ void __launch_bounds__(kClThreads, 2) gn_cluster_backward_kernel(cons
     R* slots = (R*)smem + tid;
     X* xslots = (X*)(smem + slab * sizeof(R)) + tid;
     uint8_t* eslots = smem + slab * (sizeof(R) + sizeof(X)) + tid;
-    const ClusterSmem<V> m(smem + slab * (sizeof(R) + sizeof(X)) + (SRC == kSrcSame ? 0 : (slab + 15) / 16 * 16), w, sh.groups, 2);
-    const int rank = w.k > 1 ? (int)tc::cluster_ctarank() : 0;
-    const long long n = blockIdx.x / w.k;
+    const ClusterSmem<V> m(smem + slab * (sizeof(R) + sizeof(X)) + (SRC == kSrcSame ? 0 : (slab + 15) / 16 * 16), w, 2);
+    const ClusterSpot b(w);
+    const long long n = b.n, gb = n * sh.groups + b.g0;       // gb: this block's first group
     const int row = tid / w.cols, v = tid - row * w.cols;
     const bool has = row < w.rows && v < w.vecs;
-    const int p0 = rank * w.ppc, np = max(0, min(w.HW - p0, w.ppc));
+    const int p0 = b.rank * w.ppc, np = max(0, min(w.HW - p0, w.ppc));
     const int cnt = has && row < np ? (np - row + w.rows - 1) / w.rows : 0;
-    const T* dp = dy + n * gdy.sn + V * v;
-    const int blocks = (w.C + 31) / 32, kept = min(cnt, w.keep), batch = (w.keep + kClBatches - 1) / kClBatches;
-    const T* xp = SRC == kSrcSame ? (const T*)src.x + n * gx.sn + V * v : nullptr;
-    const uint8_t* cp = SRC == kSrcSame ? nullptr : src.codes + (n * w.HW + p0 + row) * w.C + V * v;
+    const T* dp = dy + n * gdy.sn + b.c0 + V * v;
+    const int cv = b.c0 / V + v, blocks = (w.C + 31) / 32, kept = min(cnt, w.keep), batch = (w.keep + kClBatches - 1) / kClBatches;
+    const T* xp = SRC == kSrcSame ? (const T*)src.x + n * gx.sn + V * cv : nullptr;
+    const uint8_t* cp = SRC == kSrcSame ? nullptr : src.codes + (n * w.HW + p0 + row) * w.C + V * cv;
     Cursor cdy(gdy, p0 + row), cx(gx, p0 + row);
     #pragma unroll 1
-    for (int b = 0; b < kClBatches; ++b) {
-        const int e = min(kept, (b + 1) * batch);
+    for (int bt = 0; bt < kClBatches; ++bt) {
+        const int e = min(kept, (bt + 1) * batch);
         #pragma unroll 2
-        for (int it = b * batch; it < e; ++it) {
+        for (int it = bt * batch; it < e; ++it) {
             fill_slot(slots + it * w.threads, dp + cdy.off);
             cdy.next(gdy, w.rows);
             if constexpr (SRC == kSrcSame) {
@@ -737,12 +792,12 @@ __global__ void __launch_bounds__(kClThreads, 2) gn_cluster_backward_kernel(cons
         copies_commit();
     }
     if constexpr (SRC != kSrcSame) {
-        const uint8_t* ep = src.scales + (n * w.HW + p0 + row) * blocks + V * v / 32;
+        const uint8_t* ep = src.scales + (n * w.HW + p0 + row) * blocks + V * cv / 32;
         #pragma unroll 8
         for (int it = 0; it < kept; ++it) eslots[it * w.threads] = ep[(long long)it * w.rows * blocks];
     }
     Chan<V> k;
-    if (has) load_chan<V>(k, sh, A.mean, A.rstd, A.weight, A.bias, n, V * v);
+    if (has) load_chan<V>(k, sh, A.mean, A.rstd, A.weight, A.bias, n, V * cv);
     float S1[V], S2[V];
     #pragma unroll
     for (int i = 0; i < V; ++i) S1[i] = S2[i] = 0.f;
@@ -757,10 +812,10 @@ __global__ void __launch_bounds__(kClThreads, 2) gn_cluster_backward_kernel(cons
         } else {
             const int p = p0 + row + it * w.rows;
             r = *(const R*)(dp + gdy.at(p));
-            fx.load(src, gx, Walk{w.C, w.HW}, n, p, v);
+            fx.load(src, gx, Walk{w.C, w.HW}, n, p, cv);
         }
         unpack<T, V>(r, q);
-        activation_gradient<T, V, SRC, ACT>(sh, k, A, n, V * v, fx, f, q);
+        activation_gradient<T, V, SRC, ACT>(sh, k, A, n, V * cv, fx, f, q);
     };
     auto add = [&](int it) {
         float f[V], q[V];
@@ -769,34 +824,37 @@ __global__ void __launch_bounds__(kClThreads, 2) gn_cluster_backward_kernel(cons
         v_fma<V>(f, q, S2, S2);
     };
     #pragma unroll 1
-    for (int b = 0; b < kClBatches; ++b) {
-        copies_wait(kClBatches - 1 - b);
-        const int e = min(kept, (b + 1) * batch);
+    for (int bt = 0; bt < kClBatches; ++bt) {
+        copies_wait(kClBatches - 1 - bt);
+        const int e = min(kept, (bt + 1) * batch);
         #pragma unroll 1
-        for (int it = b * batch; it < e; ++it) add(it);
+        for (int it = bt * batch; it < e; ++it) add(it);
     }
     #pragma unroll 2
     for (int it = kept; it < cnt; ++it) add(it);
     #pragma unroll
     for (int i = 0; i < V; ++i) { m.part.at(0, i, tid) = S1[i]; m.part.at(1, i, tid) = S2[i]; }
     __syncthreads();
-    for (int c = tid; c < w.C; c += w.threads) {
+    for (int c = tid; c < w.Cs; c += w.threads) {
         float2 t = make_float2(0.f, 0.f);
         #pragma unroll 4
         for (int r = 0; r < w.rows; ++r) { t.x += m.part.at(0, c % V, r * w.cols + c / V); t.y += m.part.at(1, c % V, r * w.cols + c / V); }
         m.chan[c] = t.x;
-        m.chan[w.C + c] = t.y * A.rstd[n * sh.groups + sh.group(c)];            // of xhat
+        m.chan[w.Cs + c] = t.y * A.rstd[gb + sh.group(c)];            // of xhat
     }
     __syncthreads();
-    for (int g = warp; g < sh.groups; g += warps) {
+    for (int g0 = warp * (32 / w.lanes); g0 < w.groups; g0 += warps * (32 / w.lanes)) {
+        const int g = g0 + lane / w.lanes;
         float2 t = make_float2(0.f, 0.f);
-        for (int c = g * sh.cg + lane; c < (g + 1) * sh.cg; c += 32) {
-            const float wt = A.weight ? A.weight[c] : 1.f;
-            t.x = fmaf(wt, m.chan[c], t.x);
-            t.y = fmaf(wt, m.chan[w.C + c], t.y);
-        }
-        t = warp_sum(t);
-        if (lane == 0) { m.grp[g] = t.x; m.grp[sh.groups + g] = t.y; }
+        if (g < w.groups)
+            for (int c = g * sh.cg + lane % w.lanes; c < (g + 1) * sh.cg; c += w.lanes) {
+                const float wt = A.weight ? A.weight[b.c0 + c] : 1.f;
+                t.x = fmaf(wt, m.chan[c], t.x);
+                t.y = fmaf(wt, m.chan[w.Cs + c], t.y);
+            }
+        t.x = lanes_sum(t.x, w.lanes);
+        t.y = lanes_sum(t.y, w.lanes);
+        if (g < w.groups && lane % w.lanes == 0) { m.grp[g] = t.x; m.grp[w.groups + g] = t.y; }
     }
     __syncwarp();
     if (w.k > 1) tc::cluster_sync_all();
@@ -810,10 +868,10 @@ __global__ void __launch_bounds__(kClThreads, 2) gn_cluster_backward_kernel(cons
         return t;
     };
     const float count = (float)sh.HW * (float)sh.cg;
-    for (int g = tid; g < sh.groups; g += w.threads) m.res[g] = make_float2(__fdiv_rn(over_cluster(m.grp + g), count), __fdiv_rn(over_cluster(m.grp + sh.groups + g), count));
-    for (int c = rank + w.k * tid; c < w.C; c += w.k * w.threads) {
-        partial[n * 2 * w.C + c] = over_cluster(m.chan + c);
-        partial[n * 2 * w.C + w.C + c] = over_cluster(m.chan + w.C + c);
+    for (int g = tid; g < w.groups; g += w.threads) m.res[g] = make_float2(__fdiv_rn(over_cluster(m.grp + g), count), __fdiv_rn(over_cluster(m.grp + w.groups + g), count));
+    for (int c = b.rank + w.k * tid; c < w.Cs; c += w.k * w.threads) {
+        partial[n * 2 * w.C + b.c0 + c] = over_cluster(m.chan + c);
+        partial[n * 2 * w.C + w.C + b.c0 + c] = over_cluster(m.chan + w.Cs + c);
     }
     if (w.k > 1) { __syncwarp(); tc::cluster_arrive(); }
     __syncthreads();
@@ -823,11 +881,11 @@ __global__ void __launch_bounds__(kClThreads, 2) gn_cluster_backward_kernel(cons
         for (int i = 0; i < V; ++i) {
             const int g = sh.group(V * v + i);
             const float2 c = m.res[g];
-            const float r = A.rstd[n * sh.groups + g];
+            const float r = A.rstd[gb + g];
             B[i] = -r * r * c.y;
             D[i] = -r * c.x;
         }
-        T* op = dx + n * gdx.sn + V * v;
+        T* op = dx + n * gdx.sn + V * cv;
         Cursor c(gdx, p0 + row);
         #pragma unroll 1
         for (int it = 0; it < cnt; ++it) {

@@ -177,38 +177,49 @@ size_t forward_ws(const Walk& w, const Dims& d) { return (size_t)(d.n * w.chunks
 size_t backward_ws(const Walk& w, const Dims& d, int groups) { return (size_t)(d.n * groups) * sizeof(float2) + (size_t)(d.n * w.chunks) * 2 * d.C * sizeof(float); }
 
 constexpr size_t kSmSmem = 228 * 1024, kCtaSmem = 227 * 1024;
-// How clusters walk a tensor, `slot` bytes kept per vector of V channels and `moved` bytes to and from memory; k = 0: not at all (rows wider than a
-// block, or too few samples to fill the device with their clusters).  By a model in cycles: an SM moves 22 bytes per cycle, a round of CTAs
-// costs 5000 more for its first loads and the sums' way around, and vectors that do not stay on chip are read again at 40 bytes.
+// How clusters walk a tensor, `slot` bytes kept per vector of V channels, `moved` bytes per vector to and from memory and K sums per thread and
+// vector element; k = 0: not at all (rows wider than a block, or too few samples to fill the device with their clusters).  By a model in
+// cycles: an SM moves 22 bytes per cycle when it has 18 warps of three CTAs (in different phases), a round of CTAs costs 4500 or 6000
+// more for its first loads and the sums' way around, and vectors that do not stay on chip are read again at 40 bytes.
 template <int V>
 ClusterWalk cluster_walk(const Dims& d, int groups, int slot, int moved, int K) {
     ClusterWalk best{};
     ClusterWalk w{};
-    w.C = d.C; w.HW = d.h * d.w; w.vecs = d.C / V;
-    w.cols = (int)ceil_div(w.vecs, V == 8 ? 4 : 1) * (V == 8 ? 4 : 1);
-    if (w.cols > kClThreads || groups > 1024 || d.n > kMaxGrid / 8) return best;
+    w.C = d.C; w.HW = d.h * d.w;
+    const int cg = d.C / groups;
     double cost = 1e30;
-    for (w.k = 1; w.k <= 8; w.k *= 2) {
-        if (w.k > w.HW) break;
-        w.ppc = (int)ceil_div(w.HW, w.k);
-        for (w.threads = 128; w.threads <= kClThreads; w.threads += 32) {
-            if (w.threads < w.cols) continue;
-            w.rows = w.threads / w.cols;
-            w.its = (int)ceil_div(w.ppc, w.rows);
-            const size_t scratch = cluster_scratch<V>(w, groups, K) + 64, per_it = (size_t)w.threads * slot;
-            if (scratch + 1024 > kCtaSmem) continue;
-            for (int occ = 1; occ <= 4 && occ * w.threads <= 2 * kClThreads; ++occ) {
-                const size_t room = std::min(kCtaSmem, kSmSmem / occ - 1024);
-                if (room < scratch) break;
-                w.keep = (int)std::min<size_t>(w.its, (room - scratch) / per_it);
-                const double work = (double)w.its * w.threads * moved / 22 + (double)(w.its - w.keep) * w.threads * moved / 40;
-                const double per_sm = (double)ceil_div(d.n * w.k, kSms), c = per_sm * work + 5000 * std::ceil(per_sm / occ);
-                if (c < cost) { cost = c; best = w; }
+    for (w.slices = 1; w.slices <= 64; w.slices *= 2) {
+        w.Cs = d.C / w.slices; w.groups = groups / w.slices;
+        if (w.slices > 1 && (groups % w.slices || w.Cs % 32 || w.Cs * 2 < 64)) break;
+        w.vecs = w.Cs / V;
+        w.cols = (int)ceil_div(w.vecs, V == 8 ? 4 : 1) * (V == 8 ? 4 : 1);
+        if (w.cols > kClThreads || w.groups > 1024 || d.n > kMaxGrid / 512) continue;
+        for (w.k = 1; w.k <= 8; w.k *= 2) {
+            if (w.k > w.HW) break;
+            w.ppc = (int)ceil_div(w.HW, w.k);
+            for (w.threads = 128; w.threads <= kClThreads; w.threads += 32) {
+                if (w.threads < w.cols) continue;
+                w.rows = w.threads / w.cols;
+                w.its = (int)ceil_div(w.ppc, w.rows);
+                const size_t scratch = cluster_scratch<V>(w, K) + 64, per_it = (size_t)w.threads * slot;
+                if (scratch + 1024 > kCtaSmem) continue;
+                for (int occ = 1; occ <= 6 && occ * w.threads <= 2 * kClThreads; ++occ) {
+                    const size_t room = std::min(kCtaSmem, kSmSmem / occ - 1024);
+                    if (room < scratch) break;
+                    w.keep = (int)std::min<size_t>(w.its, (room - scratch) / per_it);
+                    const double busy = std::min(1.0, occ * w.threads / 576.0) * (occ == 1 ? 0.55 : occ == 2 ? 0.8 : 1.0);
+                    const double work = ((double)w.its * w.threads * moved / 22 + (double)(w.its - w.keep) * w.threads * moved / 40) / busy;
+                    const double per_sm = (double)ceil_div(d.n * w.slices * w.k, kSms), c = per_sm * work + (w.k > 1 ? 6000 : 4500) * std::ceil(per_sm / occ);
+                    if (c < cost) { cost = c; best = w; }
+                }
             }
         }
     }
-    // a sample's cluster is at most eight SMs: a few large samples go faster through the kernels that spread over all of them
-    if (best.k && (double)d.n * best.k < kSms / 2 && (double)best.its * best.threads * moved > 2.0e5) best.k = 0;
+    if (!best.k) return best;
+    // a sample's blocks are few SMs: a few large samples go faster through the kernels that spread over all of them
+    if ((double)d.n * best.slices * best.k < kSms / 2 && (double)best.its * best.threads * moved > 2.0e5) best.k = 0;
+    best.lanes = 1;
+    while (best.lanes < 32 && best.lanes * 2 * best.groups <= best.threads && best.lanes < cg * best.rows) best.lanes *= 2;
     return best;
 }
 template <typename K>
@@ -226,9 +237,9 @@ void forward(Launcher& go, const alexnet_group_norm_forward_t* a, const Dims& d)
             if (a->keep_y.codes) ky = {(uint8_t*)a->keep_y.codes, a->keep_y.scales, src_of(a->keep_y.format)};
         }
         if (go.e == cudaSuccess) go.e = allow_smem(gn_cluster_forward_kernel<T, V, ACT>);
-        go.smem = (size_t)cw.keep * cw.threads * sizeof(T) * V + cluster_scratch<V>(cw, s.groups, 3);
+        go.smem = (size_t)cw.keep * cw.threads * sizeof(T) * V + cluster_scratch<V>(cw, 3);
         go.cluster = cw.k;
-        go(gn_cluster_forward_kernel<T, V, ACT>, d.n * cw.k, cw.threads, (const T*)a->x.data, geo_of(a->x, d), cw, s, a->weight, a->bias, (T*)a->y.data, geo_of(a->y, d), a->mean, a->rstd, kx, ky);
+        go(gn_cluster_forward_kernel<T, V, ACT>, d.n * cw.slices * cw.k, cw.threads, (const T*)a->x.data, geo_of(a->x, d), cw, s, a->weight, a->bias, (T*)a->y.data, geo_of(a->y, d), a->mean, a->rstd, kx, ky);
         if (V != 8) {
             if (a->keep_x.codes) encode<T>(go, d, a->x, a->keep_x, a->shape.dtype);
             if (a->keep_y.codes) encode<T>(go, d, a->y, a->keep_y, a->shape.dtype);
@@ -268,9 +279,9 @@ void backward(Launcher& go, const alexnet_group_norm_backward_t* a, const Dims& 
         auto* kernel = gn_cluster_backward_kernel<T, V, SRC, ACT>;
         if (go.e == cudaSuccess) go.e = allow_smem(kernel);
         const size_t slab = (size_t)cw.keep * cw.threads;
-        go.smem = slab * (kSlot - (SRC == kSrcSame ? 0 : 1)) + (SRC == kSrcSame ? 0 : (slab + 15) / 16 * 16) + cluster_scratch<V>(cw, s.groups, 2);
+        go.smem = slab * (kSlot - (SRC == kSrcSame ? 0 : 1)) + (SRC == kSrcSame ? 0 : (slab + 15) / 16 * 16) + cluster_scratch<V>(cw, 2);
         go.cluster = cw.k;
-        go(kernel, d.n * cw.k, cw.threads, dy, gdy, src, gx, cw, s, A, (T*)a->dx.data, gdx, partial);
+        go(kernel, d.n * cw.slices * cw.k, cw.threads, dy, gdy, src, gx, cw, s, A, (T*)a->dx.data, gdx, partial);
         if (a->dweight || a->dbias) go(gn_parameter_gradient_kernel, ceil_div(d.C, 32), 1024, (const float*)partial, d.C, d.n, a->dweight, a->dbias);
         return;
     }
