@@ -545,7 +545,7 @@ struct ClusterWalk {
     int k, ppc, its, keep;                    // CTAs of the cluster; positions of a CTA, at most; iterations of a thread, and those whose vectors stay
     int lanes;                                // a power of two: lanes that join a group's sums
 };
-constexpr int kClThreads = 384;               // at most; two CTAs per SM with 80 registers
+constexpr int kClThreads = 256;               // at most; two CTAs per SM with 128 registers
 
 template <int BYTES> __device__ __forceinline__ void copy_async(uint32_t dst, const void* src) {
     if constexpr (BYTES == 32) { copy_async<16>(dst, src); copy_async<16>(dst + 16, (const uint8_t*)src + 16); }
@@ -575,7 +575,7 @@ __device__ __forceinline__ float ld_cluster(const float* p, uint32_t rank) {
 // shared memory behind the slots: K sums per thread and vector element, K per channel, K per group of this CTA, and the groups' results
 template <int V> struct ClusterSmem {
     Table<V> part;
-    float *chan, *grp;       // [K][C], [K][groups]
+    float *chan, *grp;       // [K][Cs], [K][groups]; K = 2 (backward): the samples' sums of this CTA's channels behind them
     float2* res;
     __device__ __forceinline__ ClusterSmem(uint8_t* p, const ClusterWalk& w, int K) {
         res = (float2*)p;
@@ -584,15 +584,17 @@ template <int V> struct ClusterSmem {
         grp = chan + K * w.Cs;
     }
 };
-template <int V> inline size_t cluster_scratch(const ClusterWalk& w, int K) { return ((size_t)K * V * (w.threads + 4) + K * w.Cs + K * w.groups) * sizeof(float) + w.groups * sizeof(float2); }
-// a block's place: sample, first channel, first group (within the sample), rank in its cluster
+template <int V> inline size_t cluster_scratch(const ClusterWalk& w, int K) {
+    return ((size_t)K * V * (w.threads + 4) + K * w.Cs + K * w.groups + (K == 2 ? 2 * (w.Cs + w.k - 1) / w.k + 2 : 0)) * sizeof(float) + w.groups * sizeof(float2);
+}
+// A cluster's work: a slice of the channels (from channel c0, group g0 on) of the samples n0, n0 + step, ...
 struct ClusterSpot {
-    long long n;
+    long long n0, step;
     int c0, g0, rank;
     __device__ __forceinline__ ClusterSpot(const ClusterWalk& w) {
-        const long long b = blockIdx.x / w.k;
-        n = b / w.slices;
-        const int slice = (int)(b - n * w.slices);
+        const uint32_t id = blockIdx.x / (uint32_t)w.k, slice = id % (uint32_t)w.slices;
+        n0 = id / (uint32_t)w.slices;
+        step = gridDim.x / (uint32_t)(w.k * w.slices);
         c0 = slice * w.Cs;
         g0 = slice * w.groups;
         rank = w.k > 1 ? (int)tc::cluster_ctarank() : 0;
@@ -609,10 +611,15 @@ template <int V> __device__ __forceinline__ void load_parameters(const float* p,
     }
 }
 
+// Clusters are persistent: while a sample's results are formed, the vectors of the cluster's next sample are copied into the slots that have been
+// read, so memory is read and written at the same time and the sums' way around the cluster is not waited for by both.
+//
+// The sums' shift is here one value per group and CTA, the mean over the first position of every thread: sums of differences and of squares can then
+// simply be added up, and the square of a wrong shift (an outlier among the first positions) is divided by the square of their number.
 template <typename T, int V, int ACT>
-__global__ void __launch_bounds__(kClThreads, 2) gn_cluster_forward_kernel(const T* __restrict__ x, const Geo gx, const ClusterWalk w, const NormShape sh, const float* __restrict__ weight,
-                                                                           const float* __restrict__ bias, T* __restrict__ y, const Geo gy, float* __restrict__ mean,
-                                                                           float* __restrict__ rstd, const Keep kx, const Keep ky) {
+__global__ void __launch_bounds__(kClThreads, 2) gn_cluster_forward_kernel(const T* __restrict__ x, const Geo gx, const ClusterWalk w, const NormShape sh, long long samples,
+                                                                           const float* __restrict__ weight, const float* __restrict__ bias, T* __restrict__ y, const Geo gy,
+                                                                           float* __restrict__ mean, float* __restrict__ rstd, const Keep kx, const Keep ky) {
     kn::pdl_sync();
     extern __shared__ __align__(16) uint8_t smem[];
     using R = Raw<T, V>;
@@ -620,139 +627,196 @@ __global__ void __launch_bounds__(kClThreads, 2) gn_cluster_forward_kernel(const
     R* slots = (R*)smem + tid;
     const ClusterSmem<V> m(smem + (size_t)w.keep * w.threads * sizeof(R), w, 3);
     const ClusterSpot b(w);
-    const long long n = b.n;
-    const int row = tid / w.cols, v = tid - row * w.cols;
+    const int row = tid / w.cols, v = tid - row * w.cols, cv = b.c0 / V + v;      // cv: vector within the tensor's row
     const bool on = row < w.rows, has = on && v < w.vecs;
     const int p0 = b.rank * w.ppc, np = max(0, min(w.HW - p0, w.ppc));
     const int cnt = on && row < np ? (np - row + w.rows - 1) / w.rows : 0;      // iterations of this thread
-    const T* xp = x + n * gx.sn + b.c0 + V * v;
-    Chan<V> k = {};                             // (weight and bias; the statistics join them)
-    if (has) {
-        load_parameters<V>(weight, b.c0 + V * v, 1.f, k.a);
-        load_parameters<V>(bias, b.c0 + V * v, 0.f, k.b);
-    }
-
-    // sums
-    float nK[V], S[V], Q[V];
-    #pragma unroll
-    for (int i = 0; i < V; ++i) nK[i] = S[i] = Q[i] = 0.f;
     const int kept = has ? min(cnt, w.keep) : 0, batch = (w.keep + kClBatches - 1) / kClBatches;
-    Cursor cur(gx, p0 + row);
-    #pragma unroll 1
-    for (int bt = 0; bt < kClBatches; ++bt) {
-        const int e = min(kept, (bt + 1) * batch);
-        #pragma unroll 4
-        for (int it = bt * batch; it < e; ++it) {
-            fill_slot(slots + it * w.threads, xp + cur.off);
-            cur.next(gx, w.rows);
-        }
-        copies_commit();
-    }
-    auto shift = [&](const R& r) {             // the first value
-        unpack<T, V>(r, nK);
-        #pragma unroll
-        for (int i = 0; i < V; ++i) nK[i] = -nK[i];
-    };
-    auto add = [&](const R& r) {
-        float f[V];
-        unpack<T, V>(r, f);
-        v_add<V>(f, nK, f);
-        v_add<V>(S, f, S);
-        v_fma<V>(f, f, Q, Q);
-    };
-    #pragma unroll 1
-    for (int bt = 0; bt < kClBatches; ++bt) {
-        copies_wait(kClBatches - 1 - bt);
-        const int e = min(kept, (bt + 1) * batch);
-        if (bt == 0 && kept > 0) shift(slots[0]);
-        #pragma unroll 2
-        for (int it = bt * batch; it < e; ++it) add(slots[it * w.threads]);
-    }
-    if (has) {
-        if (kept == 0 && cnt > 0) shift(*(const R*)(xp + cur.off));
-        constexpr int U = 4;
-        for (int it = kept; it < cnt; it += U) {
-            R r[U];
-            #pragma unroll
-            for (int u = 0; u < U; ++u) {
-                if (it + u < cnt) r[u] = *(const R*)(xp + cur.off);
-                cur.next(gx, w.rows);
+    const int rows = min(w.rows, np), at_once = 32 / w.lanes, lane_g = lane / w.lanes, lane_i = lane % w.lanes;
+    const float n_cta = (float)np * (float)sh.cg;
+    if (b.n0 < samples) {
+        Cursor c(gx, p0 + row);
+        const T* xp = x + b.n0 * gx.sn + V * cv;
+        #pragma unroll 1
+        for (int bt = 0; bt < kClBatches; ++bt) {
+            const int e = min(kept, (bt + 1) * batch);
+            #pragma unroll 4
+            for (int it = bt * batch; it < e; ++it) {
+                fill_slot(slots + it * w.threads, xp + c.off);
+                c.next(gx, w.rows);
             }
-            #pragma unroll
-            for (int u = 0; u < U; ++u)
-                if (it + u < cnt) add(r[u]);
+            copies_commit();
         }
     }
-    #pragma unroll
-    for (int i = 0; i < V; ++i) {
-        const Part t = moments(cnt, nK[i], S[i], Q[i]);
-        m.part.at(0, i, tid) = t.hi; m.part.at(1, i, tid) = t.lo; m.part.at(2, i, tid) = t.m2;
-    }
-    __syncthreads();
-    {
-        // of this CTA: the parts of the group's channels and of the rows of threads that have positions, the first `more` rows one more than the others
-        const int rows = min(w.rows, np), more = np % w.rows;
-        const float n_lo = (float)(np / w.rows), inv = np ? __fdividef(1.f, (float)np * (float)sh.cg) : 0.f;
-        const int at_once = 32 / w.lanes;
+    bool first = true;
+    #pragma unroll 1
+    for (long long n = b.n0; n < samples; n += b.step) {
+        const T* xp = x + n * gx.sn + V * cv;
+        // the shift
+        copies_wait(kClBatches - 1);
+        if (has && cnt > 0) {
+            float f[V];
+            unpack<T, V>(kept > 0 ? slots[0] : *(const R*)(xp + gx.at(p0 + row)), f);
+            #pragma unroll
+            for (int i = 0; i < V; ++i) m.part.at(0, i, tid) = f[i];
+        }
+        __syncthreads();
         for (int g0 = warp * at_once; g0 < w.groups; g0 += warps * at_once) {
-            const int g = g0 + lane / w.lanes, c0 = g * sh.cg;
-            const Part t = join_lanes(g < w.groups ? rows * sh.cg : 0, w.lanes, inv, [&](int i) {
-                const int r = sh.group(i), c = c0 + i - r * sh.cg, at = r * w.cols + c / V;
-                return Part{m.part.at(0, c % V, at), m.part.at(1, c % V, at), m.part.at(2, c % V, at)};
-            }, [&](int i) { return sh.group(i) < more ? n_lo + 1.f : n_lo; });
-            if (g < w.groups && lane % w.lanes == 0) { m.grp[g] = t.hi; m.grp[w.groups + g] = t.lo; m.grp[2 * w.groups + g] = t.m2; }
+            const int g = g0 + lane_g, total = g < w.groups ? rows * sh.cg : 0;
+            float t = 0.f;
+            #pragma unroll 2
+            for (int i = lane_i; i < total; i += w.lanes) {
+                const int r = sh.group(i), c = g * sh.cg + i - r * sh.cg;
+                t += m.part.at(0, c % V, r * w.cols + c / V);
+            }
+            t = lanes_sum(t, w.lanes);
+            if (lane_i == 0 && total) m.res[g].x = __fdividef(t, (float)total);
         }
-    }
-    __syncwarp();
-    if (w.k > 1) tc::cluster_sync_all();
-    else __syncthreads();
-    for (int g = tid; g < w.groups; g += w.threads) {        // the CTAs of the cluster
-        Part t = {m.grp[g], m.grp[w.groups + g], m.grp[2 * w.groups + g]};
-        if (w.k > 1) {
-            Part q[8];
-            #pragma unroll
-            for (int i = 0; i < 8; ++i)
-                q[i] = i < w.k ? Part{ld_cluster(m.grp + g, i), ld_cluster(m.grp + w.groups + g, i), ld_cluster(m.grp + 2 * w.groups + g, i)} : Part{0.f, 0.f, 0.f};
-            // (CTAs beyond the cluster, and those without positions, count for nothing)
-            t = join<8>(8, __fdividef(1.f, (float)w.HW * (float)sh.cg), [&](int i) { return q[i]; }, [&](int i) { return i < w.k ? (float)max(0, min(w.HW - i * w.ppc, w.ppc)) * (float)sh.cg : 0.f; });
+        __syncthreads();
+        // sums
+        float nK[V], S[V], Q[V];
+        #pragma unroll
+        for (int i = 0; i < V; ++i) {
+            nK[i] = np > 0 ? -m.res[sh.group(min(V * v + i, w.Cs - 1))].x : 0.f;
+            S[i] = Q[i] = 0.f;
         }
-        const float2 r = statistics(t, sh);
-        m.res[g] = r;
-        if (b.rank == 0) { mean[n * sh.groups + b.g0 + g] = r.x; rstd[n * sh.groups + b.g0 + g] = r.y; }
-    }
-    if (w.k > 1) { __syncwarp(); tc::cluster_arrive(); }        // this CTA has read the others' sums
-    __syncthreads();
+        auto add = [&](const R& r) {
+            float f[V];
+            unpack<T, V>(r, f);
+            v_add<V>(f, nK, f);
+            v_add<V>(S, f, S);
+            v_fma<V>(f, f, Q, Q);
+        };
+        #pragma unroll 1
+        for (int bt = 0; bt < kClBatches; ++bt) {
+            copies_wait(kClBatches - 1 - bt);
+            const int e = min(kept, (bt + 1) * batch);
+            #pragma unroll 2
+            for (int it = bt * batch; it < e; ++it) add(slots[it * w.threads]);
+        }
+        if (has && kept < cnt) {
+            constexpr int U = 4;
+            Cursor c(gx, p0 + row + kept * w.rows);
+            for (int it = kept; it < cnt; it += U) {
+                R r[U];
+                #pragma unroll
+                for (int u = 0; u < U; ++u) {
+                    if (it + u < cnt) r[u] = *(const R*)(xp + c.off);
+                    c.next(gx, w.rows);
+                }
+                #pragma unroll
+                for (int u = 0; u < U; ++u)
+                    if (it + u < cnt) add(r[u]);
+            }
+        }
+        #pragma unroll
+        for (int i = 0; i < V; ++i) { m.part.at(1, i, tid) = S[i]; m.part.at(2, i, tid) = Q[i]; }
+        __syncthreads();
+        if (w.k > 1 && !first) tc::cluster_wait();               // the others have read this CTA's sums of the sample before
+        for (int g0 = warp * at_once; g0 < w.groups; g0 += warps * at_once) {
+            const int g = g0 + lane_g, total = g < w.groups ? rows * sh.cg : 0;
+            float s = 0.f, q = 0.f;
+            #pragma unroll 2
+            for (int i = lane_i; i < total; i += w.lanes) {
+                const int r = sh.group(i), c = g * sh.cg + i - r * sh.cg, at = r * w.cols + c / V;
+                s += m.part.at(1, c % V, at);
+                q += m.part.at(2, c % V, at);
+            }
+            s = lanes_sum(s, w.lanes);
+            q = lanes_sum(q, w.lanes);
+            if (lane_i == 0 && g < w.groups) {
+                const float K = total ? m.res[g].x : 0.f, d = total ? __fdividef(s, n_cta) : 0.f, hi = K + d;
+                m.grp[g] = hi;
+                m.grp[w.groups + g] = (K - hi) + d;
+                m.grp[2 * w.groups + g] = fmaf(-s, d, q);
+            }
+        }
+        __syncwarp();
+        if (w.k > 1) tc::cluster_sync_all();
+        else __syncthreads();
+        for (int i0 = warp * 32; i0 < w.groups * w.k; i0 += warps * 32) {      // the CTAs of the cluster: a lane each
+            const int g = (i0 + lane) / w.k;
+            Part t = {0.f, 0.f, 0.f};
+            if (w.k > 1) {
+                auto get = [&](int i) { return Part{ld_cluster(m.grp + g, i), ld_cluster(m.grp + w.groups + g, i), ld_cluster(m.grp + 2 * w.groups + g, i)}; };
+                t = join_lanes(g < w.groups ? w.k : 0, w.k, __fdividef(1.f, (float)w.HW * (float)sh.cg), get, [&](int i) { return (float)max(0, min(w.HW - i * w.ppc, w.ppc)) * (float)sh.cg; });
+            } else if (g < w.groups) t = {m.grp[g], m.grp[w.groups + g], m.grp[2 * w.groups + g]};
+            if (g < w.groups && (i0 + lane) % w.k == 0) {
+                const float2 r = statistics(t, sh);
+                m.res[g] = r;
+                if (b.rank == 0) { mean[n * sh.groups + b.g0 + g] = r.x; rstd[n * sh.groups + b.g0 + g] = r.y; }
+            }
+        }
+        __syncwarp();
+        if (w.k > 1) tc::cluster_arrive();                       // this CTA has read the others' sums
+        first = false;
+        __syncthreads();
 
-    // result
-    if (cnt > 0) {
+        // results, and the next sample's copies
+        Chan<V> k = {};
+        if (has) {
+            load_parameters<V>(weight, V * cv, 1.f, k.a);
+            load_parameters<V>(bias, V * cv, 0.f, k.b);
+        }
         #pragma unroll
         for (int i = 0; i < V; ++i) {
             const float2 r = m.res[sh.group(min(V * v + i, w.Cs - 1))];
             k.nm[i] = -r.x;
             k.a[i] *= r.y;
         }
-        T* yp = y + n * gy.sn + b.c0 + V * v;
-        const int cv = b.c0 / V + v;                // vector within the tensor's row
+        const bool more = n + b.step < samples;
+        const T* xn = xp + b.step * gx.sn;
+        T* yp = y + n * gy.sn + V * cv;
+        Cursor cy(gy, p0 + row), cx(gx, p0 + row);               // cx: the next sample's copies, then this one's vectors that are read again
+        CodesCursor ckx(kx.codes, kx.scales, n * w.HW + p0 + row, cv, w.C), cky(ky.codes, ky.scales, n * w.HW + p0 + row, cv, w.C);
+        auto emit = [&](const R& r) {
+            float f[V], z[V];
+            unpack<T, V>(r, f);
+            if constexpr (V == 8)
+                if (kx.codes) { keep_codes<T>(kx, r, f, has, ckx); ckx.next(w.rows, w.C); }
+            v_add<V>(f, k.nm, f);
+            v_fma<V>(f, k.a, k.b, z);
+            activate<T, V, ACT>(sh.act, z);
+            R out = pack<T, V>(z);
+            if (has) *(R*)(yp + cy.off) = out;
+            cy.next(gy, w.rows);
+            if constexpr (V == 8)
+                if (ky.codes) {                     // of y as it is stored
+                    if (!has) out = R{};
+                    unpack<T, 8>(out, f);
+                    keep_codes<T>(ky, out, f, has, cky);
+                    cky.next(w.rows, w.C);
+                }
+        };
         const int split = min(cnt, w.keep);
-        apply_positions<T, V, ACT>(k, sh, p0 + row, w.rows, 0, split, n * w.HW, cv, has, yp, gy, kx, ky, [&](int it) { return has ? slots[it * w.threads] : R{}; });
-        if (split < cnt) {
-            Cursor c(gx, p0 + row + split * w.rows);
-            apply_positions<T, V, ACT>(k, sh, p0 + row, w.rows, split, cnt, n * w.HW, cv, has, yp, gy, kx, ky, [&](int) {
-                R r = {};
-                if (has) r = *(const R*)(xp + c.off);
-                c.next(gx, w.rows);
-                return r;
-            });
+        #pragma unroll 1
+        for (int bt = 0; bt < kClBatches; ++bt) {
+            const int e = min(split, (bt + 1) * batch);
+            #pragma unroll 2
+            for (int it = bt * batch; it < e; ++it) {
+                const R r = has ? slots[it * w.threads] : R{};
+                emit(r);
+                if (more && has) fill_slot(slots + it * w.threads, xn + cx.off);
+                cx.next(gx, w.rows);
+            }
+            copies_commit();
+        }
+        #pragma unroll 2
+        for (int it = split; it < cnt; ++it) {
+            R r = {};
+            if (has) r = *(const R*)(xp + cx.off);
+            cx.next(gx, w.rows);
+            emit(r);
         }
     }
-    if (w.k > 1) { __syncwarp(); tc::cluster_wait(); }          // no CTA leaves while another may read its sums
+    if (w.k > 1 && !first) { __syncwarp(); tc::cluster_wait(); }          // no CTA leaves while another may read its sums
 }
 
 // The same for the backward pass: sums of dz and dz d per channel, around the cluster for c1 and c2, then dx.  The samples' sums for dweight and
-// dbias go to partial [n][2][C] (a CTA joins the channels rank, rank + k, ... of its cluster) and are added over the samples by a second launch.
+// dbias are added up in shared memory (a CTA takes the channels rank, rank + k, ... of its cluster) and go to partial [cluster][2][C] at the end.
 template <typename T, int V, int SRC, int ACT>
 __global__ void __launch_bounds__(kClThreads, 2) gn_cluster_backward_kernel(const T* __restrict__ dy, const Geo gdy, const Source src, const Geo gx, const ClusterWalk w, const NormShape sh,
-                                                                            const BackwardArgs A, T* __restrict__ dx, const Geo gdx, float* __restrict__ partial) {
+                                                                            long long samples, const BackwardArgs A, T* __restrict__ dx, const Geo gdx, float* __restrict__ partial) {
     kn::pdl_sync();
     extern __shared__ __align__(16) uint8_t smem[];
     using R = Raw<T, V>;
@@ -763,140 +827,201 @@ __global__ void __launch_bounds__(kClThreads, 2) gn_cluster_backward_kernel(cons
     X* xslots = (X*)(smem + slab * sizeof(R)) + tid;
     uint8_t* eslots = smem + slab * (sizeof(R) + sizeof(X)) + tid;
     const ClusterSmem<V> m(smem + slab * (sizeof(R) + sizeof(X)) + (SRC == kSrcSame ? 0 : (slab + 15) / 16 * 16), w, 2);
+    float* acc = m.grp + 2 * w.groups;                          // [2][ceil(Cs / k)]
     const ClusterSpot b(w);
-    const long long n = b.n, gb = n * sh.groups + b.g0;       // gb: this block's first group
-    const int row = tid / w.cols, v = tid - row * w.cols;
+    const int row = tid / w.cols, v = tid - row * w.cols, cv = b.c0 / V + v;
     const bool has = row < w.rows && v < w.vecs;
     const int p0 = b.rank * w.ppc, np = max(0, min(w.HW - p0, w.ppc));
     const int cnt = has && row < np ? (np - row + w.rows - 1) / w.rows : 0;
-    const T* dp = dy + n * gdy.sn + b.c0 + V * v;
-    const int cv = b.c0 / V + v, blocks = (w.C + 31) / 32, kept = min(cnt, w.keep), batch = (w.keep + kClBatches - 1) / kClBatches;
-    const T* xp = SRC == kSrcSame ? (const T*)src.x + n * gx.sn + V * cv : nullptr;
-    const uint8_t* cp = SRC == kSrcSame ? nullptr : src.codes + (n * w.HW + p0 + row) * w.C + V * cv;
-    Cursor cdy(gdy, p0 + row), cx(gx, p0 + row);
-    #pragma unroll 1
-    for (int bt = 0; bt < kClBatches; ++bt) {
-        const int e = min(kept, (bt + 1) * batch);
-        #pragma unroll 2
-        for (int it = bt * batch; it < e; ++it) {
-            fill_slot(slots + it * w.threads, dp + cdy.off);
-            cdy.next(gdy, w.rows);
-            if constexpr (SRC == kSrcSame) {
-                fill_slot(xslots + it * w.threads, xp + cx.off);
-                cx.next(gx, w.rows);
-            } else {
-                fill_slot(xslots + it * w.threads, cp);
-                cp += (long long)w.rows * w.C;
+    const int blocks = (w.C + 31) / 32, kept = min(cnt, w.keep), batch = (w.keep + kClBatches - 1) / kClBatches, own = (w.Cs + w.k - 1) / w.k;
+    const T* xbase = SRC == kSrcSame ? (const T*)src.x + V * cv : nullptr;
+    auto codes_at = [&](long long n, int it) { return src.codes + (n * w.HW + p0 + row + (long long)it * w.rows) * w.C + V * cv; };
+    auto scale_at = [&](long long n, int it) { return src.scales + (n * w.HW + p0 + row + (long long)it * w.rows) * blocks + V * cv / 32; };
+    if (b.n0 < samples) {
+        Cursor cdy(gdy, p0 + row), cx(gx, p0 + row);
+        const T* dp = dy + b.n0 * gdy.sn + V * cv;
+        #pragma unroll 1
+        for (int bt = 0; bt < kClBatches; ++bt) {
+            const int e = min(kept, (bt + 1) * batch);
+            #pragma unroll 2
+            for (int it = bt * batch; it < e; ++it) {
+                fill_slot(slots + it * w.threads, dp + cdy.off);
+                cdy.next(gdy, w.rows);
+                if constexpr (SRC == kSrcSame) {
+                    fill_slot(xslots + it * w.threads, xbase + b.n0 * gx.sn + cx.off);
+                    cx.next(gx, w.rows);
+                } else fill_slot(xslots + it * w.threads, codes_at(b.n0, it));
             }
+            copies_commit();
         }
-        copies_commit();
+        if constexpr (SRC != kSrcSame) {
+            #pragma unroll 8
+            for (int it = 0; it < kept; ++it) eslots[it * w.threads] = *scale_at(b.n0, it);
+        }
     }
-    if constexpr (SRC != kSrcSame) {
-        const uint8_t* ep = src.scales + (n * w.HW + p0 + row) * blocks + V * cv / 32;
-        #pragma unroll 8
-        for (int it = 0; it < kept; ++it) eslots[it * w.threads] = ep[(long long)it * w.rows * blocks];
-    }
-    Chan<V> k;
-    if (has) load_chan<V>(k, sh, A.mean, A.rstd, A.weight, A.bias, n, V * cv);
-    float S1[V], S2[V];
-    #pragma unroll
-    for (int i = 0; i < V; ++i) S1[i] = S2[i] = 0.f;
-    // d and dz of iteration it
-    auto values = [&](int it, float* f, float* q) {
-        Fetch<T, V, SRC> fx;
-        R r;
-        if (it < kept) {
+    for (int i = tid; i < 2 * own; i += w.threads) acc[i] = 0.f;
+    bool first = true;
+    #pragma unroll 1
+    for (long long n = b.n0; n < samples; n += b.step) {
+        const long long gb = n * sh.groups + b.g0;              // this block's first group
+        const T* dp = dy + n * gdy.sn + V * cv;
+        Chan<V> k;
+        if (has) load_chan<V>(k, sh, A.mean, A.rstd, A.weight, A.bias, n, V * cv);
+        // d and dz from what has been read
+        auto values = [&](const R& r, const Fetch<T, V, SRC>& fx, float* f, float* q) {
+            unpack<T, V>(r, q);
+            activation_gradient<T, V, SRC, ACT>(sh, k, A, n, V * cv, fx, f, q);
+        };
+        auto from_slot = [&](int it, R& r, Fetch<T, V, SRC>& fx) {
             r = slots[it * w.threads];
             fx.r = xslots[it * w.threads];
             if constexpr (SRC != kSrcSame) fx.e = eslots[it * w.threads];
-        } else {
+        };
+        auto from_memory = [&](int it, R& r, Fetch<T, V, SRC>& fx) {
             const int p = p0 + row + it * w.rows;
             r = *(const R*)(dp + gdy.at(p));
-            fx.load(src, gx, Walk{w.C, w.HW}, n, p, cv);
-        }
-        unpack<T, V>(r, q);
-        activation_gradient<T, V, SRC, ACT>(sh, k, A, n, V * cv, fx, f, q);
-    };
-    auto add = [&](int it) {
-        float f[V], q[V];
-        values(it, f, q);
-        v_add<V>(S1, q, S1);
-        v_fma<V>(f, q, S2, S2);
-    };
-    #pragma unroll 1
-    for (int bt = 0; bt < kClBatches; ++bt) {
-        copies_wait(kClBatches - 1 - bt);
-        const int e = min(kept, (bt + 1) * batch);
-        #pragma unroll 1
-        for (int it = bt * batch; it < e; ++it) add(it);
-    }
-    #pragma unroll 2
-    for (int it = kept; it < cnt; ++it) add(it);
-    #pragma unroll
-    for (int i = 0; i < V; ++i) { m.part.at(0, i, tid) = S1[i]; m.part.at(1, i, tid) = S2[i]; }
-    __syncthreads();
-    for (int c = tid; c < w.Cs; c += w.threads) {
-        float2 t = make_float2(0.f, 0.f);
-        #pragma unroll 4
-        for (int r = 0; r < w.rows; ++r) { t.x += m.part.at(0, c % V, r * w.cols + c / V); t.y += m.part.at(1, c % V, r * w.cols + c / V); }
-        m.chan[c] = t.x;
-        m.chan[w.Cs + c] = t.y * A.rstd[gb + sh.group(c)];            // of xhat
-    }
-    __syncthreads();
-    for (int g0 = warp * (32 / w.lanes); g0 < w.groups; g0 += warps * (32 / w.lanes)) {
-        const int g = g0 + lane / w.lanes;
-        float2 t = make_float2(0.f, 0.f);
-        if (g < w.groups)
-            for (int c = g * sh.cg + lane % w.lanes; c < (g + 1) * sh.cg; c += w.lanes) {
-                const float wt = A.weight ? A.weight[b.c0 + c] : 1.f;
-                t.x = fmaf(wt, m.chan[c], t.x);
-                t.y = fmaf(wt, m.chan[w.Cs + c], t.y);
-            }
-        t.x = lanes_sum(t.x, w.lanes);
-        t.y = lanes_sum(t.y, w.lanes);
-        if (g < w.groups && lane % w.lanes == 0) { m.grp[g] = t.x; m.grp[w.groups + g] = t.y; }
-    }
-    __syncwarp();
-    if (w.k > 1) tc::cluster_sync_all();
-    else __syncthreads();
-    auto over_cluster = [&](const float* p) {
-        if (w.k == 1) return *p;
-        float t = 0.f;
+            if constexpr (SRC == kSrcSame) fx.r = *(const X*)(xbase + n * gx.sn + gx.at(p));
+            else { fx.r = *(const X*)codes_at(n, it); fx.e = *scale_at(n, it); }
+        };
+        float S1[V], S2[V];
         #pragma unroll
-        for (int i = 0; i < 8; ++i)
-            if (i < w.k) t += ld_cluster(p, i);
-        return t;
-    };
-    const float count = (float)sh.HW * (float)sh.cg;
-    for (int g = tid; g < w.groups; g += w.threads) m.res[g] = make_float2(__fdiv_rn(over_cluster(m.grp + g), count), __fdiv_rn(over_cluster(m.grp + w.groups + g), count));
-    for (int c = b.rank + w.k * tid; c < w.Cs; c += w.k * w.threads) {
-        partial[n * 2 * w.C + b.c0 + c] = over_cluster(m.chan + c);
-        partial[n * 2 * w.C + w.C + b.c0 + c] = over_cluster(m.chan + w.Cs + c);
-    }
-    if (w.k > 1) { __syncwarp(); tc::cluster_arrive(); }
-    __syncthreads();
-    if (has) {
-        float B[V], D[V];
-        #pragma unroll
-        for (int i = 0; i < V; ++i) {
-            const int g = sh.group(V * v + i);
-            const float2 c = m.res[g];
-            const float r = A.rstd[gb + g];
-            B[i] = -r * r * c.y;
-            D[i] = -r * c.x;
-        }
-        T* op = dx + n * gdx.sn + V * cv;
-        Cursor c(gdx, p0 + row);
-        #pragma unroll 1
-        for (int it = 0; it < cnt; ++it) {
+        for (int i = 0; i < V; ++i) S1[i] = S2[i] = 0.f;
+        auto add = [&](const R& r, const Fetch<T, V, SRC>& fx) {
             float f[V], q[V];
-            values(it, f, q);
-            v_fma<V>(f, B, D, f);
-            v_fma<V>(q, k.a, f, q);
-            *(R*)(op + c.off) = pack<T, V>(q);
-            c.next(gdx, w.rows);
+            values(r, fx, f, q);
+            v_add<V>(S1, q, S1);
+            v_fma<V>(f, q, S2, S2);
+        };
+        #pragma unroll 1
+        for (int bt = 0; bt < kClBatches; ++bt) {
+            copies_wait(kClBatches - 1 - bt);
+            const int e = min(kept, (bt + 1) * batch);
+            #pragma unroll 1
+            for (int it = bt * batch; it < e; ++it) {
+                R r; Fetch<T, V, SRC> fx;
+                from_slot(it, r, fx);
+                add(r, fx);
+            }
+        }
+        #pragma unroll 1
+        for (int it = kept; it < cnt; it += 2) {
+            R r[2]; Fetch<T, V, SRC> fx[2];
+            from_memory(it, r[0], fx[0]);
+            if (it + 1 < cnt) from_memory(it + 1, r[1], fx[1]);
+            add(r[0], fx[0]);
+            if (it + 1 < cnt) add(r[1], fx[1]);
+        }
+        #pragma unroll
+        for (int i = 0; i < V; ++i) { m.part.at(0, i, tid) = S1[i]; m.part.at(1, i, tid) = S2[i]; }
+        __syncthreads();
+        if (w.k > 1 && !first) tc::cluster_wait();               // the others have read this CTA's sums of the sample before
+        for (int c = tid; c < w.Cs; c += w.threads) {
+            float2 t = make_float2(0.f, 0.f);
+            #pragma unroll 8
+            for (int r = 0; r < w.rows; ++r) { t.x += m.part.at(0, c % V, r * w.cols + c / V); t.y += m.part.at(1, c % V, r * w.cols + c / V); }
+            m.chan[c] = t.x;
+            m.chan[w.Cs + c] = t.y * A.rstd[gb + sh.group(c)];            // of xhat
+        }
+        __syncthreads();
+        for (int g0 = warp * (32 / w.lanes); g0 < w.groups; g0 += warps * (32 / w.lanes)) {
+            const int g = g0 + lane / w.lanes;
+            float2 t = make_float2(0.f, 0.f);
+            if (g < w.groups)
+                for (int c = g * sh.cg + lane % w.lanes; c < (g + 1) * sh.cg; c += w.lanes) {
+                    const float wt = A.weight ? A.weight[b.c0 + c] : 1.f;
+                    t.x = fmaf(wt, m.chan[c], t.x);
+                    t.y = fmaf(wt, m.chan[w.Cs + c], t.y);
+                }
+            t.x = lanes_sum(t.x, w.lanes);
+            t.y = lanes_sum(t.y, w.lanes);
+            if (g < w.groups && lane % w.lanes == 0) { m.grp[g] = t.x; m.grp[w.groups + g] = t.y; }
+        }
+        __syncwarp();
+        if (w.k > 1) tc::cluster_sync_all();
+        else __syncthreads();
+        auto over_cluster = [&](const float* p) {
+            if (w.k == 1) return *p;
+            float t = 0.f;
+            #pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (i < w.k) t += ld_cluster(p, i);
+            return t;
+        };
+        const float per = __frcp_rn((float)sh.HW * (float)sh.cg);
+        for (int g = tid; g < w.groups; g += w.threads) m.res[g] = make_float2(over_cluster(m.grp + g) * per, over_cluster(m.grp + w.groups + g) * per);
+        for (int i = tid; b.rank + w.k * i < w.Cs; i += w.threads) {
+            acc[i] += over_cluster(m.chan + b.rank + w.k * i);
+            acc[own + i] += over_cluster(m.chan + w.Cs + b.rank + w.k * i);
+        }
+        __syncwarp();
+        if (w.k > 1) tc::cluster_arrive();
+        first = false;
+        __syncthreads();
+        if (has) {
+            float B[V], D[V];
+            #pragma unroll
+            for (int i = 0; i < V; ++i) {
+                const int g = sh.group(V * v + i);
+                const float2 c = m.res[g];
+                const float r = A.rstd[gb + g];
+                B[i] = -r * r * c.y;
+                D[i] = -r * c.x;
+            }
+            const bool more = n + b.step < samples;
+            const long long n1 = n + b.step;
+            const T* dn = dp + b.step * gdy.sn;
+            T* op = dx + n * gdx.sn + V * cv;
+            Cursor c(gdx, p0 + row), cdy(gdy, p0 + row), cx(gx, p0 + row);
+            uint8_t e_next = 0;                                 // the exponent of the next sample's copies, stored an iteration after it was asked for
+            auto emit = [&](const R& r, const Fetch<T, V, SRC>& fx) {
+                float f[V], q[V];
+                values(r, fx, f, q);
+                v_fma<V>(f, B, D, f);
+                v_fma<V>(q, k.a, f, q);
+                *(R*)(op + c.off) = pack<T, V>(q);
+                c.next(gdx, w.rows);
+            };
+            #pragma unroll 1
+            for (int bt = 0; bt < kClBatches; ++bt) {
+                const int e = min(kept, (bt + 1) * batch);
+                #pragma unroll 1
+                for (int it = bt * batch; it < e; ++it) {
+                    R r; Fetch<T, V, SRC> fx;
+                    from_slot(it, r, fx);
+                    if (SRC != kSrcSame && more) {
+                        if (it > 0) eslots[(it - 1) * w.threads] = e_next;
+                        e_next = *scale_at(n1, it);
+                    }
+                    emit(r, fx);
+                    if (more) {
+                        fill_slot(slots + it * w.threads, dn + cdy.off);
+                        cdy.next(gdy, w.rows);
+                        if constexpr (SRC == kSrcSame) {
+                            fill_slot(xslots + it * w.threads, xbase + n1 * gx.sn + cx.off);
+                            cx.next(gx, w.rows);
+                        } else fill_slot(xslots + it * w.threads, codes_at(n1, it));
+                    }
+                }
+                copies_commit();
+            }
+            if (SRC != kSrcSame && more && kept > 0) eslots[(kept - 1) * w.threads] = e_next;
+            #pragma unroll 1
+            for (int it = kept; it < cnt; ++it) {
+                R r; Fetch<T, V, SRC> fx;
+                from_memory(it, r, fx);
+                emit(r, fx);
+            }
         }
     }
-    if (w.k > 1) { __syncwarp(); tc::cluster_wait(); }
+    if (!first) {
+        __syncthreads();
+        float* out = partial + b.n0 * 2 * w.C + b.c0;
+        for (int i = tid; b.rank + w.k * i < w.Cs; i += w.threads) {
+            out[b.rank + w.k * i] = acc[i];
+            out[w.C + b.rank + w.k * i] = acc[own + i];
+        }
+        if (w.k > 1) { __syncwarp(); tc::cluster_wait(); }
+    }
 }
+
 }  // namespace op

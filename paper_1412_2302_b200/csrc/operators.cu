@@ -179,7 +179,7 @@ size_t backward_ws(const Walk& w, const Dims& d, int groups) { return (size_t)(d
 constexpr size_t kSmSmem = 228 * 1024, kCtaSmem = 227 * 1024;
 // How clusters walk a tensor, `slot` bytes kept per vector of V channels, `moved` bytes per vector to and from memory and K sums per thread and
 // vector element; k = 0: not at all (rows wider than a block, or too few samples to fill the device with their clusters).  By a model in
-// cycles: an SM moves 22 bytes per cycle when it has 18 warps of three CTAs (in different phases), a round of CTAs costs 4500 or 6000
+// cycles: an SM moves 22 bytes per cycle when it has 15 warps of three CTAs (in different phases), a round of CTAs costs 4500 or 6000
 // more for its first loads and the sums' way around, and vectors that do not stay on chip are read again at 40 bytes.
 template <int V>
 ClusterWalk cluster_walk(const Dims& d, int groups, int slot, int moved, int K) {
@@ -207,7 +207,7 @@ ClusterWalk cluster_walk(const Dims& d, int groups, int slot, int moved, int K) 
                     const size_t room = std::min(kCtaSmem, kSmSmem / occ - 1024);
                     if (room < scratch) break;
                     w.keep = (int)std::min<size_t>(w.its, (room - scratch) / per_it);
-                    const double busy = std::min(1.0, occ * w.threads / 576.0) * (occ == 1 ? 0.55 : occ == 2 ? 0.8 : 1.0);
+                    const double busy = std::min(1.0, occ * w.threads / 480.0) * (occ == 1 ? 0.55 : occ == 2 ? 0.8 : 1.0);
                     const double work = ((double)w.its * w.threads * moved / 22 + (double)(w.its - w.keep) * w.threads * moved / 40) / busy;
                     const double per_sm = (double)ceil_div(d.n * w.slices * w.k, kSms), c = per_sm * work + (w.k > 1 ? 6000 : 4500) * std::ceil(per_sm / occ);
                     if (c < cost) { cost = c; best = w; }
@@ -224,6 +224,30 @@ ClusterWalk cluster_walk(const Dims& d, int groups, int slot, int moved, int K) 
 }
 template <typename K>
 cudaError_t allow_smem(K* kernel) { return cudaFuncSetAttribute((const void*)kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kCtaSmem); }
+// Samples that are under way at once: as many clusters per slice as the device holds (asked once per kernel and launch shape).
+template <typename K>
+long long cluster_rows(Launcher& go, K* kernel, const ClusterWalk& w, const Dims& d, size_t smem) {
+    struct Known { const void* kernel = nullptr; int device, threads, k, clusters; size_t smem; };
+    static thread_local Known known[16];      // (of all kernels with this signature)
+    static thread_local unsigned next = 0;
+    int dev = 0;
+    if (go.e == cudaSuccess) go.e = cudaGetDevice(&dev);
+    int clusters = 0;
+    for (const Known& q : known)
+        if (q.kernel == (const void*)kernel && q.device == dev && q.threads == w.threads && q.k == w.k && q.smem == smem) clusters = q.clusters;
+    if (!clusters && go.e == cudaSuccess) {
+        go.e = allow_smem(kernel);
+        cudaLaunchConfig_t lc{};
+        lc.gridDim = dim3((unsigned)w.k); lc.blockDim = w.threads; lc.dynamicSmemBytes = smem;
+        cudaLaunchAttribute at{};
+        at.id = cudaLaunchAttributeClusterDimension;
+        at.val.clusterDim.x = w.k; at.val.clusterDim.y = 1; at.val.clusterDim.z = 1;
+        lc.attrs = &at; lc.numAttrs = 1;
+        if (go.e == cudaSuccess) go.e = cudaOccupancyMaxActiveClusters(&clusters, kernel, &lc);
+        if (go.e == cudaSuccess) known[next++ % 16] = {(const void*)kernel, dev, w.threads, w.k, clusters, smem};
+    }
+    return std::min<long long>(d.n, std::max(1, clusters / w.slices));
+}
 
 template <typename T, int V, int ACT>
 void forward(Launcher& go, const alexnet_group_norm_forward_t* a, const Dims& d) {
@@ -236,10 +260,12 @@ void forward(Launcher& go, const alexnet_group_norm_forward_t* a, const Dims& d)
             if (a->keep_x.codes) kx = {(uint8_t*)a->keep_x.codes, a->keep_x.scales, src_of(a->keep_x.format)};
             if (a->keep_y.codes) ky = {(uint8_t*)a->keep_y.codes, a->keep_y.scales, src_of(a->keep_y.format)};
         }
-        if (go.e == cudaSuccess) go.e = allow_smem(gn_cluster_forward_kernel<T, V, ACT>);
-        go.smem = (size_t)cw.keep * cw.threads * sizeof(T) * V + cluster_scratch<V>(cw, 3);
+        const size_t smem = (size_t)cw.keep * cw.threads * sizeof(T) * V + cluster_scratch<V>(cw, 3);
+        const long long rows = cluster_rows(go, gn_cluster_forward_kernel<T, V, ACT>, cw, d, smem);
+        go.smem = smem;
         go.cluster = cw.k;
-        go(gn_cluster_forward_kernel<T, V, ACT>, d.n * cw.slices * cw.k, cw.threads, (const T*)a->x.data, geo_of(a->x, d), cw, s, a->weight, a->bias, (T*)a->y.data, geo_of(a->y, d), a->mean, a->rstd, kx, ky);
+        go(gn_cluster_forward_kernel<T, V, ACT>, rows * cw.slices * cw.k, cw.threads, (const T*)a->x.data, geo_of(a->x, d), cw, s, (long long)d.n, a->weight, a->bias, (T*)a->y.data,
+           geo_of(a->y, d), a->mean, a->rstd, kx, ky);
         if (V != 8) {
             if (a->keep_x.codes) encode<T>(go, d, a->x, a->keep_x, a->shape.dtype);
             if (a->keep_y.codes) encode<T>(go, d, a->y, a->keep_y, a->shape.dtype);
@@ -277,12 +303,13 @@ void backward(Launcher& go, const alexnet_group_norm_backward_t* a, const Dims& 
     if (cw.k) {
         partial = (float*)a->workspace;
         auto* kernel = gn_cluster_backward_kernel<T, V, SRC, ACT>;
-        if (go.e == cudaSuccess) go.e = allow_smem(kernel);
         const size_t slab = (size_t)cw.keep * cw.threads;
-        go.smem = slab * (kSlot - (SRC == kSrcSame ? 0 : 1)) + (SRC == kSrcSame ? 0 : (slab + 15) / 16 * 16) + cluster_scratch<V>(cw, 2);
+        const size_t smem = slab * (kSlot - (SRC == kSrcSame ? 0 : 1)) + (SRC == kSrcSame ? 0 : (slab + 15) / 16 * 16) + cluster_scratch<V>(cw, 2);
+        const long long rows = cluster_rows(go, kernel, cw, d, smem);
+        go.smem = smem;
         go.cluster = cw.k;
-        go(kernel, d.n * cw.slices * cw.k, cw.threads, dy, gdy, src, gx, cw, s, A, (T*)a->dx.data, gdx, partial);
-        if (a->dweight || a->dbias) go(gn_parameter_gradient_kernel, ceil_div(d.C, 32), 1024, (const float*)partial, d.C, d.n, a->dweight, a->dbias);
+        go(kernel, rows * cw.slices * cw.k, cw.threads, dy, gdy, src, gx, cw, s, (long long)d.n, A, (T*)a->dx.data, gdx, partial);
+        if (a->dweight || a->dbias) go(gn_parameter_gradient_kernel, ceil_div(d.C, 32), 1024, (const float*)partial, d.C, rows, a->dweight, a->dbias);
         return;
     }
     go(gn_backward_sums_kernel<T, V, SRC, ACT>, grid_of(w, d), 256, dy, gdy, src, gx, w, s, A, partial);
