@@ -87,10 +87,11 @@ inline FastDiv fast_div(uint32_t d) {
     return {d, (uint32_t)(((1ull << (31 + s)) / d) + 1), 31 + s};
 }
 // strides in elements; flat: position p of a sample lies at p * sw
+// step: positions between a thread's; inc = step * sw, wrap = sh - w * sw (0: flat)
 struct Geo {
-    long long sn, sh, sw;
+    long long sn, sh, sw, inc, wrap;
     FastDiv w;
-    int flat;
+    int flat, step;
     __device__ __forceinline__ long long at(uint32_t p) const {
         if (flat) return (long long)p * sw;
         const uint32_t h = w.div(p);
@@ -98,14 +99,17 @@ struct Geo {
     }
 };
 
-// A thread's walk over positions that lie `step` apart: its offset in a tensor, by one addition where the tensor is flat.
+// A thread's walk over positions that lie g.step apart: its offset in a tensor, by one addition, and another where it passes the end of a row.
 struct Cursor {
     long long off;
-    uint32_t p;
-    __device__ __forceinline__ Cursor(const Geo& g, uint32_t p0) : off(g.at(p0)), p(p0) {}
-    __device__ __forceinline__ void next(const Geo& g, int step) {
-        if (g.flat) off += (long long)step * g.sw;
-        else { p += step; off = g.at(p); }
+    int x;
+    __device__ __forceinline__ Cursor(const Geo& g, uint32_t p) : off(g.at(p)), x(g.flat ? 0 : (int)(p - g.w.div(p) * g.w.d)) {}
+    __device__ __forceinline__ void next(const Geo& g) {
+        off += g.inc;
+        if (!g.flat) {
+            x += g.step;
+            while (x >= (int)g.w.d) { x -= (int)g.w.d; off += g.wrap; }
+        }
     }
 };
 
@@ -241,11 +245,13 @@ __device__ __forceinline__ void store_codes(const Raw<T, 8>& r, const float* f, 
         if ((threadIdx.x & 3) == 0) *scales = (uint8_t)e;
     }
 }
-// where a thread's codes go, position by position
+// where a thread's codes go, position by position, `step` positions apart
+struct Dense { int C, blocks, inc_scales; long long inc_codes; };
+inline Dense dense_of(int C, int step) { return {C, (C + 31) / 32, (C + 31) / 32 * step, (long long)C * step}; }
 struct CodesCursor {
     uint8_t *codes, *scales;
-    __device__ __forceinline__ CodesCursor(uint8_t* c, uint8_t* s, long long row, int vec, int C) : codes(c + row * C + 8 * vec), scales(s + row * ((C + 31) / 32) + (vec >> 2)) {}
-    __device__ __forceinline__ void next(int step, int C) { codes += (long long)step * C; scales += (long long)step * ((C + 31) / 32); }
+    __device__ __forceinline__ CodesCursor(uint8_t* c, uint8_t* s, long long row, int vec, const Dense& d) : codes(c + row * d.C + 8 * vec), scales(s + row * d.blocks + (vec >> 2)) {}
+    __device__ __forceinline__ void next(const Dense& d) { codes += d.inc_codes; scales += d.inc_scales; }
 };
 
 // How a launch walks a tensor: a block takes the positions [chunk * ppc, + ppc) of a sample and `cols` vectors of V channels; thread
@@ -254,6 +260,7 @@ struct CodesCursor {
 struct Walk {
     int C, HW, vecs, cols, rows, colblocks, ppc;
     long long chunks;           // per sample
+    Dense dense;                // codes of positions `rows` apart
 };
 struct Spot { int col, row, v, p0, p1; long long n, chunk; bool on, has; };
 __device__ __forceinline__ Spot spot(const Walk& w) {
@@ -283,13 +290,13 @@ __global__ void __launch_bounds__(256) checkpoint_encode_kernel(const T* __restr
     const T* xp = x + s.n * g.sn + 8 * s.v;
     constexpr int U = 4;
     Cursor c(g, s.p0 + s.row);
-    CodesCursor k(codes, scales, s.n * w.HW + s.p0 + s.row, s.v, w.C);
+    CodesCursor k(codes, scales, s.n * w.HW + s.p0 + s.row, s.v, w.dense);
     for (int p = s.p0 + s.row; p < s.p1; p += U * w.rows) {
         Raw<T, 8> r[U] = {};
         #pragma unroll
         for (int u = 0; u < U; ++u) {
             if (s.has && p + u * w.rows < s.p1) r[u] = *(const Raw<T, 8>*)(xp + c.off);
-            c.next(g, w.rows);
+            c.next(g);
         }
         #pragma unroll
         for (int u = 0; u < U; ++u) {
@@ -298,7 +305,7 @@ __global__ void __launch_bounds__(256) checkpoint_encode_kernel(const T* __restr
                 unpack<T, 8>(r[u], f);
                 store_codes<T, FMT>(r[u], f, s.has, k.codes, k.scales);
             }
-            k.next(w.rows, w.C);
+            k.next(w.dense);
         }
     }
 }
@@ -310,14 +317,14 @@ __global__ void __launch_bounds__(256) checkpoint_decode_kernel(const uint8_t* _
     T* op = out + s.n * g.sn + 8 * s.v;
     constexpr int U = 4;
     Cursor c(g, s.p0 + s.row);
-    CodesCursor k(const_cast<uint8_t*>(codes), const_cast<uint8_t*>(scales), s.n * w.HW + s.p0 + s.row, s.v, w.C);
+    CodesCursor k(const_cast<uint8_t*>(codes), const_cast<uint8_t*>(scales), s.n * w.HW + s.p0 + s.row, s.v, w.dense);
     for (int p = s.p0 + s.row; p < s.p1; p += U * w.rows) {
         uint2 r[U];
         uint8_t e[U];
         #pragma unroll
         for (int u = 0; u < U; ++u) {
             if (p + u * w.rows < s.p1) { r[u] = *(const uint2*)k.codes; e[u] = *k.scales; }
-            k.next(w.rows, w.C);
+            k.next(w.dense);
         }
         #pragma unroll
         for (int u = 0; u < U; ++u) {
@@ -329,7 +336,7 @@ __global__ void __launch_bounds__(256) checkpoint_decode_kernel(const uint8_t* _
                 for (int i = 0; i < 8; i += 2) un2(mul2(mk2(f[i], f[i + 1]), mk2(sc, sc)), f[i], f[i + 1]);
                 *(Raw<T, 8>*)(op + c.off) = pack<T, 8>(f);
             }
-            c.next(g, w.rows);
+            c.next(g);
         }
     }
 }

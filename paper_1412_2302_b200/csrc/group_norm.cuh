@@ -127,29 +127,17 @@ template <int UNROLL, typename G, typename N> __device__ __forceinline__ Part jo
     const float lo = e * inv;
     return {hi, lo, fmaf(-e, lo, q)};
 }
-// The same by `lanes` neighbouring lanes (a power of two): each takes every lanes-th part; the result is the same in all of them.  All 32 lanes of the warp
-// call it; inactive ones have count = 0.
+// The same by `lanes` neighbouring lanes (a power of two; all 32 of the warp call it); the result is the same in all of them.
 __device__ __forceinline__ float lanes_sum(float t, int lanes) {
     for (int o = lanes >> 1; o; o >>= 1) t += __shfl_xor_sync(~0u, t, o);
     return t;
 }
-template <typename G, typename N> __device__ __forceinline__ Part join_lanes(int count, int lanes, float inv, G get, N n) {
-    const int first = threadIdx.x & (lanes - 1);
-    const float ref = count ? get(0).hi : 0.f;
-    float m = 0.f, e = 0.f, q = 0.f;
-    #pragma unroll 4
-    for (int i = first; i < count; i += lanes) m = fmaf(n(i), get(i).hi - ref, m);
-    const float hi = fmaf(lanes_sum(m, lanes), inv, ref);
-    #pragma unroll 4
-    for (int i = first; i < count; i += lanes) {
-        const Part t = get(i);
-        const float d = (t.hi - hi) + t.lo, w = n(i) * d;
-        e += w;
-        q += fmaf(w, d, t.m2);
-    }
-    e = lanes_sum(e, lanes);
-    q = lanes_sum(q, lanes);
-    const float lo = e * inv;
+// a part of n values per lane
+__device__ __forceinline__ Part join_lanes(const Part& t, float n, int lanes, float inv) {
+    const float ref = __shfl_sync(~0u, t.hi, threadIdx.x & 31 & ~(lanes - 1));
+    const float hi = fmaf(lanes_sum(n > 0.f ? n * (t.hi - ref) : 0.f, lanes), inv, ref);
+    const float d = (t.hi - hi) + t.lo, w = n > 0.f ? n * d : 0.f;
+    const float e = lanes_sum(w, lanes), q = lanes_sum(fmaf(w, d, t.m2), lanes), lo = e * inv;
     return {hi, lo, fmaf(-e, lo, q)};
 }
 // Per-thread sums of a block in shared memory, by vector element and thread: pitch = threads + 4, so that neighbouring threads' stores and the
@@ -201,7 +189,7 @@ __global__ void __launch_bounds__(256) gn_sums_kernel(const T* __restrict__ x, c
             #pragma unroll
             for (int u = 0; u < U; ++u) {
                 if (it + u < cnt) r[u] = *(const Raw<T, V>*)(xp + c.off);
-                c.next(g, w.rows);
+                c.next(g);
             }
             #pragma unroll
             for (int u = 0; u < U; ++u)
@@ -236,36 +224,42 @@ __device__ __forceinline__ float2 block_sum(float2 t, float2* red) {        // o
     for (int k = 1; k < 8; ++k) { t.x += red[k].x; t.y += red[k].y; }
     return t;
 }
-// a block per group: the chunks' parts [chunks][C] of its channels
-__global__ void __launch_bounds__(256) gn_statistics_kernel(const float4* __restrict__ partial, const NormShape s, int chunks, int ppc, float* __restrict__ mean, float* __restrict__ rstd) {
+// The chunks' parts [chunks][C] of a group's channels, joined by a block, or by a warp where there are groups enough (4096 groups of 30 parts: 7.6 -> 2.5 us).
+template <bool BLOCK>
+__global__ void __launch_bounds__(256) gn_statistics_kernel(const float4* __restrict__ partial, const NormShape s, long long all_groups, int chunks, int ppc, float* __restrict__ mean, float* __restrict__ rstd) {
     kn::pdl_sync();
     __shared__ float2 red[8];
-    const long long n = blockIdx.x / s.groups;
-    const int g = (int)(blockIdx.x - n * s.groups), total = chunks * s.cg;
+    const long long id = BLOCK ? blockIdx.x : blockIdx.x * 8ll + (threadIdx.x >> 5);
+    if (id >= all_groups) return;
+    constexpr int N = BLOCK ? 256 : 32;
+    const int me = threadIdx.x % N;
+    const long long n = id / s.groups;
+    const int g = (int)(id - n * s.groups), total = chunks * s.cg;
     const float4* p = partial + n * chunks * s.C + (long long)g * s.cg;
     const float ref = p[0].x, lo = (float)ppc, last = (float)(s.HW - (chunks - 1) * ppc), count = (float)s.HW * (float)s.cg;
+    auto sum = [&](float2 t) { return BLOCK ? block_sum(t, red) : warp_sum(t); };
     float2 t = make_float2(0.f, 0.f);
     #pragma unroll 4
-    for (int i = threadIdx.x; i < total; i += 256) {
+    for (int i = me; i < total; i += N) {
         const int k = s.group(i);
         t.x = fmaf(k == chunks - 1 ? last : lo, p[(long long)k * s.C + (i - k * s.cg)].x - ref, t.x);
     }
-    const float hi = ref + __fdiv_rn(block_sum(t, red).x, count);
+    const float hi = ref + __fdiv_rn(sum(t).x, count);
     t.x = 0.f;
     #pragma unroll 4
-    for (int i = threadIdx.x; i < total; i += 256) {
+    for (int i = me; i < total; i += N) {
         const int k = s.group(i);
         const float4 q = p[(long long)k * s.C + (i - k * s.cg)];
         const float d = (q.x - hi) + q.y, w = (k == chunks - 1 ? last : lo) * d;
         t.x += w;
         t.y += fmaf(w, d, q.z);
     }
-    t = block_sum(t, red);
-    if (threadIdx.x == 0) {
+    t = sum(t);
+    if (me == 0) {
         const float l = __fdiv_rn(t.x, count);
         const float2 r = statistics(Part{hi, l, fmaf(-t.x, l, t.y)}, s);
-        mean[blockIdx.x] = r.x;
-        rstd[blockIdx.x] = r.y;
+        mean[id] = r.x;
+        rstd[id] = r.y;
     }
 }
 struct Keep { uint8_t *codes, *scales; int fmt; };        // codes == nullptr: nothing kept
@@ -276,29 +270,29 @@ __device__ __forceinline__ void keep_codes(const Keep& k, const Raw<T, 8>& r, co
 }
 // A thread's positions from p on, `rows` apart, `cnt` of them: results (and checkpoints) of the vectors that fetch(it) gives.
 template <typename T, int V, int ACT, typename F>
-__device__ __forceinline__ void apply_positions(const Chan<V>& k, const NormShape& sh, int p, int rows, int it0, int cnt, long long row0, int v, bool has, T* y, const Geo& gy, const Keep& kx, const Keep& ky,
-                                                F fetch) {
+__device__ __forceinline__ void apply_positions(const Chan<V>& k, const NormShape& sh, int p, int rows, int it0, int cnt, long long row0, int v, bool has, T* y, const Geo& gy, const Dense& dense, const Keep& kx,
+                                                const Keep& ky, F fetch) {
     Cursor c(gy, p + it0 * rows);
-    CodesCursor cx(kx.codes, kx.scales, row0 + p + it0 * rows, v, sh.C), cy(ky.codes, ky.scales, row0 + p + it0 * rows, v, sh.C);
+    CodesCursor cx(kx.codes, kx.scales, row0 + p + it0 * rows, v, dense), cy(ky.codes, ky.scales, row0 + p + it0 * rows, v, dense);
     #pragma unroll 2
     for (int it = it0; it < cnt; ++it) {
         const Raw<T, V> r = fetch(it);
         float f[V], z[V];
         unpack<T, V>(r, f);
         if constexpr (V == 8)
-            if (kx.codes) { keep_codes<T>(kx, r, f, has, cx); cx.next(rows, sh.C); }
+            if (kx.codes) { keep_codes<T>(kx, r, f, has, cx); cx.next(dense); }
         v_add<V>(f, k.nm, f);
         v_fma<V>(f, k.a, k.b, z);
         activate<T, V, ACT>(sh.act, z);
         Raw<T, V> out = pack<T, V>(z);
         if (has) *(Raw<T, V>*)(y + c.off) = out;
-        c.next(gy, rows);
+        c.next(gy);
         if constexpr (V == 8)
             if (ky.codes) {                     // of y as it is stored
                 if (!has) out = Raw<T, 8>{};
                 unpack<T, 8>(out, f);
                 keep_codes<T>(ky, out, f, has, cy);
-                cy.next(rows, sh.C);
+                cy.next(dense);
             }
     }
 }
@@ -314,10 +308,10 @@ __global__ void __launch_bounds__(256) gn_apply_kernel(const T* __restrict__ x, 
     if (s.has) load_chan<V>(k, sh, mean, rstd, weight, bias, s.n, V * s.v);
     const T* xp = x + s.n * gx.sn + V * s.v;
     Cursor c(gx, p);
-    apply_positions<T, V, ACT>(k, sh, p, w.rows, 0, (s.p1 - p + w.rows - 1) / w.rows, s.n * w.HW, s.v, s.has, y + s.n * gy.sn + V * s.v, gy, kx, ky, [&](int) {
+    apply_positions<T, V, ACT>(k, sh, p, w.rows, 0, (s.p1 - p + w.rows - 1) / w.rows, s.n * w.HW, s.v, s.has, y + s.n * gy.sn + V * s.v, gy, w.dense, kx, ky, [&](int) {
         Raw<T, V> r = {};
         if (s.has) r = *(const Raw<T, V>*)(xp + c.off);
-        c.next(gx, w.rows);
+        c.next(gx);
         return r;
     });
 }
@@ -329,14 +323,6 @@ template <typename T, int V, int SRC> struct Fetch {
     using R = typename std::conditional<SRC == kSrcSame, Raw<T, V>, Raw<uint8_t, V>>::type;
     R r;
     uint8_t e;
-    __device__ __forceinline__ void load(const Source& s, const Geo& g, const Walk& w, long long n, int p, int v) {
-        if constexpr (SRC == kSrcSame) r = *(const R*)((const T*)s.x + n * g.sn + g.at(p) + V * v);
-        else {
-            const long long row = n * w.HW + p;
-            r = *(const R*)(s.codes + row * w.C + V * v);
-            e = s.scales[row * ((w.C + 31) / 32) + V * v / 32];
-        }
-    }
     // f = x, or the code that stands for it (x = f * scale(), exactly); d = x - mean, rounded once
     __device__ __forceinline__ float scale() const {
         if constexpr (SRC == kSrcSame) return 1.f;
@@ -354,6 +340,25 @@ template <typename T, int V, int SRC> struct Fetch {
             for (int i = 0; i < V; ++i) s[i] = sc;
             v_fma<V>(f, s, nm, d);
         }
+    }
+};
+// a thread's walk over x in either form
+template <typename T, int V, int SRC> struct SourceCursor {
+    Cursor c;
+    const T* x;
+    const uint8_t *codes, *scales;
+    template <typename W> __device__ __forceinline__ SourceCursor(const Source& s, const Geo& g, const W& w, long long n, int p, int v)
+        : c(g, SRC == kSrcSame ? p : 0), x(SRC == kSrcSame ? (const T*)s.x + n * g.sn + V * v : nullptr), codes(SRC == kSrcSame ? nullptr : s.codes + (n * w.HW + p) * w.C + V * v),
+          scales(SRC == kSrcSame ? nullptr : s.scales + (n * w.HW + p) * w.dense.blocks + V * v / 32) {}
+    __device__ __forceinline__ void load(Fetch<T, V, SRC>& f) const {
+        using R = typename Fetch<T, V, SRC>::R;
+        if constexpr (SRC == kSrcSame) f.r = *(const R*)(x + c.off);
+        else { f.r = *(const R*)codes; f.e = *scales; }
+    }
+    __device__ __forceinline__ const void* place() const { return SRC == kSrcSame ? (const void*)(x + c.off) : (const void*)codes; }
+    template <typename W> __device__ __forceinline__ void next(const Geo& g, const W& w) {
+        if constexpr (SRC == kSrcSame) c.next(g);
+        else { codes += w.dense.inc_codes; scales += w.dense.inc_scales; }
     }
 };
 // The side of ReLU's kink that a value is on, where fp32 cannot tell: d and a carry a rounding each, so z = d a + b is off by up to 2^-23 |b| or so when it
@@ -415,15 +420,20 @@ __global__ void __launch_bounds__(256) gn_backward_sums_kernel(const T* __restri
         Chan<V> k;
         load_chan<V>(k, sh, A.mean, A.rstd, A.weight, A.bias, s.n, V * s.v);
         const T* dp = dy + s.n * gdy.sn + V * s.v;
+        Cursor c(gdy, s.p0 + s.row);
+        SourceCursor<T, V, SRC> cx(src, gx, w, s.n, s.p0 + s.row, s.v);
         for (int p = s.p0 + s.row; p < s.p1; p += U * w.rows) {
             Raw<T, V> r[U];
             Fetch<T, V, SRC> fx[U];
             #pragma unroll
-            for (int u = 0; u < U; ++u)
+            for (int u = 0; u < U; ++u) {
                 if (p + u * w.rows < s.p1) {
-                    r[u] = *(const Raw<T, V>*)(dp + gdy.at(p + u * w.rows));
-                    fx[u].load(src, gx, w, s.n, p + u * w.rows, s.v);
+                    r[u] = *(const Raw<T, V>*)(dp + c.off);
+                    cx.load(fx[u]);
                 }
+                c.next(gdy);
+                cx.next(gx, w);
+            }
             #pragma unroll
             for (int u = 0; u < U; ++u)
                 if (p + u * w.rows < s.p1) {
@@ -448,25 +458,30 @@ __global__ void __launch_bounds__(256) gn_backward_sums_kernel(const T* __restri
         o[w.C] = t2 * A.rstd[s.n * sh.groups + sh.group(c0 + j)];       // of xhat
     }
 }
-// c1 and c2 of a group per block, from the chunks' sums [chunks][2][C]
-__global__ void __launch_bounds__(256) gn_backward_group_kernel(const float* __restrict__ partial, const NormShape sh, int chunks, const BackwardArgs A, float2* __restrict__ c12) {
+// c1 and c2 of a group from the chunks' sums [chunks][2][C], by a block or a warp
+template <bool BLOCK>
+__global__ void __launch_bounds__(256) gn_backward_group_kernel(const float* __restrict__ partial, const NormShape sh, long long all_groups, int chunks, const BackwardArgs A, float2* __restrict__ c12) {
     kn::pdl_sync();
     __shared__ float2 red[8];
-    const long long n = blockIdx.x / sh.groups;
-    const int g = (int)(blockIdx.x - n * sh.groups), total = chunks * sh.cg;
+    const long long id = BLOCK ? blockIdx.x : blockIdx.x * 8ll + (threadIdx.x >> 5);
+    if (id >= all_groups) return;
+    constexpr int N = BLOCK ? 256 : 32;
+    const int me = threadIdx.x % N;
+    const long long n = id / sh.groups;
+    const int g = (int)(id - n * sh.groups), total = chunks * sh.cg;
     const float* p = partial + n * chunks * 2 * sh.C + (long long)g * sh.cg;
     float2 t = make_float2(0.f, 0.f);
     #pragma unroll 4
-    for (int i = threadIdx.x; i < total; i += 256) {
+    for (int i = me; i < total; i += N) {
         const int k = sh.group(i), c = i - k * sh.cg;
         const float wt = A.weight ? A.weight[g * sh.cg + c] : 1.f;
         const float* q = p + (long long)k * 2 * sh.C + c;
         t.x = fmaf(wt, q[0], t.x);
         t.y = fmaf(wt, q[sh.C], t.y);
     }
-    t = block_sum(t, red);
+    t = BLOCK ? block_sum(t, red) : warp_sum(t);
     const float m = (float)sh.HW * (float)sh.cg;
-    if (threadIdx.x == 0) c12[blockIdx.x] = make_float2(__fdiv_rn(t.x, m), __fdiv_rn(t.y, m));
+    if (me == 0) c12[id] = make_float2(__fdiv_rn(t.x, m), __fdiv_rn(t.y, m));
 }
 // dweight and dbias: the sums [n][2][C] of the samples (or of their chunks).  A block takes 32 channels, its warps every 32nd row.
 __global__ void __launch_bounds__(1024) gn_parameter_gradient_kernel(const float* __restrict__ partial, int C, long long n, float* __restrict__ dweight, float* __restrict__ dbias) {
@@ -508,15 +523,20 @@ __global__ void __launch_bounds__(256) gn_backward_apply_kernel(const T* __restr
     const T* dp = dy + s.n * gdy.sn + V * s.v;
     T* op = dx + s.n * gdx.sn + V * s.v;
     constexpr int U = V == 8 ? 2 : 4;
+    Cursor c(gdy, s.p0 + s.row), co(gdx, s.p0 + s.row);
+    SourceCursor<T, V, SRC> cx(src, gx, w, s.n, s.p0 + s.row, s.v);
     for (int p = s.p0 + s.row; p < s.p1; p += U * w.rows) {
         Raw<T, V> r[U];
         Fetch<T, V, SRC> fx[U];
         #pragma unroll
-        for (int u = 0; u < U; ++u)
+        for (int u = 0; u < U; ++u) {
             if (p + u * w.rows < s.p1) {
-                r[u] = *(const Raw<T, V>*)(dp + gdy.at(p + u * w.rows));
-                fx[u].load(src, gx, w, s.n, p + u * w.rows, s.v);
+                r[u] = *(const Raw<T, V>*)(dp + c.off);
+                cx.load(fx[u]);
             }
+            c.next(gdy);
+            cx.next(gx, w);
+        }
         #pragma unroll
         for (int u = 0; u < U; ++u)
             if (p + u * w.rows < s.p1) {
@@ -525,7 +545,8 @@ __global__ void __launch_bounds__(256) gn_backward_apply_kernel(const T* __restr
                 activation_gradient<T, V, SRC, ACT>(sh, k, A, s.n, V * s.v, fx[u], f, q);
                 v_fma<V>(f, B, D, f);
                 v_fma<V>(q, k.a, f, q);
-                *(Raw<T, V>*)(op + gdx.at(p + u * w.rows)) = pack<T, V>(q);
+                *(Raw<T, V>*)(op + co.off) = pack<T, V>(q);
+                co.next(gdx);
             }
     }
 }
@@ -542,8 +563,9 @@ struct ClusterWalk {
     int C, HW;                                // of the tensor
     int slices, Cs, groups;                   // channel slices; channels and groups of one
     int vecs, cols, rows, threads;            // vectors of a slice's row; rows = threads / cols
+    Dense dense;                              // codes of positions `rows` apart
     int k, ppc, its, keep;                    // CTAs of the cluster; positions of a CTA, at most; iterations of a thread, and those whose vectors stay
-    int lanes;                                // a power of two: lanes that join a group's sums
+    int lanes, lc, lc_shift;                  // lanes that join a group's sums, lc = 2^lc_shift of them over its channels (powers of two)
 };
 constexpr int kClThreads = 256;               // at most; two CTAs per SM with 128 registers
 
@@ -572,20 +594,26 @@ __device__ __forceinline__ float ld_cluster(const float* p, uint32_t rank) {
     asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(tc::mapa_u32(tc::smem_u32(p), rank)) : "memory");
     return v;
 }
-// shared memory behind the slots: K sums per thread and vector element, K per channel, K per group of this CTA, and the groups' results
+// shared memory behind the slots: the groups' results, two sums per thread and vector element, K per group of this CTA; backward (K = 2) also two sums per
+// channel, and those of all samples
 template <int V> struct ClusterSmem {
     Table<V> part;
-    float *chan, *grp;       // [K][Cs], [K][groups]; K = 2 (backward): the samples' sums of this CTA's channels behind them
+    float *chan, *grp;       // [2][Cs], [K][groups]
+    float *weight, *rstd;    // backward: of the slice's channels, and of the groups of the sample
+    float* acc;              // backward: the samples' sums of this CTA's channels, [2][ceil(Cs / k)]
     float2* res;
     __device__ __forceinline__ ClusterSmem(uint8_t* p, const ClusterWalk& w, int K) {
         res = (float2*)p;
         part = {(float*)(res + w.groups), w.threads + 4};
-        chan = part.p + K * V * part.pitch;
-        grp = chan + K * w.Cs;
+        chan = part.p + 2 * V * part.pitch;
+        grp = chan + (K == 2 ? 2 * w.Cs : 0);
+        weight = grp + K * w.groups;
+        rstd = weight + w.Cs;
+        acc = rstd + w.groups;
     }
 };
 template <int V> inline size_t cluster_scratch(const ClusterWalk& w, int K) {
-    return ((size_t)K * V * (w.threads + 4) + K * w.Cs + K * w.groups + (K == 2 ? 2 * (w.Cs + w.k - 1) / w.k + 2 : 0)) * sizeof(float) + w.groups * sizeof(float2);
+    return ((size_t)2 * V * (w.threads + 4) + K * w.groups + (K == 2 ? 3 * w.Cs + w.groups + 2 * ((w.Cs + w.k - 1) / w.k) : 0)) * sizeof(float) + w.groups * sizeof(float2);
 }
 // A cluster's work: a slice of the channels (from channel c0, group g0 on) of the samples n0, n0 + step, ...
 struct ClusterSpot {
@@ -600,6 +628,20 @@ struct ClusterSpot {
         rank = w.k > 1 ? (int)tc::cluster_ctarank() : 0;
     }
 };
+// What the lanes of a group add up: the table's K sums of the channels c0 .. c0 + cg - 1 over the rows of threads r < rows, dealt to lanes by channel
+// (w.lc of them) and by row.  These loops run a warp at a time with nothing to hide their latency, so they are kept to a load and an addition.
+template <int V, int K> __device__ __forceinline__ void group_sums(const ClusterWalk& w, const Table<V>& table, uint32_t c0, uint32_t cg, int rows, uint32_t lane, float* out) {
+    const uint32_t ci = lane & (w.lc - 1);
+    const int ri = lane >> w.lc_shift, lr = w.lanes >> w.lc_shift, step = lr * w.cols, next = V * table.pitch;
+    for (uint32_t c = c0 + ci; c < c0 + cg; c += w.lc) {
+        const float* p = table.p + (c % V) * table.pitch + c / V + ri * w.cols;
+        #pragma unroll 4
+        for (int r = ri; r < rows; r += lr, p += step) {
+            #pragma unroll
+            for (int k = 0; k < K; ++k) out[k] += p[k * next];
+        }
+    }
+}
 // V channels' parameters, or `other` where there are none
 template <int V> __device__ __forceinline__ void load_parameters(const float* p, int c, float other, float* out) {
     if (V == 8 && p && ((uintptr_t)p & 15) == 0) {
@@ -643,7 +685,7 @@ __global__ void __launch_bounds__(kClThreads, 2) gn_cluster_forward_kernel(const
             #pragma unroll 4
             for (int it = bt * batch; it < e; ++it) {
                 fill_slot(slots + it * w.threads, xp + c.off);
-                c.next(gx, w.rows);
+                c.next(gx);
             }
             copies_commit();
         }
@@ -662,15 +704,11 @@ __global__ void __launch_bounds__(kClThreads, 2) gn_cluster_forward_kernel(const
         }
         __syncthreads();
         for (int g0 = warp * at_once; g0 < w.groups; g0 += warps * at_once) {
-            const int g = g0 + lane_g, total = g < w.groups ? rows * sh.cg : 0;
+            const int g = g0 + lane_g, first_rows = g < w.groups ? min(rows, 1 + 32 / sh.cg) : 0;      // at least 32 values, where there are as many
             float t = 0.f;
-            #pragma unroll 2
-            for (int i = lane_i; i < total; i += w.lanes) {
-                const int r = sh.group(i), c = g * sh.cg + i - r * sh.cg;
-                t += m.part.at(0, c % V, r * w.cols + c / V);
-            }
+            if (first_rows) group_sums<V, 1>(w, m.part, g * sh.cg, sh.cg, first_rows, lane_i, &t);
             t = lanes_sum(t, w.lanes);
-            if (lane_i == 0 && total) m.res[g].x = __fdividef(t, (float)total);
+            if (lane_i == 0 && first_rows) m.res[g].x = __fdividef(t, (float)(first_rows * sh.cg));
         }
         __syncthreads();
         // sums
@@ -691,7 +729,7 @@ __global__ void __launch_bounds__(kClThreads, 2) gn_cluster_forward_kernel(const
         for (int bt = 0; bt < kClBatches; ++bt) {
             copies_wait(kClBatches - 1 - bt);
             const int e = min(kept, (bt + 1) * batch);
-            #pragma unroll 2
+            #pragma unroll 4
             for (int it = bt * batch; it < e; ++it) add(slots[it * w.threads]);
         }
         if (has && kept < cnt) {
@@ -702,7 +740,7 @@ __global__ void __launch_bounds__(kClThreads, 2) gn_cluster_forward_kernel(const
                 #pragma unroll
                 for (int u = 0; u < U; ++u) {
                     if (it + u < cnt) r[u] = *(const R*)(xp + c.off);
-                    c.next(gx, w.rows);
+                    c.next(gx);
                 }
                 #pragma unroll
                 for (int u = 0; u < U; ++u)
@@ -710,18 +748,14 @@ __global__ void __launch_bounds__(kClThreads, 2) gn_cluster_forward_kernel(const
             }
         }
         #pragma unroll
-        for (int i = 0; i < V; ++i) { m.part.at(1, i, tid) = S[i]; m.part.at(2, i, tid) = Q[i]; }
+        for (int i = 0; i < V; ++i) { m.part.at(0, i, tid) = S[i]; m.part.at(1, i, tid) = Q[i]; }
         __syncthreads();
         if (w.k > 1 && !first) tc::cluster_wait();               // the others have read this CTA's sums of the sample before
         for (int g0 = warp * at_once; g0 < w.groups; g0 += warps * at_once) {
-            const int g = g0 + lane_g, total = g < w.groups ? rows * sh.cg : 0;
-            float s = 0.f, q = 0.f;
-            #pragma unroll 2
-            for (int i = lane_i; i < total; i += w.lanes) {
-                const int r = sh.group(i), c = g * sh.cg + i - r * sh.cg, at = r * w.cols + c / V;
-                s += m.part.at(1, c % V, at);
-                q += m.part.at(2, c % V, at);
-            }
+            const int g = g0 + lane_g, total = g < w.groups ? rows : 0;
+            float sq[2] = {0.f, 0.f};
+            if (total) group_sums<V, 2>(w, m.part, g * sh.cg, sh.cg, total, lane_i, sq);
+            float s = sq[0], q = sq[1];
             s = lanes_sum(s, w.lanes);
             q = lanes_sum(q, w.lanes);
             if (lane_i == 0 && g < w.groups) {
@@ -738,8 +772,9 @@ __global__ void __launch_bounds__(kClThreads, 2) gn_cluster_forward_kernel(const
             const int g = (i0 + lane) / w.k;
             Part t = {0.f, 0.f, 0.f};
             if (w.k > 1) {
-                auto get = [&](int i) { return Part{ld_cluster(m.grp + g, i), ld_cluster(m.grp + w.groups + g, i), ld_cluster(m.grp + 2 * w.groups + g, i)}; };
-                t = join_lanes(g < w.groups ? w.k : 0, w.k, __fdividef(1.f, (float)w.HW * (float)sh.cg), get, [&](int i) { return (float)max(0, min(w.HW - i * w.ppc, w.ppc)) * (float)sh.cg; });
+                const int i = (i0 + lane) % w.k;
+                if (g < w.groups) t = Part{ld_cluster(m.grp + g, i), ld_cluster(m.grp + w.groups + g, i), ld_cluster(m.grp + 2 * w.groups + g, i)};
+                t = join_lanes(t, (float)max(0, min(w.HW - i * w.ppc, w.ppc)) * (float)sh.cg, w.k, __fdividef(1.f, (float)w.HW * (float)sh.cg));
             } else if (g < w.groups) t = {m.grp[g], m.grp[w.groups + g], m.grp[2 * w.groups + g]};
             if (g < w.groups && (i0 + lane) % w.k == 0) {
                 const float2 r = statistics(t, sh);
@@ -748,7 +783,7 @@ __global__ void __launch_bounds__(kClThreads, 2) gn_cluster_forward_kernel(const
             }
         }
         __syncwarp();
-        if (w.k > 1) tc::cluster_arrive();                       // this CTA has read the others' sums
+        if (w.k > 1) tc::cluster_arrive_relaxed();               // this CTA has read the others' sums
         first = false;
         __syncthreads();
 
@@ -768,24 +803,24 @@ __global__ void __launch_bounds__(kClThreads, 2) gn_cluster_forward_kernel(const
         const T* xn = xp + b.step * gx.sn;
         T* yp = y + n * gy.sn + V * cv;
         Cursor cy(gy, p0 + row), cx(gx, p0 + row);               // cx: the next sample's copies, then this one's vectors that are read again
-        CodesCursor ckx(kx.codes, kx.scales, n * w.HW + p0 + row, cv, w.C), cky(ky.codes, ky.scales, n * w.HW + p0 + row, cv, w.C);
+        CodesCursor ckx(kx.codes, kx.scales, n * w.HW + p0 + row, cv, w.dense), cky(ky.codes, ky.scales, n * w.HW + p0 + row, cv, w.dense);
         auto emit = [&](const R& r) {
             float f[V], z[V];
             unpack<T, V>(r, f);
             if constexpr (V == 8)
-                if (kx.codes) { keep_codes<T>(kx, r, f, has, ckx); ckx.next(w.rows, w.C); }
+                if (kx.codes) { keep_codes<T>(kx, r, f, has, ckx); ckx.next(w.dense); }
             v_add<V>(f, k.nm, f);
             v_fma<V>(f, k.a, k.b, z);
             activate<T, V, ACT>(sh.act, z);
             R out = pack<T, V>(z);
             if (has) *(R*)(yp + cy.off) = out;
-            cy.next(gy, w.rows);
+            cy.next(gy);
             if constexpr (V == 8)
                 if (ky.codes) {                     // of y as it is stored
                     if (!has) out = R{};
                     unpack<T, 8>(out, f);
                     keep_codes<T>(ky, out, f, has, cky);
-                    cky.next(w.rows, w.C);
+                    cky.next(w.dense);
                 }
         };
         const int split = min(cnt, w.keep);
@@ -797,7 +832,7 @@ __global__ void __launch_bounds__(kClThreads, 2) gn_cluster_forward_kernel(const
                 const R r = has ? slots[it * w.threads] : R{};
                 emit(r);
                 if (more && has) fill_slot(slots + it * w.threads, xn + cx.off);
-                cx.next(gx, w.rows);
+                cx.next(gx);
             }
             copies_commit();
         }
@@ -805,7 +840,7 @@ __global__ void __launch_bounds__(kClThreads, 2) gn_cluster_forward_kernel(const
         for (int it = split; it < cnt; ++it) {
             R r = {};
             if (has) r = *(const R*)(xp + cx.off);
-            cx.next(gx, w.rows);
+            cx.next(gx);
             emit(r);
         }
     }
@@ -827,7 +862,7 @@ __global__ void __launch_bounds__(kClThreads, 2) gn_cluster_backward_kernel(cons
     X* xslots = (X*)(smem + slab * sizeof(R)) + tid;
     uint8_t* eslots = smem + slab * (sizeof(R) + sizeof(X)) + tid;
     const ClusterSmem<V> m(smem + slab * (sizeof(R) + sizeof(X)) + (SRC == kSrcSame ? 0 : (slab + 15) / 16 * 16), w, 2);
-    float* acc = m.grp + 2 * w.groups;                          // [2][ceil(Cs / k)]
+    float* acc = m.acc;
     const ClusterSpot b(w);
     const int row = tid / w.cols, v = tid - row * w.cols, cv = b.c0 / V + v;
     const bool has = row < w.rows && v < w.vecs;
@@ -838,7 +873,8 @@ __global__ void __launch_bounds__(kClThreads, 2) gn_cluster_backward_kernel(cons
     auto codes_at = [&](long long n, int it) { return src.codes + (n * w.HW + p0 + row + (long long)it * w.rows) * w.C + V * cv; };
     auto scale_at = [&](long long n, int it) { return src.scales + (n * w.HW + p0 + row + (long long)it * w.rows) * blocks + V * cv / 32; };
     if (b.n0 < samples) {
-        Cursor cdy(gdy, p0 + row), cx(gx, p0 + row);
+        Cursor cdy(gdy, p0 + row);
+        SourceCursor<T, V, SRC> cx(src, gx, w, b.n0, p0 + row, cv);
         const T* dp = dy + b.n0 * gdy.sn + V * cv;
         #pragma unroll 1
         for (int bt = 0; bt < kClBatches; ++bt) {
@@ -846,11 +882,9 @@ __global__ void __launch_bounds__(kClThreads, 2) gn_cluster_backward_kernel(cons
             #pragma unroll 2
             for (int it = bt * batch; it < e; ++it) {
                 fill_slot(slots + it * w.threads, dp + cdy.off);
-                cdy.next(gdy, w.rows);
-                if constexpr (SRC == kSrcSame) {
-                    fill_slot(xslots + it * w.threads, xbase + b.n0 * gx.sn + cx.off);
-                    cx.next(gx, w.rows);
-                } else fill_slot(xslots + it * w.threads, codes_at(b.n0, it));
+                cdy.next(gdy);
+                fill_slot(xslots + it * w.threads, cx.place());
+                cx.next(gx, w);
             }
             copies_commit();
         }
@@ -860,11 +894,13 @@ __global__ void __launch_bounds__(kClThreads, 2) gn_cluster_backward_kernel(cons
         }
     }
     for (int i = tid; i < 2 * own; i += w.threads) acc[i] = 0.f;
+    for (int c = tid; c < w.Cs; c += w.threads) m.weight[c] = A.weight ? A.weight[b.c0 + c] : 1.f;
     bool first = true;
     #pragma unroll 1
     for (long long n = b.n0; n < samples; n += b.step) {
         const long long gb = n * sh.groups + b.g0;              // this block's first group
         const T* dp = dy + n * gdy.sn + V * cv;
+        for (int g = tid; g < w.groups; g += w.threads) m.rstd[g] = A.rstd[gb + g];
         Chan<V> k;
         if (has) load_chan<V>(k, sh, A.mean, A.rstd, A.weight, A.bias, n, V * cv);
         // d and dz from what has been read
@@ -915,22 +951,23 @@ __global__ void __launch_bounds__(kClThreads, 2) gn_cluster_backward_kernel(cons
         for (int i = 0; i < V; ++i) { m.part.at(0, i, tid) = S1[i]; m.part.at(1, i, tid) = S2[i]; }
         __syncthreads();
         if (w.k > 1 && !first) tc::cluster_wait();               // the others have read this CTA's sums of the sample before
-        for (int c = tid; c < w.Cs; c += w.threads) {
+        for (uint32_t c = tid; c < (uint32_t)w.Cs; c += w.threads) {
+            const float* p = m.part.p + (c % V) * m.part.pitch + c / V;
             float2 t = make_float2(0.f, 0.f);
             #pragma unroll 8
-            for (int r = 0; r < w.rows; ++r) { t.x += m.part.at(0, c % V, r * w.cols + c / V); t.y += m.part.at(1, c % V, r * w.cols + c / V); }
+            for (int r = 0; r < w.rows; ++r, p += w.cols) { t.x += p[0]; t.y += p[V * m.part.pitch]; }
             m.chan[c] = t.x;
-            m.chan[w.Cs + c] = t.y * A.rstd[gb + sh.group(c)];            // of xhat
+            m.chan[w.Cs + c] = t.y * m.rstd[sh.group(c)];                 // of xhat
         }
         __syncthreads();
         for (int g0 = warp * (32 / w.lanes); g0 < w.groups; g0 += warps * (32 / w.lanes)) {
             const int g = g0 + lane / w.lanes;
             float2 t = make_float2(0.f, 0.f);
             if (g < w.groups)
+                #pragma unroll 2
                 for (int c = g * sh.cg + lane % w.lanes; c < (g + 1) * sh.cg; c += w.lanes) {
-                    const float wt = A.weight ? A.weight[b.c0 + c] : 1.f;
-                    t.x = fmaf(wt, m.chan[c], t.x);
-                    t.y = fmaf(wt, m.chan[w.Cs + c], t.y);
+                    t.x = fmaf(m.weight[c], m.chan[c], t.x);
+                    t.y = fmaf(m.weight[c], m.chan[w.Cs + c], t.y);
                 }
             t.x = lanes_sum(t.x, w.lanes);
             t.y = lanes_sum(t.y, w.lanes);
@@ -954,7 +991,7 @@ __global__ void __launch_bounds__(kClThreads, 2) gn_cluster_backward_kernel(cons
             acc[own + i] += over_cluster(m.chan + w.Cs + b.rank + w.k * i);
         }
         __syncwarp();
-        if (w.k > 1) tc::cluster_arrive();
+        if (w.k > 1) tc::cluster_arrive_relaxed();
         first = false;
         __syncthreads();
         if (has) {
@@ -963,7 +1000,7 @@ __global__ void __launch_bounds__(kClThreads, 2) gn_cluster_backward_kernel(cons
             for (int i = 0; i < V; ++i) {
                 const int g = sh.group(V * v + i);
                 const float2 c = m.res[g];
-                const float r = A.rstd[gb + g];
+                const float r = m.rstd[g];
                 B[i] = -r * r * c.y;
                 D[i] = -r * c.x;
             }
@@ -971,7 +1008,8 @@ __global__ void __launch_bounds__(kClThreads, 2) gn_cluster_backward_kernel(cons
             const long long n1 = n + b.step;
             const T* dn = dp + b.step * gdy.sn;
             T* op = dx + n * gdx.sn + V * cv;
-            Cursor c(gdx, p0 + row), cdy(gdy, p0 + row), cx(gx, p0 + row);
+            Cursor c(gdx, p0 + row), cdy(gdy, p0 + row);
+            SourceCursor<T, V, SRC> cx(src, gx, w, n1, p0 + row, cv);
             uint8_t e_next = 0;                                 // the exponent of the next sample's copies, stored an iteration after it was asked for
             auto emit = [&](const R& r, const Fetch<T, V, SRC>& fx) {
                 float f[V], q[V];
@@ -979,7 +1017,7 @@ __global__ void __launch_bounds__(kClThreads, 2) gn_cluster_backward_kernel(cons
                 v_fma<V>(f, B, D, f);
                 v_fma<V>(q, k.a, f, q);
                 *(R*)(op + c.off) = pack<T, V>(q);
-                c.next(gdx, w.rows);
+                c.next(gdx);
             };
             #pragma unroll 1
             for (int bt = 0; bt < kClBatches; ++bt) {
@@ -990,16 +1028,14 @@ __global__ void __launch_bounds__(kClThreads, 2) gn_cluster_backward_kernel(cons
                     from_slot(it, r, fx);
                     if (SRC != kSrcSame && more) {
                         if (it > 0) eslots[(it - 1) * w.threads] = e_next;
-                        e_next = *scale_at(n1, it);
+                        e_next = *cx.scales;
                     }
                     emit(r, fx);
                     if (more) {
                         fill_slot(slots + it * w.threads, dn + cdy.off);
-                        cdy.next(gdy, w.rows);
-                        if constexpr (SRC == kSrcSame) {
-                            fill_slot(xslots + it * w.threads, xbase + n1 * gx.sn + cx.off);
-                            cx.next(gx, w.rows);
-                        } else fill_slot(xslots + it * w.threads, codes_at(n1, it));
+                        cdy.next(gdy);
+                        fill_slot(xslots + it * w.threads, cx.place());
+                        cx.next(gx, w);
                     }
                 }
                 copies_commit();

@@ -9,6 +9,7 @@
 #include <atomic>
 #include <cmath>
 #include <cstdio>
+#include <cstdlib>
 #include <utility>
 
 #include "checkpoint.cuh"
@@ -82,7 +83,7 @@ const char* check_view(const alexnet_view_t& v, const Dims& d, int dtype, bool o
     }
     return nullptr;
 }
-Geo geo_of(const alexnet_view_t& v, const Dims& d) {
+Geo geo_of(const alexnet_view_t& v, const Dims& d, int step) {
     Geo g{};
     g.sn = d.n > 1 ? v.stride_n : 0;
     g.sh = d.h > 1 ? v.stride_h : 0;
@@ -90,6 +91,9 @@ Geo geo_of(const alexnet_view_t& v, const Dims& d) {
     g.w = fast_div((uint32_t)d.w);
     g.flat = d.h == 1 || d.w == 1 || g.sh == (long long)d.w * g.sw;
     if (d.w == 1) g.sw = g.sh;
+    g.step = step;
+    g.inc = step * g.sw;
+    g.wrap = g.flat ? 0 : g.sh - d.w * g.sw;
     return g;
 }
 // vectors of eight channels at 16-byte boundaries everywhere
@@ -107,12 +111,14 @@ Walk walk_of(const Dims& d, int V) {
     w.colblocks = (int)ceil_div(padded, 256);
     w.cols = (int)ceil_div(ceil_div(padded, w.colblocks), q) * q;
     w.rows = 256 / w.cols;
-    long long chunks = ceil_div(8 * kSms, std::max<long long>(1, d.n * w.colblocks));
+    const char* ev = getenv("GN_BLK"); const int per = ev ? atoi(ev) : 8;
+    long long chunks = ceil_div(per * kSms, std::max<long long>(1, d.n * w.colblocks));
     chunks = std::min(chunks, ceil_div(w.HW, 4 * w.rows));
     chunks = std::max(chunks, ceil_div((long long)w.HW * ceil_div(d.C, 32), 1 << 30));      // indices of a chunk's blocks fit 31 bits
     chunks = std::max<long long>(1, std::min<long long>(chunks, w.HW));
     w.ppc = (int)ceil_div(w.HW, chunks);
     w.chunks = ceil_div(w.HW, w.ppc);
+    w.dense = dense_of(d.C, w.rows);
     return w;
 }
 long long grid_of(const Walk& w, const Dims& d) { return d.n * w.chunks * w.colblocks; }
@@ -120,19 +126,19 @@ constexpr long long kMaxGrid = 0x7fffffffll;
 
 template <typename T>
 void encode(Launcher& go, const Dims& d, const alexnet_view_t& x, const alexnet_checkpoint_t& k, int dtype) {
-    const Geo g = geo_of(x, d);
     const FastDiv blocks = fast_div((uint32_t)ceil_div(d.C, 32));
     const bool vec = vec_ok(x, d, dtype) && vec_ok(k, d);
     const Walk w = walk_of(d, vec ? 8 : 1);
+    const Geo g = geo_of(x, d, w.rows);
     if (vec) go(k.format == ALEXNET_CODES_INT8 ? checkpoint_encode_kernel<T, kSrcInt8> : checkpoint_encode_kernel<T, kSrcE4m3>, grid_of(w, d), 256, (const T*)x.data, g, w, (uint8_t*)k.codes, k.scales);
     else go(checkpoint_encode_any_kernel<T>, d.n * w.chunks, 256, (const T*)x.data, g, w, blocks, src_of(k.format), (uint8_t*)k.codes, k.scales);
 }
 template <typename T>
 void decode(Launcher& go, const Dims& d, const alexnet_view_t& x, const alexnet_checkpoint_t& k, int dtype) {
-    const Geo g = geo_of(x, d);
     const FastDiv blocks = fast_div((uint32_t)ceil_div(d.C, 32));
     const bool vec = vec_ok(x, d, dtype) && vec_ok(k, d);
     const Walk w = walk_of(d, vec ? 8 : 1);
+    const Geo g = geo_of(x, d, w.rows);
     if (vec) go(k.format == ALEXNET_CODES_INT8 ? checkpoint_decode_kernel<T, kSrcInt8> : checkpoint_decode_kernel<T, kSrcE4m3>, grid_of(w, d), 256, (const uint8_t*)k.codes, (const uint8_t*)k.scales, g, w,
                 (T*)x.data);
     else go(checkpoint_decode_any_kernel<T>, d.n * w.chunks, 256, (const uint8_t*)k.codes, (const uint8_t*)k.scales, src_of(k.format), g, w, blocks, (T*)x.data);
@@ -177,10 +183,10 @@ size_t forward_ws(const Walk& w, const Dims& d) { return (size_t)(d.n * w.chunks
 size_t backward_ws(const Walk& w, const Dims& d, int groups) { return (size_t)(d.n * groups) * sizeof(float2) + (size_t)(d.n * w.chunks) * 2 * d.C * sizeof(float); }
 
 constexpr size_t kSmSmem = 228 * 1024, kCtaSmem = 227 * 1024;
-// How clusters walk a tensor, `slot` bytes kept per vector of V channels, `moved` bytes per vector to and from memory and K sums per thread and
-// vector element; k = 0: not at all (rows wider than a block, or too few samples to fill the device with their clusters).  By a model in
-// cycles: an SM moves 22 bytes per cycle when it has 15 warps of three CTAs (in different phases), a round of CTAs costs 4500 or 6000
-// more for its first loads and the sums' way around, and vectors that do not stay on chip are read again at 40 bytes.
+// How clusters walk a tensor, `slot` bytes kept per vector of V channels, `moved` bytes per vector to and from memory and K sums per group; k = 0: not at
+// all (rows wider than a block, or too few samples to fill the device with their clusters).  By a model in cycles: an SM moves 22 bytes per
+// cycle when it has 14 warps of three CTAs (in different phases), a sample costs 3500 or (in a cluster) 5000 more for the sums' way around, and
+// vectors that do not stay on chip are read again at 40 bytes and 600 cycles each.
 template <int V>
 ClusterWalk cluster_walk(const Dims& d, int groups, int slot, int moved, int K) {
     ClusterWalk best{};
@@ -207,19 +213,23 @@ ClusterWalk cluster_walk(const Dims& d, int groups, int slot, int moved, int K) 
                     const size_t room = std::min(kCtaSmem, kSmSmem / occ - 1024);
                     if (room < scratch) break;
                     w.keep = (int)std::min<size_t>(w.its, (room - scratch) / per_it);
-                    const double busy = std::min(1.0, occ * w.threads / 480.0) * (occ == 1 ? 0.55 : occ == 2 ? 0.8 : 1.0);
-                    const double work = ((double)w.its * w.threads * moved / 22 + (double)(w.its - w.keep) * w.threads * moved / 40) / busy;
-                    const double per_sm = (double)ceil_div(d.n * w.slices * w.k, kSms), c = per_sm * work + (w.k > 1 ? 6000 : 4500) * std::ceil(per_sm / occ);
+                    const double busy = std::min(1.0, occ * w.threads / 448.0) * (occ == 1 ? 0.7 : occ == 2 ? 0.9 : 1.0);
+                    const double work = occ * ((double)w.its * w.threads * moved / 22 + (double)(w.its - w.keep) * w.threads * moved / 40) / busy + (w.its - w.keep) * 600.0;
+                    const double at_once = std::max(1.0, std::floor((double)kSms * occ / w.k * (w.k >= 4 ? 15 : 16) / 16));
+                    const double c = std::ceil((double)d.n * w.slices / at_once) * (work + (w.k > 1 ? 5000 : 3500)) + 6000;
                     if (c < cost) { cost = c; best = w; }
                 }
             }
         }
     }
+    if (getenv("GN_GENERAL")) best.k = 0;
     if (!best.k) return best;
     // a sample's blocks are few SMs: a few large samples go faster through the kernels that spread over all of them
     if ((double)d.n * best.slices * best.k < kSms / 2 && (double)best.its * best.threads * moved > 2.0e5) best.k = 0;
+    best.dense = dense_of(d.C, best.rows);
     best.lanes = 1;
     while (best.lanes < 32 && best.lanes * 2 * best.groups <= best.threads && best.lanes < cg * best.rows) best.lanes *= 2;
+    for (best.lc = 1; best.lc < best.lanes && best.lc < cg; best.lc *= 2) ++best.lc_shift;
     return best;
 }
 template <typename K>
@@ -264,15 +274,15 @@ void forward(Launcher& go, const alexnet_group_norm_forward_t* a, const Dims& d)
         const long long rows = cluster_rows(go, gn_cluster_forward_kernel<T, V, ACT>, cw, d, smem);
         go.smem = smem;
         go.cluster = cw.k;
-        go(gn_cluster_forward_kernel<T, V, ACT>, rows * cw.slices * cw.k, cw.threads, (const T*)a->x.data, geo_of(a->x, d), cw, s, (long long)d.n, a->weight, a->bias, (T*)a->y.data,
-           geo_of(a->y, d), a->mean, a->rstd, kx, ky);
+        go(gn_cluster_forward_kernel<T, V, ACT>, rows * cw.slices * cw.k, cw.threads, (const T*)a->x.data, geo_of(a->x, d, cw.rows), cw, s, (long long)d.n, a->weight, a->bias, (T*)a->y.data,
+           geo_of(a->y, d, cw.rows), a->mean, a->rstd, kx, ky);
         if (V != 8) {
             if (a->keep_x.codes) encode<T>(go, d, a->x, a->keep_x, a->shape.dtype);
             if (a->keep_y.codes) encode<T>(go, d, a->y, a->keep_y, a->shape.dtype);
         }
         return;
     }
-    const Geo gx = geo_of(a->x, d), gy = geo_of(a->y, d);
+    const Geo gx = geo_of(a->x, d, w.rows), gy = geo_of(a->y, d, w.rows);
     float4* partial = (float4*)a->workspace;
     const T *x = (const T*)a->x.data;
     Keep kx{}, ky{};
@@ -281,7 +291,9 @@ void forward(Launcher& go, const alexnet_group_norm_forward_t* a, const Dims& d)
         if (a->keep_y.codes) ky = {(uint8_t*)a->keep_y.codes, a->keep_y.scales, src_of(a->keep_y.format)};
     }
     go(gn_sums_kernel<T, V>, grid_of(w, d), 256, x, gx, w, partial);
-    go(gn_statistics_kernel, d.n * s.groups, 256, (const float4*)partial, s, (int)w.chunks, w.ppc, a->mean, a->rstd);
+    const long long groups = d.n * s.groups;
+    const bool block = groups < 8 * kSms;
+    go(block ? gn_statistics_kernel<true> : gn_statistics_kernel<false>, block ? groups : ceil_div(groups, 8), 256, (const float4*)partial, s, groups, (int)w.chunks, w.ppc, a->mean, a->rstd);
     go(gn_apply_kernel<T, V, ACT>, grid_of(w, d), 256, x, gx, w, s, a->weight, a->bias, (const float*)a->mean, (const float*)a->rstd, (T*)a->y.data, gy, kx, ky);
     if (V != 8) {
         if (a->keep_x.codes) encode<T>(go, d, a->x, a->keep_x, a->shape.dtype);
@@ -292,7 +304,6 @@ template <typename T, int V, int SRC, int ACT>
 void backward(Launcher& go, const alexnet_group_norm_backward_t* a, const Dims& d) {
     const Walk w = walk_of(d, V);
     const NormShape s = norm_shape(a->shape);
-    const Geo gdy = geo_of(a->dy, d), gx = geo_of(a->x, d), gdx = geo_of(a->dx, d);
     float2* c12 = (float2*)a->workspace;
     float* partial = (float*)(c12 + d.n * s.groups);
     const Source src{a->x.data, (const uint8_t*)a->kept.codes, a->kept.scales};
@@ -308,12 +319,16 @@ void backward(Launcher& go, const alexnet_group_norm_backward_t* a, const Dims& 
         const long long rows = cluster_rows(go, kernel, cw, d, smem);
         go.smem = smem;
         go.cluster = cw.k;
-        go(kernel, rows * cw.slices * cw.k, cw.threads, dy, gdy, src, gx, cw, s, (long long)d.n, A, (T*)a->dx.data, gdx, partial);
+        go(kernel, rows * cw.slices * cw.k, cw.threads, dy, geo_of(a->dy, d, cw.rows), src, geo_of(a->x, d, cw.rows), cw, s, (long long)d.n, A, (T*)a->dx.data,
+           geo_of(a->dx, d, cw.rows), partial);
         if (a->dweight || a->dbias) go(gn_parameter_gradient_kernel, ceil_div(d.C, 32), 1024, (const float*)partial, d.C, rows, a->dweight, a->dbias);
         return;
     }
+    const Geo gdy = geo_of(a->dy, d, w.rows), gx = geo_of(a->x, d, w.rows), gdx = geo_of(a->dx, d, w.rows);
     go(gn_backward_sums_kernel<T, V, SRC, ACT>, grid_of(w, d), 256, dy, gdy, src, gx, w, s, A, partial);
-    go(gn_backward_group_kernel, d.n * s.groups, 256, (const float*)partial, s, (int)w.chunks, A, c12);
+    const long long groups = d.n * s.groups;
+    const bool block = groups < 8 * kSms;
+    go(block ? gn_backward_group_kernel<true> : gn_backward_group_kernel<false>, block ? groups : ceil_div(groups, 8), 256, (const float*)partial, s, groups, (int)w.chunks, A, c12);
     if (a->dweight || a->dbias) go(gn_parameter_gradient_kernel, ceil_div(d.C, 32), 1024, (const float*)partial, d.C, d.n * w.chunks, a->dweight, a->dbias);
     go(gn_backward_apply_kernel<T, V, SRC, ACT>, grid_of(w, d), 256, dy, gdy, src, gx, w, s, A, (const float2*)c12, (T*)a->dx.data, gdx);
 }
