@@ -263,9 +263,9 @@ struct Walk {
     Dense dense;                // codes of positions `rows` apart
 };
 struct Spot { int col, row, v, p0, p1; long long n, chunk; bool on, has; };
-__device__ __forceinline__ Spot spot(const Walk& w) {
+__device__ __forceinline__ Spot spot(const Walk& w, int skip = 0) {
     Spot s;
-    const long long b = blockIdx.x;
+    const long long b = blockIdx.x - skip;
     const long long t = b / w.colblocks;
     const int cb = (int)(b - t * w.colblocks);
     s.n = t / w.chunks;

@@ -268,52 +268,50 @@ __device__ __forceinline__ void keep_codes(const Keep& k, const Raw<T, 8>& r, co
     if (k.fmt == kSrcInt8) store_codes<T, kSrcInt8>(r, f, has, c.codes, c.scales);
     else store_codes<T, kSrcE4m3>(r, f, has, c.codes, c.scales);
 }
-// A thread's positions from p on, `rows` apart, `cnt` of them: results (and checkpoints) of the vectors that fetch(it) gives.
-template <typename T, int V, int ACT, typename F>
-__device__ __forceinline__ void apply_positions(const Chan<V>& k, const NormShape& sh, int p, int rows, int it0, int cnt, long long row0, int v, bool has, T* y, const Geo& gy, const Dense& dense, const Keep& kx,
-                                                const Keep& ky, F fetch) {
-    Cursor c(gy, p + it0 * rows);
-    CodesCursor cx(kx.codes, kx.scales, row0 + p + it0 * rows, v, dense), cy(ky.codes, ky.scales, row0 + p + it0 * rows, v, dense);
-    #pragma unroll 2
-    for (int it = it0; it < cnt; ++it) {
-        const Raw<T, V> r = fetch(it);
-        float f[V], z[V];
-        unpack<T, V>(r, f);
-        if constexpr (V == 8)
-            if (kx.codes) { keep_codes<T>(kx, r, f, has, cx); cx.next(dense); }
-        v_add<V>(f, k.nm, f);
-        v_fma<V>(f, k.a, k.b, z);
-        activate<T, V, ACT>(sh.act, z);
-        Raw<T, V> out = pack<T, V>(z);
-        if (has) *(Raw<T, V>*)(y + c.off) = out;
-        c.next(gy);
-        if constexpr (V == 8)
-            if (ky.codes) {                     // of y as it is stored
-                if (!has) out = Raw<T, 8>{};
-                unpack<T, 8>(out, f);
-                keep_codes<T>(ky, out, f, has, cy);
-                cy.next(dense);
-            }
-    }
-}
-template <typename T, int V, int ACT>
-__global__ void __launch_bounds__(256) gn_apply_kernel(const T* __restrict__ x, const Geo gx, const Walk w, const NormShape sh, const float* __restrict__ weight,
-                                                       const float* __restrict__ bias, const float* __restrict__ mean, const float* __restrict__ rstd,
-                                                       T* __restrict__ y, const Geo gy, const Keep kx, const Keep ky) {
+template <typename T, int V, int ACT, bool KEEP>
+__global__ void __launch_bounds__(256, V == 8 && !KEEP ? 4 : 3) gn_apply_kernel(const T* __restrict__ x, const Geo gx, const Walk w, const NormShape sh, const float* __restrict__ weight,
+                                                                              const float* __restrict__ bias, const float* __restrict__ mean, const float* __restrict__ rstd,
+                                                                              T* __restrict__ y, const Geo gy, const Keep kx, const Keep ky) {
     kn::pdl_sync();
     const Spot s = spot(w);
-    const int p = s.p0 + s.row;
-    if (!s.on || p >= s.p1) return;
+    const int p0 = s.p0 + s.row;
+    if (!s.on || p0 >= s.p1) return;
     Chan<V> k = {};
     if (s.has) load_chan<V>(k, sh, mean, rstd, weight, bias, s.n, V * s.v);
     const T* xp = x + s.n * gx.sn + V * s.v;
-    Cursor c(gx, p);
-    apply_positions<T, V, ACT>(k, sh, p, w.rows, 0, (s.p1 - p + w.rows - 1) / w.rows, s.n * w.HW, s.v, s.has, y + s.n * gy.sn + V * s.v, gy, w.dense, kx, ky, [&](int) {
-        Raw<T, V> r = {};
-        if (s.has) r = *(const Raw<T, V>*)(xp + c.off);
-        c.next(gx);
-        return r;
-    });
+    T* yp = y + s.n * gy.sn + V * s.v;
+    Cursor cx(gx, p0), cy(gy, p0);
+    CodesCursor ckx(kx.codes, kx.scales, s.n * w.HW + p0, s.v, w.dense), cky(ky.codes, ky.scales, s.n * w.HW + p0, s.v, w.dense);
+    constexpr int U = 4;                       // vectors in flight: bound by their number (two: 155 us for 512 x 55 x 55 x 96, 3.8 TB/s)
+    for (int p = p0; p < s.p1; p += U * w.rows) {
+        Raw<T, V> r[U] = {};
+        #pragma unroll
+        for (int u = 0; u < U; ++u) {
+            if (s.has && p + u * w.rows < s.p1) r[u] = *(const Raw<T, V>*)(xp + cx.off);
+            cx.next(gx);
+        }
+        #pragma unroll
+        for (int u = 0; u < U; ++u) {
+            if (p + u * w.rows >= s.p1) break;
+            float f[V], z[V];
+            unpack<T, V>(r[u], f);
+            if constexpr (V == 8 && KEEP)
+                if (kx.codes) { keep_codes<T>(kx, r[u], f, s.has, ckx); ckx.next(w.dense); }
+            v_add<V>(f, k.nm, f);
+            v_fma<V>(f, k.a, k.b, z);
+            activate<T, V, ACT>(sh.act, z);
+            Raw<T, V> out = pack<T, V>(z);
+            if (s.has) *(Raw<T, V>*)(yp + cy.off) = out;
+            cy.next(gy);
+            if constexpr (V == 8 && KEEP)
+                if (ky.codes) {                     // of y as it is stored
+                    if (!s.has) out = Raw<T, V>{};
+                    unpack<T, 8>(out, f);
+                    keep_codes<T>(ky, out, f, s.has, cky);
+                    cky.next(w.dense);
+                }
+        }
+    }
 }
 
 // ---------------------------------------------------------------- backward
@@ -406,7 +404,7 @@ __device__ __forceinline__ void activation_gradient(const NormShape& sh, const C
     }
 }
 template <typename T, int V, int SRC, int ACT>
-__global__ void __launch_bounds__(256) gn_backward_sums_kernel(const T* __restrict__ dy, const Geo gdy, const Source src, const Geo gx, const Walk w, const NormShape sh,
+__global__ void __launch_bounds__(256, 3) gn_backward_sums_kernel(const T* __restrict__ dy, const Geo gdy, const Source src, const Geo gx, const Walk w, const NormShape sh,
                                                                const BackwardArgs A, float* __restrict__ partial) {
     kn::pdl_sync();
     __shared__ float sums[2 * V * 260];
@@ -483,31 +481,39 @@ __global__ void __launch_bounds__(256) gn_backward_group_kernel(const float* __r
     const float m = (float)sh.HW * (float)sh.cg;
     if (me == 0) c12[id] = make_float2(__fdiv_rn(t.x, m), __fdiv_rn(t.y, m));
 }
-// dweight and dbias: the sums [n][2][C] of the samples (or of their chunks).  A block takes 32 channels, its warps every 32nd row.
-__global__ void __launch_bounds__(1024) gn_parameter_gradient_kernel(const float* __restrict__ partial, int C, long long n, float* __restrict__ dweight, float* __restrict__ dbias) {
-    kn::pdl_sync();
-    __shared__ float2 red[32][33];
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, c = blockIdx.x * 32 + lane;
+// dweight and dbias: the sums [n][2][C] of the samples (or of their chunks).  A block takes 32 channels, its warps every WARPS-th row.
+template <int WARPS>
+__device__ __forceinline__ void parameter_gradient(const float* __restrict__ partial, int C, long long n, int block, float2* red /* [WARPS][33] */, float* __restrict__ dweight, float* __restrict__ dbias) {
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, c = block * 32 + lane;
     float2 t = make_float2(0.f, 0.f);
     if (c < C) {
         const float* p = partial + c;
         #pragma unroll 8
-        for (long long i = warp; i < n; i += 32) { t.x += p[i * 2 * C]; t.y += p[i * 2 * C + C]; }
+        for (long long i = warp; i < n; i += WARPS) { t.x += p[i * 2 * C]; t.y += p[i * 2 * C + C]; }
     }
-    red[warp][lane] = t;
+    red[warp * 33 + lane] = t;
     __syncthreads();
-    t = warp_sum(red[lane][warp]);               // lane: part, warp: channel
-    const int cw = blockIdx.x * 32 + warp;
-    if (lane == 0 && cw < C) {
-        if (dbias) dbias[cw] = t.x;
-        if (dweight) dweight[cw] = t.y;
+    if (warp == 0 && c < C) {
+        #pragma unroll 8
+        for (int k = 1; k < WARPS; ++k) { t.x += red[k * 33 + lane].x; t.y += red[k * 33 + lane].y; }
+        if (dbias) dbias[c] = t.x;
+        if (dweight) dweight[c] = t.y;
     }
 }
-template <typename T, int V, int SRC, int ACT>
-__global__ void __launch_bounds__(256) gn_backward_apply_kernel(const T* __restrict__ dy, const Geo gdy, const Source src, const Geo gx, const Walk w, const NormShape sh,
-                                                                const BackwardArgs A, const float2* __restrict__ c12, T* __restrict__ dx, const Geo gdx) {
+__global__ void __launch_bounds__(1024) gn_parameter_gradient_kernel(const float* __restrict__ partial, int C, long long n, float* __restrict__ dweight, float* __restrict__ dbias) {
     kn::pdl_sync();
-    const Spot s = spot(w);
+    __shared__ float2 red[32 * 33];
+    parameter_gradient<32>(partial, C, n, blockIdx.x, red, dweight, dbias);
+}
+template <typename T, int V, int SRC, int ACT>
+__global__ void __launch_bounds__(256, 3) gn_backward_apply_kernel(const T* __restrict__ dy, const Geo gdy, const Source src, const Geo gx, const Walk w, const NormShape sh,
+                                                                const BackwardArgs A, const float2* __restrict__ c12, T* __restrict__ dx, const Geo gdx, const float* __restrict__ partial,
+                                                                long long partials, int extra, float* __restrict__ dweight, float* __restrict__ dbias) {
+    kn::pdl_sync();
+    // the first `extra` blocks add up the parameters' gradients beside the others' work (a launch of their own took 8 us)
+    __shared__ float2 red[8 * 33];
+    if (blockIdx.x < extra) { parameter_gradient<8>(partial, w.C, partials, blockIdx.x, red, dweight, dbias); return; }
+    const Spot s = spot(w, extra);
     if (!s.has) return;
     Chan<V> k;
     load_chan<V>(k, sh, A.mean, A.rstd, A.weight, A.bias, s.n, V * s.v);

@@ -294,7 +294,8 @@ void forward(Launcher& go, const alexnet_group_norm_forward_t* a, const Dims& d)
     const long long groups = d.n * s.groups;
     const bool block = groups < 8 * kSms;
     go(block ? gn_statistics_kernel<true> : gn_statistics_kernel<false>, block ? groups : ceil_div(groups, 8), 256, (const float4*)partial, s, groups, (int)w.chunks, w.ppc, a->mean, a->rstd);
-    go(gn_apply_kernel<T, V, ACT>, grid_of(w, d), 256, x, gx, w, s, a->weight, a->bias, (const float*)a->mean, (const float*)a->rstd, (T*)a->y.data, gy, kx, ky);
+    const bool keep = kx.codes || ky.codes;
+    go(keep ? gn_apply_kernel<T, V, ACT, V == 8> : gn_apply_kernel<T, V, ACT, false>, grid_of(w, d), 256, x, gx, w, s, a->weight, a->bias, (const float*)a->mean, (const float*)a->rstd, (T*)a->y.data, gy, kx, ky);
     if (V != 8) {
         if (a->keep_x.codes) encode<T>(go, d, a->x, a->keep_x, a->shape.dtype);
         if (a->keep_y.codes) encode<T>(go, d, a->y, a->keep_y, a->shape.dtype);
@@ -329,8 +330,9 @@ void backward(Launcher& go, const alexnet_group_norm_backward_t* a, const Dims& 
     const long long groups = d.n * s.groups;
     const bool block = groups < 8 * kSms;
     go(block ? gn_backward_group_kernel<true> : gn_backward_group_kernel<false>, block ? groups : ceil_div(groups, 8), 256, (const float*)partial, s, groups, (int)w.chunks, A, c12);
-    if (a->dweight || a->dbias) go(gn_parameter_gradient_kernel, ceil_div(d.C, 32), 1024, (const float*)partial, d.C, d.n * w.chunks, a->dweight, a->dbias);
-    go(gn_backward_apply_kernel<T, V, SRC, ACT>, grid_of(w, d), 256, dy, gdy, src, gx, w, s, A, (const float2*)c12, (T*)a->dx.data, gdx);
+    const int extra = a->dweight || a->dbias ? (int)ceil_div(d.C, 32) : 0;
+    go(gn_backward_apply_kernel<T, V, SRC, ACT>, grid_of(w, d) + extra, 256, dy, gdy, src, gx, w, s, A, (const float2*)c12, (T*)a->dx.data, gdx, (const float*)partial, d.n * w.chunks, extra, a->dweight,
+       a->dbias);
 }
 template <typename T, int V, int SRC>
 void backward(Launcher& go, const alexnet_group_norm_backward_t* a, const Dims& d) {
