@@ -127,18 +127,10 @@ template <int UNROLL, typename G, typename N> __device__ __forceinline__ Part jo
     const float lo = e * inv;
     return {hi, lo, fmaf(-e, lo, q)};
 }
-// The same by `lanes` neighbouring lanes (a power of two; all 32 of the warp call it); the result is the same in all of them.
+// the sum over `lanes` neighbouring lanes (a power of two; all 32 of the warp call it)
 __device__ __forceinline__ float lanes_sum(float t, int lanes) {
     for (int o = lanes >> 1; o; o >>= 1) t += __shfl_xor_sync(~0u, t, o);
     return t;
-}
-// a part of n values per lane
-__device__ __forceinline__ Part join_lanes(const Part& t, float n, int lanes, float inv) {
-    const float ref = __shfl_sync(~0u, t.hi, threadIdx.x & 31 & ~(lanes - 1));
-    const float hi = fmaf(lanes_sum(n > 0.f ? n * (t.hi - ref) : 0.f, lanes), inv, ref);
-    const float d = (t.hi - hi) + t.lo, w = n > 0.f ? n * d : 0.f;
-    const float e = lanes_sum(w, lanes), q = lanes_sum(fmaf(w, d, t.m2), lanes), lo = e * inv;
-    return {hi, lo, fmaf(-e, lo, q)};
 }
 // Per-thread sums of a block in shared memory, by vector element and thread: pitch = threads + 4, so that neighbouring threads' stores and the
 // reads of neighbouring channels (elements of neighbouring threads) each fall into different banks.
@@ -163,7 +155,8 @@ template <int V> __device__ __forceinline__ Part join_rows(const Table<V>& s, in
     return join<4>(rows, inv, [&](int r) { return Part{s.at(0, i, r * cols + t), s.at(1, i, r * cols + t), s.at(2, i, r * cols + t)}; }, [&](int r) { return r < more ? n_lo + 1.f : n_lo; });
 }
 __device__ __forceinline__ float2 statistics(const Part& t, const NormShape& s) {
-    return make_float2(t.hi + t.lo, __frsqrt_rn(__fdiv_rn(t.m2, (float)s.HW * (float)s.cg) + s.eps));
+    const float var = __fdiv_rn(t.m2, (float)s.HW * (float)s.cg);
+    return make_float2(t.hi + t.lo, __frsqrt_rn((var < 0.f ? 0.f : var) + s.eps));      // (keeps NaN)
 }
 
 template <typename T, int V>
@@ -172,7 +165,7 @@ __global__ void __launch_bounds__(256) gn_sums_kernel(const T* __restrict__ x, c
     __shared__ float sums[3 * V * 260];
     const Table<V> table{sums, 260};
     const Spot s = spot(w);
-    constexpr int U = V == 8 ? 4 : 8;
+    constexpr int U = 8;
     float nK[V], S[V], Q[V];
     #pragma unroll
     for (int i = 0; i < V; ++i) nK[i] = S[i] = Q[i] = 0.f;
@@ -359,40 +352,44 @@ template <typename T, int V, int SRC> struct SourceCursor {
         else { codes += w.dense.inc_codes; scales += w.dense.inc_scales; }
     }
 };
-// The side of ReLU's kink that a value is on, where fp32 cannot tell: d and a carry a rounding each, so z = d a + b is off by up to 2^-23 |b| or so when it
-// is near zero.  Such values (a few in a million) are taken again with the roundings of x + nm, rstd w, d a and the last sum carried along (Knuth's
-// and the fused multiply-add's exact errors): off by 2^-45 of b.
-__device__ __forceinline__ float relu_side(float x, float nm, float b, float rstd, float w) {
-    const float d = x + nm, u = d - x, de = (x - (d - u)) + (nm - u);
-    const float a = rstd * w, ae = fmaf(rstd, w, -a);
-    const float p = d * a, pe = fmaf(d, a, -p);
-    const float s = p + b, t = s - p, se = (p - (s - t)) + (b - t);
-    return s + (se + (pe + fmaf(d, ae, de * a)));
-}
 struct BackwardArgs {
     const float *mean, *rstd, *weight, *bias;
 };
+// A thread's channels in a backward pass: nm, a and b, where ReLU has in the place of b a number to compare with.  z > 0 holds for x > theta (w > 0) or x < theta
+// (w < 0) with theta = mean - b / (rstd w): theta in fp64, rounded to fp32 downwards (upwards), decides for every fp32 x as the real one does, where
+// z in fp32 is off by 2^-23 |b| about zero.  b holds -theta; the sign of (x - theta) a is z's.  (No weight: z is b, for all x.)
+template <int V, int ACT>
+__device__ __forceinline__ void load_backward_chan(Chan<V>& k, const NormShape& sh, const BackwardArgs& A, long long n, int c0) {
+    load_chan<V>(k, sh, A.mean, A.rstd, A.weight, A.bias, n, c0);
+    if (ACT == kActRelu || (ACT == kActAny && sh.act == kActRelu)) {
+        #pragma unroll
+        for (int i = 0; i < V; ++i) {
+            const double a = (double)A.rstd[n * sh.groups + sh.group(c0 + i)] * (A.weight ? (double)A.weight[c0 + i] : 1.);
+            const double theta = -(double)k.nm[i] - (double)k.b[i] / a;
+            k.b[i] = a == 0. ? 0.f : -(a > 0. ? __double2float_rd(theta) : __double2float_ru(theta));
+        }
+    }
+}
 // d = x - mean, and dz in the place of dy
 template <typename T, int V, int SRC, int ACT>
-__device__ __forceinline__ void activation_gradient(const NormShape& sh, const Chan<V>& k, const BackwardArgs& A, long long n, int c0, const Fetch<T, V, SRC>& fx, float* d, float* dy) {
+__device__ __forceinline__ void activation_gradient(int act, const Chan<V>& k, const Fetch<T, V, SRC>& fx, float* d, float* dy) {
     float x[V];
     fx.value(k.nm, x, d);
-    const int act = ACT == kActAny ? sh.act : ACT;
+    if (ACT != kActAny) act = ACT;
     if (act == kActNone) return;
     float z[V];
-    v_fma<V>(d, k.a, k.b, z);
     if (act == kActRelu) {
-        bool near = false;
-        #pragma unroll
-        for (int i = 0; i < V; ++i) near = near || fabsf(z[i]) < fabsf(1e-6f * k.b[i]);
-        if (near) {
+        const float sc = fx.scale();
+        if constexpr (SRC != kSrcSame) {
             #pragma unroll
-            for (int i = 0; i < V; ++i)
-                if (fabsf(z[i]) < fabsf(1e-6f * k.b[i])) z[i] = relu_side(x[i] * fx.scale(), k.nm[i], k.b[i], A.rstd[n * sh.groups + sh.group(c0 + i)], A.weight ? A.weight[c0 + i] : 1.f);
+            for (int i = 0; i < V; ++i) x[i] *= sc;
         }
+        v_add<V>(x, k.b, z);
+        v_mul<V>(z, k.a, z);
         #pragma unroll
-        for (int i = 0; i < V; ++i) dy[i] = z[i] <= 0.f ? 0.f : dy[i];
+        for (int i = 0; i < V; ++i) dy[i] = z[i] > 0.f ? dy[i] : 0.f;
     } else {
+        v_fma<V>(d, k.a, k.b, z);
         float s[V], u[V], one[V], minus[V];
         #pragma unroll
         for (int i = 0; i < V; ++i) { one[i] = 1.f; minus[i] = -1.f; }
@@ -416,7 +413,7 @@ __global__ void __launch_bounds__(256, 3) gn_backward_sums_kernel(const T* __res
     for (int i = 0; i < V; ++i) S1[i] = S2[i] = 0.f;
     if (s.has) {
         Chan<V> k;
-        load_chan<V>(k, sh, A.mean, A.rstd, A.weight, A.bias, s.n, V * s.v);
+        load_backward_chan<V, ACT>(k, sh, A, s.n, V * s.v);
         const T* dp = dy + s.n * gdy.sn + V * s.v;
         Cursor c(gdy, s.p0 + s.row);
         SourceCursor<T, V, SRC> cx(src, gx, w, s.n, s.p0 + s.row, s.v);
@@ -437,7 +434,7 @@ __global__ void __launch_bounds__(256, 3) gn_backward_sums_kernel(const T* __res
                 if (p + u * w.rows < s.p1) {
                     float f[V], q[V];
                     unpack<T, V>(r[u], q);
-                    activation_gradient<T, V, SRC, ACT>(sh, k, A, s.n, V * s.v, fx[u], f, q);
+                    activation_gradient<T, V, SRC, ACT>(sh.act, k, fx[u], f, q);
                     v_add<V>(S1, q, S1);
                     v_fma<V>(f, q, S2, S2);
                 }
@@ -516,7 +513,7 @@ __global__ void __launch_bounds__(256, 3) gn_backward_apply_kernel(const T* __re
     const Spot s = spot(w, extra);
     if (!s.has) return;
     Chan<V> k;
-    load_chan<V>(k, sh, A.mean, A.rstd, A.weight, A.bias, s.n, V * s.v);
+    load_backward_chan<V, ACT>(k, sh, A, s.n, V * s.v);
     float B[V], D[V];
     #pragma unroll
     for (int i = 0; i < V; ++i) {
@@ -548,7 +545,7 @@ __global__ void __launch_bounds__(256, 3) gn_backward_apply_kernel(const T* __re
             if (p + u * w.rows < s.p1) {
                 float f[V], q[V];
                 unpack<T, V>(r[u], q);
-                activation_gradient<T, V, SRC, ACT>(sh, k, A, s.n, V * s.v, fx[u], f, q);
+                activation_gradient<T, V, SRC, ACT>(sh.act, k, fx[u], f, q);
                 v_fma<V>(f, B, D, f);
                 v_fma<V>(q, k.a, f, q);
                 *(Raw<T, V>*)(op + co.off) = pack<T, V>(q);
@@ -558,22 +555,26 @@ __global__ void __launch_bounds__(256, 3) gn_backward_apply_kernel(const T* __re
 }
 
 
-// ---------------------------------------------------------------- one launch per direction: a sample per cluster
+// ---------------------------------------------------------------- one launch per direction: whole groups of a sample per block
 //
-// The CTAs of a cluster share the positions of one sample.  A thread keeps the vectors it has read (raw, in its own slots of shared memory, filled by
-// asynchronous copies) while the sums go around the cluster through distributed shared memory, then turns them into the result:
-// every value is read from memory once.  Slots are private to a thread, so no barrier stands between its copies and its reads.
-// Iterations beyond `keep` (samples too large for the cluster's shared memory) are read again, from L2.
-// A block may also take a slice of the channels, of whole groups (and whole checkpoint blocks): slices have nothing to do with one another.
-struct ClusterWalk {
+// A block takes a slice of the channels (of whole groups, and of whole checkpoint blocks) of a sample and keeps it: a thread's vectors stay raw in its own slots
+// of shared memory, filled by asynchronous copies, while the block forms its groups' sums, and are then turned into the result, so every value is
+// read from memory once.  Slots are private to a thread: no barrier stands between its copies and its reads.  Blocks are persistent: while a
+// sample's results are formed, the vectors of the block's next sample are copied into the slots that have been read, so memory is read and
+// written at the same time and does not wait for the sums.
+//
+// Slices that do not fit take the launches above, which read x twice.  (Spread over a cluster of up to eight blocks, with the sums going around it
+// through distributed shared memory, they took longer than that: 128 x 55 x 55 x 96 forward 68 us against 57, backward from a checkpoint 149
+// against 112.  The fixed work per sample, some 2000 instructions of each warp, was then paid for 20 vectors per thread.)
+struct SliceWalk {
     int C, HW;                                // of the tensor
     int slices, Cs, groups;                   // channel slices; channels and groups of one
     int vecs, cols, rows, threads;            // vectors of a slice's row; rows = threads / cols
-    Dense dense;                              // codes of positions `rows` apart
-    int k, ppc, its, keep;                    // CTAs of the cluster; positions of a CTA, at most; iterations of a thread, and those whose vectors stay
+    int its;                                  // positions of a thread, at most
     int lanes, lc, lc_shift;                  // lanes that join a group's sums, lc = 2^lc_shift of them over its channels (powers of two)
+    Dense dense;                              // codes of positions `rows` apart
 };
-constexpr int kClThreads = 256;               // at most; two CTAs per SM with 128 registers
+constexpr int kSlThreads = 256;               // at most; two blocks per SM with 128 registers
 
 template <int BYTES> __device__ __forceinline__ void copy_async(uint32_t dst, const void* src) {
     if constexpr (BYTES == 32) { copy_async<16>(dst, src); copy_async<16>(dst + 16, (const uint8_t*)src + 16); }
@@ -593,50 +594,41 @@ __device__ __forceinline__ void copies_wait(int pending) {
     else if (pending == 2) asm volatile("cp.async.wait_group 2;" ::: "memory");
     else asm volatile("cp.async.wait_group 3;" ::: "memory");
 }
-constexpr int kClBatches = 4;                 // groups of copies
+constexpr int kSlBatches = 4;                 // groups of copies
 
-__device__ __forceinline__ float ld_cluster(const float* p, uint32_t rank) {
-    float v;
-    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(tc::mapa_u32(tc::smem_u32(p), rank)) : "memory");
-    return v;
-}
-// shared memory behind the slots: the groups' results, two sums per thread and vector element, K per group of this CTA; backward (K = 2) also two sums per
-// channel, and those of all samples
-template <int V> struct ClusterSmem {
-    Table<V> part;
-    float *chan, *grp;       // [2][Cs], [K][groups]
-    float *weight, *rstd;    // backward: of the slice's channels, and of the groups of the sample
-    float* acc;              // backward: the samples' sums of this CTA's channels, [2][ceil(Cs / k)]
+// Shared memory behind the slots: the groups' results, two sums per thread and vector element; backward also two sums per channel, those of all samples, the
+// channels' weights and the groups' rstd.
+template <int V> struct SliceSmem {
     float2* res;
-    __device__ __forceinline__ ClusterSmem(uint8_t* p, const ClusterWalk& w, int K) {
+    Table<V> part;
+    float *chan, *acc, *weight, *rstd;
+    __device__ __forceinline__ SliceSmem(uint8_t* p, const SliceWalk& w) {
         res = (float2*)p;
         part = {(float*)(res + w.groups), w.threads + 4};
         chan = part.p + 2 * V * part.pitch;
-        grp = chan + (K == 2 ? 2 * w.Cs : 0);
-        weight = grp + K * w.groups;
+        acc = chan + 2 * w.Cs;
+        weight = acc + 2 * w.Cs;
         rstd = weight + w.Cs;
-        acc = rstd + w.groups;
     }
 };
-template <int V> inline size_t cluster_scratch(const ClusterWalk& w, int K) {
-    return ((size_t)2 * V * (w.threads + 4) + K * w.groups + (K == 2 ? 3 * w.Cs + w.groups + 2 * ((w.Cs + w.k - 1) / w.k) : 0)) * sizeof(float) + w.groups * sizeof(float2);
+template <int V> inline size_t slice_scratch(const SliceWalk& w, bool backward) {
+    return ((size_t)2 * V * (w.threads + 4) + (backward ? 5 * w.Cs + w.groups : 0)) * sizeof(float) + w.groups * sizeof(float2);
 }
-// A cluster's work: a slice of the channels (from channel c0, group g0 on) of the samples n0, n0 + step, ...
-struct ClusterSpot {
+// a block's work: a slice (from channel c0, group g0 on) of the samples n0, n0 + step, ...
+struct SliceSpot {
     long long n0, step;
-    int c0, g0, rank;
-    __device__ __forceinline__ ClusterSpot(const ClusterWalk& w) {
-        const uint32_t id = blockIdx.x / (uint32_t)w.k, slice = id % (uint32_t)w.slices;
-        n0 = id / (uint32_t)w.slices;
-        step = gridDim.x / (uint32_t)(w.k * w.slices);
+    int c0, g0;
+    __device__ __forceinline__ SliceSpot(const SliceWalk& w) {
+        const uint32_t slice = blockIdx.x % (uint32_t)w.slices;
+        n0 = blockIdx.x / (uint32_t)w.slices;
+        step = gridDim.x / (uint32_t)w.slices;
         c0 = slice * w.Cs;
         g0 = slice * w.groups;
-        rank = w.k > 1 ? (int)tc::cluster_ctarank() : 0;
     }
 };
 // What the lanes of a group add up: the table's K sums of the channels c0 .. c0 + cg - 1 over the rows of threads r < rows, dealt to lanes by channel
 // (w.lc of them) and by row.  These loops run a warp at a time with nothing to hide their latency, so they are kept to a load and an addition.
-template <int V, int K> __device__ __forceinline__ void group_sums(const ClusterWalk& w, const Table<V>& table, uint32_t c0, uint32_t cg, int rows, uint32_t lane, float* out) {
+template <int V, int K> __device__ __forceinline__ void group_sums(const SliceWalk& w, const Table<V>& table, uint32_t c0, uint32_t cg, int rows, uint32_t lane, float* out) {
     const uint32_t ci = lane & (w.lc - 1);
     const int ri = lane >> w.lc_shift, lr = w.lanes >> w.lc_shift, step = lr * w.cols, next = V * table.pitch;
     for (uint32_t c = c0 + ci; c < c0 + cg; c += w.lc) {
@@ -659,35 +651,31 @@ template <int V> __device__ __forceinline__ void load_parameters(const float* p,
     }
 }
 
-// Clusters are persistent: while a sample's results are formed, the vectors of the cluster's next sample are copied into the slots that have been
-// read, so memory is read and written at the same time and the sums' way around the cluster is not waited for by both.
-//
-// The sums' shift is here one value per group and CTA, the mean over the first position of every thread: sums of differences and of squares can then
-// simply be added up, and the square of a wrong shift (an outlier among the first positions) is divided by the square of their number.
+// The values are at hand, so the sums go over them twice: the first sum's mean, off by some 2^-24 of the values' size, is the shift of the second, whose sums of
+// differences and of squares then cancel nothing and can simply be added up.
 template <typename T, int V, int ACT>
-__global__ void __launch_bounds__(kClThreads, 2) gn_cluster_forward_kernel(const T* __restrict__ x, const Geo gx, const ClusterWalk w, const NormShape sh, long long samples,
-                                                                           const float* __restrict__ weight, const float* __restrict__ bias, T* __restrict__ y, const Geo gy,
-                                                                           float* __restrict__ mean, float* __restrict__ rstd, const Keep kx, const Keep ky) {
+__global__ void __launch_bounds__(kSlThreads, 2) gn_slice_forward_kernel(const T* __restrict__ x, const Geo gx, const SliceWalk w, const NormShape sh, long long samples,
+                                                                         const float* __restrict__ weight, const float* __restrict__ bias, T* __restrict__ y, const Geo gy,
+                                                                         float* __restrict__ mean, float* __restrict__ rstd, const Keep kx, const Keep ky) {
     kn::pdl_sync();
     extern __shared__ __align__(16) uint8_t smem[];
     using R = Raw<T, V>;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, warps = w.threads >> 5;
     R* slots = (R*)smem + tid;
-    const ClusterSmem<V> m(smem + (size_t)w.keep * w.threads * sizeof(R), w, 3);
-    const ClusterSpot b(w);
+    const SliceSmem<V> m(smem + (size_t)w.its * w.threads * sizeof(R), w);
+    const SliceSpot b(w);
     const int row = tid / w.cols, v = tid - row * w.cols, cv = b.c0 / V + v;      // cv: vector within the tensor's row
     const bool on = row < w.rows, has = on && v < w.vecs;
-    const int p0 = b.rank * w.ppc, np = max(0, min(w.HW - p0, w.ppc));
-    const int cnt = on && row < np ? (np - row + w.rows - 1) / w.rows : 0;      // iterations of this thread
-    const int kept = has ? min(cnt, w.keep) : 0, batch = (w.keep + kClBatches - 1) / kClBatches;
-    const int rows = min(w.rows, np), at_once = 32 / w.lanes, lane_g = lane / w.lanes, lane_i = lane % w.lanes;
-    const float n_cta = (float)np * (float)sh.cg;
+    const int cnt = on && row < w.HW ? (w.HW - row + w.rows - 1) / w.rows : 0;  // positions of this thread
+    const int filled = has ? cnt : 0, batch = (w.its + kSlBatches - 1) / kSlBatches;
+    const int rows = min(w.rows, w.HW), at_once = 32 / w.lanes, lane_g = lane / w.lanes, lane_i = lane % w.lanes;
+    const float count = (float)w.HW * (float)sh.cg, per = __frcp_rn(count);
     if (b.n0 < samples) {
-        Cursor c(gx, p0 + row);
+        Cursor c(gx, row);
         const T* xp = x + b.n0 * gx.sn + V * cv;
         #pragma unroll 1
-        for (int bt = 0; bt < kClBatches; ++bt) {
-            const int e = min(kept, (bt + 1) * batch);
+        for (int bt = 0; bt < kSlBatches; ++bt) {
+            const int e = min(filled, (bt + 1) * batch);
             #pragma unroll 4
             for (int it = bt * batch; it < e; ++it) {
                 fill_slot(slots + it * w.threads, xp + c.off);
@@ -696,101 +684,62 @@ __global__ void __launch_bounds__(kClThreads, 2) gn_cluster_forward_kernel(const
             copies_commit();
         }
     }
-    bool first = true;
     #pragma unroll 1
     for (long long n = b.n0; n < samples; n += b.step) {
-        const T* xp = x + n * gx.sn + V * cv;
+        float nK[V], S[V], Q[V];
         // the shift
-        copies_wait(kClBatches - 1);
-        if (has && cnt > 0) {
-            float f[V];
-            unpack<T, V>(kept > 0 ? slots[0] : *(const R*)(xp + gx.at(p0 + row)), f);
-            #pragma unroll
-            for (int i = 0; i < V; ++i) m.part.at(0, i, tid) = f[i];
+        #pragma unroll
+        for (int i = 0; i < V; ++i) S[i] = Q[i] = 0.f;
+        #pragma unroll 1
+        for (int bt = 0; bt < kSlBatches; ++bt) {
+            copies_wait(kSlBatches - 1 - bt);
+            const int e = min(filled, (bt + 1) * batch);
+            #pragma unroll 4
+            for (int it = bt * batch; it < e; ++it) {
+                float f[V];
+                unpack<T, V>(slots[it * w.threads], f);
+                v_add<V>(S, f, S);
+            }
         }
+        #pragma unroll
+        for (int i = 0; i < V; ++i) { m.part.at(0, i, tid) = S[i]; S[i] = 0.f; }
         __syncthreads();
         for (int g0 = warp * at_once; g0 < w.groups; g0 += warps * at_once) {
-            const int g = g0 + lane_g, first_rows = g < w.groups ? min(rows, 1 + 32 / sh.cg) : 0;      // at least 32 values, where there are as many
+            const int g = g0 + lane_g;
             float t = 0.f;
-            if (first_rows) group_sums<V, 1>(w, m.part, g * sh.cg, sh.cg, first_rows, lane_i, &t);
+            if (g < w.groups) group_sums<V, 1>(w, m.part, g * sh.cg, sh.cg, rows, lane_i, &t);
             t = lanes_sum(t, w.lanes);
-            if (lane_i == 0 && first_rows) m.res[g].x = __fdividef(t, (float)(first_rows * sh.cg));
+            if (lane_i == 0 && g < w.groups) m.res[g].x = t * per;
         }
         __syncthreads();
         // sums
-        float nK[V], S[V], Q[V];
         #pragma unroll
-        for (int i = 0; i < V; ++i) {
-            nK[i] = np > 0 ? -m.res[sh.group(min(V * v + i, w.Cs - 1))].x : 0.f;
-            S[i] = Q[i] = 0.f;
-        }
-        auto add = [&](const R& r) {
+        for (int i = 0; i < V; ++i) nK[i] = -m.res[sh.group(min(V * v + i, w.Cs - 1))].x;
+        #pragma unroll 4
+        for (int it = 0; it < filled; ++it) {
             float f[V];
-            unpack<T, V>(r, f);
+            unpack<T, V>(slots[it * w.threads], f);
             v_add<V>(f, nK, f);
             v_add<V>(S, f, S);
             v_fma<V>(f, f, Q, Q);
-        };
-        #pragma unroll 1
-        for (int bt = 0; bt < kClBatches; ++bt) {
-            copies_wait(kClBatches - 1 - bt);
-            const int e = min(kept, (bt + 1) * batch);
-            #pragma unroll 4
-            for (int it = bt * batch; it < e; ++it) add(slots[it * w.threads]);
-        }
-        if (has && kept < cnt) {
-            constexpr int U = 4;
-            Cursor c(gx, p0 + row + kept * w.rows);
-            for (int it = kept; it < cnt; it += U) {
-                R r[U];
-                #pragma unroll
-                for (int u = 0; u < U; ++u) {
-                    if (it + u < cnt) r[u] = *(const R*)(xp + c.off);
-                    c.next(gx);
-                }
-                #pragma unroll
-                for (int u = 0; u < U; ++u)
-                    if (it + u < cnt) add(r[u]);
-            }
         }
         #pragma unroll
         for (int i = 0; i < V; ++i) { m.part.at(0, i, tid) = S[i]; m.part.at(1, i, tid) = Q[i]; }
         __syncthreads();
-        if (w.k > 1 && !first) tc::cluster_wait();               // the others have read this CTA's sums of the sample before
         for (int g0 = warp * at_once; g0 < w.groups; g0 += warps * at_once) {
-            const int g = g0 + lane_g, total = g < w.groups ? rows : 0;
+            const int g = g0 + lane_g;
             float sq[2] = {0.f, 0.f};
-            if (total) group_sums<V, 2>(w, m.part, g * sh.cg, sh.cg, total, lane_i, sq);
-            float s = sq[0], q = sq[1];
-            s = lanes_sum(s, w.lanes);
-            q = lanes_sum(q, w.lanes);
+            if (g < w.groups) group_sums<V, 2>(w, m.part, g * sh.cg, sh.cg, rows, lane_i, sq);
+            const float s = lanes_sum(sq[0], w.lanes), q = lanes_sum(sq[1], w.lanes);
             if (lane_i == 0 && g < w.groups) {
-                const float K = total ? m.res[g].x : 0.f, d = total ? __fdividef(s, n_cta) : 0.f, hi = K + d;
-                m.grp[g] = hi;
-                m.grp[w.groups + g] = (K - hi) + d;
-                m.grp[2 * w.groups + g] = fmaf(-s, d, q);
-            }
-        }
-        __syncwarp();
-        if (w.k > 1) tc::cluster_sync_all();
-        else __syncthreads();
-        for (int i0 = warp * 32; i0 < w.groups * w.k; i0 += warps * 32) {      // the CTAs of the cluster: a lane each
-            const int g = (i0 + lane) / w.k;
-            Part t = {0.f, 0.f, 0.f};
-            if (w.k > 1) {
-                const int i = (i0 + lane) % w.k;
-                if (g < w.groups) t = Part{ld_cluster(m.grp + g, i), ld_cluster(m.grp + w.groups + g, i), ld_cluster(m.grp + 2 * w.groups + g, i)};
-                t = join_lanes(t, (float)max(0, min(w.HW - i * w.ppc, w.ppc)) * (float)sh.cg, w.k, __fdividef(1.f, (float)w.HW * (float)sh.cg));
-            } else if (g < w.groups) t = {m.grp[g], m.grp[w.groups + g], m.grp[2 * w.groups + g]};
-            if (g < w.groups && (i0 + lane) % w.k == 0) {
-                const float2 r = statistics(t, sh);
+                const float d = s * per, mu = m.res[g].x + d;
+                const float var = fmaf(-s, d, q) * per;
+                const float2 r = make_float2(mu, __frsqrt_rn((var < 0.f ? 0.f : var) + sh.eps));      // (keeps NaN)
                 m.res[g] = r;
-                if (b.rank == 0) { mean[n * sh.groups + b.g0 + g] = r.x; rstd[n * sh.groups + b.g0 + g] = r.y; }
+                mean[n * sh.groups + b.g0 + g] = r.x;
+                rstd[n * sh.groups + b.g0 + g] = r.y;
             }
         }
-        __syncwarp();
-        if (w.k > 1) tc::cluster_arrive_relaxed();               // this CTA has read the others' sums
-        first = false;
         __syncthreads();
 
         // results, and the next sample's copies
@@ -806,85 +755,67 @@ __global__ void __launch_bounds__(kClThreads, 2) gn_cluster_forward_kernel(const
             k.a[i] *= r.y;
         }
         const bool more = n + b.step < samples;
-        const T* xn = xp + b.step * gx.sn;
+        const T* xn = x + (n + b.step) * gx.sn + V * cv;
         T* yp = y + n * gy.sn + V * cv;
-        Cursor cy(gy, p0 + row), cx(gx, p0 + row);               // cx: the next sample's copies, then this one's vectors that are read again
-        CodesCursor ckx(kx.codes, kx.scales, n * w.HW + p0 + row, cv, w.dense), cky(ky.codes, ky.scales, n * w.HW + p0 + row, cv, w.dense);
-        auto emit = [&](const R& r) {
-            float f[V], z[V];
-            unpack<T, V>(r, f);
-            if constexpr (V == 8)
-                if (kx.codes) { keep_codes<T>(kx, r, f, has, ckx); ckx.next(w.dense); }
-            v_add<V>(f, k.nm, f);
-            v_fma<V>(f, k.a, k.b, z);
-            activate<T, V, ACT>(sh.act, z);
-            R out = pack<T, V>(z);
-            if (has) *(R*)(yp + cy.off) = out;
-            cy.next(gy);
-            if constexpr (V == 8)
-                if (ky.codes) {                     // of y as it is stored
-                    if (!has) out = R{};
-                    unpack<T, 8>(out, f);
-                    keep_codes<T>(ky, out, f, has, cky);
-                    cky.next(w.dense);
-                }
-        };
-        const int split = min(cnt, w.keep);
+        Cursor cy(gy, row), cx(gx, row);
+        CodesCursor ckx(kx.codes, kx.scales, n * w.HW + row, cv, w.dense), cky(ky.codes, ky.scales, n * w.HW + row, cv, w.dense);
         #pragma unroll 1
-        for (int bt = 0; bt < kClBatches; ++bt) {
-            const int e = min(split, (bt + 1) * batch);
+        for (int bt = 0; bt < kSlBatches; ++bt) {
+            const int e = min(cnt, (bt + 1) * batch);
             #pragma unroll 2
             for (int it = bt * batch; it < e; ++it) {
                 const R r = has ? slots[it * w.threads] : R{};
-                emit(r);
+                float f[V], z[V];
+                unpack<T, V>(r, f);
+                if constexpr (V == 8)
+                    if (kx.codes) { keep_codes<T>(kx, r, f, has, ckx); ckx.next(w.dense); }
+                v_add<V>(f, k.nm, f);
+                v_fma<V>(f, k.a, k.b, z);
+                activate<T, V, ACT>(sh.act, z);
+                R out = pack<T, V>(z);
+                if (has) *(R*)(yp + cy.off) = out;
+                cy.next(gy);
+                if constexpr (V == 8)
+                    if (ky.codes) {                     // of y as it is stored
+                        if (!has) out = R{};
+                        unpack<T, 8>(out, f);
+                        keep_codes<T>(ky, out, f, has, cky);
+                        cky.next(w.dense);
+                    }
                 if (more && has) fill_slot(slots + it * w.threads, xn + cx.off);
                 cx.next(gx);
             }
             copies_commit();
         }
-        #pragma unroll 2
-        for (int it = split; it < cnt; ++it) {
-            R r = {};
-            if (has) r = *(const R*)(xp + cx.off);
-            cx.next(gx);
-            emit(r);
-        }
     }
-    if (w.k > 1 && !first) { __syncwarp(); tc::cluster_wait(); }          // no CTA leaves while another may read its sums
 }
 
-// The same for the backward pass: sums of dz and dz d per channel, around the cluster for c1 and c2, then dx.  The samples' sums for dweight and
-// dbias are added up in shared memory (a CTA takes the channels rank, rank + k, ... of its cluster) and go to partial [cluster][2][C] at the end.
+// The same for the backward pass: sums of dz and dz d per channel, c1 and c2 of the groups, then dx.  The samples' sums for dweight and dbias are added up in
+// shared memory and go to partial [block of the slice][2][C] at the end.
 template <typename T, int V, int SRC, int ACT>
-__global__ void __launch_bounds__(kClThreads, 2) gn_cluster_backward_kernel(const T* __restrict__ dy, const Geo gdy, const Source src, const Geo gx, const ClusterWalk w, const NormShape sh,
-                                                                            long long samples, const BackwardArgs A, T* __restrict__ dx, const Geo gdx, float* __restrict__ partial) {
+__global__ void __launch_bounds__(kSlThreads, 2) gn_slice_backward_kernel(const T* __restrict__ dy, const Geo gdy, const Source src, const Geo gx, const SliceWalk w, const NormShape sh,
+                                                                          long long samples, const BackwardArgs A, T* __restrict__ dx, const Geo gdx, float* __restrict__ partial) {
     kn::pdl_sync();
     extern __shared__ __align__(16) uint8_t smem[];
     using R = Raw<T, V>;
     using X = typename Fetch<T, V, SRC>::R;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, warps = w.threads >> 5;
-    const size_t slab = (size_t)w.keep * w.threads;
+    const size_t slab = (size_t)w.its * w.threads;
     R* slots = (R*)smem + tid;
     X* xslots = (X*)(smem + slab * sizeof(R)) + tid;
     uint8_t* eslots = smem + slab * (sizeof(R) + sizeof(X)) + tid;
-    const ClusterSmem<V> m(smem + slab * (sizeof(R) + sizeof(X)) + (SRC == kSrcSame ? 0 : (slab + 15) / 16 * 16), w, 2);
-    float* acc = m.acc;
-    const ClusterSpot b(w);
+    const SliceSmem<V> m(smem + slab * (sizeof(R) + sizeof(X) + (SRC == kSrcSame ? 0 : 1)), w);       // (slab is a multiple of 32)
+    const SliceSpot b(w);
     const int row = tid / w.cols, v = tid - row * w.cols, cv = b.c0 / V + v;
     const bool has = row < w.rows && v < w.vecs;
-    const int p0 = b.rank * w.ppc, np = max(0, min(w.HW - p0, w.ppc));
-    const int cnt = has && row < np ? (np - row + w.rows - 1) / w.rows : 0;
-    const int blocks = (w.C + 31) / 32, kept = min(cnt, w.keep), batch = (w.keep + kClBatches - 1) / kClBatches, own = (w.Cs + w.k - 1) / w.k;
-    const T* xbase = SRC == kSrcSame ? (const T*)src.x + V * cv : nullptr;
-    auto codes_at = [&](long long n, int it) { return src.codes + (n * w.HW + p0 + row + (long long)it * w.rows) * w.C + V * cv; };
-    auto scale_at = [&](long long n, int it) { return src.scales + (n * w.HW + p0 + row + (long long)it * w.rows) * blocks + V * cv / 32; };
+    const int cnt = has && row < w.HW ? (w.HW - row + w.rows - 1) / w.rows : 0, batch = (w.its + kSlBatches - 1) / kSlBatches;
     if (b.n0 < samples) {
-        Cursor cdy(gdy, p0 + row);
-        SourceCursor<T, V, SRC> cx(src, gx, w, b.n0, p0 + row, cv);
+        Cursor cdy(gdy, row);
+        SourceCursor<T, V, SRC> cx(src, gx, w, b.n0, row, cv);
         const T* dp = dy + b.n0 * gdy.sn + V * cv;
         #pragma unroll 1
-        for (int bt = 0; bt < kClBatches; ++bt) {
-            const int e = min(kept, (bt + 1) * batch);
+        for (int bt = 0; bt < kSlBatches; ++bt) {
+            const int e = min(cnt, (bt + 1) * batch);
             #pragma unroll 2
             for (int it = bt * batch; it < e; ++it) {
                 fill_slot(slots + it * w.threads, dp + cdy.off);
@@ -895,77 +826,60 @@ __global__ void __launch_bounds__(kClThreads, 2) gn_cluster_backward_kernel(cons
             copies_commit();
         }
         if constexpr (SRC != kSrcSame) {
+            const uint8_t* ep = src.scales + (b.n0 * w.HW + row) * w.dense.blocks + V * cv / 32;
             #pragma unroll 8
-            for (int it = 0; it < kept; ++it) eslots[it * w.threads] = *scale_at(b.n0, it);
+            for (int it = 0; it < cnt; ++it, ep += w.dense.inc_scales) eslots[it * w.threads] = *ep;
         }
     }
-    for (int i = tid; i < 2 * own; i += w.threads) acc[i] = 0.f;
-    for (int c = tid; c < w.Cs; c += w.threads) m.weight[c] = A.weight ? A.weight[b.c0 + c] : 1.f;
-    bool first = true;
+    for (int c = tid; c < w.Cs; c += w.threads) {
+        m.acc[c] = m.acc[w.Cs + c] = 0.f;
+        m.weight[c] = A.weight ? A.weight[b.c0 + c] : 1.f;
+    }
     #pragma unroll 1
     for (long long n = b.n0; n < samples; n += b.step) {
         const long long gb = n * sh.groups + b.g0;              // this block's first group
-        const T* dp = dy + n * gdy.sn + V * cv;
         for (int g = tid; g < w.groups; g += w.threads) m.rstd[g] = A.rstd[gb + g];
         Chan<V> k;
-        if (has) load_chan<V>(k, sh, A.mean, A.rstd, A.weight, A.bias, n, V * cv);
-        // d and dz from what has been read
-        auto values = [&](const R& r, const Fetch<T, V, SRC>& fx, float* f, float* q) {
-            unpack<T, V>(r, q);
-            activation_gradient<T, V, SRC, ACT>(sh, k, A, n, V * cv, fx, f, q);
-        };
-        auto from_slot = [&](int it, R& r, Fetch<T, V, SRC>& fx) {
-            r = slots[it * w.threads];
+        if (has) load_backward_chan<V, ACT>(k, sh, A, n, V * cv);
+        // d and dz of the thread's position `it`
+        auto values = [&](int it, float* f, float* q) {
+            Fetch<T, V, SRC> fx;
             fx.r = xslots[it * w.threads];
             if constexpr (SRC != kSrcSame) fx.e = eslots[it * w.threads];
-        };
-        auto from_memory = [&](int it, R& r, Fetch<T, V, SRC>& fx) {
-            const int p = p0 + row + it * w.rows;
-            r = *(const R*)(dp + gdy.at(p));
-            if constexpr (SRC == kSrcSame) fx.r = *(const X*)(xbase + n * gx.sn + gx.at(p));
-            else { fx.r = *(const X*)codes_at(n, it); fx.e = *scale_at(n, it); }
+            unpack<T, V>(slots[it * w.threads], q);
+            activation_gradient<T, V, SRC, ACT>(sh.act, k, fx, f, q);
         };
         float S1[V], S2[V];
         #pragma unroll
         for (int i = 0; i < V; ++i) S1[i] = S2[i] = 0.f;
-        auto add = [&](const R& r, const Fetch<T, V, SRC>& fx) {
-            float f[V], q[V];
-            values(r, fx, f, q);
-            v_add<V>(S1, q, S1);
-            v_fma<V>(f, q, S2, S2);
-        };
         #pragma unroll 1
-        for (int bt = 0; bt < kClBatches; ++bt) {
-            copies_wait(kClBatches - 1 - bt);
-            const int e = min(kept, (bt + 1) * batch);
+        for (int bt = 0; bt < kSlBatches; ++bt) {
+            copies_wait(kSlBatches - 1 - bt);
+            const int e = min(cnt, (bt + 1) * batch);
             #pragma unroll 1
             for (int it = bt * batch; it < e; ++it) {
-                R r; Fetch<T, V, SRC> fx;
-                from_slot(it, r, fx);
-                add(r, fx);
+                float f[V], q[V];
+                values(it, f, q);
+                v_add<V>(S1, q, S1);
+                v_fma<V>(f, q, S2, S2);
             }
-        }
-        #pragma unroll 1
-        for (int it = kept; it < cnt; it += 2) {
-            R r[2]; Fetch<T, V, SRC> fx[2];
-            from_memory(it, r[0], fx[0]);
-            if (it + 1 < cnt) from_memory(it + 1, r[1], fx[1]);
-            add(r[0], fx[0]);
-            if (it + 1 < cnt) add(r[1], fx[1]);
         }
         #pragma unroll
         for (int i = 0; i < V; ++i) { m.part.at(0, i, tid) = S1[i]; m.part.at(1, i, tid) = S2[i]; }
         __syncthreads();
-        if (w.k > 1 && !first) tc::cluster_wait();               // the others have read this CTA's sums of the sample before
         for (uint32_t c = tid; c < (uint32_t)w.Cs; c += w.threads) {
             const float* p = m.part.p + (c % V) * m.part.pitch + c / V;
             float2 t = make_float2(0.f, 0.f);
             #pragma unroll 8
             for (int r = 0; r < w.rows; ++r, p += w.cols) { t.x += p[0]; t.y += p[V * m.part.pitch]; }
+            t.y *= m.rstd[sh.group(c)];                         // of xhat
             m.chan[c] = t.x;
-            m.chan[w.Cs + c] = t.y * m.rstd[sh.group(c)];                 // of xhat
+            m.chan[w.Cs + c] = t.y;
+            m.acc[c] += t.x;
+            m.acc[w.Cs + c] += t.y;
         }
         __syncthreads();
+        const float per = __frcp_rn((float)sh.HW * (float)sh.cg);
         for (int g0 = warp * (32 / w.lanes); g0 < w.groups; g0 += warps * (32 / w.lanes)) {
             const int g = g0 + lane / w.lanes;
             float2 t = make_float2(0.f, 0.f);
@@ -977,31 +891,11 @@ __global__ void __launch_bounds__(kClThreads, 2) gn_cluster_backward_kernel(cons
                 }
             t.x = lanes_sum(t.x, w.lanes);
             t.y = lanes_sum(t.y, w.lanes);
-            if (g < w.groups && lane % w.lanes == 0) { m.grp[g] = t.x; m.grp[w.groups + g] = t.y; }
+            if (g < w.groups && lane % w.lanes == 0) m.res[g] = make_float2(t.x * per, t.y * per);
         }
-        __syncwarp();
-        if (w.k > 1) tc::cluster_sync_all();
-        else __syncthreads();
-        auto over_cluster = [&](const float* p) {
-            if (w.k == 1) return *p;
-            float t = 0.f;
-            #pragma unroll
-            for (int i = 0; i < 8; ++i)
-                if (i < w.k) t += ld_cluster(p, i);
-            return t;
-        };
-        const float per = __frcp_rn((float)sh.HW * (float)sh.cg);
-        for (int g = tid; g < w.groups; g += w.threads) m.res[g] = make_float2(over_cluster(m.grp + g) * per, over_cluster(m.grp + w.groups + g) * per);
-        for (int i = tid; b.rank + w.k * i < w.Cs; i += w.threads) {
-            acc[i] += over_cluster(m.chan + b.rank + w.k * i);
-            acc[own + i] += over_cluster(m.chan + w.Cs + b.rank + w.k * i);
-        }
-        __syncwarp();
-        if (w.k > 1) tc::cluster_arrive_relaxed();
-        first = false;
         __syncthreads();
+        float B[V], D[V];
         if (has) {
-            float B[V], D[V];
             #pragma unroll
             for (int i = 0; i < V; ++i) {
                 const int g = sh.group(V * v + i);
@@ -1010,59 +904,47 @@ __global__ void __launch_bounds__(kClThreads, 2) gn_cluster_backward_kernel(cons
                 B[i] = -r * r * c.y;
                 D[i] = -r * c.x;
             }
-            const bool more = n + b.step < samples;
-            const long long n1 = n + b.step;
-            const T* dn = dp + b.step * gdy.sn;
-            T* op = dx + n * gdx.sn + V * cv;
-            Cursor c(gdx, p0 + row), cdy(gdy, p0 + row);
-            SourceCursor<T, V, SRC> cx(src, gx, w, n1, p0 + row, cv);
-            uint8_t e_next = 0;                                 // the exponent of the next sample's copies, stored an iteration after it was asked for
-            auto emit = [&](const R& r, const Fetch<T, V, SRC>& fx) {
+        }
+        const bool more = n + b.step < samples;
+        const long long n1 = n + b.step;
+        const T* dn = dy + n1 * gdy.sn + V * cv;
+        T* op = dx + n * gdx.sn + V * cv;
+        Cursor c(gdx, row), cdy(gdy, row);
+        SourceCursor<T, V, SRC> cx(src, gx, w, n1, row, cv);
+        uint8_t e_next = 0;                                     // the exponent of the next sample's copies, stored a position after it was asked for
+        #pragma unroll 1
+        for (int bt = 0; bt < kSlBatches; ++bt) {
+            const int e = min(cnt, (bt + 1) * batch);
+            #pragma unroll 1
+            for (int it = bt * batch; it < e; ++it) {
                 float f[V], q[V];
-                values(r, fx, f, q);
+                values(it, f, q);
+                if (SRC != kSrcSame && more) {
+                    if (it > 0) eslots[(it - 1) * w.threads] = e_next;
+                    e_next = *cx.scales;
+                }
                 v_fma<V>(f, B, D, f);
                 v_fma<V>(q, k.a, f, q);
                 *(R*)(op + c.off) = pack<T, V>(q);
                 c.next(gdx);
-            };
-            #pragma unroll 1
-            for (int bt = 0; bt < kClBatches; ++bt) {
-                const int e = min(kept, (bt + 1) * batch);
-                #pragma unroll 1
-                for (int it = bt * batch; it < e; ++it) {
-                    R r; Fetch<T, V, SRC> fx;
-                    from_slot(it, r, fx);
-                    if (SRC != kSrcSame && more) {
-                        if (it > 0) eslots[(it - 1) * w.threads] = e_next;
-                        e_next = *cx.scales;
-                    }
-                    emit(r, fx);
-                    if (more) {
-                        fill_slot(slots + it * w.threads, dn + cdy.off);
-                        cdy.next(gdy);
-                        fill_slot(xslots + it * w.threads, cx.place());
-                        cx.next(gx, w);
-                    }
+                if (more) {
+                    fill_slot(slots + it * w.threads, dn + cdy.off);
+                    cdy.next(gdy);
+                    fill_slot(xslots + it * w.threads, cx.place());
+                    cx.next(gx, w);
                 }
-                copies_commit();
             }
-            if (SRC != kSrcSame && more && kept > 0) eslots[(kept - 1) * w.threads] = e_next;
-            #pragma unroll 1
-            for (int it = kept; it < cnt; ++it) {
-                R r; Fetch<T, V, SRC> fx;
-                from_memory(it, r, fx);
-                emit(r, fx);
-            }
+            copies_commit();
         }
+        if (SRC != kSrcSame && more && cnt > 0) eslots[(cnt - 1) * w.threads] = e_next;
+        __syncthreads();                                        // (the groups' rstd and results are free for the next sample)
     }
-    if (!first) {
-        __syncthreads();
+    if (b.n0 < samples) {
         float* out = partial + b.n0 * 2 * w.C + b.c0;
-        for (int i = tid; b.rank + w.k * i < w.Cs; i += w.threads) {
-            out[b.rank + w.k * i] = acc[i];
-            out[w.C + b.rank + w.k * i] = acc[own + i];
+        for (int c = tid; c < w.Cs; c += w.threads) {
+            out[c] = m.acc[c];
+            out[w.C + c] = m.acc[w.Cs + c];
         }
-        if (w.k > 1) { __syncwarp(); tc::cluster_wait(); }
     }
 }
 

@@ -9,7 +9,6 @@
 #include <atomic>
 #include <cmath>
 #include <cstdio>
-#include <cstdlib>
 #include <utility>
 
 #include "checkpoint.cuh"
@@ -103,7 +102,7 @@ bool vec_ok(const alexnet_view_t& v, const Dims& d, int dtype) {
 }
 bool vec_ok(const alexnet_checkpoint_t& k, const Dims& d) { return d.C % 8 == 0 && (uintptr_t)k.codes % 8 == 0; }
 
-// how a launch walks [n][h w][C] with vectors of V channels: about eight blocks per SM, of at least four positions per thread
+// how a launch walks [n][h w][C] with vectors of V channels: about eight blocks per SM, of at least eight positions per thread
 Walk walk_of(const Dims& d, int V) {
     Walk w{};
     w.C = d.C; w.HW = d.h * d.w; w.vecs = d.C / V;
@@ -111,9 +110,8 @@ Walk walk_of(const Dims& d, int V) {
     w.colblocks = (int)ceil_div(padded, 256);
     w.cols = (int)ceil_div(ceil_div(padded, w.colblocks), q) * q;
     w.rows = 256 / w.cols;
-    const char* ev = getenv("GN_BLK"); const int per = ev ? atoi(ev) : 8;
-    long long chunks = ceil_div(per * kSms, std::max<long long>(1, d.n * w.colblocks));
-    chunks = std::min(chunks, ceil_div(w.HW, 4 * w.rows));
+    long long chunks = ceil_div(8 * kSms, std::max<long long>(1, d.n * w.colblocks));
+    chunks = std::min(chunks, ceil_div(w.HW, 8 * w.rows));
     chunks = std::max(chunks, ceil_div((long long)w.HW * ceil_div(d.C, 32), 1 << 30));      // indices of a chunk's blocks fit 31 bits
     chunks = std::max<long long>(1, std::min<long long>(chunks, w.HW));
     w.ppc = (int)ceil_div(w.HW, chunks);
@@ -183,99 +181,74 @@ size_t forward_ws(const Walk& w, const Dims& d) { return (size_t)(d.n * w.chunks
 size_t backward_ws(const Walk& w, const Dims& d, int groups) { return (size_t)(d.n * groups) * sizeof(float2) + (size_t)(d.n * w.chunks) * 2 * d.C * sizeof(float); }
 
 constexpr size_t kSmSmem = 228 * 1024, kCtaSmem = 227 * 1024;
-// How clusters walk a tensor, `slot` bytes kept per vector of V channels, `moved` bytes per vector to and from memory and K sums per group; k = 0: not at
-// all (rows wider than a block, or too few samples to fill the device with their clusters).  By a model in cycles: an SM moves 22 bytes per
-// cycle when it has 14 warps of three CTAs (in different phases), a sample costs 3500 or (in a cluster) 5000 more for the sums' way around, and
-// vectors that do not stay on chip are read again at 40 bytes and 600 cycles each.
+// How blocks that keep whole groups of a sample walk a tensor, `slot` bytes kept per vector of V channels; threads = 0: not at all.  As many slices as there are
+// (powers of two) until a slice takes at most 112 KB, so that two blocks share an SM, and further while the device is not full; but no rows below 64
+// bytes, which cost more sectors than they use.
 template <int V>
-ClusterWalk cluster_walk(const Dims& d, int groups, int slot, int moved, int K) {
-    ClusterWalk best{};
-    ClusterWalk w{};
+SliceWalk slice_walk(const Dims& d, int groups, int slot, int elem, bool backward) {
+    SliceWalk best{}, w{};
     w.C = d.C; w.HW = d.h * d.w;
     const int cg = d.C / groups;
-    double cost = 1e30;
     for (w.slices = 1; w.slices <= 64; w.slices *= 2) {
         w.Cs = d.C / w.slices; w.groups = groups / w.slices;
-        if (w.slices > 1 && (groups % w.slices || w.Cs % 32 || w.Cs * 2 < 64)) break;
+        if (w.slices > 1 && (groups % w.slices || w.Cs % 32 || w.Cs * elem < 64)) break;
         w.vecs = w.Cs / V;
         w.cols = (int)ceil_div(w.vecs, V == 8 ? 4 : 1) * (V == 8 ? 4 : 1);
-        if (w.cols > kClThreads || w.groups > 1024 || d.n > kMaxGrid / 512) continue;
-        for (w.k = 1; w.k <= 8; w.k *= 2) {
-            if (w.k > w.HW) break;
-            w.ppc = (int)ceil_div(w.HW, w.k);
-            for (w.threads = 128; w.threads <= kClThreads; w.threads += 32) {
-                if (w.threads < w.cols) continue;
-                w.rows = w.threads / w.cols;
-                w.its = (int)ceil_div(w.ppc, w.rows);
-                const size_t scratch = cluster_scratch<V>(w, K) + 64, per_it = (size_t)w.threads * slot;
-                if (scratch + 1024 > kCtaSmem) continue;
-                for (int occ = 1; occ <= 6 && occ * w.threads <= 2 * kClThreads; ++occ) {
-                    const size_t room = std::min(kCtaSmem, kSmSmem / occ - 1024);
-                    if (room < scratch) break;
-                    w.keep = (int)std::min<size_t>(w.its, (room - scratch) / per_it);
-                    const double busy = std::min(1.0, occ * w.threads / 448.0) * (occ == 1 ? 0.7 : occ == 2 ? 0.9 : 1.0);
-                    const double work = occ * ((double)w.its * w.threads * moved / 22 + (double)(w.its - w.keep) * w.threads * moved / 40) / busy + (w.its - w.keep) * 600.0;
-                    const double at_once = std::max(1.0, std::floor((double)kSms * occ / w.k * (w.k >= 4 ? 15 : 16) / 16));
-                    const double c = std::ceil((double)d.n * w.slices / at_once) * (work + (w.k > 1 ? 5000 : 3500)) + 6000;
-                    if (c < cost) { cost = c; best = w; }
-                }
-            }
+        if (w.cols > kSlThreads || w.groups > 1024 || d.n > kMaxGrid / 64) continue;
+        // threads: the fewest slots, and among alike the most
+        long long slots = 1ll << 60;
+        SliceWalk t = w;
+        for (t.threads = 128; t.threads <= kSlThreads; t.threads += 32) {
+            if (t.threads < w.cols) continue;
+            t.rows = t.threads / w.cols;
+            t.its = (int)ceil_div(w.HW, t.rows);
+            if (t.its * (long long)t.threads <= slots + slots / 16) { slots = std::min(slots, t.its * (long long)t.threads); w.threads = t.threads; w.rows = t.rows; w.its = t.its; }
         }
+        if (!w.threads || (size_t)w.its * w.threads * slot + slice_scratch<V>(w, backward) > kSmSmem / 2 - 1024) continue;
+        best = w;
+        if (d.n * w.slices >= 2 * kSms) break;
     }
-    if (getenv("GN_GENERAL")) best.k = 0;
-    if (!best.k) return best;
-    // a sample's blocks are few SMs: a few large samples go faster through the kernels that spread over all of them
-    if ((double)d.n * best.slices * best.k < kSms / 2 && (double)best.its * best.threads * moved > 2.0e5) best.k = 0;
+    if (!best.threads) return best;
     best.dense = dense_of(d.C, best.rows);
     best.lanes = 1;
     while (best.lanes < 32 && best.lanes * 2 * best.groups <= best.threads && best.lanes < cg * best.rows) best.lanes *= 2;
     for (best.lc = 1; best.lc < best.lanes && best.lc < cg; best.lc *= 2) ++best.lc_shift;
     return best;
 }
+// Samples that are under way at once: as many blocks per slice as the device holds (asked once per kernel and launch shape).
 template <typename K>
-cudaError_t allow_smem(K* kernel) { return cudaFuncSetAttribute((const void*)kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kCtaSmem); }
-// Samples that are under way at once: as many clusters per slice as the device holds (asked once per kernel and launch shape).
-template <typename K>
-long long cluster_rows(Launcher& go, K* kernel, const ClusterWalk& w, const Dims& d, size_t smem) {
-    struct Known { const void* kernel = nullptr; int device, threads, k, clusters; size_t smem; };
+long long slice_rows(Launcher& go, K* kernel, const SliceWalk& w, const Dims& d, size_t smem) {
+    struct Known { const void* kernel = nullptr; int device, threads, blocks; size_t smem; };
     static thread_local Known known[16];      // (of all kernels with this signature)
     static thread_local unsigned next = 0;
-    int dev = 0;
+    int dev = 0, blocks = 0;
     if (go.e == cudaSuccess) go.e = cudaGetDevice(&dev);
-    int clusters = 0;
     for (const Known& q : known)
-        if (q.kernel == (const void*)kernel && q.device == dev && q.threads == w.threads && q.k == w.k && q.smem == smem) clusters = q.clusters;
-    if (!clusters && go.e == cudaSuccess) {
-        go.e = allow_smem(kernel);
-        cudaLaunchConfig_t lc{};
-        lc.gridDim = dim3((unsigned)w.k); lc.blockDim = w.threads; lc.dynamicSmemBytes = smem;
-        cudaLaunchAttribute at{};
-        at.id = cudaLaunchAttributeClusterDimension;
-        at.val.clusterDim.x = w.k; at.val.clusterDim.y = 1; at.val.clusterDim.z = 1;
-        lc.attrs = &at; lc.numAttrs = 1;
-        if (go.e == cudaSuccess) go.e = cudaOccupancyMaxActiveClusters(&clusters, kernel, &lc);
-        if (go.e == cudaSuccess) known[next++ % 16] = {(const void*)kernel, dev, w.threads, w.k, clusters, smem};
+        if (q.kernel == (const void*)kernel && q.device == dev && q.threads == w.threads && q.smem == smem) blocks = q.blocks;
+    if (!blocks && go.e == cudaSuccess) {
+        go.e = cudaFuncSetAttribute((const void*)kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kCtaSmem);
+        if (go.e == cudaSuccess) go.e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&blocks, kernel, w.threads, smem);
+        if (go.e == cudaSuccess) known[next++ % 16] = {(const void*)kernel, dev, w.threads, blocks, smem};
     }
-    return std::min<long long>(d.n, std::max(1, clusters / w.slices));
+    return std::min<long long>(d.n, std::max(1, blocks * kSms / w.slices));
 }
 
 template <typename T, int V, int ACT>
 void forward(Launcher& go, const alexnet_group_norm_forward_t* a, const Dims& d) {
     const Walk w = walk_of(d, V);
     const NormShape s = norm_shape(a->shape);
-    const ClusterWalk cw = cluster_walk<V>(d, s.groups, sizeof(T) * V, 2 * sizeof(T) * V, 3);
-    if (cw.k) {
-        Keep kx{}, ky{};
-        if (V == 8) {
-            if (a->keep_x.codes) kx = {(uint8_t*)a->keep_x.codes, a->keep_x.scales, src_of(a->keep_x.format)};
-            if (a->keep_y.codes) ky = {(uint8_t*)a->keep_y.codes, a->keep_y.scales, src_of(a->keep_y.format)};
-        }
-        const size_t smem = (size_t)cw.keep * cw.threads * sizeof(T) * V + cluster_scratch<V>(cw, 3);
-        const long long rows = cluster_rows(go, gn_cluster_forward_kernel<T, V, ACT>, cw, d, smem);
+    Keep kx{}, ky{};
+    if (V == 8) {
+        if (a->keep_x.codes) kx = {(uint8_t*)a->keep_x.codes, a->keep_x.scales, src_of(a->keep_x.format)};
+        if (a->keep_y.codes) ky = {(uint8_t*)a->keep_y.codes, a->keep_y.scales, src_of(a->keep_y.format)};
+    }
+    const SliceWalk sw = slice_walk<V>(d, s.groups, sizeof(T) * V, sizeof(T), false);
+    if (sw.threads) {
+        const size_t smem = (size_t)sw.its * sw.threads * sizeof(T) * V + slice_scratch<V>(sw, false);
+        const long long rows = slice_rows(go, gn_slice_forward_kernel<T, V, ACT>, sw, d, smem);
         go.smem = smem;
-        go.cluster = cw.k;
-        go(gn_cluster_forward_kernel<T, V, ACT>, rows * cw.slices * cw.k, cw.threads, (const T*)a->x.data, geo_of(a->x, d, cw.rows), cw, s, (long long)d.n, a->weight, a->bias, (T*)a->y.data,
-           geo_of(a->y, d, cw.rows), a->mean, a->rstd, kx, ky);
+        go(gn_slice_forward_kernel<T, V, ACT>, rows * sw.slices, sw.threads, (const T*)a->x.data, geo_of(a->x, d, sw.rows), sw, s, (long long)d.n, a->weight, a->bias, (T*)a->y.data,
+           geo_of(a->y, d, sw.rows), a->mean, a->rstd, kx, ky);
         if (V != 8) {
             if (a->keep_x.codes) encode<T>(go, d, a->x, a->keep_x, a->shape.dtype);
             if (a->keep_y.codes) encode<T>(go, d, a->y, a->keep_y, a->shape.dtype);
@@ -285,11 +258,6 @@ void forward(Launcher& go, const alexnet_group_norm_forward_t* a, const Dims& d)
     const Geo gx = geo_of(a->x, d, w.rows), gy = geo_of(a->y, d, w.rows);
     float4* partial = (float4*)a->workspace;
     const T *x = (const T*)a->x.data;
-    Keep kx{}, ky{};
-    if (V == 8) {
-        if (a->keep_x.codes) kx = {(uint8_t*)a->keep_x.codes, a->keep_x.scales, src_of(a->keep_x.format)};
-        if (a->keep_y.codes) ky = {(uint8_t*)a->keep_y.codes, a->keep_y.scales, src_of(a->keep_y.format)};
-    }
     go(gn_sums_kernel<T, V>, grid_of(w, d), 256, x, gx, w, partial);
     const long long groups = d.n * s.groups;
     const bool block = groups < 8 * kSms;
@@ -310,18 +278,15 @@ void backward(Launcher& go, const alexnet_group_norm_backward_t* a, const Dims& 
     const Source src{a->x.data, (const uint8_t*)a->kept.codes, a->kept.scales};
     const BackwardArgs A{a->mean, a->rstd, a->weight, a->bias};
     const T* dy = (const T*)a->dy.data;
-    constexpr int kX = SRC == kSrcSame ? (int)sizeof(T) * V : V, kSlot = (int)sizeof(T) * V + kX + (SRC == kSrcSame ? 0 : 1);
-    const ClusterWalk cw = cluster_walk<V>(d, s.groups, kSlot, 2 * (int)sizeof(T) * V + kX, 2);
-    if (cw.k) {
+    constexpr int kSlot = (int)sizeof(T) * V + (SRC == kSrcSame ? (int)sizeof(T) * V : V + 1);
+    const SliceWalk sw = slice_walk<V>(d, s.groups, kSlot, SRC == kSrcSame ? (int)sizeof(T) : 2, true);
+    if (sw.threads) {
         partial = (float*)a->workspace;
-        auto* kernel = gn_cluster_backward_kernel<T, V, SRC, ACT>;
-        const size_t slab = (size_t)cw.keep * cw.threads;
-        const size_t smem = slab * (kSlot - (SRC == kSrcSame ? 0 : 1)) + (SRC == kSrcSame ? 0 : (slab + 15) / 16 * 16) + cluster_scratch<V>(cw, 2);
-        const long long rows = cluster_rows(go, kernel, cw, d, smem);
+        auto* kernel = gn_slice_backward_kernel<T, V, SRC, ACT>;
+        const size_t smem = (size_t)sw.its * sw.threads * kSlot + slice_scratch<V>(sw, true);
+        const long long rows = slice_rows(go, kernel, sw, d, smem);
         go.smem = smem;
-        go.cluster = cw.k;
-        go(kernel, rows * cw.slices * cw.k, cw.threads, dy, geo_of(a->dy, d, cw.rows), src, geo_of(a->x, d, cw.rows), cw, s, (long long)d.n, A, (T*)a->dx.data,
-           geo_of(a->dx, d, cw.rows), partial);
+        go(kernel, rows * sw.slices, sw.threads, dy, geo_of(a->dy, d, sw.rows), src, geo_of(a->x, d, sw.rows), sw, s, (long long)d.n, A, (T*)a->dx.data, geo_of(a->dx, d, sw.rows), partial);
         if (a->dweight || a->dbias) go(gn_parameter_gradient_kernel, ceil_div(d.C, 32), 1024, (const float*)partial, d.C, rows, a->dweight, a->dbias);
         return;
     }
