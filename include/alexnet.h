@@ -491,7 +491,8 @@ typedef struct alexnet_group_norm {
     float eps;
     int32_t reserved;
 } alexnet_group_norm_t;
-/* bytes of workspace of one call (0: invalid shape) */
+/* bytes of workspace of one call, at least 256 (0: invalid shape); 256 means that
+ * the call needs none, and workspace may be NULL */
 size_t alexnet_group_norm_workspace_bytes(const alexnet_group_norm_t* shape, int backward);
 
 typedef struct alexnet_group_norm_forward_args {
@@ -535,7 +536,8 @@ typedef struct alexnet_linear_weight_grad_args {
     void* workspace;                    /* 16-byte aligned */
     size_t workspace_bytes;
 } alexnet_linear_weight_grad_t;
-/* bytes of workspace of a call with these arguments (the workspace and dw need not be set; 0: invalid).  It is small where rows of dy and
+/* bytes of workspace of a call with these arguments (the workspace and dw need not be set; 0: invalid; 256: none
+ * is needed, and workspace may be NULL).  None is where rows of dy and
  * x start on 16-byte boundaries and there are many outputs; else it takes a copy of them, or partial sums. */
 size_t alexnet_linear_weight_grad_workspace_bytes(const alexnet_linear_weight_grad_t* args);
 int alexnet_linear_weight_grad(const alexnet_linear_weight_grad_t* args, void* stream, char* err, size_t err_len);

@@ -791,10 +791,11 @@ __global__ void __launch_bounds__(kSlThreads, 2) gn_slice_forward_kernel(const T
 }
 
 // The same for the backward pass: sums of dz and dz d per channel, c1 and c2 of the groups, then dx.  The samples' sums for dweight and dbias are added up in
-// shared memory and go to partial [block of the slice][2][C] at the end.
+// shared memory and go to sum1 and sum2 [block of the slice] at the end, rows sum_pitch apart; with one block per slice these are the gradients.
 template <typename T, int V, int SRC, int ACT>
 __global__ void __launch_bounds__(kSlThreads, 2) gn_slice_backward_kernel(const T* __restrict__ dy, const Geo gdy, const Source src, const Geo gx, const SliceWalk w, const NormShape sh,
-                                                                          long long samples, const BackwardArgs A, T* __restrict__ dx, const Geo gdx, float* __restrict__ partial) {
+                                                                          long long samples, const BackwardArgs A, T* __restrict__ dx, const Geo gdx, float* __restrict__ sum1,
+                                                                          float* __restrict__ sum2, long long sum_pitch) {
     kn::pdl_sync();
     extern __shared__ __align__(16) uint8_t smem[];
     using R = Raw<T, V>;
@@ -940,10 +941,9 @@ __global__ void __launch_bounds__(kSlThreads, 2) gn_slice_backward_kernel(const 
         __syncthreads();                                        // (the groups' rstd and results are free for the next sample)
     }
     if (b.n0 < samples) {
-        float* out = partial + b.n0 * 2 * w.C + b.c0;
         for (int c = tid; c < w.Cs; c += w.threads) {
-            out[c] = m.acc[c];
-            out[w.C + c] = m.acc[w.Cs + c];
+            if (sum1) sum1[b.n0 * sum_pitch + b.c0 + c] = m.acc[c];
+            if (sum2) sum2[b.n0 * sum_pitch + b.c0 + c] = m.acc[w.Cs + c];
         }
     }
 }

@@ -177,9 +177,6 @@ const char* check_shape(const alexnet_group_norm_t& s) {
     return nullptr;
 }
 NormShape norm_shape(const alexnet_group_norm_t& s) { return {s.channels, s.h * s.w, s.groups, s.channels / s.groups, fast_div((uint32_t)(s.channels / s.groups)), s.eps, s.activation}; }
-size_t forward_ws(const Walk& w, const Dims& d) { return (size_t)(d.n * w.chunks) * d.C * sizeof(float4); }
-size_t backward_ws(const Walk& w, const Dims& d, int groups) { return (size_t)(d.n * groups) * sizeof(float2) + (size_t)(d.n * w.chunks) * 2 * d.C * sizeof(float); }
-
 constexpr size_t kSmSmem = 228 * 1024, kCtaSmem = 227 * 1024;
 // How blocks that keep whole groups of a sample walk a tensor, `slot` bytes kept per vector of V channels; threads = 0: not at all.  As many slices as there are
 // (powers of two) until a slice takes at most 112 KB, so that two blocks share an SM, and further while the device is not full; but no rows below 64
@@ -230,9 +227,25 @@ long long slice_rows(Launcher& go, K* kernel, const SliceWalk& w, const Dims& d,
         if (go.e == cudaSuccess) go.e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&blocks, kernel, w.threads, smem);
         if (go.e == cudaSuccess) known[next++ % 16] = {(const void*)kernel, dev, w.threads, blocks, smem};
     }
-    return std::min<long long>(d.n, std::max(1, blocks * kSms / w.slices));
+    return std::min<long long>(d.n, std::max(1, std::min(blocks, 32) * kSms / w.slices));
 }
 
+// Bytes of workspace of a call with vectors of V channels; 0 where it takes one launch and leaves nothing between.
+template <int V>
+size_t forward_ws(const Dims& d, int groups, int dtype) {
+    const int elem = elem_bytes(dtype);
+    if (slice_walk<V>(d, groups, elem * V, elem, false).threads) return 0;
+    const Walk w = walk_of(d, V);
+    return (size_t)(d.n * w.chunks) * d.C * sizeof(float4);
+}
+template <int V>
+size_t backward_ws(const Dims& d, int groups, int dtype, bool kept) {
+    const int elem = elem_bytes(dtype);
+    const SliceWalk s = slice_walk<V>(d, groups, elem * V + (kept ? V + 1 : elem * V), kept ? 2 : elem, true);
+    if (s.threads) return d.n == 1 ? 0 : (size_t)std::min<long long>(d.n, 32 * kSms) * 2 * d.C * sizeof(float);      // (never more blocks of a slice than 32 per SM)
+    const Walk w = walk_of(d, V);
+    return (size_t)(d.n * groups) * sizeof(float2) + (size_t)(d.n * w.chunks) * 2 * d.C * sizeof(float);
+}
 template <typename T, int V, int ACT>
 void forward(Launcher& go, const alexnet_group_norm_forward_t* a, const Dims& d) {
     const Walk w = walk_of(d, V);
@@ -286,8 +299,9 @@ void backward(Launcher& go, const alexnet_group_norm_backward_t* a, const Dims& 
         const size_t smem = (size_t)sw.its * sw.threads * kSlot + slice_scratch<V>(sw, true);
         const long long rows = slice_rows(go, kernel, sw, d, smem);
         go.smem = smem;
-        go(kernel, rows * sw.slices, sw.threads, dy, geo_of(a->dy, d, sw.rows), src, geo_of(a->x, d, sw.rows), sw, s, (long long)d.n, A, (T*)a->dx.data, geo_of(a->dx, d, sw.rows), partial);
-        if (a->dweight || a->dbias) go(gn_parameter_gradient_kernel, ceil_div(d.C, 32), 1024, (const float*)partial, d.C, rows, a->dweight, a->dbias);
+        go(kernel, rows * sw.slices, sw.threads, dy, geo_of(a->dy, d, sw.rows), src, geo_of(a->x, d, sw.rows), sw, s, (long long)d.n, A, (T*)a->dx.data, geo_of(a->dx, d, sw.rows),
+           rows > 1 ? partial : a->dbias, rows > 1 ? partial + d.C : a->dweight, rows > 1 ? 2ll * d.C : 0ll);
+        if (rows > 1 && (a->dweight || a->dbias)) go(gn_parameter_gradient_kernel, ceil_div(d.C, 32), 1024, (const float*)partial, d.C, rows, a->dweight, a->dbias);
         return;
     }
     const Geo gdy = geo_of(a->dy, d, w.rows), gx = geo_of(a->x, d, w.rows), gdx = geo_of(a->dx, d, w.rows);
@@ -379,7 +393,7 @@ LinearPlan linear_plan(const alexnet_linear_weight_grad_t& a) {
     b.move_x = (uintptr_t)a.x.codes % 16 != 0 || a.n_in % 16 != 0;
     b.dy_at = (size_t)b.splits * (b.tiles - b.whole) * b.BN * 128 * b.cg * sizeof(float);
     b.x_at = b.dy_at + (b.move_dy ? ((size_t)a.rows * b.dy_pitch + 255) / 256 * 256 : 0);
-    b.bytes = b.x_at + (b.move_x ? (size_t)a.rows * b.x_pitch : 0) + 256;
+    b.bytes = b.x_at + (b.move_x ? ((size_t)a.rows * b.x_pitch + 255) / 256 * 256 : 0);      // 0: none needed
     return b;
 }
 long long repitch_grid(long long rows, long long pitch) { return std::min<long long>(16 * kSms, ceil_div(rows * (pitch / 16), 256)); }
@@ -397,13 +411,13 @@ int alexnet_checkpoint_decode(const alexnet_checkpoint_args_t* args, void* strea
 size_t alexnet_group_norm_workspace_bytes(const alexnet_group_norm_t* s, int backward) {
     if (!s || check_shape(*s)) return 0;
     const Dims d{s->n, s->h, s->w, s->channels};
+    // by sizes alone, so for any alignment, and for x in either form
     size_t bytes = 0;
-    for (int V : {8, 1})
-        if (d.C % V == 0) {
-            const Walk w = walk_of(d, V);
-            bytes = std::max(bytes, backward ? backward_ws(w, d, s->groups) : forward_ws(w, d));
-        }
-    return (bytes + 256) / 256 * 256;
+    for (int kept = 0; kept <= (backward ? 1 : 0); ++kept) {
+        if (d.C % 8 == 0) bytes = std::max(bytes, backward ? backward_ws<8>(d, s->groups, s->dtype, kept) : forward_ws<8>(d, s->groups, s->dtype));
+        bytes = std::max(bytes, backward ? backward_ws<1>(d, s->groups, s->dtype, kept) : forward_ws<1>(d, s->groups, s->dtype));
+    }
+    return bytes ? (bytes + 511) / 256 * 256 : 256;
 }
 
 int alexnet_group_norm_forward(const alexnet_group_norm_forward_t* a, void* stream, char* err_buf, size_t err_len) {
@@ -418,13 +432,14 @@ int alexnet_group_norm_forward(const alexnet_group_norm_forward_t* a, void* stre
         if (k->codes || k->scales)
             if (const char* m = check_codes(*k, d)) return err.arg(m);
     if (d.n == 0) return ALEXNET_OK;
-    if (!a->mean || !a->rstd || !a->workspace) return err.arg("NULL pointer");
+    if (!a->mean || !a->rstd) return err.arg("NULL pointer");
     if (a->x.data == a->y.data) return err.arg("y must not share memory with x");
-    if ((uintptr_t)a->workspace % 16 || a->workspace_bytes < alexnet_group_norm_workspace_bytes(&s, 0)) return err.arg("the workspace is too small or not 16-byte aligned");
     if (grid_of(walk_of(d, 1), d) > kMaxGrid) return err.arg("the tensor is too large");
     bool vec = vec_ok(a->x, d, s.dtype) && vec_ok(a->y, d, s.dtype);
     if (a->keep_x.codes) vec = vec && vec_ok(a->keep_x, d);
     if (a->keep_y.codes) vec = vec && vec_ok(a->keep_y, d);
+    const size_t need = vec ? forward_ws<8>(d, s.groups, s.dtype) : forward_ws<1>(d, s.groups, s.dtype);
+    if (need && (!a->workspace || (uintptr_t)a->workspace % 16 || a->workspace_bytes < need)) return err.arg("the workspace is too small or not 16-byte aligned");
     Launcher go{(cudaStream_t)stream};
     switch (s.dtype) {
     case ALEXNET_DTYPE_BF16: vec ? forward<bf16, 8>(go, a, d) : forward<bf16, 1>(go, a, d); break;
@@ -451,11 +466,12 @@ int alexnet_group_norm_backward(const alexnet_group_norm_backward_t* a, void* st
             if (p && e == cudaSuccess) e = cudaMemsetAsync(p, 0, (size_t)d.C * sizeof(float), (cudaStream_t)stream);
         return e == cudaSuccess ? ALEXNET_OK : err.cuda(e);
     }
-    if (!a->mean || !a->rstd || !a->workspace) return err.arg("NULL pointer");
+    if (!a->mean || !a->rstd) return err.arg("NULL pointer");
     if (a->dx.data == a->x.data || a->dx.data == a->dy.data) return err.arg("dx must not share memory with x or dy");
-    if ((uintptr_t)a->workspace % 16 || a->workspace_bytes < alexnet_group_norm_workspace_bytes(&s, 1)) return err.arg("the workspace is too small or not 16-byte aligned");
     if (grid_of(walk_of(d, 1), d) > kMaxGrid) return err.arg("the tensor is too large");
     const bool vec = vec_ok(a->dy, d, s.dtype) && vec_ok(a->dx, d, s.dtype) && (kept ? vec_ok(a->kept, d) : vec_ok(a->x, d, s.dtype));
+    const size_t need = vec ? backward_ws<8>(d, s.groups, s.dtype, kept) : backward_ws<1>(d, s.groups, s.dtype, kept);
+    if (need && (!a->workspace || (uintptr_t)a->workspace % 16 || a->workspace_bytes < need)) return err.arg("the workspace is too small or not 16-byte aligned");
     Launcher go{(cudaStream_t)stream};
     switch (s.dtype) {
     case ALEXNET_DTYPE_BF16: vec ? backward<bf16, 8>(go, a, d) : backward<bf16, 1>(go, a, d); break;
@@ -467,7 +483,8 @@ int alexnet_group_norm_backward(const alexnet_group_norm_backward_t* a, void* st
 
 size_t alexnet_linear_weight_grad_workspace_bytes(const alexnet_linear_weight_grad_t* a) {
     if (!a || check_linear(*a)) return 0;
-    return linear_plan(*a).bytes;
+    const size_t bytes = linear_plan(*a).bytes;
+    return bytes ? bytes + 256 : 256;
 }
 
 int alexnet_linear_weight_grad(const alexnet_linear_weight_grad_t* a, void* stream, char* err_buf, size_t err_len) {
@@ -477,7 +494,7 @@ int alexnet_linear_weight_grad(const alexnet_linear_weight_grad_t* a, void* stre
     if (!a->dw || (uintptr_t)a->dw % 4) return err.arg("dw is NULL or not aligned");
     if (a->rows > 0 && (!a->dy || !a->x.codes || !a->x.scales)) return err.arg("NULL pointer");
     const LinearPlan pl = linear_plan(*a);
-    if (!a->workspace || (uintptr_t)a->workspace % 16 || a->workspace_bytes < pl.bytes) return err.arg("the workspace is too small or not 16-byte aligned");
+    if (pl.bytes && (!a->workspace || (uintptr_t)a->workspace % 16 || a->workspace_bytes < pl.bytes)) return err.arg("the workspace is too small or not 16-byte aligned");
     cudaStream_t st = (cudaStream_t)stream;
     if (a->rows == 0) {
         const cudaError_t e = cudaMemsetAsync(a->dw, 0, (size_t)a->n_in * a->n_out * sizeof(float), st);

@@ -89,61 +89,53 @@ def _name(table, key, what):
         _refuse(f"unknown {what} {key!r}: one of {', '.join(map(str, table))}")
 
 
-class _Call:
-    """The device, the stream and the error buffer of one call."""
-    __slots__ = ("device", "stream", "_device_guard", "_stream_guard")
-
-    def __init__(self, tensor, stream):
-        self.device = tensor.device
-        if self.device.type != "cuda":
-            _refuse("the tensors must be on a CUDA device (there is no CPU fallback)")
-        self._device_guard = self._stream_guard = None
-        if stream is not None:
-            if stream.device != self.device:
-                _refuse(f"the stream belongs to {stream.device}, the tensors are on {self.device}")
-            self._stream_guard = torch.cuda.stream(stream)        # sets the device too
-            self.stream = stream.cuda_stream
-        else:
-            if torch.cuda.current_device() != self.device.index:
-                self._device_guard = torch.cuda.device(self.device)
-            self.stream = torch.cuda.current_stream(self.device).cuda_stream
-
-    def __enter__(self):
-        for guard in (self._device_guard, self._stream_guard):
-            if guard is not None:
-                guard.__enter__()
-        return self
-
-    def __exit__(self, *exc):
-        for guard in (self._stream_guard, self._device_guard):
-            if guard is not None:
-                guard.__exit__(*exc)
-
-    def run(self, function, block):
-        err = getattr(_local, "err", None)
-        if err is None:
-            err = _local.err = ctypes.create_string_buffer(256)
-        rc = function(block, self.stream, err, 256)
-        if rc != OK:
-            raise AlexNetError(rc, err.value.decode())
+# The calls below cost the host about ten microseconds, most of it in the tensors they create; so they are written without helper objects.
+_current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
 
 
-def _same(call, *tensors):
-    for t in tensors:
-        if t is not None and t.device != call.device:
-            _refuse(f"tensors on {t.device} and {call.device}: all of a call are on one device")
+def _raw_stream(index):
+    return torch.cuda.current_stream(index).cuda_stream
+
+
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", _raw_stream)
+
+
+def _elsewhere(index, stream):
+    """The context in which to repeat a call whose tensors are not on the current device, or that was given a stream."""
+    if index < 0:
+        _refuse("the tensors must be on a CUDA device (there is no CPU fallback)")
+    if stream is None:
+        return torch.cuda.device(index)
+    if stream.device.index != index:
+        _refuse(f"the stream belongs to {stream.device}, the tensors are on cuda:{index}")
+    return torch.cuda.stream(stream)                # sets the device too
+
+
+def _run(function, block, index):
+    err = getattr(_local, "err", None)
+    if err is None:
+        err = _local.err = ctypes.create_string_buffer(256)
+    rc = function(block, _raw_stream(index), err, 256)
+    if rc != OK:
+        raise AlexNetError(rc, err.value.decode())
+
+
+def _other_device():
+    _refuse("all tensors of a call must be on one device")
 
 
 def _rows(t, what):
     """(n, h, w, c) and the strides of n, h, w of a channels-last tensor of two to four dimensions."""
-    d, shape = t.dim(), t.shape
+    shape, st = t.shape, t.stride()
+    d = len(shape)
+    if d == 4:
+        if st[3] != 1 and shape[3] > 1:
+            _refuse(f"the channels of {what} are not adjacent")
+        return shape, st[:3]
     if d < 2 or d > 4:
         _refuse(f"{what} has {d} dimensions: [n, h, w, c], [n, l, c] or [n, c] is wanted")
-    st = t.stride()
     if st[-1] != 1 and shape[-1] > 1:
         _refuse(f"the channels of {what} are not adjacent")
-    if d == 4:
-        return (shape[0], shape[1], shape[2], shape[3]), st[:3]
     if d == 3:
         return (shape[0], 1, shape[1], shape[2]), (st[0], 0, st[1])
     return (shape[0], 1, 1, shape[1]), (st[0], 0, 0)
@@ -162,37 +154,46 @@ def _rows_any(t, what):
     return _rows(t, what)
 
 
-def _vector(t, n, what):
+def _vector(t, n, what, index):
     if t is None:
         return 0
-    if t.dtype != torch.float32 or t.shape != (n,) or not t.is_contiguous():
+    if t.dtype is not torch.float32 or t.dim() != 1 or t.numel() != n or not t.is_contiguous():
         _refuse(f"{what} must be a dense float32 vector of {n}")
+    if t.get_device() != index:
+        _other_device()
     return t.data_ptr()
 
 
-def _output(out, like_shape, dtype, what, device):
-    if out is None:
-        return torch.empty(like_shape, dtype=dtype, device=device)
-    if out.dtype != dtype or out.shape != like_shape:
-        _refuse(f"{what} must be {dtype} {tuple(like_shape)}, not {out.dtype} {tuple(out.shape)}")
+def _output(out, shape, dtype, index):
+    if out.dtype is not dtype or out.shape != shape:
+        _refuse(f"out must be {dtype} {tuple(shape)}, not {out.dtype} {tuple(out.shape)}")
+    if out.get_device() != index:
+        _other_device()
     return out
 
 
-def _new_checkpoint(shape, fmt, device):
-    codes = torch.empty(shape, dtype=_name(CODE_DTYPES, fmt, "checkpoint format"), device=device)
-    return Checkpoint(codes, torch.empty((*shape[:-1], (shape[-1] + 31) // 32), dtype=torch.uint8, device=device))
+def _new_checkpoint(x, fmt):
+    shape = x.shape
+    k = Checkpoint.__new__(Checkpoint)
+    k.codes = x.new_empty(shape, dtype=_name(CODE_DTYPES, fmt, "checkpoint format"))
+    k.scales = x.new_empty((*shape[:-1], (shape[-1] + 31) // 32), dtype=torch.uint8)
+    return k
+
+
+_NOT_KEPT = (0, 0, 0, 0)
 
 
 def _kept(k):
-    return (0, 0, 0, 0) if k is None else (k.codes.data_ptr(), k.scales.data_ptr(), FORMATS[_FORMAT_OF[k.codes.dtype]], 0)
+    return k.codes.data_ptr(), k.scales.data_ptr(), FORMATS[_FORMAT_OF[k.codes.dtype]], 0
 
 
 @functools.lru_cache(maxsize=1024)
 def _norm_workspace(shape, backward):
+    """bytes of workspace for the sizes (0: the call needs none)"""
     n = int(_alexnet.load_library().alexnet_group_norm_workspace_bytes(_pack_shape(*shape), backward))
     if n == 0:
-        raise AlexNetError(ERR_ARG, f"invalid group norm: n, h, w, channels, groups = {shape[:5]}, eps = {shape[7]}")
-    return n
+        raise AlexNetError(ERR_ARG, f"invalid group norm: n, h, w, channels, groups = {tuple(shape[:5])}, eps = {shape[7]}")
+    return n if n > 256 else 0
 
 
 @functools.lru_cache(maxsize=1024)
@@ -202,7 +203,7 @@ def _linear_workspace(rows, n_in, n_out, stride, dy_offset, codes_offset, fmt):
         _pack_linear(rows, n_in, n_out, 16 + dy_offset, stride, 16 + codes_offset, 16, fmt, 0, 0, 0, 0)))
     if n == 0:
         raise AlexNetError(ERR_ARG, f"invalid linear weight gradient: rows, in, out = {rows, n_in, n_out}, stride {stride}")
-    return n
+    return n if n > 256 else 0
 
 
 def check():
@@ -214,28 +215,34 @@ def check():
 
 def checkpoint_encode(x, format="int8", out=None, stream=None):
     """The 8-bit checkpoint of x: 33 bytes for 32 values.  out: a Checkpoint to write instead of a new one."""
+    index = x.get_device()
+    if stream is not None or index < 0 or index != _current_device():
+        with _elsewhere(index, stream):
+            return checkpoint_encode(x, format, out)
     dtype = _name(DTYPES, x.dtype, "dtype")
-    lib = _alexnet.load_library()
-    with _Call(x, stream) as call:
-        (n, h, w, c), st = _rows_any(x, "x")
-        if out is None:
-            out = _new_checkpoint(x.shape, format, call.device)
-        elif out.shape != x.shape or out.codes.dtype != _name(CODE_DTYPES, format, "checkpoint format"):
+    (n, h, w, c), st = _rows_any(x, "x")
+    if out is None:
+        out = _new_checkpoint(x, format)
+    else:
+        if out.shape != x.shape or out.codes.dtype != _name(CODE_DTYPES, format, "checkpoint format"):
             _refuse("out is a checkpoint of another shape or format")
-        _same(call, out.codes)
-        call.run(lib.alexnet_checkpoint_encode, _pack_checkpoint(n, h, w, c, dtype, x.data_ptr(), *st, *_kept(out)))
+        if out.codes.get_device() != index:
+            _other_device()
+    _run(_alexnet.load_library().alexnet_checkpoint_encode, _pack_checkpoint(n, h, w, c, dtype, x.data_ptr(), *st, *_kept(out)), index)
     return out
 
 
 def checkpoint_decode(checkpoint, dtype=torch.bfloat16, out=None, stream=None):
     """The values that a checkpoint stands for, rounded to dtype (exact in bfloat16 and float32)."""
+    codes = checkpoint.codes
+    index = codes.get_device()
+    if stream is not None or index < 0 or index != _current_device():
+        with _elsewhere(index, stream):
+            return checkpoint_decode(checkpoint, dtype, out)
     code = _name(DTYPES, dtype, "dtype")
-    lib = _alexnet.load_library()
-    with _Call(checkpoint.codes, stream) as call:
-        out = _output(out, checkpoint.shape, dtype, "out", call.device)
-        _same(call, out)
-        (n, h, w, c), st = _rows_any(out, "out")
-        call.run(lib.alexnet_checkpoint_decode, _pack_checkpoint(n, h, w, c, code, out.data_ptr(), *st, *_kept(checkpoint)))
+    out = codes.new_empty(codes.shape, dtype=dtype) if out is None else _output(out, codes.shape, dtype, index)
+    (n, h, w, c), st = _rows_any(out, "out")
+    _run(_alexnet.load_library().alexnet_checkpoint_decode, _pack_checkpoint(n, h, w, c, code, out.data_ptr(), *st, *_kept(checkpoint)), index)
     return out
 
 
@@ -244,61 +251,61 @@ def group_norm(x, groups, weight=None, bias=None, eps=1e-5, activation="none", k
 
     x [n, h, w, c], [n, l, c] or [n, c]; activation "none", "relu" or "silu"; keep_input / keep_output: "int8" or "e4m3" writes a
     checkpoint of x (what group_norm_backward needs) or of y (what the weight gradient of a layer behind needs) on the way."""
-    dtype, act = _name(DTYPES, x.dtype, "dtype"), _name(ACTIVATIONS, activation, "activation")
-    lib = _alexnet.load_library()
-    with _Call(x, stream) as call:
-        (n, h, w, c), xs = _rows(x, "x")
-        shape = (n, h, w, c, groups, dtype, act, eps, 0)
-        nbytes = _norm_workspace(shape, 0)
-        wp, bp = _vector(weight, c, "weight"), _vector(bias, c, "bias")
-        device = call.device
-        y = _output(out, x.shape, x.dtype, "out", device)
-        _, ys = _rows(y, "out")
-        stats = torch.empty((2, n, groups), dtype=torch.float32, device=device)
-        mean, rstd = stats.unbind(0)
-        kx = None if keep_input is None else _new_checkpoint(x.shape, keep_input, device)
-        ky = None if keep_output is None else _new_checkpoint(x.shape, keep_output, device)
-        ws = torch.empty(nbytes, dtype=torch.uint8, device=device)
-        _same(call, y, weight, bias)
-        sp = stats.data_ptr()
-        call.run(lib.alexnet_group_norm_forward,
-                 _pack_forward(*shape, x.data_ptr(), *xs, y.data_ptr(), *ys, wp, bp, sp, sp + 4 * n * groups, *_kept(kx), *_kept(ky), ws.data_ptr(), nbytes))
+    index = x.get_device()
+    if stream is not None or index < 0 or index != _current_device():
+        with _elsewhere(index, stream):
+            return group_norm(x, groups, weight, bias, eps, activation, keep_input, keep_output, out)
+    (n, h, w, c), xs = _rows(x, "x")
+    shape = (n, h, w, c, groups, _name(DTYPES, x.dtype, "dtype"), _name(ACTIVATIONS, activation, "activation"), eps, 0)
+    nbytes = _norm_workspace(shape, 0)
+    y = torch.empty(x.shape, dtype=x.dtype, device=x.device) if out is None else _output(out, x.shape, x.dtype, index)
+    mean, rstd = x.new_empty((n, groups), dtype=torch.float32), x.new_empty((n, groups), dtype=torch.float32)
+    kx = ky = None
+    pkx = pky = _NOT_KEPT
+    if keep_input is not None:
+        kx = _new_checkpoint(x, keep_input)
+        pkx = _kept(kx)
+    if keep_output is not None:
+        ky = _new_checkpoint(x, keep_output)
+        pky = _kept(ky)
+    ws = x.new_empty(nbytes, dtype=torch.uint8) if nbytes else None
+    _run(_alexnet.load_library().alexnet_group_norm_forward,
+         _pack_forward(*shape, x.data_ptr(), *xs, y.data_ptr(), *_rows(y, "out")[1], _vector(weight, c, "weight", index), _vector(bias, c, "bias", index), mean.data_ptr(), rstd.data_ptr(),
+                       *pkx, *pky, 0 if ws is None else ws.data_ptr(), nbytes), index)
     return GroupNormResult(y, mean, rstd, kx, ky)
 
 
 def group_norm_backward(dy, x, mean, rstd, weight=None, bias=None, activation="none", out=None, stream=None):
     """(dx, dweight, dbias) of group_norm for the gradient dy of y.  x: the tensor that group_norm was given, or a Checkpoint of it; mean and
     rstd [n, groups] as group_norm returned them.  out: the tensor that takes dx."""
-    dtype, act = _name(DTYPES, dy.dtype, "dtype"), _name(ACTIVATIONS, activation, "activation")
-    lib = _alexnet.load_library()
-    with _Call(dy, stream) as call:
-        (n, h, w, c), ds = _rows(dy, "dy")
-        if x.shape != dy.shape:
-            _refuse(f"x {tuple(x.shape)} and dy {tuple(dy.shape)} differ in shape")
-        if isinstance(x, Checkpoint):
-            kept, xv = _kept(x), (0, 0, 0, 0)
-            _same(call, x.codes)
-        else:
-            if x.dtype != dy.dtype:
-                _refuse(f"x is {x.dtype}, dy {dy.dtype}")
-            kept, xv = (0, 0, 0, 0), (x.data_ptr(), *_rows(x, "x")[1])
-            _same(call, x)
-        if mean.dim() != 2 or mean.shape[0] != n or mean.dtype != torch.float32 or rstd.shape != mean.shape or rstd.dtype != torch.float32 \
-                or not mean.is_contiguous() or not rstd.is_contiguous():
-            _refuse("mean and rstd must be dense float32 [n, groups]")
-        shape = (n, h, w, c, mean.shape[1], dtype, act, 1.0, 0)
-        nbytes = _norm_workspace(shape, 1)
-        wp, bp = _vector(weight, c, "weight"), _vector(bias, c, "bias")
-        device = call.device
-        dx = _output(out, dy.shape, dy.dtype, "out", device)
-        _, os = _rows(dx, "out")
-        grads = torch.empty((2, c), dtype=torch.float32, device=device)
-        ws = torch.empty(nbytes, dtype=torch.uint8, device=device)
-        _same(call, dx, mean, rstd, weight, bias)
-        gp = grads.data_ptr()
-        call.run(lib.alexnet_group_norm_backward,
-                 _pack_backward(*shape, dy.data_ptr(), *ds, *xv, dx.data_ptr(), *os, *kept, mean.data_ptr(), rstd.data_ptr(), wp, bp, gp, gp + 4 * c, ws.data_ptr(), nbytes))
-    dweight, dbias = grads.unbind(0)
+    index = dy.get_device()
+    if stream is not None or index < 0 or index != _current_device():
+        with _elsewhere(index, stream):
+            return group_norm_backward(dy, x, mean, rstd, weight, bias, activation, out)
+    (n, h, w, c), ds = _rows(dy, "dy")
+    if x.shape != dy.shape:
+        _refuse(f"x {tuple(x.shape)} and dy {tuple(dy.shape)} differ in shape")
+    if isinstance(x, Checkpoint):
+        kept, xv = _kept(x), _NOT_KEPT
+        other = x.codes.get_device() != index
+    else:
+        if x.dtype is not dy.dtype:
+            _refuse(f"x is {x.dtype}, dy {dy.dtype}")
+        kept, xv = _NOT_KEPT, (x.data_ptr(), *_rows(x, "x")[1])
+        other = x.get_device() != index
+    if mean.dim() != 2 or mean.shape[0] != n or mean.dtype is not torch.float32 or rstd.shape != mean.shape or rstd.dtype is not torch.float32 \
+            or not mean.is_contiguous() or not rstd.is_contiguous():
+        _refuse("mean and rstd must be dense float32 [n, groups]")
+    if other or mean.get_device() != index or rstd.get_device() != index:
+        _other_device()
+    shape = (n, h, w, c, mean.shape[1], _name(DTYPES, dy.dtype, "dtype"), _name(ACTIVATIONS, activation, "activation"), 1.0, 0)
+    nbytes = _norm_workspace(shape, 1)
+    dx = torch.empty(dy.shape, dtype=dy.dtype, device=dy.device) if out is None else _output(out, dy.shape, dy.dtype, index)
+    dweight, dbias = dy.new_empty(c, dtype=torch.float32), dy.new_empty(c, dtype=torch.float32)
+    ws = dy.new_empty(nbytes, dtype=torch.uint8) if nbytes else None
+    _run(_alexnet.load_library().alexnet_group_norm_backward,
+         _pack_backward(*shape, dy.data_ptr(), *ds, *xv, dx.data_ptr(), *_rows(dx, "out")[1], *kept, mean.data_ptr(), rstd.data_ptr(), _vector(weight, c, "weight", index),
+                        _vector(bias, c, "bias", index), dweight.data_ptr(), dbias.data_ptr(), 0 if ws is None else ws.data_ptr(), nbytes), index)
     return dx, dweight, dbias
 
 
@@ -306,26 +313,34 @@ def linear_weight_grad(dy, x, out=None, stream=None):
     """dw [out features, in features] = dy^T x, float32, for dy bfloat16 [..., out features] and a Checkpoint x of [..., in features]."""
     if not isinstance(x, Checkpoint):
         _refuse("x must be a Checkpoint")
-    if dy.dtype != torch.bfloat16:
+    if dy.dtype is not torch.bfloat16:
         _refuse(f"dy must be bfloat16, not {dy.dtype}")
-    if dy.dim() < 1 or dy.shape[:-1] != x.shape[:-1]:
-        _refuse(f"dy {tuple(dy.shape)} and x {tuple(x.shape)} differ in their rows")
-    lib = _alexnet.load_library()
-    with _Call(dy, stream) as call:
-        n_in, n_out = x.shape[-1], dy.shape[-1]
-        if dy.dim() != 2:
-            if not dy.is_contiguous():
-                _refuse("dy of other than two dimensions must be dense")
-            dy = dy.view(-1, n_out)
-        if dy.stride(1) != 1 and n_out > 1:
-            _refuse("the features of dy are not adjacent")
-        rows = dy.shape[0]
-        dw = _output(out, (n_out, n_in), torch.float32, "out", call.device)
+    codes = x.codes
+    if dy.dim() < 1 or dy.shape[:-1] != codes.shape[:-1]:
+        _refuse(f"dy {tuple(dy.shape)} and x {tuple(codes.shape)} differ in their rows")
+    index = dy.get_device()
+    if stream is not None or index < 0 or index != _current_device():
+        with _elsewhere(index, stream):
+            return linear_weight_grad(dy, x, out)
+    n_in, n_out = codes.shape[-1], dy.shape[-1]
+    if dy.dim() != 2:
+        if not dy.is_contiguous():
+            _refuse("dy of other than two dimensions must be dense")
+        dy = dy.view(-1, n_out)
+    rows, (stride, last) = dy.shape[0], dy.stride()
+    if last != 1 and n_out > 1:
+        _refuse("the features of dy are not adjacent")
+    if codes.get_device() != index:
+        _other_device()
+    if out is None:
+        dw = dy.new_empty((n_out, n_in), dtype=torch.float32)
+    else:
+        dw = _output(out, (n_out, n_in), torch.float32, index)
         if not dw.is_contiguous():
             _refuse("out must be dense")
-        _same(call, x.codes, dw)
-        nbytes = _linear_workspace(rows, n_in, n_out, dy.stride(0), dy.data_ptr() % 16, x.codes.data_ptr() % 16, FORMATS[x.format])
-        ws = torch.empty(nbytes, dtype=torch.uint8, device=call.device)
-        call.run(lib.alexnet_linear_weight_grad,
-                 _pack_linear(rows, n_in, n_out, dy.data_ptr(), dy.stride(0), *_kept(x), dw.data_ptr(), ws.data_ptr(), nbytes))
+    p, q = dy.data_ptr(), codes.data_ptr()
+    nbytes = _linear_workspace(rows, n_in, n_out, stride, p % 16, q % 16, FORMATS[x.format])
+    ws = dy.new_empty(nbytes, dtype=torch.uint8) if nbytes else None
+    _run(_alexnet.load_library().alexnet_linear_weight_grad,
+         _pack_linear(rows, n_in, n_out, p, stride, *_kept(x), dw.data_ptr(), 0 if ws is None else ws.data_ptr(), nbytes), index)
     return dw

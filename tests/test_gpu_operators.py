@@ -605,6 +605,9 @@ def test_refusals_on_the_gpu(ops):
             f(*args, **kw)
         assert e.value.code == A.ERR_ARG
     refused("groups", ops.group_norm, x, 7)
+    refused("dtype", ops.group_norm, x.double(), 8)
+    refused("activation", ops.group_norm, x, 8, activation="gelu")
+    refused("dtype", ops.checkpoint_decode, ops.checkpoint_encode(x), torch.int8)
     refused("eps", ops.group_norm, x, 8, eps=0.0)
     refused("adjacent", ops.group_norm, x.permute(0, 3, 1, 2), 4)
     refused("dimensions", ops.group_norm, x[0, 0, 0], 8)

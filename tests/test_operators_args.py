@@ -77,8 +77,11 @@ def forward_block(s=shape(), x=VIEW(3, 4, 64), y=VIEW(3, 4, 64, 2 * P), mean=P, 
     return ops._pack_forward(*s, *x, *y, P, P, mean, rstd, *kx, *ky, ws, nbytes)
 
 
-FORWARD = [(dict(x=VIEW(3, 4, 64, 0)), "NULL"), (dict(y=VIEW(3, 4, 64, 0)), "NULL"), (dict(mean=0), "NULL"), (dict(rstd=0), "NULL"), (dict(ws=0), "NULL"),
-           (dict(x=VIEW(3, 4, 64, P + 1)), "aligned"), (dict(s=shape(dtype=2), x=VIEW(3, 4, 64, P + 2)), "aligned"), (dict(ws=P + 8), "workspace"), (dict(nbytes=16), "workspace"),
+# a sample that no block can keep, so that the call needs its workspace
+LARGE = dict(s=shape(h=400, w=400), x=VIEW(400, 400, 64), y=VIEW(400, 400, 64, 2 * P))
+LARGE_BACK = dict(s=shape(h=400, w=400), dy=VIEW(400, 400, 64), x=VIEW(400, 400, 64, 2 * P), dx=VIEW(400, 400, 64, 3 * P))
+FORWARD = [(dict(x=VIEW(3, 4, 64, 0)), "NULL"), (dict(y=VIEW(3, 4, 64, 0)), "NULL"), (dict(mean=0), "NULL"), (dict(rstd=0), "NULL"), (dict(LARGE, ws=0), "workspace"),
+           (dict(x=VIEW(3, 4, 64, P + 1)), "aligned"), (dict(s=shape(dtype=2), x=VIEW(3, 4, 64, P + 2)), "aligned"), (dict(LARGE, ws=P + 8), "workspace"), (dict(LARGE, nbytes=16), "workspace"),
            (dict(y=VIEW(3, 4, 64)), "share"), (dict(x=(P, -768, 256, 64)), "stride"), (dict(x=(P, 768, 1 << 50, 64)), "stride"),
            (dict(y=(2 * P, 768, 256, 63)), "overlap"), (dict(y=(2 * P, 768, 255, 64)), "overlap"), (dict(y=(2 * P, 0, 256, 64)), "overlap"),
            (dict(y=(2 * P, 64, 256, 64)), "overlap"),
@@ -97,7 +100,8 @@ def backward_block(s=shape(), dy=VIEW(3, 4, 64), x=VIEW(3, 4, 64, 2 * P), dx=VIE
 
 BACKWARD = [(dict(dy=VIEW(3, 4, 64, 0)), "NULL"), (dict(x=VIEW(3, 4, 64, 0)), "NULL"), (dict(dx=VIEW(3, 4, 64, 0)), "NULL"), (dict(mean=0), "NULL"), (dict(rstd=0), "NULL"),
             (dict(kept=KEPT), "twice"), (dict(x=NONE, kept=(P, P, 9, 0)), "format"), (dict(x=NONE, kept=(P, 0, 1, 0)), "NULL"), (dict(dx=VIEW(3, 4, 64)), "share"),
-            (dict(dx=VIEW(3, 4, 64, 2 * P)), "share"), (dict(dx=(3 * P, 768, 0, 64)), "overlap"), (dict(ws=P + 4), "workspace"), (dict(nbytes=0), "workspace"), (dict(ws=0), "NULL")]
+            (dict(dx=VIEW(3, 4, 64, 2 * P)), "share"), (dict(dx=(3 * P, 768, 0, 64)), "overlap"), (dict(LARGE_BACK, ws=P + 4), "workspace"), (dict(LARGE_BACK, nbytes=0), "workspace"),
+            (dict(LARGE_BACK, ws=0), "workspace")]
 
 
 @pytest.mark.parametrize("bad,word", BACKWARD)
@@ -123,7 +127,7 @@ def test_checkpoint_refuses(lib, bad, word):
 
 LINEAR = [(dict(rows=-1), "rows"), (dict(rows=1 << 31), "rows"), (dict(n_in=0), "features"), (dict(n_out=0), "features"), (dict(n_in=1 << 21), "features"), (dict(dy=0), "NULL"),
           (dict(dy=P + 1), "aligned"), (dict(stride=-8), "stride"), (dict(kept=(P, 0, 1, 0)), "NULL"), (dict(kept=(0, P, 1, 0)), "NULL"), (dict(kept=(P, P, 0, 0)), "format"), (dict(dw=0), "dw"),
-          (dict(dw=P + 2), "dw"), (dict(ws=0), "workspace"), (dict(ws=P + 8), "workspace"), (dict(nbytes=0), "workspace")]
+          (dict(dw=P + 2), "dw"), (dict(rows=4096, ws=0), "workspace"), (dict(rows=4096, ws=P + 8), "workspace"), (dict(stride=65, nbytes=0), "workspace")]
 
 
 @pytest.mark.parametrize("bad,word", LINEAR)
@@ -133,6 +137,15 @@ def test_linear_weight_grad_refuses(lib, bad, word):
     assert rc == A.ERR_ARG and word in msg, msg
     if word in ("rows", "features", "format", "stride"):
         assert lib.alexnet_linear_weight_grad_workspace_bytes(ops._pack_linear(a["rows"], a["n_in"], a["n_out"], a["dy"], a["stride"], *a["kept"], 0, 0, 0)) == 0
+
+
+def test_small_calls_need_no_workspace(lib):
+    """256 bytes say so; the larger ones name what they need."""
+    for backward in (0, 1):
+        assert lib.alexnet_group_norm_workspace_bytes(ops._pack_shape(*shape(n=1, h=13, w=13, c=384, groups=32)), backward) == 256
+        assert lib.alexnet_group_norm_workspace_bytes(ops._pack_shape(*shape(h=400, w=400)), backward) > 256
+    small, large = (ops._pack_linear(rows, 64, 64, P, 64, *KEPT, 0, 0, 0) for rows in (64, 4096))
+    assert lib.alexnet_linear_weight_grad_workspace_bytes(small) == 256 and lib.alexnet_linear_weight_grad_workspace_bytes(large) > 4 * 64 * 64 * 4
 
 
 def test_null_blocks_and_no_samples(lib):
@@ -158,9 +171,6 @@ def test_binding_refuses(lib):
     refused("no CPU fallback", ops.checkpoint_decode, ops.Checkpoint(codes, scales))
     refused("no CPU fallback", ops.group_norm_backward, x, x, torch.zeros(2, 8), torch.zeros(2, 8))
     refused("no CPU fallback", ops.linear_weight_grad, torch.zeros(2, 8, dtype=torch.bfloat16), ops.Checkpoint(codes, scales))
-    refused("dtype", ops.group_norm, x.double(), 8)
-    refused("activation", ops.group_norm, x, 8, activation="gelu")
-    refused("dtype", ops.checkpoint_decode, ops.Checkpoint(codes, scales), torch.int8)
     refused("int8", ops.Checkpoint, codes.float(), scales)
     refused("uint8", ops.Checkpoint, codes, scales.int())
     refused("rounded up", ops.Checkpoint, codes, scales[:, :1])
