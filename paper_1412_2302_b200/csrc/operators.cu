@@ -182,7 +182,7 @@ constexpr size_t kSmSmem = 228 * 1024, kCtaSmem = 227 * 1024;
 // (powers of two) until a slice takes at most 112 KB, so that two blocks share an SM, and further while the device is not full; but no rows below 64
 // bytes, which cost more sectors than they use.
 template <int V>
-SliceWalk slice_walk(const Dims& d, int groups, int slot, int elem, bool backward) {
+SliceWalk find_slice_walk(const Dims& d, int groups, int slot, int elem, bool backward) {
     SliceWalk best{}, w{};
     w.C = d.C; w.HW = d.h * d.w;
     const int cg = d.C / groups;
@@ -211,6 +211,18 @@ SliceWalk slice_walk(const Dims& d, int groups, int slot, int elem, bool backwar
     while (best.lanes < 32 && best.lanes * 2 * best.groups <= best.threads && best.lanes < cg * best.rows) best.lanes *= 2;
     for (best.lc = 1; best.lc < best.lanes && best.lc < cg; best.lc *= 2) ++best.lc_shift;
     return best;
+}
+// (found once for the sizes of a thread's last calls: the search takes 2 us)
+template <int V>
+const SliceWalk& slice_walk(const Dims& d, int groups, int slot, int elem, bool backward) {
+    struct Known { long long n = -1; int h, w, C, groups, slot, elem; bool backward; SliceWalk walk; };
+    static thread_local Known known[16];
+    static thread_local unsigned next = 0;
+    for (const Known& q : known)
+        if (q.n == d.n && q.h == d.h && q.w == d.w && q.C == d.C && q.groups == groups && q.slot == slot && q.elem == elem && q.backward == backward) return q.walk;
+    Known& q = known[next++ % 16];
+    q = {d.n, d.h, d.w, d.C, groups, slot, elem, backward, find_slice_walk<V>(d, groups, slot, elem, backward)};
+    return q.walk;
 }
 // Samples that are under way at once: as many blocks per slice as the device holds (asked once per kernel and launch shape).
 template <typename K>
@@ -241,7 +253,7 @@ size_t forward_ws(const Dims& d, int groups, int dtype) {
 template <int V>
 size_t backward_ws(const Dims& d, int groups, int dtype, bool kept) {
     const int elem = elem_bytes(dtype);
-    const SliceWalk s = slice_walk<V>(d, groups, elem * V + (kept ? V + 1 : elem * V), kept ? 2 : elem, true);
+    const SliceWalk& s = slice_walk<V>(d, groups, elem * V + (kept ? V + 1 : elem * V), kept ? 2 : elem, true);
     if (s.threads) return d.n == 1 ? 0 : (size_t)std::min<long long>(d.n, 32 * kSms) * 2 * d.C * sizeof(float);      // (never more blocks of a slice than 32 per SM)
     const Walk w = walk_of(d, V);
     return (size_t)(d.n * groups) * sizeof(float2) + (size_t)(d.n * w.chunks) * 2 * d.C * sizeof(float);
@@ -255,7 +267,7 @@ void forward(Launcher& go, const alexnet_group_norm_forward_t* a, const Dims& d)
         if (a->keep_x.codes) kx = {(uint8_t*)a->keep_x.codes, a->keep_x.scales, src_of(a->keep_x.format)};
         if (a->keep_y.codes) ky = {(uint8_t*)a->keep_y.codes, a->keep_y.scales, src_of(a->keep_y.format)};
     }
-    const SliceWalk sw = slice_walk<V>(d, s.groups, sizeof(T) * V, sizeof(T), false);
+    const SliceWalk& sw = slice_walk<V>(d, s.groups, sizeof(T) * V, sizeof(T), false);
     if (sw.threads) {
         const size_t smem = (size_t)sw.its * sw.threads * sizeof(T) * V + slice_scratch<V>(sw, false);
         const long long rows = slice_rows(go, gn_slice_forward_kernel<T, V, ACT>, sw, d, smem);
@@ -292,7 +304,7 @@ void backward(Launcher& go, const alexnet_group_norm_backward_t* a, const Dims& 
     const BackwardArgs A{a->mean, a->rstd, a->weight, a->bias};
     const T* dy = (const T*)a->dy.data;
     constexpr int kSlot = (int)sizeof(T) * V + (SRC == kSrcSame ? (int)sizeof(T) * V : V + 1);
-    const SliceWalk sw = slice_walk<V>(d, s.groups, kSlot, SRC == kSrcSame ? (int)sizeof(T) : 2, true);
+    const SliceWalk& sw = slice_walk<V>(d, s.groups, kSlot, SRC == kSrcSame ? (int)sizeof(T) : 2, true);
     if (sw.threads) {
         partial = (float*)a->workspace;
         auto* kernel = gn_slice_backward_kernel<T, V, SRC, ACT>;

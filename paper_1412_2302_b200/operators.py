@@ -164,6 +164,11 @@ def _vector(t, n, what, index):
     return t.data_ptr()
 
 
+def _dense_like(t):
+    """a dense tensor of t's shape and type (of a dense one empty_like is the cheapest)"""
+    return torch.empty_like(t) if t.is_contiguous() else torch.empty(t.shape, dtype=t.dtype, device=t.device)
+
+
 def _output(out, shape, dtype, index):
     if out.dtype is not dtype or out.shape != shape:
         _refuse(f"out must be {dtype} {tuple(shape)}, not {out.dtype} {tuple(out.shape)}")
@@ -175,7 +180,8 @@ def _output(out, shape, dtype, index):
 def _new_checkpoint(x, fmt):
     shape = x.shape
     k = Checkpoint.__new__(Checkpoint)
-    k.codes = x.new_empty(shape, dtype=_name(CODE_DTYPES, fmt, "checkpoint format"))
+    dtype = _name(CODE_DTYPES, fmt, "checkpoint format")
+    k.codes = torch.empty_like(x, dtype=dtype) if x.is_contiguous() else x.new_empty(shape, dtype=dtype)
     k.scales = x.new_empty((*shape[:-1], (shape[-1] + 31) // 32), dtype=torch.uint8)
     return k
 
@@ -258,8 +264,9 @@ def group_norm(x, groups, weight=None, bias=None, eps=1e-5, activation="none", k
     (n, h, w, c), xs = _rows(x, "x")
     shape = (n, h, w, c, groups, _name(DTYPES, x.dtype, "dtype"), _name(ACTIVATIONS, activation, "activation"), eps, 0)
     nbytes = _norm_workspace(shape, 0)
-    y = torch.empty(x.shape, dtype=x.dtype, device=x.device) if out is None else _output(out, x.shape, x.dtype, index)
-    mean, rstd = x.new_empty((n, groups), dtype=torch.float32), x.new_empty((n, groups), dtype=torch.float32)
+    y = _dense_like(x) if out is None else _output(out, x.shape, x.dtype, index)
+    mean = x.new_empty((n, groups), dtype=torch.float32)
+    rstd = torch.empty_like(mean)
     kx = ky = None
     pkx = pky = _NOT_KEPT
     if keep_input is not None:
@@ -300,8 +307,9 @@ def group_norm_backward(dy, x, mean, rstd, weight=None, bias=None, activation="n
         _other_device()
     shape = (n, h, w, c, mean.shape[1], _name(DTYPES, dy.dtype, "dtype"), _name(ACTIVATIONS, activation, "activation"), 1.0, 0)
     nbytes = _norm_workspace(shape, 1)
-    dx = torch.empty(dy.shape, dtype=dy.dtype, device=dy.device) if out is None else _output(out, dy.shape, dy.dtype, index)
-    dweight, dbias = dy.new_empty(c, dtype=torch.float32), dy.new_empty(c, dtype=torch.float32)
+    dx = _dense_like(dy) if out is None else _output(out, dy.shape, dy.dtype, index)
+    dweight = dy.new_empty(c, dtype=torch.float32)
+    dbias = torch.empty_like(dweight)
     ws = dy.new_empty(nbytes, dtype=torch.uint8) if nbytes else None
     _run(_alexnet.load_library().alexnet_group_norm_backward,
          _pack_backward(*shape, dy.data_ptr(), *ds, *xv, dx.data_ptr(), *_rows(dx, "out")[1], *kept, mean.data_ptr(), rstd.data_ptr(), _vector(weight, c, "weight", index),
