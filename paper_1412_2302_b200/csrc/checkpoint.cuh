@@ -340,72 +340,75 @@ __global__ void __launch_bounds__(256) checkpoint_decode_kernel(const uint8_t* _
         }
     }
 }
-// Any other rows: a warp per block, a lane per value.
-template <typename T>
-__global__ void __launch_bounds__(256) checkpoint_encode_any_kernel(const T* __restrict__ x, const Geo g, const Walk w, FastDiv blocks, int fmt,
-                                                                    uint8_t* __restrict__ codes, uint8_t* __restrict__ scales) {
+// Any other rows: a warp per block (Walk's vectors), a lane per value; a warp walks down the positions of its block.
+struct WarpSpot { int lane, c, p0, p1; long long n; bool on; };
+__device__ __forceinline__ WarpSpot warp_spot(const Walk& w) {
+    const long long b = blockIdx.x, t = b / w.colblocks, n = t / w.chunks;
+    const int warp = threadIdx.x >> 5, row = warp / w.cols, block = (int)(b - t * w.colblocks) * w.cols + warp - row * w.cols, p0 = (int)(t - n * w.chunks) * w.ppc;
+    WarpSpot s;
+    s.lane = threadIdx.x & 31;
+    s.c = block * 32 + s.lane;
+    s.n = n;
+    s.p0 = p0 + row;
+    s.p1 = min(w.HW, p0 + w.ppc);
+    s.on = row < w.rows && block < w.vecs;
+    return s;
+}
+template <typename T, int FMT>
+__global__ void __launch_bounds__(256) checkpoint_encode_any_kernel(const T* __restrict__ x, const Geo g, const Walk w, uint8_t* __restrict__ codes, uint8_t* __restrict__ scales) {
     kn::pdl_sync();
-    const long long n = blockIdx.x / w.chunks, chunk = blockIdx.x - n * w.chunks;
-    const int p0 = (int)chunk * w.ppc, np = min(w.HW, p0 + w.ppc) - p0, lane = threadIdx.x & 31;
-    const T* xp = x + n * g.sn;
-    const int total = np * (int)blocks.d;
-    constexpr int U = 4;
-    for (int i = threadIdx.x >> 5; i < total; i += 8 * U) {
+    const WarpSpot s = warp_spot(w);
+    if (!s.on) return;
+    const bool has = s.c < w.C;
+    const T* xp = x + s.n * g.sn + s.c;
+    const long long row0 = s.n * w.HW + s.p0;
+    uint8_t *cp = codes + row0 * w.C + s.c, *ep = scales + row0 * w.dense.blocks + (s.c >> 5);
+    Cursor c(g, s.p0);
+    constexpr int U = 8;
+    for (int p = s.p0; p < s.p1; p += U * w.rows) {
         float f[U];
-        int pos[U], c[U];
         #pragma unroll
         for (int u = 0; u < U; ++u) {
-            const int j = i + 8 * u;
-            const int q = (int)blocks.div((uint32_t)j);
-            pos[u] = p0 + q;
-            c[u] = (j - q * (int)blocks.d) * 32 + lane;
-            f[u] = j < total && c[u] < w.C ? to_f<T>(xp[g.at(pos[u]) + c[u]]) : 0.f;
+            f[u] = has && p + u * w.rows < s.p1 ? to_f<T>(xp[c.off]) : 0.f;
+            c.next(g);
         }
         #pragma unroll
         for (int u = 0; u < U; ++u) {
-            if (i + 8 * u >= total) break;
-            const uint32_t m = __reduce_max_sync(~0u, __float_as_uint(f[u]) & 0x7fffffffu);
-            const uint32_t e = fmt == kSrcInt8 ? scale_byte<kSrcInt8>(m) : scale_byte<kSrcE4m3>(m);
-            const float inv = inverse_scale(e);
-            const long long row = n * w.HW + pos[u];
-            if (c[u] < w.C)
-                codes[row * w.C + c[u]] = fmt == kSrcInt8 ? codes_of<kSrcInt8, 1>(f + u, inv, e == 255u) : codes_of<kSrcE4m3, 1>(f + u, inv, e == 255u);
-            if (lane == 0) scales[row * blocks.d + (c[u] >> 5)] = (uint8_t)e;
+            if (p + u * w.rows >= s.p1) break;
+            const uint32_t e = scale_byte<FMT>(__reduce_max_sync(~0u, __float_as_uint(f[u]) & 0x7fffffffu));
+            if (has) *cp = codes_of<FMT, 1>(f + u, inverse_scale(e), e == 255u);
+            if (s.lane == 0) *ep = (uint8_t)e;
+            cp += w.dense.inc_codes;
+            ep += w.dense.inc_scales;
         }
     }
 }
-template <typename T>
-__global__ void __launch_bounds__(256) checkpoint_decode_any_kernel(const uint8_t* __restrict__ codes, const uint8_t* __restrict__ scales, int fmt, const Geo g, const Walk w,
-                                                                    FastDiv blocks, T* __restrict__ out) {
+template <typename T, int FMT>
+__global__ void __launch_bounds__(256) checkpoint_decode_any_kernel(const uint8_t* __restrict__ codes, const uint8_t* __restrict__ scales, const Geo g, const Walk w, T* __restrict__ out) {
     kn::pdl_sync();
-    const long long n = blockIdx.x / w.chunks, chunk = blockIdx.x - n * w.chunks;
-    const int p0 = (int)chunk * w.ppc, np = min(w.HW, p0 + w.ppc) - p0, lane = threadIdx.x & 31;
-    T* op = out + n * g.sn;
-    const int total = np * (int)blocks.d;
-    constexpr int U = 4;
-    for (int i = threadIdx.x >> 5; i < total; i += 8 * U) {
+    const WarpSpot s = warp_spot(w);
+    if (!s.on || s.c >= w.C) return;
+    T* op = out + s.n * g.sn + s.c;
+    const long long row0 = s.n * w.HW + s.p0;
+    const uint8_t *cp = codes + row0 * w.C + s.c, *ep = scales + row0 * w.dense.blocks + (s.c >> 5);
+    Cursor c(g, s.p0);
+    constexpr int U = 8;
+    for (int p = s.p0; p < s.p1; p += U * w.rows) {
         uint8_t q[U], e[U];
-        int pos[U], c[U];
         #pragma unroll
         for (int u = 0; u < U; ++u) {
-            const int j = i + 8 * u;
-            const int d = (int)blocks.div((uint32_t)j);
-            pos[u] = p0 + d;
-            c[u] = (j - d * (int)blocks.d) * 32 + lane;
-            if (j < total && c[u] < w.C) {
-                const long long row = n * w.HW + pos[u];
-                q[u] = codes[row * w.C + c[u]];
-                e[u] = scales[row * blocks.d + (c[u] >> 5)];
-            }
+            if (p + u * w.rows < s.p1) { q[u] = *cp; e[u] = *ep; }
+            cp += w.dense.inc_codes;
+            ep += w.dense.inc_scales;
         }
         #pragma unroll
-        for (int u = 0; u < U; ++u)
-            if (i + 8 * u < total && c[u] < w.C) {
-                float f;
-                if (fmt == kSrcInt8) code_values<kSrcInt8, 1>(q[u], &f);
-                else code_values<kSrcE4m3, 1>(q[u], &f);
-                op[g.at(pos[u]) + c[u]] = from_f<T>(f * scale_of(e[u]));
-            }
+        for (int u = 0; u < U; ++u) {
+            if (p + u * w.rows >= s.p1) break;
+            float f;
+            code_values<FMT, 1>(q[u], &f);
+            op[c.off] = from_f<T>(f * scale_of(e[u]));
+            c.next(g);
+        }
     }
 }
 

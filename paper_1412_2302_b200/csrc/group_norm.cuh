@@ -41,9 +41,9 @@ template <int V> __device__ __forceinline__ void v_fma(const float* a, const flo
         for (int i = 0; i < V; i += 2) un2(fma2(mk2(a[i], a[i + 1]), mk2(b[i], b[i + 1]), mk2(c[i], c[i + 1])), o[i], o[i + 1]);
     }
 }
-// s = 1 / (1 + e^-z).  fp32 tensors take the accurate functions; 16-bit ones the hardware's approximate ones (relative error below 2^-20 for |z| < 16, next to
-// a rounding of 2^-9 or 2^-12).  The special-function unit takes 16 values per SM and cycle and bounds SiLU's passes, so two values share
-// one reciprocal: 1 / a = b / (a b).  For that e^-z stops at 2^63: below z = -43 s is 2^-63, which is off by less than 2^-57 in any result.
+// s = 1 / (1 + e^-z).  fp32 tensors take the accurate functions; 16-bit ones the hardware's approximate ones, without their care for subnormal
+// numbers (relative error below 2^-20 for |z| < 16, next to a rounding of 2^-9 or 2^-12; below z = -87 the result is 0).  SiLU's passes are bound by the
+// instructions they issue: two values sharing a reciprocal (1 / a = b / (a b)) save half of those, but take 20 instructions more per eight values.
 template <typename T, int V> __device__ __forceinline__ void sigmoid(const float* z, float* s) {
     if constexpr (sizeof(T) == 4) {
         #pragma unroll
@@ -54,17 +54,10 @@ template <typename T, int V> __device__ __forceinline__ void sigmoid(const float
         for (int i = 0; i < V; ++i) { one[i] = 1.f; ls[i] = -1.44269504f; }
         v_mul<V>(z, ls, t);
         #pragma unroll
-        for (int i = 0; i < V; ++i) asm("min.NaN.f32 %0, %0, %1;\n\tex2.approx.ftz.f32 %0, %0;" : "+f"(t[i]) : "f"(63.f));
+        for (int i = 0; i < V; ++i) asm("ex2.approx.ftz.f32 %0, %0;" : "+f"(t[i]));
         v_add<V>(t, one, t);
-        if constexpr (V == 1) asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(s[0]) : "f"(t[0]));
-        else {
-            #pragma unroll
-            for (int i = 0; i < V; i += 2) {
-                float r;
-                asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(t[i] * t[i + 1]));
-                un2(mul2(mk2(t[i + 1], t[i]), mk2(r, r)), s[i], s[i + 1]);
-            }
-        }
+        #pragma unroll
+        for (int i = 0; i < V; ++i) asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(s[i]) : "f"(t[i]));
     }
 }
 // ACT: the activation, or kActAny to take it from `act`
