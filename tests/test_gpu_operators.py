@@ -225,10 +225,11 @@ def test_checkpoint_every_code_is_decoded(ops):
 
 # ---------------------------------------------------------------- group norm, forward
 # (shape, groups): one position, one channel, one group and as many as channels, groups that straddle vectors, rows longer than a block,
-# few and many samples, slices of several blocks
+# few and many samples (more than blocks that keep them fit the device), slices of
+# several blocks
 NORM_SHAPES = [((1, 1, 1, 1), 1), ((1, 1, 1, 64), 8), ((3, 1, 1, 4096), 32), ((2, 3, 5, 12), 4), ((2, 13, 13, 96), 32), ((1, 13, 13, 384), 32), ((2, 27, 27, 40), 5), ((5, 9, 11, 100), 20),
                ((2, 7, 5, 37), 1), ((3, 6, 1, 48), 48), ((1, 1, 50, 2560), 10), ((2, 2, 2, 2064), 3), ((1, 57, 55, 8), 1), ((300, 2, 2, 16), 4), ((7, 1, 1, 6), 3), ((2, 33, 31, 256), 32),
-               ((1, 96, 90, 64), 32), ((1, 130, 127, 24), 2), ((2, 128, 128, 128), 32)]
+               ((2100, 3, 2, 32), 4), ((700, 9, 9, 64), 8), ((1500, 2, 3, 20), 5), ((1, 96, 90, 64), 32), ((1, 130, 127, 24), 2), ((2, 128, 128, 128), 32)]
 ACTS = ["none", "relu", "silu"]
 
 
