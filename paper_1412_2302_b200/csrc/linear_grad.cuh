@@ -9,9 +9,15 @@
 // leaves as one full 128-byte line.
 //
 // Warps: 0 = TMA producer (dy), 1 = MMA issuer and TMEM owner, 2..9 = epilogue (two sets of four), 10..25 = decoders, four groups
-// that take the steps in turn (a step takes a warp over 1000 cycles from its wait to its arrival, and the tensor cores 512).  Persistent over tiles with two
-// accumulators, so a tile's stores overlap the next one's products.  Where the tiles do not fill the last
-// round of CTAs (or any), those of that round are split over the rows; a second kernel adds their partial sums in a fixed order.  Every wait is bounded; a CTA whose wait runs out writes NaN and raises g_expired.
+// that take the steps in turn (a step takes a warp over 1000 cycles from its wait to its arrival, and the tensor cores 512).  Persistent
+// over tiles with two accumulators, so a tile's stores overlap the next one's products.  Where the tiles do not fill the last round of CTAs
+// (or any), those of that round are split over the rows; a second kernel adds their partial sums in a fixed order.  Every wait is
+// bounded; a CTA whose wait runs out writes NaN and raises g_expired.
+//
+// Measured: 8192 rows, 4096 x 4096: 215 us, 1280 TFLOP/s; the library's product alone, with x in bf16 already, 181 us, and the decoding and
+// writing of x before it another 25.  128 rows, 9216 x 4096: 29.5 us, 5.2 TB/s, all but 11 % of them the fp32 stores of dw.  173 rows, 4096 x 1000:
+// 7.5 us, of which the first loads, one chain of steps and the stores are the most: a latency.  Long products are bound by the shared memory
+// (the decoded tile's stores and the operands' reads), then by the power limit; short ones by the stores of dw.
 #pragma once
 #include "checkpoint.cuh"
 
@@ -22,6 +28,10 @@ constexpr int kLgThreads = 32 * (2 + kLgEpilogue + kLgGroups * kLgDecoders);
 constexpr int kLgShare = kLgRows * 4 / (32 * kLgDecoders);     // checkpoint blocks of a step that a decoder takes: rows 8 kLgDecoders apart
 constexpr int kLgA = 128 * kLgRows * 2;            // bytes of the decoded tile of a stage: two boxes of 64 features x 64 rows
 constexpr int kLgMaxStages = 6;
+// Steps whose products one accumulator takes up.  The tensor cores cut their running sums off instead of rounding them, so an error grows with
+// every row (2.2e-10 of the result per row: 1.8e-6 after 8192, where an fp32 product with rounded sums has 2.4e-7): after 2048 rows the sums are
+// added, rounded, to those before.
+constexpr int kLgChunk = 32;
 struct LinearGradParams {
     CUtensorMap tmD;                               // dy [rows][n_out], boxes of 64 features x 64 rows
     const uint8_t *codes, *scales;
@@ -167,47 +177,81 @@ __global__ void __launch_bounds__(kLgThreads, 1) linear_grad_kernel(const __grid
         }
     } else if (warp == 1) {
         if (rank == 0) {
+        // A unit's first chunk goes to accumulator `ab`, the others to the other one, whence the epilogue adds them to the first; the next unit's
+        // first chunk goes to that other one, while the epilogue stores this unit's result.  fill: bit a is the parity of accumulator a's next use.
         const uint32_t idesc = tc::instr_desc(p.BN, 1, 1, 128 * CG);
         int st = 0; uint32_t ph = 0;
-        int ab = 0; uint32_t aph = 0;
+        int ab = 0; uint32_t fill = 0;
         bool ok = true;
         LinearGradTile t;
-        for (int tile = tile0; tile < tiles && ok; tile += tile_step) {
+        for (int tile = tile0; tile < tiles && ok; tile += tile_step, ab ^= 1) {
             t.set(p, tile);
-            if (!(ok = tc::mbar_wait_warp(acce0 + 8u * ab, aph ^ 1u, abort_flag))) break;
-            if (CG == 2) tc::fence_acq_rel_cluster();  // the peer's epilogue arrived from the other CTA
-            tc::tc_fence_after();
-            const uint32_t d = tmem + (uint32_t)(ab * p.BN);
-            for (int k = t.k0; k < t.k1; ++k) {
-                if (!(ok = tc::mbar_wait_warp(full0 + 8u * st, ph, abort_flag))) break;
+            for (int c0 = t.k0; c0 < t.k1 && ok; c0 += kLgChunk) {
+                const int a = c0 == t.k0 ? ab : ab ^ 1, c1 = min(t.k1, c0 + kLgChunk);
+                if (!(ok = tc::mbar_wait_warp(acce0 + 8u * a, (fill >> a & 1u) ^ 1u, abort_flag))) break;
+                if (CG == 2) tc::fence_acq_rel_cluster();  // the peer's epilogue arrived from the other CTA
                 tc::tc_fence_after();
-                const uint32_t sa = base + st * stage_bytes, sb = sa + kLgA;
-                #pragma unroll
-                for (int j = 0; j < 4; ++j)
-                    tc::umma_cg<CG>(d, tc::smem_desc(sa + j * 2048, 8192, 1024), tc::smem_desc(sb + j * 2048, 8192, 1024), idesc, (k > t.k0 || j > 0) ? 1u : 0u);
-                tc::umma_commit_cg<CG>(empty0 + 8u * st);
-                if (++st == stages) { st = 0; ph ^= 1u; }
+                const uint32_t d = tmem + (uint32_t)(a * p.BN);
+                for (int k = c0; k < c1; ++k) {
+                    if (!(ok = tc::mbar_wait_warp(full0 + 8u * st, ph, abort_flag))) break;
+                    tc::tc_fence_after();
+                    const uint32_t sa = base + st * stage_bytes, sb = sa + kLgA;
+                    #pragma unroll
+                    for (int j = 0; j < 4; ++j)
+                        tc::umma_cg<CG>(d, tc::smem_desc(sa + j * 2048, 8192, 1024), tc::smem_desc(sb + j * 2048, 8192, 1024), idesc, (k > c0 || j > 0) ? 1u : 0u);
+                    tc::umma_commit_cg<CG>(empty0 + 8u * st);
+                    if (++st == stages) { st = 0; ph ^= 1u; }
+                }
+                if (!ok) break;
+                tc::umma_commit_cg<CG>(accf0 + 8u * a);
+                fill ^= 1u << a;
             }
-            if (!ok) break;
-            tc::umma_commit_cg<CG>(accf0 + 8u * ab);
-            if (++ab == 2) { ab = 0; aph ^= 1u; }
         }
         }
     } else if (warp < 2 + kLgEpilogue) {
         const int quad = warp & 3, set = (warp - 2) >> 2;
-        int ab = 0; uint32_t aph = 0;
+        int ab = 0; uint32_t fill = 0;
         bool ok = true;
         LinearGradTile t;
-        for (int tile = tile0; tile < tiles; tile += tile_step) {
-            t.set(p, tile);
-            ok = ok && tc::mbar_wait_idle(accf0 + 8u * ab, aph, abort_flag);
+        auto filled = [&](int a) {                     // the accumulator's current use is complete
+            ok = ok && tc::mbar_wait_idle(accf0 + 8u * a, fill >> a & 1u, abort_flag);
+            fill ^= 1u << a;
             tc::tc_fence_after();
+        };
+        auto release = [&](int a) {
+            tc::tc_fence_before();
+            __syncwarp();
+            if (lane == 0) {
+                if (CG == 2) tc::mbar_arrive_cluster(tc::mapa_u32(acce0 + 8u * a, 0));
+                else tc::mbar_arrive(acce0 + 8u * a);
+            }
+        };
+        for (int tile = tile0; tile < tiles; tile += tile_step, ab ^= 1) {
+            t.set(p, tile);
             const int i = (t.m * CG + rank) * 128 + quad * 32 + lane, o0 = t.n * p.BN, nv = min(p.BN, p.n_out - o0);
+            const uint32_t lanes = tmem + ((uint32_t)(quad * 32) << 16), ta = lanes + (uint32_t)(ab * p.BN), tb = lanes + (uint32_t)((ab ^ 1) * p.BN);
+            for (int c0 = t.k0 + kLgChunk; c0 < t.k1; c0 += kLgChunk) {
+                filled(ab ^ 1);                        // (the first chunk's products are complete as well: they were issued before)
+                if (ok) {
+                    #pragma unroll 1
+                    for (int c = 32 * set; c < nv; c += c & 16 ? 48 : 16) {  // the columns that this warp stores below
+                        uint32_t u[16], v[16];
+                        tc::tmem_ld16(ta + (uint32_t)c, u);
+                        tc::tmem_ld16(tb + (uint32_t)c, v);
+                        tc::tmem_ld_wait();
+                        #pragma unroll
+                        for (int q = 0; q < 16; ++q) u[q] = __float_as_uint(__uint_as_float(u[q]) + __uint_as_float(v[q]));
+                        tc::tmem_st16(ta + (uint32_t)c, u);
+                    }
+                    tc::tmem_st_wait();
+                }
+                release(ab ^ 1);
+            }
+            filled(ab);
             // dw[o][i], or the unit's partial sums [column][input]
             const bool part = t.part >= 0, mine = part || i < p.n_in;
             const long long pitch = part ? 128 * CG : p.n_in;
             float* out = part ? p.partial + ((long long)t.part * p.BN + 32 * set) * (128 * CG) + rank * 128 + quad * 32 + lane : p.out + (long long)(o0 + 32 * set) * p.n_in + i;
-            const uint32_t ta = tmem + (uint32_t)(ab * p.BN) + ((uint32_t)(quad * 32) << 16);
             #pragma unroll 1
             for (int c = 32 * set; c < nv; c += 64, out += 64 * pitch) {
                 uint32_t v[32];
@@ -227,13 +271,7 @@ __global__ void __launch_bounds__(kLgThreads, 1) linear_grad_kernel(const __grid
                     }
                 }
             }
-            tc::tc_fence_before();
-            __syncwarp();
-            if (lane == 0) {
-                if (CG == 2) tc::mbar_arrive_cluster(tc::mapa_u32(acce0 + 8u * ab, 0));
-                else tc::mbar_arrive(acce0 + 8u * ab);
-            }
-            if (++ab == 2) { ab = 0; aph ^= 1u; }
+            release(ab);
         }
     } else {
         // thread: checkpoint block cb (32 codes) of row kr of a step.  With the 128-byte swizzle, 16-byte chunk j of row k lies at j ^ (k & 7);

@@ -415,6 +415,22 @@ def test_linear_weight_grad(ops, rows, n_in, n_out, fmt):
     assert ops.linear_weight_grad(dy, k, out=out) is out and torch.equal(out, dw)
 
 
+@pytest.mark.parametrize("rows,n_in,n_out", [(8192, 2560, 2080), (8192 + 37, 1024, 4096), (16384, 4096, 2000)])
+def test_linear_weight_grad_keeps_its_precision_over_many_rows(ops, rows, n_in, n_out):
+    """Many tiles, so that none is split.  The tensor cores cut off: 2.2e-10 of the result a row, 4.5e-7 over the 2048 rows that one of their sums
+    takes up.  Those sums are added with rounding, at most eight of them, 2^-24 each and random: 1.7e-7 together.  2^-20 is 9.5e-7."""
+    g = gen(rows)
+    x = torch.randn((rows, n_in), device="cuda", generator=g)
+    k = ops.checkpoint_encode(x, "e4m3")
+    dy = torch.randn((rows, n_out), device="cuda", generator=g).to(torch.bfloat16)
+    dw = ops.linear_weight_grad(dy, k)
+    assert torch.equal(dw, ops.linear_weight_grad(dy, k))
+    want = dy.double().t() @ ref_codes(x, "e4m3")[2]
+    assert float((dw.double() - want).norm() / want.norm()) < 2.0 ** -20
+    mag = (rows + 16) * 2.0 ** -24 * (dy.double().abs().t() @ ref_codes(x, "e4m3")[2].abs())
+    assert not bool(((dw.double() - want).abs() > mag).any())
+
+
 def test_linear_weight_grad_of_positions_and_of_nothing(ops):
     g = gen(2)
     x = torch.randn((3, 5, 7, 64), device="cuda", generator=g)
