@@ -339,6 +339,29 @@ def test_group_norm_backward(ops, shape, groups, dtype):
             assert got[0] is out and bool((grid[:, shape[1]:] == 7).all()) and bool((grid[:, :, shape[2]:] == 7).all())
 
 
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("shape,groups", [((3, 6, 6, 64), 8), ((3, 6, 6, 36), 6), ((1, 150, 150, 64), 4), ((1, 150, 150, 33), 3)])
+def test_group_norm_backward_of_weights_of_zero(ops, shape, groups, dtype):
+    """z is the bias for every x: ReLU passes the gradient on to weight and bias where that is positive, and to x nowhere."""
+    g = gen(21 + sum(shape))
+    c = shape[-1]
+    x, dy = tensor(g, shape, TYPES[dtype]), tensor(g, shape, TYPES[dtype])
+    w = torch.randn(c, device="cuda", generator=g)
+    w[::2] = 0
+    w[:c // groups] = 0                                 # all of a group
+    w[1] = -0.0
+    b = torch.tensor([0.5, 0.5, -0.5, 0.0, -0.5], device="cuda").repeat(c // 5 + 1)[:c]
+    for act, src in itertools.product(ACTS, ("x", "int8", "e4m3")):
+        mean, rstd = (t.float() for t in ref_stats(x, groups))
+        kept = x if src == "x" else ops.checkpoint_encode(x, src)
+        value = x if src == "x" else ref_codes(x, src)[2]
+        got = ops.group_norm_backward(dy, kept, mean, rstd, w, b, activation=act)
+        want, mag = ref_backward(dy, value, mean, rstd, w, b, act)
+        for name, t, v, m in zip(("dx", "dweight", "dbias"), got, want, mag):
+            close(t, v, m, (name, act, src))
+        assert not bool(got[0][..., :c // groups].any())
+
+
 def test_reference_gradient_is_the_forward_passes(ops):
     """The formula that the gradients above are held against, against central differences of the definition in 64 bits."""
     g = torch.Generator().manual_seed(4)
