@@ -9,13 +9,15 @@ activation checkpoints, and the weight gradient of a linear layer from such a ch
 Tensors are channels-last: [n, h, w, c], [n, l, c] or [n, c] (`checkpoint_*` and `linear_weight_grad`: any number of leading dimensions that
 form rows) with adjacent channels, dense or a view of a larger grid; bfloat16, float16 or float32.  Weights, biases, statistics and their
 gradients are float32.  Every call queues its work on `stream` (a torch.cuda.Stream; default: the current stream of the tensors' device)
-and returns without waiting.  Outputs and workspace come from torch's allocator on that stream unless `out` gives the output.  A wrong
+and returns without waiting; tensors that are let go before that stream has passed the call need their record_stream, as with any
+other work on a stream of one's own.  Outputs and workspace come from torch's allocator on that stream unless `out` gives the output.  A wrong
 argument raises AlexNetError with code ERR_ARG before anything is launched.  There is no CPU fallback.
 """
 from __future__ import annotations
 
 import ctypes
 import functools
+import operator
 import struct
 import threading
 from typing import NamedTuple, Optional
@@ -111,11 +113,18 @@ def _elsewhere(index, stream):
     return torch.cuda.stream(stream)                # sets the device too
 
 
-def _run(function, block, index):
+def _pack(pack, *fields):
+    try:
+        return pack(*fields)
+    except (struct.error, OverflowError):
+        _refuse("a size, a stride or eps is not a number that the library's arguments hold")
+
+
+def _run(function, index, pack, *fields):
     err = getattr(_local, "err", None)
     if err is None:
         err = _local.err = ctypes.create_string_buffer(256)
-    rc = function(block, _raw_stream(index), err, 256)
+    rc = function(_pack(pack, *fields), _raw_stream(index), err, 256)
     if rc != OK:
         raise AlexNetError(rc, err.value.decode())
 
@@ -196,7 +205,7 @@ def _kept(k):
 @functools.lru_cache(maxsize=1024)
 def _norm_workspace(shape, backward):
     """bytes of workspace for the sizes (0: the call needs none)"""
-    n = int(_alexnet.load_library().alexnet_group_norm_workspace_bytes(_pack_shape(*shape), backward))
+    n = int(_alexnet.load_library().alexnet_group_norm_workspace_bytes(_pack(_pack_shape, *shape), backward))
     if n == 0:
         raise AlexNetError(ERR_ARG, f"invalid group norm: n, h, w, channels, groups = {tuple(shape[:5])}, eps = {shape[7]}")
     return n if n > 256 else 0
@@ -206,7 +215,7 @@ def _norm_workspace(shape, backward):
 def _linear_workspace(rows, n_in, n_out, stride, dy_offset, codes_offset, fmt):
     """by sizes and alignment: the pointers are given modulo 16"""
     n = int(_alexnet.load_library().alexnet_linear_weight_grad_workspace_bytes(
-        _pack_linear(rows, n_in, n_out, 16 + dy_offset, stride, 16 + codes_offset, 16, fmt, 0, 0, 0, 0)))
+        _pack(_pack_linear, rows, n_in, n_out, 16 + dy_offset, stride, 16 + codes_offset, 16, fmt, 0, 0, 0, 0)))
     if n == 0:
         raise AlexNetError(ERR_ARG, f"invalid linear weight gradient: rows, in, out = {rows, n_in, n_out}, stride {stride}")
     return n if n > 256 else 0
@@ -234,7 +243,7 @@ def checkpoint_encode(x, format="int8", out=None, stream=None):
             _refuse("out is a checkpoint of another shape or format")
         if out.codes.get_device() != index:
             _other_device()
-    _run(_alexnet.load_library().alexnet_checkpoint_encode, _pack_checkpoint(n, h, w, c, dtype, x.data_ptr(), *st, *_kept(out)), index)
+    _run(_alexnet.load_library().alexnet_checkpoint_encode, index, _pack_checkpoint, n, h, w, c, dtype, x.data_ptr(), *st, *_kept(out))
     return out
 
 
@@ -248,7 +257,7 @@ def checkpoint_decode(checkpoint, dtype=torch.bfloat16, out=None, stream=None):
     code = _name(DTYPES, dtype, "dtype")
     out = codes.new_empty(codes.shape, dtype=dtype) if out is None else _output(out, codes.shape, dtype, index)
     (n, h, w, c), st = _rows_any(out, "out")
-    _run(_alexnet.load_library().alexnet_checkpoint_decode, _pack_checkpoint(n, h, w, c, code, out.data_ptr(), *st, *_kept(checkpoint)), index)
+    _run(_alexnet.load_library().alexnet_checkpoint_decode, index, _pack_checkpoint, n, h, w, c, code, out.data_ptr(), *st, *_kept(checkpoint))
     return out
 
 
@@ -261,6 +270,11 @@ def group_norm(x, groups, weight=None, bias=None, eps=1e-5, activation="none", k
     if stream is not None or index < 0 or index != _current_device():
         with _elsewhere(index, stream):
             return group_norm(x, groups, weight, bias, eps, activation, keep_input, keep_output, out)
+    if type(groups) is not int or type(eps) is not float:
+        try:
+            groups, eps = operator.index(groups), float(eps)
+        except (TypeError, ValueError):
+            _refuse(f"groups must be an integer and eps a number, not {groups!r} and {eps!r}")
     (n, h, w, c), xs = _rows(x, "x")
     shape = (n, h, w, c, groups, _name(DTYPES, x.dtype, "dtype"), _name(ACTIVATIONS, activation, "activation"), eps, 0)
     nbytes = _norm_workspace(shape, 0)
@@ -276,9 +290,9 @@ def group_norm(x, groups, weight=None, bias=None, eps=1e-5, activation="none", k
         ky = _new_checkpoint(x, keep_output)
         pky = _kept(ky)
     ws = x.new_empty(nbytes, dtype=torch.uint8) if nbytes else None
-    _run(_alexnet.load_library().alexnet_group_norm_forward,
-         _pack_forward(*shape, x.data_ptr(), *xs, y.data_ptr(), *_rows(y, "out")[1], _vector(weight, c, "weight", index), _vector(bias, c, "bias", index), mean.data_ptr(), rstd.data_ptr(),
-                       *pkx, *pky, 0 if ws is None else ws.data_ptr(), nbytes), index)
+    _run(_alexnet.load_library().alexnet_group_norm_forward, index, _pack_forward,
+         *shape, x.data_ptr(), *xs, y.data_ptr(), *_rows(y, "out")[1], _vector(weight, c, "weight", index), _vector(bias, c, "bias", index), mean.data_ptr(), rstd.data_ptr(),
+         *pkx, *pky, 0 if ws is None else ws.data_ptr(), nbytes)
     return GroupNormResult(y, mean, rstd, kx, ky)
 
 
@@ -311,9 +325,9 @@ def group_norm_backward(dy, x, mean, rstd, weight=None, bias=None, activation="n
     dweight = dy.new_empty(c, dtype=torch.float32)
     dbias = torch.empty_like(dweight)
     ws = dy.new_empty(nbytes, dtype=torch.uint8) if nbytes else None
-    _run(_alexnet.load_library().alexnet_group_norm_backward,
-         _pack_backward(*shape, dy.data_ptr(), *ds, *xv, dx.data_ptr(), *_rows(dx, "out")[1], *kept, mean.data_ptr(), rstd.data_ptr(), _vector(weight, c, "weight", index),
-                        _vector(bias, c, "bias", index), dweight.data_ptr(), dbias.data_ptr(), 0 if ws is None else ws.data_ptr(), nbytes), index)
+    _run(_alexnet.load_library().alexnet_group_norm_backward, index, _pack_backward,
+         *shape, dy.data_ptr(), *ds, *xv, dx.data_ptr(), *_rows(dx, "out")[1], *kept, mean.data_ptr(), rstd.data_ptr(), _vector(weight, c, "weight", index),
+         _vector(bias, c, "bias", index), dweight.data_ptr(), dbias.data_ptr(), 0 if ws is None else ws.data_ptr(), nbytes)
     return dx, dweight, dbias
 
 
@@ -349,6 +363,6 @@ def linear_weight_grad(dy, x, out=None, stream=None):
     p, q = dy.data_ptr(), codes.data_ptr()
     nbytes = _linear_workspace(rows, n_in, n_out, stride, p % 16, q % 16, FORMATS[x.format])
     ws = dy.new_empty(nbytes, dtype=torch.uint8) if nbytes else None
-    _run(_alexnet.load_library().alexnet_linear_weight_grad,
-         _pack_linear(rows, n_in, n_out, p, stride, *_kept(x), dw.data_ptr(), 0 if ws is None else ws.data_ptr(), nbytes), index)
+    _run(_alexnet.load_library().alexnet_linear_weight_grad, index, _pack_linear,
+         rows, n_in, n_out, p, stride, *_kept(x), dw.data_ptr(), 0 if ws is None else ws.data_ptr(), nbytes)
     return dw

@@ -637,6 +637,19 @@ def test_offsets_beyond_32_bits(ops):
     assert torch.equal(back[-1], ops.checkpoint_decode(tail, torch.bfloat16)[0]) and bool((back[-2] == 1).all())
 
 
+def test_numbers_of_other_types(ops):
+    x = torch.randn((2, 3, 3, 16), device="cuda")
+    want = ops.group_norm(x, 4, eps=1.0)
+    assert torch.equal(ops.group_norm(x, np.int64(4), eps=1).y, want.y)
+    many = torch.zeros((1, 1, 1, 4), device="cuda").expand(1, 1 << 31, 1, 4)
+    for call in (lambda: ops.group_norm(x, 4.0), lambda: ops.group_norm(x, "4"), lambda: ops.group_norm(x, 4, eps="tiny"), lambda: ops.group_norm(x, 1 << 40),
+                 lambda: ops.group_norm(x, 4, eps=1e300), lambda: ops.group_norm(many, 4),
+                 lambda: ops.group_norm_backward(many, many, torch.ones((1, 4), device="cuda"), torch.ones((1, 4), device="cuda"))):
+        with pytest.raises(A.AlexNetError) as e:
+            call()
+        assert e.value.code == A.ERR_ARG
+
+
 def test_refusals_on_the_gpu(ops):
     x = torch.zeros((2, 4, 4, 64), device="cuda")
 

@@ -178,3 +178,18 @@ def test_binding_refuses(lib):
     refused("Checkpoint", ops.linear_weight_grad, torch.zeros(2, 8, dtype=torch.bfloat16), codes)
     refused("bfloat16", ops.linear_weight_grad, torch.zeros(2, 8), ops.Checkpoint(codes, scales))
     refused("rows", ops.linear_weight_grad, torch.zeros(3, 8, dtype=torch.bfloat16), ops.Checkpoint(codes, scales))
+
+
+def test_numbers_that_no_argument_block_holds(lib):
+    """Refused like any wrong argument, not by an error of the packing; a view may have as many rows as it likes."""
+    for bad in (dict(h=1 << 31), dict(groups=1 << 40), dict(n=1 << 64), dict(eps=1e300), dict(groups=8.0)):
+        for backward in (0, 1):
+            with pytest.raises(A.AlexNetError) as e:
+                ops._norm_workspace(shape(**bad), backward)
+            assert e.value.code == A.ERR_ARG
+    with pytest.raises(A.AlexNetError) as e:
+        ops._linear_workspace(64, 1 << 32, 64, 64, 0, 0, 1)
+    assert e.value.code == A.ERR_ARG
+    with pytest.raises(A.AlexNetError) as e:
+        ops._run(lib.alexnet_checkpoint_encode, 0, ops._pack_checkpoint, 1, 1, 1 << 31, 1, 0, P, 0, 0, 0, *KEPT)
+    assert e.value.code == A.ERR_ARG
