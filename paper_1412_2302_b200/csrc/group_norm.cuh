@@ -394,14 +394,18 @@ __device__ __forceinline__ void activation_gradient(int act, const Chan<V>& k, c
         v_mul<V>(dy, u, dy);
     }
 }
+// Positions whose loads a thread of the two kernels below has under way, of two tensors each, with 128 registers and two blocks per SM.  512 x 55 x 55 x 96 bf16,
+// ReLU, both kernels: four from x 289 us, from int8 codes 315; three 297 and 325; two, with three blocks of 80 registers, 322 and 418.  From e4m3 codes three
+// take 322, four 339; in fp32 (a quarter of the samples) three take 131, four 147.
+template <typename T, int V, int SRC> constexpr int kBackwardLoads = V == 8 && (sizeof(T) == 4 || SRC == kSrcE4m3) ? 3 : 4;
 template <typename T, int V, int SRC, int ACT>
-__global__ void __launch_bounds__(256, 3) gn_backward_sums_kernel(const T* __restrict__ dy, const Geo gdy, const Source src, const Geo gx, const Walk w, const NormShape sh,
+__global__ void __launch_bounds__(256, V == 8 ? 2 : 3) gn_backward_sums_kernel(const T* __restrict__ dy, const Geo gdy, const Source src, const Geo gx, const Walk w, const NormShape sh,
                                                                const BackwardArgs A, float* __restrict__ partial) {
     kn::pdl_sync();
     __shared__ float sums[2 * V * 260];
     const Table<V> table{sums, 260};
     const Spot s = spot(w);
-    constexpr int U = V == 8 ? 2 : 4;
+    constexpr int U = kBackwardLoads<T, V, SRC>;
     float S1[V], S2[V];
     #pragma unroll
     for (int i = 0; i < V; ++i) S1[i] = S2[i] = 0.f;
@@ -497,7 +501,7 @@ __global__ void __launch_bounds__(1024) gn_parameter_gradient_kernel(const float
     parameter_gradient<32>(partial, C, n, blockIdx.x, red, dweight, dbias);
 }
 template <typename T, int V, int SRC, int ACT>
-__global__ void __launch_bounds__(256, 3) gn_backward_apply_kernel(const T* __restrict__ dy, const Geo gdy, const Source src, const Geo gx, const Walk w, const NormShape sh,
+__global__ void __launch_bounds__(256, V == 8 ? 2 : 3) gn_backward_apply_kernel(const T* __restrict__ dy, const Geo gdy, const Source src, const Geo gx, const Walk w, const NormShape sh,
                                                                 const BackwardArgs A, const float2* __restrict__ c12, T* __restrict__ dx, const Geo gdx, const float* __restrict__ partial,
                                                                 long long partials, int extra, float* __restrict__ dweight, float* __restrict__ dbias) {
     kn::pdl_sync();
@@ -519,7 +523,7 @@ __global__ void __launch_bounds__(256, 3) gn_backward_apply_kernel(const T* __re
     }
     const T* dp = dy + s.n * gdy.sn + V * s.v;
     T* op = dx + s.n * gdx.sn + V * s.v;
-    constexpr int U = V == 8 ? 2 : 4;
+    constexpr int U = kBackwardLoads<T, V, SRC>;
     Cursor c(gdy, s.p0 + s.row), co(gdx, s.p0 + s.row);
     SourceCursor<T, V, SRC> cx(src, gx, w, s.n, s.p0 + s.row, s.v);
     for (int p = s.p0 + s.row; p < s.p1; p += U * w.rows) {

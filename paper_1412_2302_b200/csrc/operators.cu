@@ -102,10 +102,11 @@ bool vec_ok(const alexnet_view_t& v, const Dims& d, int dtype) {
 }
 bool vec_ok(const alexnet_checkpoint_t& k, const Dims& d) { return d.C % 8 == 0 && (uintptr_t)k.codes % 8 == 0; }
 
-// How a launch walks [n][h w][C] with vectors of V channels.  Elementwise passes (reduces = false): eight blocks per SM, of at least four positions per thread.
-// Passes whose blocks end with a reduction: whole rounds of what an SM holds of them (three with 80 registers, six with 40), a block being as dear as
+// How a launch walks [n][h w][C] with vectors of V channels.  Elementwise passes: eight blocks per SM, of at least four positions per thread.
+// Passes whose blocks end with a reduction: whole rounds of what an SM holds of them (vectors of eight: three, in backward passes two), a block being as dear as
 // its positions and ten more.
-Walk walk_of(const Dims& d, int V, bool reduces) {
+enum Pass { kElementwise, kForwardSums, kBackward };
+Walk walk_of(const Dims& d, int V, Pass pass) {
     Walk w{};
     w.C = d.C; w.HW = d.h * d.w; w.vecs = d.C / V;
     const int q = V == 8 ? 4 : 1, padded = (int)ceil_div(w.vecs, q) * q;
@@ -114,8 +115,8 @@ Walk walk_of(const Dims& d, int V, bool reduces) {
     w.rows = 256 / w.cols;
     const long long blocks = std::max<long long>(1, d.n * w.colblocks), most = std::max<long long>(1, ceil_div(w.HW, 4 * w.rows));
     long long chunks = std::min(most, ceil_div(8 * kSms, blocks));
-    if (reduces) {
-        const int slots = (V == 8 ? 3 : 6) * kSms;
+    if (pass != kElementwise) {
+        const int slots = (V != 8 ? 6 : pass == kBackward ? 2 : 3) * kSms;
         long long cost = 1ll << 62;
         for (long long c = 1; c <= std::min(most, ceil_div(32 * kSms, blocks)); ++c) {
             const long long t = ceil_div(blocks * c, slots) * (ceil_div(ceil_div(w.HW, c), w.rows) + 10);
@@ -147,7 +148,7 @@ constexpr long long kMaxGrid = 0x7fffffffll;
 template <typename T>
 void encode(Launcher& go, const Dims& d, const alexnet_view_t& x, const alexnet_checkpoint_t& k, int dtype) {
     const bool vec = vec_ok(x, d, dtype) && vec_ok(k, d), int8 = k.format == ALEXNET_CODES_INT8;
-    const Walk w = vec ? walk_of(d, 8, false) : walk_any(d);
+    const Walk w = vec ? walk_of(d, 8, kElementwise) : walk_any(d);
     const Geo g = geo_of(x, d, w.rows);
     if (vec) go(int8 ? checkpoint_encode_kernel<T, kSrcInt8> : checkpoint_encode_kernel<T, kSrcE4m3>, grid_of(w, d), 256, (const T*)x.data, g, w, (uint8_t*)k.codes, k.scales);
     else go(int8 ? checkpoint_encode_any_kernel<T, kSrcInt8> : checkpoint_encode_any_kernel<T, kSrcE4m3>, grid_of(w, d), 256, (const T*)x.data, g, w, (uint8_t*)k.codes, k.scales);
@@ -155,7 +156,7 @@ void encode(Launcher& go, const Dims& d, const alexnet_view_t& x, const alexnet_
 template <typename T>
 void decode(Launcher& go, const Dims& d, const alexnet_view_t& x, const alexnet_checkpoint_t& k, int dtype) {
     const bool vec = vec_ok(x, d, dtype) && vec_ok(k, d), int8 = k.format == ALEXNET_CODES_INT8;
-    const Walk w = vec ? walk_of(d, 8, false) : walk_any(d);
+    const Walk w = vec ? walk_of(d, 8, kElementwise) : walk_any(d);
     const Geo g = geo_of(x, d, w.rows);
     const uint8_t *codes = (const uint8_t*)k.codes, *scales = k.scales;
     if (vec) go(int8 ? checkpoint_decode_kernel<T, kSrcInt8> : checkpoint_decode_kernel<T, kSrcE4m3>, grid_of(w, d), 256, codes, scales, g, w, (T*)x.data);
@@ -176,7 +177,7 @@ int checkpoint_call(const alexnet_checkpoint_args_t* a, cudaStream_t st, const E
     if (const char* m = check_view(a->x, d, a->dtype, !enc)) return err.arg(m);
     if (const char* m = check_codes(a->checkpoint, d)) return err.arg(m);
     if (d.n == 0) return ALEXNET_OK;
-    if (grid_of(walk_any(d), d) > kMaxGrid || grid_of(walk_of(d, 1, false), d) > kMaxGrid) return err.arg("the tensor is too large");
+    if (grid_of(walk_any(d), d) > kMaxGrid || grid_of(walk_of(d, 1, kElementwise), d) > kMaxGrid) return err.arg("the tensor is too large");
     Launcher go{st};
     switch (a->dtype) {
     case ALEXNET_DTYPE_BF16: enc ? encode<bf16>(go, d, a->x, a->checkpoint, a->dtype) : decode<bf16>(go, d, a->x, a->checkpoint, a->dtype); break;
@@ -267,7 +268,7 @@ template <int V>
 size_t forward_ws(const Dims& d, int groups, int dtype) {
     const int elem = elem_bytes(dtype);
     if (slice_walk<V>(d, groups, elem * V, elem, false).threads) return 0;
-    const Walk w = walk_of(d, V, true);
+    const Walk w = walk_of(d, V, kForwardSums);
     return (size_t)(d.n * w.chunks) * d.C * sizeof(float4);
 }
 template <int V>
@@ -275,12 +276,12 @@ size_t backward_ws(const Dims& d, int groups, int dtype, bool kept) {
     const int elem = elem_bytes(dtype);
     const SliceWalk& s = slice_walk<V>(d, groups, elem * V + (kept ? V + 1 : elem * V), kept ? 2 : elem, true);
     if (s.threads) return d.n == 1 ? 0 : (size_t)std::min<long long>(d.n, 32 * kSms) * 2 * d.C * sizeof(float);      // (never more blocks of a slice than 32 per SM)
-    const Walk w = walk_of(d, V, true);
+    const Walk w = walk_of(d, V, kBackward);
     return (size_t)(d.n * groups) * sizeof(float2) + (size_t)(d.n * w.chunks) * 2 * d.C * sizeof(float);
 }
 template <typename T, int V, int ACT>
 void forward(Launcher& go, const alexnet_group_norm_forward_t* a, const Dims& d) {
-    const Walk w = walk_of(d, V, true);
+    const Walk w = walk_of(d, V, kForwardSums);
     const NormShape s = norm_shape(a->shape);
     Keep kx{}, ky{};
     if (V == 8) {
@@ -300,7 +301,7 @@ void forward(Launcher& go, const alexnet_group_norm_forward_t* a, const Dims& d)
         }
         return;
     }
-    const Walk wa = walk_of(d, V, false);
+    const Walk wa = walk_of(d, V, kElementwise);
     const Geo gx = geo_of(a->x, d, w.rows), gy = geo_of(a->y, d, w.rows);      // (the same threads' rows in both walks)
     float4* partial = (float4*)a->workspace;
     const T *x = (const T*)a->x.data;
@@ -317,7 +318,7 @@ void forward(Launcher& go, const alexnet_group_norm_forward_t* a, const Dims& d)
 }
 template <typename T, int V, int SRC, int ACT>
 void backward(Launcher& go, const alexnet_group_norm_backward_t* a, const Dims& d) {
-    const Walk w = walk_of(d, V, true);
+    const Walk w = walk_of(d, V, kBackward);
     const NormShape s = norm_shape(a->shape);
     float2* c12 = (float2*)a->workspace;
     float* partial = (float*)(c12 + d.n * s.groups);
@@ -467,7 +468,7 @@ int alexnet_group_norm_forward(const alexnet_group_norm_forward_t* a, void* stre
     if (d.n == 0) return ALEXNET_OK;
     if (!a->mean || !a->rstd) return err.arg("NULL pointer");
     if (a->x.data == a->y.data) return err.arg("y must not share memory with x");
-    if (grid_of(walk_of(d, 1, false), d) > kMaxGrid) return err.arg("the tensor is too large");
+    if (grid_of(walk_of(d, 1, kElementwise), d) > kMaxGrid) return err.arg("the tensor is too large");
     bool vec = vec_ok(a->x, d, s.dtype) && vec_ok(a->y, d, s.dtype);
     if (a->keep_x.codes) vec = vec && vec_ok(a->keep_x, d);
     if (a->keep_y.codes) vec = vec && vec_ok(a->keep_y, d);
@@ -501,7 +502,7 @@ int alexnet_group_norm_backward(const alexnet_group_norm_backward_t* a, void* st
     }
     if (!a->mean || !a->rstd) return err.arg("NULL pointer");
     if (a->dx.data == a->x.data || a->dx.data == a->dy.data) return err.arg("dx must not share memory with x or dy");
-    if (grid_of(walk_of(d, 1, false), d) > kMaxGrid) return err.arg("the tensor is too large");
+    if (grid_of(walk_of(d, 1, kElementwise), d) > kMaxGrid) return err.arg("the tensor is too large");
     const bool vec = vec_ok(a->dy, d, s.dtype) && vec_ok(a->dx, d, s.dtype) && (kept ? vec_ok(a->kept, d) : vec_ok(a->x, d, s.dtype));
     const size_t need = vec ? backward_ws<8>(d, s.groups, s.dtype, kept) : backward_ws<1>(d, s.groups, s.dtype, kept);
     if (need && (!a->workspace || (uintptr_t)a->workspace % 16 || a->workspace_bytes < need)) return err.arg("the workspace is too small or not 16-byte aligned");
