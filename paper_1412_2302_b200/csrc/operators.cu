@@ -245,6 +245,23 @@ const SliceWalk& slice_walk(const Dims& d, int groups, int slot, int elem, bool 
     q = {d.n, d.h, d.w, d.C, groups, slot, elem, backward, find_slice_walk<V>(d, groups, slot, elem, backward)};
     return q.walk;
 }
+// Forward passes: samples of more than 64 positions are kept by blocks where they are read in vectors of eight.  (With single channels the three launches are
+// faster or alike: 1 x 13 x 13 x 75 6.4 us against 18, 512 samples of it 23.6 both; 512 x 7 x 7 x 75 takes 13.2 against 11.3.)
+template <int V>
+const SliceWalk& forward_slices(const Dims& d, int groups, int elem) {
+    static const SliceWalk none{};
+    if (d.h * d.w > 64 && V == 1) return none;
+    return slice_walk<V>(d, groups, elem * V, elem, false);
+}
+// Backward passes: samples of more than 64 positions are kept by blocks where x is read as it is, in vectors of eight.  (From int8 codes, or with single
+// channels, the three launches are faster, SiLU: 128 x 27 x 27 x 256 60 us against 79, 512 x 13 x 13 x 384 92 against 108, 256 x 13 x 13 x 75 bf16 from x 23
+// against 37; with fewer positions they are not: 2048 x 7 x 7 x 512 154 against 139; nor from x: 512 x 27 x 27 x 256 without an activation 167 against 134.)
+template <int V>
+const SliceWalk& backward_slices(const Dims& d, int groups, int elem, bool kept) {
+    static const SliceWalk none{};
+    if (d.h * d.w > 64 && (kept || V == 1)) return none;
+    return slice_walk<V>(d, groups, elem * V + (kept ? V + 1 : elem * V), kept ? 2 : elem, true);
+}
 // Samples that are under way at once: as many blocks per slice as the device holds (asked once per kernel and launch shape).
 template <typename K>
 long long slice_rows(Launcher& go, K* kernel, const SliceWalk& w, const Dims& d, size_t smem) {
@@ -266,15 +283,14 @@ long long slice_rows(Launcher& go, K* kernel, const SliceWalk& w, const Dims& d,
 // Bytes of workspace of a call with vectors of V channels; 0 where it takes one launch and leaves nothing between.
 template <int V>
 size_t forward_ws(const Dims& d, int groups, int dtype) {
-    const int elem = elem_bytes(dtype);
-    if (slice_walk<V>(d, groups, elem * V, elem, false).threads) return 0;
+    if (forward_slices<V>(d, groups, elem_bytes(dtype)).threads) return 0;
     const Walk w = walk_of(d, V, kForwardSums);
     return (size_t)(d.n * w.chunks) * d.C * sizeof(float4);
 }
 template <int V>
 size_t backward_ws(const Dims& d, int groups, int dtype, bool kept) {
     const int elem = elem_bytes(dtype);
-    const SliceWalk& s = slice_walk<V>(d, groups, elem * V + (kept ? V + 1 : elem * V), kept ? 2 : elem, true);
+    const SliceWalk& s = backward_slices<V>(d, groups, elem, kept);
     if (s.threads) return d.n == 1 ? 0 : (size_t)std::min<long long>(d.n, 32 * kSms) * 2 * d.C * sizeof(float);      // (never more blocks of a slice than 32 per SM)
     const Walk w = walk_of(d, V, kBackward);
     return (size_t)(d.n * groups) * sizeof(float2) + (size_t)(d.n * w.chunks) * 2 * d.C * sizeof(float);
@@ -288,7 +304,7 @@ void forward(Launcher& go, const alexnet_group_norm_forward_t* a, const Dims& d)
         if (a->keep_x.codes) kx = {(uint8_t*)a->keep_x.codes, a->keep_x.scales, src_of(a->keep_x.format)};
         if (a->keep_y.codes) ky = {(uint8_t*)a->keep_y.codes, a->keep_y.scales, src_of(a->keep_y.format)};
     }
-    const SliceWalk& sw = slice_walk<V>(d, s.groups, sizeof(T) * V, sizeof(T), false);
+    const SliceWalk& sw = forward_slices<V>(d, s.groups, (int)sizeof(T));
     if (sw.threads) {
         const size_t smem = (size_t)sw.its * sw.threads * sizeof(T) * V + slice_scratch<V>(sw, false);
         const long long rows = slice_rows(go, gn_slice_forward_kernel<T, V, ACT>, sw, d, smem);
@@ -326,7 +342,7 @@ void backward(Launcher& go, const alexnet_group_norm_backward_t* a, const Dims& 
     const BackwardArgs A{a->mean, a->rstd, a->weight, a->bias};
     const T* dy = (const T*)a->dy.data;
     constexpr int kSlot = (int)sizeof(T) * V + (SRC == kSrcSame ? (int)sizeof(T) * V : V + 1);
-    const SliceWalk& sw = slice_walk<V>(d, s.groups, kSlot, SRC == kSrcSame ? (int)sizeof(T) : 2, true);
+    const SliceWalk& sw = backward_slices<V>(d, s.groups, (int)sizeof(T), SRC != kSrcSame);
     if (sw.threads) {
         partial = (float*)a->workspace;
         auto* kernel = gn_slice_backward_kernel<T, V, SRC, ACT>;

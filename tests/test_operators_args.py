@@ -142,7 +142,7 @@ def test_linear_weight_grad_refuses(lib, bad, word):
 def test_small_calls_need_no_workspace(lib):
     """256 bytes say so; the larger ones name what they need."""
     for backward in (0, 1):
-        assert lib.alexnet_group_norm_workspace_bytes(ops._pack_shape(*shape(n=1, h=13, w=13, c=384, groups=32)), backward) == 256
+        assert lib.alexnet_group_norm_workspace_bytes(ops._pack_shape(*shape(n=1, h=7, w=7, c=384, groups=32)), backward) == 256
         assert lib.alexnet_group_norm_workspace_bytes(ops._pack_shape(*shape(h=400, w=400)), backward) > 256
     small, large = (ops._pack_linear(rows, 64, 64, P, 64, *KEPT, 0, 0, 0) for rows in (64, 4096))
     assert lib.alexnet_linear_weight_grad_workspace_bytes(small) == 256 and lib.alexnet_linear_weight_grad_workspace_bytes(large) > 4 * 64 * 64 * 4
