@@ -281,7 +281,8 @@ __device__ __forceinline__ Spot spot(const Walk& w, int skip = 0) {
 }
 
 // ---------------------------------------------------------------- encode, decode
-// Rows of a multiple of eight channels at 16-byte boundaries: four lanes per block.  HBM-bound: 2 bytes read and 1.03 written per bf16 value.
+// Rows of a multiple of eight channels at 16-byte boundaries: four lanes per block.  HBM-bound: 2 bytes read and 1.03 written per bf16 value
+// (512 x 55 x 55 x 96: encode 83 us, decode 76, of 69 at the copy rate).
 template <typename T, int FMT>
 __global__ void __launch_bounds__(256) checkpoint_encode_kernel(const T* __restrict__ x, const Geo g, const Walk w, uint8_t* __restrict__ codes, uint8_t* __restrict__ scales) {
     kn::pdl_sync();
@@ -340,7 +341,8 @@ __global__ void __launch_bounds__(256) checkpoint_decode_kernel(const uint8_t* _
         }
     }
 }
-// Any other rows: a warp per block (Walk's vectors), a lane per value; a warp walks down the positions of its block.
+// Any other rows: a warp per block (Walk's vectors), a lane per value; a warp walks down the positions of its block.  Bound by instructions, one value each
+// (64 x 31 x 31 x 75 bf16: encode 15 us, decode 11).
 struct WarpSpot { int lane, c, p0, p1; long long n; bool on; };
 __device__ __forceinline__ WarpSpot warp_spot(const Walk& w) {
     const long long b = blockIdx.x, t = b / w.colblocks, n = t / w.chunks;

@@ -6,7 +6,9 @@
 //   dx = rstd (dz w - c1 - xhat c2),  c1 = mean(dz w), c2 = mean(dz w xhat) over the group
 //
 // Written with d = x - mean and a = rstd w as  z = d a + b  and  dx = dz a + (d (-rstd^2 c2) - rstd c1): two packed instructions per pair
-// of channels each.  Both directions are HBM-bound: x in and y out; dy and x in and dx out.
+// of channels each.  Both directions are HBM-bound: x in and y out; dy and x in and dx out.  Measured, bf16 (at the copy rate): 128 x 27 x 27 x 256, a launch per
+// direction, forward 27 us (14.6), SiLU 33, backward 44 (21.9), SiLU 65; 512 x 55 x 55 x 96, read twice, forward 164 (91), backward 258 (136), ReLU 275, SiLU 320.
+// Small calls are bound by their launches and a chain of sums and barriers: 1 x 13 x 13 x 384 7.5 us.
 //
 // Sums.  A thread sums, for each of its channels, the differences from the first value it reads and their squares, in fp32.  That value
 // is one of the summed, so the sum of squares is at most (1 + n) times the true one about the mean, however far the mean is from zero: nothing
@@ -394,12 +396,13 @@ __device__ __forceinline__ void activation_gradient(int act, const Chan<V>& k, c
         v_mul<V>(dy, u, dy);
     }
 }
-// Positions whose loads a thread of the two kernels below has under way, of two tensors each, with 128 registers and two blocks per SM.  512 x 55 x 55 x 96 bf16,
-// ReLU, both kernels: four from x 289 us, from int8 codes 315; three 297 and 325; two, with three blocks of 80 registers, 322 and 418.  From e4m3 codes three
-// take 322, four 339; in fp32 (a quarter of the samples) three take 131, four 147.
-template <typename T, int V, int SRC> constexpr int kBackwardLoads = V == 8 && (sizeof(T) == 4 || SRC == kSrcE4m3) ? 3 : 4;
+// Positions whose loads a thread of the two kernels below has under way, of two tensors each, and blocks per SM (two with 128 registers, three with 80).
+// 512 x 55 x 55 x 96 bf16, ReLU, both kernels: four and two from x 289 us, from int8 codes 315; three and two 297 and 325; two and three 314 and 396.  From e4m3
+// codes, SiLU: two and three 351, three and two 393, four and two 406.  In fp32 (a quarter of the samples, from x): three and two 131, four and two 147.
+template <typename T, int V, int SRC> constexpr int kBackwardBlocks = V == 8 && (sizeof(T) == 4 || SRC != kSrcE4m3) ? 2 : 3;
+template <typename T, int V, int SRC> constexpr int kBackwardLoads = V == 8 ? (sizeof(T) == 4 ? 3 : SRC == kSrcE4m3 ? 2 : 4) : 4;
 template <typename T, int V, int SRC, int ACT>
-__global__ void __launch_bounds__(256, V == 8 ? 2 : 3) gn_backward_sums_kernel(const T* __restrict__ dy, const Geo gdy, const Source src, const Geo gx, const Walk w, const NormShape sh,
+__global__ void __launch_bounds__(256, kBackwardBlocks<T, V, SRC>) gn_backward_sums_kernel(const T* __restrict__ dy, const Geo gdy, const Source src, const Geo gx, const Walk w, const NormShape sh,
                                                                const BackwardArgs A, float* __restrict__ partial) {
     kn::pdl_sync();
     __shared__ float sums[2 * V * 260];
@@ -501,7 +504,7 @@ __global__ void __launch_bounds__(1024) gn_parameter_gradient_kernel(const float
     parameter_gradient<32>(partial, C, n, blockIdx.x, red, dweight, dbias);
 }
 template <typename T, int V, int SRC, int ACT>
-__global__ void __launch_bounds__(256, V == 8 ? 2 : 3) gn_backward_apply_kernel(const T* __restrict__ dy, const Geo gdy, const Source src, const Geo gx, const Walk w, const NormShape sh,
+__global__ void __launch_bounds__(256, kBackwardBlocks<T, V, SRC>) gn_backward_apply_kernel(const T* __restrict__ dy, const Geo gdy, const Source src, const Geo gx, const Walk w, const NormShape sh,
                                                                 const BackwardArgs A, const float2* __restrict__ c12, T* __restrict__ dx, const Geo gdx, const float* __restrict__ partial,
                                                                 long long partials, int extra, float* __restrict__ dweight, float* __restrict__ dbias) {
     kn::pdl_sync();

@@ -102,11 +102,11 @@ bool vec_ok(const alexnet_view_t& v, const Dims& d, int dtype) {
 }
 bool vec_ok(const alexnet_checkpoint_t& k, const Dims& d) { return d.C % 8 == 0 && (uintptr_t)k.codes % 8 == 0; }
 
-// How a launch walks [n][h w][C] with vectors of V channels.  Elementwise passes: eight blocks per SM, of at least four positions per thread.
-// Passes whose blocks end with a reduction: whole rounds of what an SM holds of them (vectors of eight: three, in backward passes two), a block being as dear as
+// How a launch walks [n][h w][C] with vectors of V channels.  Elementwise passes (blocks_per_sm = 0): eight blocks per SM, of at least four positions per thread.
+// Passes whose blocks end with a reduction: whole rounds of what an SM holds of them (`blocks_per_sm` with vectors of eight, six with single channels), a block being as dear as
 // its positions and ten more.
-enum Pass { kElementwise, kForwardSums, kBackward };
-Walk walk_of(const Dims& d, int V, Pass pass) {
+constexpr int kElementwise = 0, kForwardSums = 3;
+Walk walk_of(const Dims& d, int V, int blocks_per_sm) {
     Walk w{};
     w.C = d.C; w.HW = d.h * d.w; w.vecs = d.C / V;
     const int q = V == 8 ? 4 : 1, padded = (int)ceil_div(w.vecs, q) * q;
@@ -115,8 +115,8 @@ Walk walk_of(const Dims& d, int V, Pass pass) {
     w.rows = 256 / w.cols;
     const long long blocks = std::max<long long>(1, d.n * w.colblocks), most = std::max<long long>(1, ceil_div(w.HW, 4 * w.rows));
     long long chunks = std::min(most, ceil_div(8 * kSms, blocks));
-    if (pass != kElementwise) {
-        const int slots = (V != 8 ? 6 : pass == kBackward ? 2 : 3) * kSms;
+    if (blocks_per_sm) {
+        const int slots = (V == 8 ? blocks_per_sm : 6) * kSms;
         long long cost = 1ll << 62;
         for (long long c = 1; c <= std::min(most, ceil_div(32 * kSms, blocks)); ++c) {
             const long long t = ceil_div(blocks * c, slots) * (ceil_div(ceil_div(w.HW, c), w.rows) + 10);
@@ -292,8 +292,8 @@ size_t backward_ws(const Dims& d, int groups, int dtype, bool kept) {
     const int elem = elem_bytes(dtype);
     const SliceWalk& s = backward_slices<V>(d, groups, elem, kept);
     if (s.threads) return d.n == 1 ? 0 : (size_t)std::min<long long>(d.n, 32 * kSms) * 2 * d.C * sizeof(float);      // (never more blocks of a slice than 32 per SM)
-    const Walk w = walk_of(d, V, kBackward);
-    return (size_t)(d.n * groups) * sizeof(float2) + (size_t)(d.n * w.chunks) * 2 * d.C * sizeof(float);
+    const long long chunks = std::max(walk_of(d, V, 2).chunks, walk_of(d, V, 3).chunks);       // (of either source)
+    return (size_t)(d.n * groups) * sizeof(float2) + (size_t)(d.n * chunks) * 2 * d.C * sizeof(float);
 }
 template <typename T, int V, int ACT>
 void forward(Launcher& go, const alexnet_group_norm_forward_t* a, const Dims& d) {
@@ -334,7 +334,7 @@ void forward(Launcher& go, const alexnet_group_norm_forward_t* a, const Dims& d)
 }
 template <typename T, int V, int SRC, int ACT>
 void backward(Launcher& go, const alexnet_group_norm_backward_t* a, const Dims& d) {
-    const Walk w = walk_of(d, V, kBackward);
+    const Walk w = walk_of(d, V, kBackwardBlocks<T, V, SRC>);
     const NormShape s = norm_shape(a->shape);
     float2* c12 = (float2*)a->workspace;
     float* partial = (float*)(c12 + d.n * s.groups);
