@@ -122,6 +122,17 @@ template <int UNROLL, typename G, typename N> __device__ __forceinline__ Part jo
     const float lo = e * inv;
     return {hi, lo, fmaf(-e, lo, q)};
 }
+// A running sum whose roundings are summed beside it (the error of an fp32 addition is an fp32 number), for sums that are as long as a caller's
+// tensor has samples: a plain one is off by 2^-25 of its value per term where the terms are alike, 65536 samples of 9 x 9 x 32 by 1.1e-4.
+struct LongSum {
+    float s = 0.f, e = 0.f;
+    __device__ __forceinline__ void add(float v) {
+        const float t = s + v, b = t - s;
+        e += (s - (t - b)) + (v - b);
+        s = t;
+    }
+    __device__ __forceinline__ float value() const { return e == e ? s + e : s; }      // (beside an infinity there is no error to speak of)
+};
 // the sum over `lanes` neighbouring lanes (a power of two; all 32 of the warp call it)
 __device__ __forceinline__ float lanes_sum(float t, int lanes) {
     for (int o = lanes >> 1; o; o >>= 1) t += __shfl_xor_sync(~0u, t, o);
@@ -483,12 +494,13 @@ __global__ void __launch_bounds__(256) gn_backward_group_kernel(const float* __r
 template <int WARPS>
 __device__ __forceinline__ void parameter_gradient(const float* __restrict__ partial, int C, long long n, int block, float2* red /* [WARPS][33] */, float* __restrict__ dweight, float* __restrict__ dbias) {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, c = block * 32 + lane;
-    float2 t = make_float2(0.f, 0.f);
+    LongSum b, w;
     if (c < C) {
         const float* p = partial + c;
         #pragma unroll 8
-        for (long long i = warp; i < n; i += WARPS) { t.x += p[i * 2 * C]; t.y += p[i * 2 * C + C]; }
+        for (long long i = warp; i < n; i += WARPS) { b.add(p[i * 2 * C]); w.add(p[i * 2 * C + C]); }
     }
+    float2 t = make_float2(b.value(), w.value());
     red[warp * 33 + lane] = t;
     __syncthreads();
     if (warp == 0 && c < C) {
@@ -597,23 +609,25 @@ __device__ __forceinline__ void copies_wait(int pending) {
 }
 constexpr int kSlBatches = 4;                 // groups of copies
 
-// Shared memory behind the slots: the groups' results, two sums per thread and vector element; backward also two sums per channel, those of all samples, the
-// channels' weights and the groups' rstd.
+// Shared memory behind the slots: the groups' results, two sums per thread and vector element; backward also two sums per channel, those of all samples
+// (LongSum), the channels' weights and the groups' rstd.
 template <int V> struct SliceSmem {
     float2* res;
     Table<V> part;
-    float *chan, *acc, *weight, *rstd;
+    float* chan;
+    LongSum* acc;
+    float *weight, *rstd;
     __device__ __forceinline__ SliceSmem(uint8_t* p, const SliceWalk& w) {
         res = (float2*)p;
         part = {(float*)(res + w.groups), w.threads + 4};
         chan = part.p + 2 * V * part.pitch;
-        acc = chan + 2 * w.Cs;
-        weight = acc + 2 * w.Cs;
+        acc = (LongSum*)(chan + 2 * w.Cs);
+        weight = (float*)(acc + 2 * w.Cs);
         rstd = weight + w.Cs;
     }
 };
 template <int V> inline size_t slice_scratch(const SliceWalk& w, bool backward) {
-    return ((size_t)2 * V * (w.threads + 4) + (backward ? 5 * w.Cs + w.groups : 0)) * sizeof(float) + w.groups * sizeof(float2);
+    return ((size_t)2 * V * (w.threads + 4) + (backward ? 7 * w.Cs + w.groups : 0)) * sizeof(float) + w.groups * sizeof(float2);
 }
 // a block's work: a slice (from channel c0, group g0 on) of the samples n0, n0 + step, ...
 struct SliceSpot {
@@ -834,7 +848,7 @@ __global__ void __launch_bounds__(kSlThreads, 2) gn_slice_backward_kernel(const 
         }
     }
     for (int c = tid; c < w.Cs; c += w.threads) {
-        m.acc[c] = m.acc[w.Cs + c] = 0.f;
+        m.acc[c] = m.acc[w.Cs + c] = LongSum{};
         m.weight[c] = A.weight ? A.weight[b.c0 + c] : 1.f;
     }
     #pragma unroll 1
@@ -877,8 +891,8 @@ __global__ void __launch_bounds__(kSlThreads, 2) gn_slice_backward_kernel(const 
             t.y *= m.rstd[sh.group(c)];                         // of xhat
             m.chan[c] = t.x;
             m.chan[w.Cs + c] = t.y;
-            m.acc[c] += t.x;
-            m.acc[w.Cs + c] += t.y;
+            m.acc[c].add(t.x);
+            m.acc[w.Cs + c].add(t.y);
         }
         __syncthreads();
         const float per = __frcp_rn((float)sh.HW * (float)sh.cg);
@@ -943,8 +957,8 @@ __global__ void __launch_bounds__(kSlThreads, 2) gn_slice_backward_kernel(const 
     }
     if (b.n0 < samples) {
         for (int c = tid; c < w.Cs; c += w.threads) {
-            if (sum1) sum1[b.n0 * sum_pitch + b.c0 + c] = m.acc[c];
-            if (sum2) sum2[b.n0 * sum_pitch + b.c0 + c] = m.acc[w.Cs + c];
+            if (sum1) sum1[b.n0 * sum_pitch + b.c0 + c] = m.acc[c].value();
+            if (sum2) sum2[b.n0 * sum_pitch + b.c0 + c] = m.acc[w.Cs + c].value();
         }
     }
 }

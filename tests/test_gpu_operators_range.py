@@ -1,0 +1,48 @@
+"""The operators on caller-owned tensors over the whole of their ranges: sums as long as a tensor has samples or positions, values and parameters at
+the ends of their types, against the definitions in 64 bits.
+
+Tolerances.  Where the terms of a sum are alike, an fp32 running sum of k of them is off by at most k 2^-25 of it (half a step, at most 2^-24 of
+the running sum, which is half of the last one on average).  A thread of a backward pass sums at most 192 terms so, the sums of its block's rows
+come in four chains of at most 64 each, those of warps in chains of at most 32; everything longer carries the error of its additions along
+(2^-24 in all).  192 + 64 of 2^-25 are 2^-17, FP32 below: that times the sum of the magnitudes."""
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+FP32 = 2.0 ** -17
+TYPES = {"bf16": torch.bfloat16, "fp16": torch.float16, "fp32": torch.float32}
+
+
+@pytest.fixture(scope="module")
+def ops():
+    from paper_1412_2302_b200 import operators
+    return operators
+
+
+def gen(seed):
+    return torch.Generator(device="cuda").manual_seed(seed)
+
+
+def parameter_gradients_of_alike(ops, shape, groups, src):
+    """dbias and dweight for a dy that is one number per channel, statistics of 0 and 1 and values of one sign: nothing cancels, so the running sums
+    grow and their roundings with them."""
+    n, h, w, c = shape
+    dy = torch.linspace(0.05, 0.15, c, device="cuda").expand(shape)
+    x = (torch.rand((1, h, w, c), device="cuda", generator=gen(n)) + 0.5).expand(shape)
+    mean, rstd = torch.zeros((n, groups), device="cuda"), torch.ones((n, groups), device="cuda")
+    kept, value = x, x[0]
+    if src != "x":
+        kept = ops.checkpoint_encode(x, src)
+        value = ops.checkpoint_decode(ops.Checkpoint(kept.codes[0], kept.scales[0]), torch.float32)
+    _, dw, db = ops.group_norm_backward(dy, kept, mean, rstd)
+    dy64 = dy[0, 0, 0].double()
+    want_b, want_w = dy64 * (n * h * w), dy64 * value.double().sum((0, 1)) * n
+    assert float(((db.double() - want_b).abs() / want_b).max()) < FP32
+    assert float(((dw.double() - want_w).abs() / want_w).max()) < FP32
+
+
+@pytest.mark.parametrize("src", ["x", "int8"])
+@pytest.mark.parametrize("shape,groups", [((16384, 9, 9, 64), 8), ((65536, 9, 9, 32), 8), ((65536, 9, 9, 9), 3), ((400000, 3, 2, 32), 4), ((1000000, 1, 1, 32), 4)])
+def test_parameter_gradients_of_many_samples(ops, shape, groups, src):
+    parameter_gradients_of_alike(ops, shape, groups, src)
