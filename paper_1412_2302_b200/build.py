@@ -35,7 +35,9 @@ def build(force: bool = False, verbose: bool = False, timeline: bool = False) ->
     if not force and not timeline and not _stale():
         return lib
     nvcc = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")
-    flags = [nvcc, "-gencode", "arch=compute_100a,code=sm_100a", "-O3", "-lineinfo", "-std=c++17", "-split-compile=0", "-Xcompiler", "-fPIC", "-Xcompiler", "-pthread"]
+    # (No -split-compile: it cuts a file into parts to compile them side by side, and where it cuts changes the registers and spills of kernels whose
+    # source did not change.  With it a training step of 128 images took 1.064 ms for 1.025.)
+    flags = [nvcc, "-gencode", "arch=compute_100a,code=sm_100a", "-O3", "-lineinfo", "-std=c++17", "-Xcompiler", "-fPIC", "-Xcompiler", "-pthread"]
     if verbose:
         flags.append("-Xptxas=-v")
     os.makedirs(OBJECTS, exist_ok=True)
