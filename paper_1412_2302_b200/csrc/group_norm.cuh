@@ -133,6 +133,14 @@ struct LongSum {
     }
     __device__ __forceinline__ float value() const { return e == e ? s + e : s; }      // (beside an infinity there is no error to speak of)
 };
+template <int N> __device__ __forceinline__ float sum_of(float* v) {      // N a power of two, in pairs
+    #pragma unroll
+    for (int o = N / 2; o; o /= 2) {
+        #pragma unroll
+        for (int i = 0; i < o; ++i) v[i] += v[i + o];
+    }
+    return v[0];
+}
 // the sum over `lanes` neighbouring lanes (a power of two; all 32 of the warp call it)
 __device__ __forceinline__ float lanes_sum(float t, int lanes) {
     for (int o = lanes >> 1; o; o >>= 1) t += __shfl_xor_sync(~0u, t, o);
@@ -458,11 +466,15 @@ __global__ void __launch_bounds__(256, kBackwardBlocks<T, V, SRC>) gn_backward_s
     const int nch = w.cols * V, c0 = (s.v - s.col) * V;
     for (int j = threadIdx.x; j < nch; j += 256) {
         if (c0 + j >= w.C) break;
-        float t1 = 0.f, t2 = 0.f;
-        for (int r = 0; r < w.rows; ++r) { t1 += table.at(0, j % V, r * w.cols + j / V); t2 += table.at(1, j % V, r * w.cols + j / V); }
+        float t1[4] = {}, t2[4] = {};                       // four chains: up to 256 rows
+        for (int r = 0; r < w.rows; r += 4) {
+            #pragma unroll
+            for (int q = 0; q < 4; ++q)
+                if (r + q < w.rows) { t1[q] += table.at(0, j % V, (r + q) * w.cols + j / V); t2[q] += table.at(1, j % V, (r + q) * w.cols + j / V); }
+        }
         float* o = partial + (s.n * w.chunks + s.chunk) * 2 * w.C + c0 + j;
-        o[0] = t1;
-        o[w.C] = t2 * A.rstd[s.n * sh.groups + sh.group(c0 + j)];       // of xhat
+        o[0] = (t1[0] + t1[1]) + (t1[2] + t1[3]);
+        o[w.C] = ((t2[0] + t2[1]) + (t2[2] + t2[3])) * A.rstd[s.n * sh.groups + sh.group(c0 + j)];       // of xhat
     }
 }
 // c1 and c2 of a group from the chunks' sums [chunks][2][C], by a block or a warp
@@ -477,15 +489,25 @@ __global__ void __launch_bounds__(256) gn_backward_group_kernel(const float* __r
     const long long n = id / sh.groups;
     const int g = (int)(id - n * sh.groups), total = chunks * sh.cg;
     const float* p = partial + n * chunks * 2 * sh.C + (long long)g * sh.cg;
-    float2 t = make_float2(0.f, 0.f);
-    #pragma unroll 4
-    for (int i = me; i < total; i += N) {
-        const int k = sh.group(i), c = i - k * sh.cg;
-        const float wt = A.weight ? A.weight[g * sh.cg + c] : 1.f;
-        const float* q = p + (long long)k * 2 * sh.C + c;
-        t.x = fmaf(wt, q[0], t.x);
-        t.y = fmaf(wt, q[sh.C], t.y);
+    LongSum t1, t2;
+    for (int i = me; i < total; i += 4 * N) {
+        float u1[4], u2[4];
+        #pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            const int j = i + u * N;
+            u1[u] = u2[u] = 0.f;
+            if (j < total) {
+                const int k = sh.group(j), c = j - k * sh.cg;
+                const float wt = A.weight ? A.weight[g * sh.cg + c] : 1.f;
+                const float* q = p + (long long)k * 2 * sh.C + c;
+                u1[u] = wt * q[0];
+                u2[u] = wt * q[sh.C];
+            }
+        }
+        t1.add(sum_of<4>(u1));
+        t2.add(sum_of<4>(u2));
     }
+    float2 t = make_float2(t1.value(), t2.value());
     t = BLOCK ? block_sum(t, red) : warp_sum(t);
     const float m = (float)sh.HW * (float)sh.cg;
     if (me == 0) c12[id] = make_float2(__fdiv_rn(t.x, m), __fdiv_rn(t.y, m));
@@ -497,8 +519,17 @@ __device__ __forceinline__ void parameter_gradient(const float* __restrict__ par
     LongSum b, w;
     if (c < C) {
         const float* p = partial + c;
-        #pragma unroll 8
-        for (long long i = warp; i < n; i += WARPS) { b.add(p[i * 2 * C]); w.add(p[i * 2 * C + C]); }
+        for (long long i = warp; i < n; i += 8 * WARPS) {
+            float v[8], q[8];
+            #pragma unroll
+            for (int u = 0; u < 8; ++u) {
+                const long long k = i + u * WARPS;
+                v[u] = k < n ? p[k * 2 * C] : 0.f;
+                q[u] = k < n ? p[k * 2 * C + C] : 0.f;
+            }
+            b.add(sum_of<8>(v));
+            w.add(sum_of<8>(q));
+        }
     }
     float2 t = make_float2(b.value(), w.value());
     red[warp * 33 + lane] = t;
@@ -609,25 +640,23 @@ __device__ __forceinline__ void copies_wait(int pending) {
 }
 constexpr int kSlBatches = 4;                 // groups of copies
 
-// Shared memory behind the slots: the groups' results, two sums per thread and vector element; backward also two sums per channel, those of all samples
-// (LongSum), the channels' weights and the groups' rstd.
+// Shared memory behind the slots: the groups' results, two sums per thread and vector element; backward also two sums per channel, those of the block's last samples, the
+// channels' weights and the groups' rstd.
 template <int V> struct SliceSmem {
     float2* res;
     Table<V> part;
-    float* chan;
-    LongSum* acc;
-    float *weight, *rstd;
+    float *chan, *acc, *weight, *rstd;
     __device__ __forceinline__ SliceSmem(uint8_t* p, const SliceWalk& w) {
         res = (float2*)p;
         part = {(float*)(res + w.groups), w.threads + 4};
         chan = part.p + 2 * V * part.pitch;
-        acc = (LongSum*)(chan + 2 * w.Cs);
-        weight = (float*)(acc + 2 * w.Cs);
+        acc = chan + 2 * w.Cs;
+        weight = acc + 2 * w.Cs;
         rstd = weight + w.Cs;
     }
 };
 template <int V> inline size_t slice_scratch(const SliceWalk& w, bool backward) {
-    return ((size_t)2 * V * (w.threads + 4) + (backward ? 7 * w.Cs + w.groups : 0)) * sizeof(float) + w.groups * sizeof(float2);
+    return ((size_t)2 * V * (w.threads + 4) + (backward ? 5 * w.Cs + w.groups : 0)) * sizeof(float) + w.groups * sizeof(float2);
 }
 // a block's work: a slice (from channel c0, group g0 on) of the samples n0, n0 + step, ...
 struct SliceSpot {
@@ -805,8 +834,14 @@ __global__ void __launch_bounds__(kSlThreads, 2) gn_slice_forward_kernel(const T
     }
 }
 
-// The same for the backward pass: sums of dz and dz d per channel, c1 and c2 of the groups, then dx.  The samples' sums for dweight and dbias are added up in
-// shared memory and go to sum1 and sum2 [block of the slice] at the end, rows sum_pitch apart; with one block per slice these are the gradients.
+// The same for the backward pass: sums of dz and dz d per channel, c1 and c2 of the groups, then dx.  A block's sums for dweight and dbias are added up in
+// shared memory and go to sum1 and sum2 every kSlSamples of its samples (so these running sums are short), to rows sum_pitch apart, first those of the
+// blocks' first kSlSamples samples, block by block; a single row is the gradients.
+constexpr int kSlSamples = 64;
+inline long long slice_sums(long long samples, long long step) {      // rows that a launch with `step` blocks per slice writes
+    const long long full = (samples - 1) / (kSlSamples * step);
+    return full * step + (samples - full * kSlSamples * step < step ? samples - full * kSlSamples * step : step);
+}
 template <typename T, int V, int SRC, int ACT>
 __global__ void __launch_bounds__(kSlThreads, 2) gn_slice_backward_kernel(const T* __restrict__ dy, const Geo gdy, const Source src, const Geo gx, const SliceWalk w, const NormShape sh,
                                                                           long long samples, const BackwardArgs A, T* __restrict__ dx, const Geo gdx, float* __restrict__ sum1,
@@ -848,11 +883,14 @@ __global__ void __launch_bounds__(kSlThreads, 2) gn_slice_backward_kernel(const 
         }
     }
     for (int c = tid; c < w.Cs; c += w.threads) {
-        m.acc[c] = m.acc[w.Cs + c] = LongSum{};
+        m.acc[c] = m.acc[w.Cs + c] = 0.f;
         m.weight[c] = A.weight ? A.weight[b.c0 + c] : 1.f;
     }
     #pragma unroll 1
-    for (long long n = b.n0; n < samples; n += b.step) {
+    for (long long n = b.n0, out = b.n0; n < samples; out += b.step) {
+    const long long end = min(samples, n + kSlSamples * b.step);
+    #pragma unroll 1
+    for (; n < end; n += b.step) {
         const long long gb = n * sh.groups + b.g0;              // this block's first group
         for (int g = tid; g < w.groups; g += w.threads) m.rstd[g] = A.rstd[gb + g];
         Chan<V> k;
@@ -891,8 +929,8 @@ __global__ void __launch_bounds__(kSlThreads, 2) gn_slice_backward_kernel(const 
             t.y *= m.rstd[sh.group(c)];                         // of xhat
             m.chan[c] = t.x;
             m.chan[w.Cs + c] = t.y;
-            m.acc[c].add(t.x);
-            m.acc[w.Cs + c].add(t.y);
+            m.acc[c] += t.x;
+            m.acc[w.Cs + c] += t.y;
         }
         __syncthreads();
         const float per = __frcp_rn((float)sh.HW * (float)sh.cg);
@@ -955,11 +993,11 @@ __global__ void __launch_bounds__(kSlThreads, 2) gn_slice_backward_kernel(const 
         if (SRC != kSrcSame && more && cnt > 0) eslots[(cnt - 1) * w.threads] = e_next;
         __syncthreads();                                        // (the groups' rstd and results are free for the next sample)
     }
-    if (b.n0 < samples) {
-        for (int c = tid; c < w.Cs; c += w.threads) {
-            if (sum1) sum1[b.n0 * sum_pitch + b.c0 + c] = m.acc[c].value();
-            if (sum2) sum2[b.n0 * sum_pitch + b.c0 + c] = m.acc[w.Cs + c].value();
-        }
+    for (int c = tid; c < w.Cs; c += w.threads) {               // (this thread's sums)
+        if (sum1) sum1[out * sum_pitch + b.c0 + c] = m.acc[c];
+        if (sum2) sum2[out * sum_pitch + b.c0 + c] = m.acc[w.Cs + c];
+        m.acc[c] = m.acc[w.Cs + c] = 0.f;
+    }
     }
 }
 

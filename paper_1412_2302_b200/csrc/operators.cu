@@ -104,8 +104,8 @@ bool vec_ok(const alexnet_checkpoint_t& k, const Dims& d) { return d.C % 8 == 0 
 
 // How a launch walks [n][h w][C] with vectors of V channels.  Elementwise passes (blocks_per_sm = 0): eight blocks per SM, of at least four positions per thread.
 // Passes whose blocks end with a reduction: whole rounds of what an SM holds of them (`blocks_per_sm` with vectors of eight, six with single channels), a block being as dear as
-// its positions and ten more.
-constexpr int kElementwise = 0, kForwardSums = 3;
+// its positions and ten more, and a thread adds up at most kMostTerms of them, for the sake of the sums' roundings.
+constexpr int kElementwise = 0, kForwardSums = 3, kMostTerms = 192;
 Walk walk_of(const Dims& d, int V, int blocks_per_sm) {
     Walk w{};
     w.C = d.C; w.HW = d.h * d.w; w.vecs = d.C / V;
@@ -117,8 +117,9 @@ Walk walk_of(const Dims& d, int V, int blocks_per_sm) {
     long long chunks = std::min(most, ceil_div(8 * kSms, blocks));
     if (blocks_per_sm) {
         const int slots = (V == 8 ? blocks_per_sm : 6) * kSms;
+        const long long least = ceil_div(w.HW, (long long)kMostTerms * w.rows);
         long long cost = 1ll << 62;
-        for (long long c = 1; c <= std::min(most, ceil_div(32 * kSms, blocks)); ++c) {
+        for (long long c = least; c <= std::max(least, std::min(most, ceil_div(32 * kSms, blocks))); ++c) {
             const long long t = ceil_div(blocks * c, slots) * (ceil_div(ceil_div(w.HW, c), w.rows) + 10);
             if (t < cost) { cost = t; chunks = c; }
         }
@@ -291,7 +292,8 @@ template <int V>
 size_t backward_ws(const Dims& d, int groups, int dtype, bool kept) {
     const int elem = elem_bytes(dtype);
     const SliceWalk& s = backward_slices<V>(d, groups, elem, kept);
-    if (s.threads) return d.n == 1 ? 0 : (size_t)std::min<long long>(d.n, 32 * kSms) * 2 * d.C * sizeof(float);      // (never more blocks of a slice than 32 per SM)
+    // (never more blocks of a slice than 32 per SM; slice_sums grows with them by less than their number)
+    if (s.threads) return d.n == 1 ? 0 : (size_t)(std::min<long long>(d.n, 32 * kSms) + d.n / kSlSamples) * 2 * d.C * sizeof(float);
     const long long chunks = std::max(walk_of(d, V, 2).chunks, walk_of(d, V, 3).chunks);       // (of either source)
     return (size_t)(d.n * groups) * sizeof(float2) + (size_t)(d.n * chunks) * 2 * d.C * sizeof(float);
 }
@@ -351,7 +353,7 @@ void backward(Launcher& go, const alexnet_group_norm_backward_t* a, const Dims& 
         go.smem = smem;
         go(kernel, rows * sw.slices, sw.threads, dy, geo_of(a->dy, d, sw.rows), src, geo_of(a->x, d, sw.rows), sw, s, (long long)d.n, A, (T*)a->dx.data, geo_of(a->dx, d, sw.rows),
            rows > 1 ? partial : a->dbias, rows > 1 ? partial + d.C : a->dweight, rows > 1 ? 2ll * d.C : 0ll);
-        if (rows > 1 && (a->dweight || a->dbias)) go(gn_parameter_gradient_kernel, ceil_div(d.C, 32), 1024, (const float*)partial, d.C, rows, a->dweight, a->dbias);
+        if (rows > 1 && (a->dweight || a->dbias)) go(gn_parameter_gradient_kernel, ceil_div(d.C, 32), 1024, (const float*)partial, d.C, slice_sums(d.n, rows), a->dweight, a->dbias);
         return;
     }
     const Geo gdy = geo_of(a->dy, d, w.rows), gx = geo_of(a->x, d, w.rows), gdx = geo_of(a->dx, d, w.rows);

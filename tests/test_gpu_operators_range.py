@@ -46,3 +46,22 @@ def parameter_gradients_of_alike(ops, shape, groups, src):
 @pytest.mark.parametrize("shape,groups", [((16384, 9, 9, 64), 8), ((65536, 9, 9, 32), 8), ((65536, 9, 9, 9), 3), ((400000, 3, 2, 32), 4), ((1000000, 1, 1, 32), 4)])
 def test_parameter_gradients_of_many_samples(ops, shape, groups, src):
     parameter_gradients_of_alike(ops, shape, groups, src)
+
+
+@pytest.mark.parametrize("shape,groups", [((1, 4096, 4096, 16), 4), ((1, 16384, 4096, 8), 2), ((1, 16384, 16384, 1), 1), ((444, 256, 256, 8), 1), ((888, 55, 55, 96), 32)])
+def test_gradients_of_many_positions(ops, shape, groups):
+    """The same of large samples, and what a group's sums do to dx: with an x of 0 and 1 in turn, dx = rstd (dy - mean of dy - xhat mean of dy xhat)."""
+    n, h, w, c = shape
+    dy = torch.linspace(0.05, 0.15, c, device="cuda").expand(shape)
+    x = torch.tensor([0.0, 1.0], device="cuda").view(1, 1, 2, 1).expand(1, 1, 2, c).repeat(1, 1, w // 2 + 1, 1)[:, :, :w].expand(shape)
+    mean, rstd = torch.zeros((n, groups), device="cuda"), torch.ones((n, groups), device="cuda")
+    dx, dw, db = ops.group_norm_backward(dy, x, mean, rstd)
+    dy64, ones = dy[0, 0, 0].double(), w // 2 / w
+    want_b, want_w = dy64 * (n * h * w), dy64 * (n * h * (w // 2))
+    assert float(((db.double() - want_b).abs() / want_b).max()) < FP32
+    assert float(((dw.double() - want_w).abs() / want_w).max()) < FP32
+    m = dy64.view(groups, -1).mean(1).repeat_interleave(c // groups)
+    for at in (0, 1):
+        want = dy64 - m - at * ones * m
+        # two means, and the roundings of their difference from dy
+        assert float((dx[:, :, at::2].double() - want).abs().max()) < (2 * FP32 + 2.0 ** -21) * 0.15
