@@ -10,9 +10,12 @@
 // direction, forward 27 us (14.6), SiLU 33, backward 44 (21.9), SiLU 65; 512 x 55 x 55 x 96, read twice, forward 164 (91), backward 258 (136), ReLU 275, SiLU 320.
 // Small calls are bound by their launches and a chain of sums and barriers: 1 x 13 x 13 x 384 7.5 us.
 //
-// Sums.  A thread sums, for each of its channels, the differences from the first value it reads and their squares, in fp32.  That value
-// is one of the summed, so the sum of squares is at most (1 + n) times the true one about the mean, however far the mean is from zero: nothing
-// cancels as it would in E[x^2] - mean^2.  From there on parts of n values are joined by their means, each held as hi + lo, and their squared
+// Sums.  Where a block keeps its values, it goes over them twice, the second time with the first's mean as the shift.  Elsewhere a thread sums, for
+// each of its channels, the differences from the first value and their squares, in fp32; after 8 values, 40, 72 and so on it moves to those from the mean
+// so far.  So nothing cancels as it would in E[x^2] - mean^2, however far the mean is from
+// zero, nor where the first value lies far from all others: differences
+// from that one alone left rstd off by 1.7e-3 at 444 x 256 x 256 x 8.
+// From there on parts of n values are joined by their means, each held as hi + lo, and their squared
 // deviations M2 from them (Part below): means as differences from one of them, M2 = sum M2_i + n_i (mean_i - mean)^2, all of one sign.  The order is
 // fixed, so results repeat bit for bit.  (fp64 sums of values and squares do as well but took 3 to 8 us of a call: conversions, divisions, roots.)
 #pragma once
@@ -99,7 +102,7 @@ __device__ __forceinline__ void load_chan(Chan<V>& k, const NormShape& s, const 
 // ---------------------------------------------------------------- forward, any size: sums, statistics, result
 // n values by their mean hi + lo and their squared deviations from it
 struct Part { float hi, lo, m2; };
-// a thread's values of a channel: n of them, shifted by -nK (one of them), S their sum, Q their sum of squares
+// a thread's values of a channel: n of them, S the sum of their differences from K (nK = -K), Q that of the squares
 __device__ __forceinline__ Part moments(int n, float nK, float S, float Q) {
     const float d = n ? __fdividef(S, (float)n) : 0.f, hi = d - nK;
     return {hi, (-nK - hi) + d, fmaf(-S, d, Q)};
@@ -173,6 +176,18 @@ __device__ __forceinline__ float2 statistics(const Part& t, const NormShape& s) 
     return make_float2(t.hi + t.lo, __frsqrt_rn((var < 0.f ? 0.f : var) + s.eps));      // (keeps NaN)
 }
 
+// From n values' sums of differences from K, S, and of their squares, Q, to those from a K nearer to their mean: with d the step, sum (x - K - d)
+// = S - n d and sum (x - K - d)^2 = Q - d (2 S - n d).
+template <int V> __device__ __forceinline__ void move_mean(float n, float* nK, float* S, float* Q) {
+    const float per = -__fdividef(1.f, n);
+    #pragma unroll
+    for (int i = 0; i < V; ++i) {
+        const float k = fmaf(S[i], per, nK[i]), nd = k - nK[i], r = fmaf(n, nd, S[i]);
+        Q[i] = fmaf(nd, S[i] + r, Q[i]);
+        S[i] = r;
+        nK[i] = k;
+    }
+}
 template <typename T, int V>
 __global__ void __launch_bounds__(256) gn_sums_kernel(const T* __restrict__ x, const Geo g, const Walk w, float4* __restrict__ partial) {
     kn::pdl_sync();
@@ -180,7 +195,7 @@ __global__ void __launch_bounds__(256) gn_sums_kernel(const T* __restrict__ x, c
     const Table<V> table{sums, 260};
     const Spot s = spot(w);
     constexpr int U = 8;
-    float nK[V], S[V], Q[V];
+    float nK[V], S[V], Q[V];                   // a number near the mean, negative; the sums of the differences from it and of their squares
     #pragma unroll
     for (int i = 0; i < V; ++i) nK[i] = S[i] = Q[i] = 0.f;
     int cnt = 0;
@@ -207,6 +222,7 @@ __global__ void __launch_bounds__(256) gn_sums_kernel(const T* __restrict__ x, c
                     v_add<V>(S, f, S);
                     v_fma<V>(f, f, Q, Q);
                 }
+            if (it % (4 * U) == 0) move_mean<V>((float)min(it + U, cnt), nK, S, Q);
         }
     }
     #pragma unroll
@@ -252,15 +268,25 @@ __global__ void __launch_bounds__(256) gn_statistics_kernel(const float4* __rest
         t.x = fmaf(k == chunks - 1 ? last : lo, p[(long long)k * s.C + (i - k * s.cg)].x - ref, t.x);
     }
     const float hi = ref + __fdiv_rn(sum(t).x, count);
-    t.x = 0.f;
-    #pragma unroll 4
-    for (int i = me; i < total; i += N) {
-        const int k = s.group(i);
-        const float4 q = p[(long long)k * s.C + (i - k * s.cg)];
-        const float d = (q.x - hi) + q.y, w = (k == chunks - 1 ? last : lo) * d;
-        t.x += w;
-        t.y += fmaf(w, d, q.z);
+    LongSum t1, t2;
+    for (int i = me; i < total; i += 4 * N) {
+        float u1[4], u2[4];
+        #pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            const int j = i + u * N;
+            u1[u] = u2[u] = 0.f;
+            if (j < total) {
+                const int k = s.group(j);
+                const float4 q = p[(long long)k * s.C + (j - k * s.cg)];
+                const float d = (q.x - hi) + q.y, w = (k == chunks - 1 ? last : lo) * d;
+                u1[u] = w;
+                u2[u] = fmaf(w, d, q.z);
+            }
+        }
+        t1.add(sum_of<4>(u1));
+        t2.add(sum_of<4>(u2));
     }
+    t = make_float2(t1.value(), t2.value());
     t = sum(t);
     if (me == 0) {
         const float l = __fdiv_rn(t.x, count);

@@ -65,3 +65,34 @@ def test_gradients_of_many_positions(ops, shape, groups):
         want = dy64 - m - at * ones * m
         # two means, and the roundings of their difference from dy
         assert float((dx[:, :, at::2].double() - want).abs().max()) < (2 * FP32 + 2.0 ** -21) * 0.15
+
+
+@pytest.mark.parametrize("dtype,rest", [("bf16", "normal"), ("bf16", 0.37), ("fp16", 0.0), ("fp32", "normal"), ("fp32", 0.37)])
+@pytest.mark.parametrize("shape,groups", [((444, 256, 256, 8), 1), ((888, 55, 55, 96), 32), ((128, 55, 55, 96), 32), ((64, 31, 31, 75), 5), ((600, 64, 64, 3), 1), ((1, 4096, 4096, 8), 1)])
+def test_statistics_beside_an_outlier(ops, shape, groups, dtype, rest):
+    """The first position (or the last) of every sample lies a thousand spreads away from all others, which are alike or normal: squares of the differences
+    from it would drown theirs.  A variance is a sum of squares, all positive: chains of at most 192 (about a mean so far that is
+    off by an eighth of the outlier for 32 terms, a fortieth for 32 more and so on, half as much again), at most 85 rows, all of 2^-25, and a root halves it: 187 of 2^-25, where 2^-17 is 256."""
+    n, h, w, c = shape
+    if n * h * w * c > 1 << 27 and dtype == "fp32" and rest == "normal":
+        n = n // 2 if n > 1 else n
+    g = gen(c)
+    x = torch.empty((n, h, w, c), dtype=TYPES[dtype], device="cuda")
+    if rest == "normal":
+        x.normal_(generator=g)
+    else:
+        x.fill_(rest)
+    for at in (0, -1):
+        was = x[:, at, at].clone()
+        x[:, at, at] = -1000.0
+        r = ops.group_norm(x, groups, activation="none")
+        step = max(1, n // 16)
+        for i in range(0, n, step):
+            v = x[i:i + step].double().view(-1, h * w, groups, c // groups)
+            mean = v.mean((1, 3))
+            v -= mean[:, None, :, None]
+            rstd = (v.square().mean((1, 3)) + 1e-5).rsqrt()
+            # and the rounding of the mean itself: half a step, 2^-24 of it (beside one outlier in 2^24 alike values of 0.37 that alone is 1.9e-4 of their mean deviation)
+            assert bool(((r.mean[i:i + step].double() - mean).abs() <= FP32 * v.abs().mean((1, 3)) + 2.0 ** -24 * mean.abs()).all()), (at, i)
+            assert float(((r.rstd[i:i + step].double() - rstd).abs() / rstd).max()) < FP32, (at, i)
+        x[:, at, at] = was
