@@ -590,7 +590,7 @@ __global__ void __launch_bounds__(256, kBackwardBlocks<T, V, SRC>) gn_backward_a
         const long long g = s.n * sh.groups + sh.group(V * s.v + i);
         const float2 c = c12[g];
         const float r = A.rstd[g];
-        B[i] = -r * r * c.y;
+        B[i] = -r * (r * c.y);
         D[i] = -r * c.x;
     }
     const T* dp = dy + s.n * gdy.sn + V * s.v;
@@ -981,7 +981,7 @@ __global__ void __launch_bounds__(kSlThreads, 2) gn_slice_backward_kernel(const 
                 const int g = sh.group(V * v + i);
                 const float2 c = m.res[g];
                 const float r = m.rstd[g];
-                B[i] = -r * r * c.y;
+                B[i] = -r * (r * c.y);
                 D[i] = -r * c.x;
             }
         }

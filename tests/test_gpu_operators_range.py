@@ -96,3 +96,22 @@ def test_statistics_beside_an_outlier(ops, shape, groups, dtype, rest):
             assert bool(((r.mean[i:i + step].double() - mean).abs() <= FP32 * v.abs().mean((1, 3)) + 2.0 ** -24 * mean.abs()).all()), (at, i)
             assert float(((r.rstd[i:i + step].double() - rstd).abs() / rstd).max()) < FP32, (at, i)
         x[:, at, at] = was
+
+
+@pytest.mark.parametrize("src", ["x", "int8", "e4m3"])
+@pytest.mark.parametrize("shape,groups", [((2, 8, 8, 64), 8), ((2, 8, 8, 33), 3), ((1, 150, 150, 64), 4)])
+def test_gradients_of_alike_values_with_a_tiny_eps(ops, shape, groups, src):
+    """No variance and an eps of 1e-40: rstd is 1e20 and its square no number of fp32, but dx = rstd (dy w - mean) is."""
+    g = gen(7)
+    x = torch.full(shape, 3.0, device="cuda")
+    w = torch.rand(shape[-1], device="cuda", generator=g) + 0.5
+    r = ops.group_norm(x, groups, w, eps=1e-40)
+    assert torch.equal(r.mean, torch.full_like(r.mean, 3.0))
+    dy = torch.randn(shape, device="cuda", generator=g)
+    dx, dw, db = ops.group_norm_backward(dy, x if src == "x" else ops.checkpoint_encode(x, src), r.mean, r.rstd, w)
+    n, h, ww, c = shape
+    gw = (dy.double() * w.double()).view(n, h * ww, groups, -1)
+    want = (r.rstd.double()[:, None, :, None] * (gw - gw.mean((1, 3), keepdim=True))).view(shape)
+    mag = (r.rstd.double()[:, None, :, None] * (gw.abs() + gw.abs().mean((1, 3), keepdim=True))).view(shape)
+    assert bool(((dx.double() - want).abs() <= FP32 * mag).all())
+    assert not bool(dw.any()) and bool(((db.double() - dy.double().sum((0, 1, 2))).abs() <= FP32 * dy.double().abs().sum((0, 1, 2))).all())
