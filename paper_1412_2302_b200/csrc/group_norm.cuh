@@ -87,7 +87,7 @@ struct NormShape {
 };
 
 // per-channel constants of a thread's vector
-template <int V> struct Chan { float nm[V], a[V], b[V]; };
+template <int V> struct Chan { float nm[V], a[V], b[V]; uint32_t negative; };      // negative: (backward) not 0 where an a is
 template <int V>
 __device__ __forceinline__ void load_chan(Chan<V>& k, const NormShape& s, const float* mean, const float* rstd, const float* weight, const float* bias, long long n, int c0) {
     #pragma unroll
@@ -397,17 +397,19 @@ struct BackwardArgs {
 };
 // A thread's channels in a backward pass: nm, a and b, where ReLU has in the place of b a number to compare with.  z > 0 holds for x > theta (w > 0) or x < theta
 // (w < 0) with theta = mean - b / (rstd w): theta in fp64, rounded to fp32 downwards (upwards), decides for every fp32 x as the real one does, where
-// z in fp32 is off by 2^-23 |b| about zero.  b holds -theta; the sign of (x - theta) a is z's.  Where a is zero z is b, for all x: b holds 0, for a
-// product of 0, or infinity, for one of NaN where z is positive; so what passes the gradient is a product that is not <= 0.
+// z in fp32 is off by 2^-23 |b| about zero.  b holds -theta; x - theta with a's sign has z's (their product may be too small for fp32).  Where w is zero z is
+// the bias, for all x: b holds an infinity that gives x + b the sign that is wanted.
 template <int V, int ACT>
 __device__ __forceinline__ void load_backward_chan(Chan<V>& k, const NormShape& sh, const BackwardArgs& A, long long n, int c0) {
     load_chan<V>(k, sh, A.mean, A.rstd, A.weight, A.bias, n, c0);
+    k.negative = 0;
     if (ACT == kActRelu || (ACT == kActAny && sh.act == kActRelu)) {
         #pragma unroll
         for (int i = 0; i < V; ++i) {
             const double a = (double)A.rstd[n * sh.groups + sh.group(c0 + i)] * (A.weight ? (double)A.weight[c0 + i] : 1.);
             const double theta = -(double)k.nm[i] - (double)k.b[i] / a;
-            k.b[i] = k.a[i] == 0.f ? (k.b[i] <= 0.f ? 0.f : __uint_as_float(0x7f800000u)) : -(a > 0. ? __double2float_rd(theta) : __double2float_ru(theta));
+            k.b[i] = a == 0. ? copysignf(__uint_as_float(0x7f800000u), k.b[i] <= 0.f ? -k.a[i] : k.a[i]) : -(a > 0. ? __double2float_rd(theta) : __double2float_ru(theta));
+            k.negative |= __float_as_uint(k.a[i]) & 0x80000000u;
         }
     }
 }
@@ -426,9 +428,12 @@ __device__ __forceinline__ void activation_gradient(int act, const Chan<V>& k, c
             for (int i = 0; i < V; ++i) x[i] *= sc;
         }
         v_add<V>(x, k.b, z);
-        v_mul<V>(z, k.a, z);
+        if (k.negative) {
+            #pragma unroll
+            for (int i = 0; i < V; ++i) z[i] = __uint_as_float(__float_as_uint(z[i]) ^ (__float_as_uint(k.a[i]) & 0x80000000u));
+        }
         #pragma unroll
-        for (int i = 0; i < V; ++i) dy[i] = z[i] <= 0.f ? 0.f : dy[i];
+        for (int i = 0; i < V; ++i) dy[i] = z[i] <= 0.f ? 0.f : dy[i];      // (passes NaN)
     } else {
         v_fma<V>(d, k.a, k.b, z);
         float s[V], u[V], one[V], minus[V];

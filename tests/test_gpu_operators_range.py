@@ -115,3 +115,20 @@ def test_gradients_of_alike_values_with_a_tiny_eps(ops, shape, groups, src):
     mag = (r.rstd.double()[:, None, :, None] * (gw.abs() + gw.abs().mean((1, 3), keepdim=True))).view(shape)
     assert bool(((dx.double() - want).abs() <= FP32 * mag).all())
     assert not bool(dw.any()) and bool(((db.double() - dy.double().sum((0, 1, 2))).abs() <= FP32 * dy.double().abs().sum((0, 1, 2))).all())
+
+
+@pytest.mark.parametrize("src", ["x", "int8"])
+@pytest.mark.parametrize("shape,groups", [((2, 8, 8, 64), 8), ((2, 8, 8, 33), 3), ((1, 150, 150, 64), 4), ((1, 150, 150, 33), 3)])
+def test_relu_of_weights_too_small_for_products(ops, shape, groups, src):
+    """z = xhat w + b is positive where it is, although rstd w, or its product with x - mean, is no number of fp32 any more: dbias counts the positions."""
+    g = gen(19)
+    n, h, ww, c = shape
+    x = torch.randn(shape, device="cuda", generator=g)
+    x[:, 0, 0] = 1e-12
+    w = torch.tensor([1e-38, -1e-38, 1e-44, -1e-44, 1e-30, -1e-30, 0.0, -0.0, 1.0, -1.0], device="cuda").repeat(c // 10 + 1)[:c]
+    b = torch.tensor([0.0, 0.0, 0.0, 1e-45, -1e-45, 1.0, -1.0], device="cuda").repeat(c // 7 + 1)[:c]
+    mean, rstd = torch.zeros((n, groups), device="cuda"), torch.full((n, groups), 1e-3, device="cuda")
+    kept = x if src == "x" else ops.checkpoint_encode(x, src)
+    value = (x if src == "x" else ops.checkpoint_decode(kept, torch.float32)).double()
+    dbias = ops.group_norm_backward(torch.ones_like(x), kept, mean, rstd, w, b, activation="relu")[2]
+    assert torch.equal(dbias.double(), (value * 1e-3 * w.double() + b.double() > 0).double().sum((0, 1, 2)))
