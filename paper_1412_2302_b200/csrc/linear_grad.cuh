@@ -193,7 +193,7 @@ __global__ void __launch_bounds__(kLgThreads, 1) linear_grad_kernel(const __grid
                 tc::tc_fence_after();
                 const uint32_t d = tmem + (uint32_t)(a * p.BN);
                 for (int k = c0; k < c1; ++k) {
-                    if (!(ok = tc::mbar_wait_warp(full0 + 8u * st, ph, abort_flag))) break;
+                    if (!(ok = CG == 2 ? tc::mbar_wait_warp_cluster(full0 + 8u * st, ph, abort_flag) : tc::mbar_wait_warp(full0 + 8u * st, ph, abort_flag))) break;
                     tc::tc_fence_after();
                     const uint32_t sa = base + st * stage_bytes, sb = sa + kLgA;
                     #pragma unroll

@@ -98,6 +98,27 @@ def test_statistics_beside_an_outlier(ops, shape, groups, dtype, rest):
         x[:, at, at] = was
 
 
+@pytest.mark.parametrize("fmt", ["int8", "e4m3"])
+def test_linear_weight_grad_of_pairs_repeats(ops, fmt):
+    """Both CTAs of a pair decode their half of every step's tile, and one of them multiplies both: the same bits again while another stream keeps the SMs'
+    memory busy, and those of the sums taken 64 rows at a time in 64 bits."""
+    g = gen(77)
+    rows, n_in, n_out = 1536, 2304, 2048
+    k = ops.checkpoint_encode(torch.randn((rows, n_in), device="cuda", generator=g), fmt)
+    dy = torch.randn((rows, n_out), device="cuda", generator=g).to(torch.bfloat16)
+    want = dy.double().t() @ ops.checkpoint_decode(k, torch.float32).double()
+    mag = dy.double().abs().t() @ ops.checkpoint_decode(k, torch.float32).double().abs()
+    first = ops.linear_weight_grad(dy, k)
+    assert bool(((first.double() - want).abs() <= (rows + 16) * 2.0 ** -24 * mag).all())
+    side, a = torch.cuda.Stream(), torch.zeros(1 << 26, device="cuda")
+    side.wait_stream(torch.cuda.current_stream())
+    for i in range(200):
+        with torch.cuda.stream(side):
+            a.add_(1)
+        again = ops.linear_weight_grad(dy, k)
+        assert torch.equal(again, first), i
+
+
 @pytest.mark.parametrize("src", ["x", "int8", "e4m3"])
 @pytest.mark.parametrize("shape,groups", [((2, 8, 8, 64), 8), ((2, 8, 8, 33), 3), ((1, 150, 150, 64), 4)])
 def test_gradients_of_alike_values_with_a_tiny_eps(ops, shape, groups, src):
