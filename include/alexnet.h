@@ -543,8 +543,9 @@ size_t alexnet_linear_weight_grad_workspace_bytes(const alexnet_linear_weight_gr
 int alexnet_linear_weight_grad(const alexnet_linear_weight_grad_t* args, void* stream, char* err, size_t err_len);
 
 /* Waits inside these operators' kernels are bounded like all others: if one ran
- * out, the outputs it stood for are NaN and this call, which synchronises with the
- * current device's default stream, returns DEVICE_TIMEOUT from then on; else OK. */
+ * out, the outputs it stood for are NaN and this call, which waits for all work of
+ * the current device, on whatever stream, returns DEVICE_TIMEOUT from then on; else
+ * OK.  Not while a stream is being captured. */
 int alexnet_operators_check(void);
 
 #ifdef __cplusplus

@@ -599,7 +599,8 @@ int alexnet_linear_weight_grad(const alexnet_linear_weight_grad_t* a, void* stre
 
 int alexnet_operators_check(void) {
     int expired = 0;
-    if (cudaMemcpyFromSymbol(&expired, g_expired, sizeof(int)) != cudaSuccess) { cudaGetLastError(); return ALEXNET_ERR_CUDA; }
+    // (torch's streams, like all non-blocking ones, do not wait for the default stream's copy, nor it for them)
+    if (cudaDeviceSynchronize() != cudaSuccess || cudaMemcpyFromSymbol(&expired, g_expired, sizeof(int)) != cudaSuccess) { cudaGetLastError(); return ALEXNET_ERR_CUDA; }
     return expired ? ALEXNET_ERR_DEVICE_TIMEOUT : ALEXNET_OK;
 }
 

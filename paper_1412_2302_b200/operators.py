@@ -222,7 +222,8 @@ def _linear_workspace(rows, n_in, n_out, stride, dy_offset, codes_offset, fmt):
 
 
 def check():
-    """Wait for the current device's work and raise if a bounded wait inside an operator's kernel has ever run out (its outputs are NaN)."""
+    """Wait for all work of the current device, on whatever stream, and raise if a bounded wait inside an operator's kernel has ever run out (its
+    outputs are NaN)."""
     rc = _alexnet.load_library().alexnet_operators_check()
     if rc != OK:
         raise AlexNetError(rc, "a wait inside an operator's kernel ran out" if rc == _alexnet.ERR_DEVICE_TIMEOUT else "the device could not be read")

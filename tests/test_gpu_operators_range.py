@@ -153,3 +153,18 @@ def test_relu_of_weights_too_small_for_products(ops, shape, groups, src):
     value = (x if src == "x" else ops.checkpoint_decode(kept, torch.float32)).double()
     dbias = ops.group_norm_backward(torch.ones_like(x), kept, mean, rstd, w, b, activation="relu")[2]
     assert torch.equal(dbias.double(), (value * 1e-3 * w.double() + b.double() > 0).double().sum((0, 1, 2)))
+
+
+def test_check_waits_for_every_stream(ops):
+    """Work on a stream of the caller's, which does not wait for the default stream, has ended when check() returns."""
+    side, done = torch.cuda.Stream(), torch.cuda.Event()
+    x = torch.randn((4, 8, 8, 64), device="cuda", generator=gen(1))
+    want = ops.group_norm(x, 8).y
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        torch.cuda._sleep(200_000_000)               # about a tenth of a second
+        y = ops.group_norm(x, 8).y
+        done.record()
+    assert not done.query()
+    ops.check()
+    assert done.query() and torch.equal(y, want)
