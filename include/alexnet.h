@@ -547,6 +547,13 @@ int alexnet_linear_weight_grad(const alexnet_linear_weight_grad_t* args, void* s
  * the current device, on whatever stream, returns DEVICE_TIMEOUT from then on; else
  * OK.  Not while a stream is being captured. */
 int alexnet_operators_check(void);
+/* Failure-detection self-test: linear_weight_grad with these arguments, except that
+ * the CTA `block` (0 or 1, the two CTAs of the first pair where there are pairs) never
+ * says that it has decoded its first step.  The waits for that run out after some
+ * 0.2 s; the outputs of that CTA or pair are NaN, the others right, and the GPU
+ * stays usable.  alexnet_operators_check then returns DEVICE_TIMEOUT for the rest of
+ * the process. */
+int alexnet_operators_debug_expire_wait(const alexnet_linear_weight_grad_t* args, int block, void* stream, char* err, size_t err_len);
 
 #ifdef __cplusplus
 }

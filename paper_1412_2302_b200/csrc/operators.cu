@@ -449,6 +449,62 @@ LinearPlan linear_plan(const alexnet_linear_weight_grad_t& a) {
     return b;
 }
 long long repitch_grid(long long rows, long long pitch) { return std::min<long long>(16 * kSms, ceil_div(rows * (pitch / 16), 256)); }
+int linear_call(const alexnet_linear_weight_grad_t* a, cudaStream_t st, const Err& err, int drop) {
+    if (!a) return err.arg("NULL arguments");
+    if (const char* m = check_linear(*a)) return err.arg(m);
+    if (!a->dw || (uintptr_t)a->dw % 4) return err.arg("dw is NULL or not aligned");
+    if (a->rows > 0 && (!a->dy || !a->x.codes || !a->x.scales)) return err.arg("NULL pointer");
+    const LinearPlan pl = linear_plan(*a);
+    if (pl.bytes && (!a->workspace || (uintptr_t)a->workspace % 16 || a->workspace_bytes < pl.bytes)) return err.arg("the workspace is too small or not 16-byte aligned");
+    if (a->rows == 0) {
+        const cudaError_t e = cudaMemsetAsync(a->dw, 0, (size_t)a->n_in * a->n_out * sizeof(float), st);
+        return e == cudaSuccess ? ALEXNET_OK : err.cuda(e);
+    }
+    LinearGradParams p{};
+    Launcher go{st};
+    const void* dy = a->dy;
+    long long dy_pitch = a->dy_stride * 2;
+    if (pl.move_dy) {
+        uint8_t* t = (uint8_t*)a->workspace + pl.dy_at;
+        go(repitch_kernel<uint16_t>, repitch_grid(a->rows, pl.dy_pitch), 256, (const uint8_t*)a->dy, a->rows > 1 ? a->dy_stride * 2 : 0ll, a->n_out * 2, pl.dy_pitch, a->rows, t);
+        dy = t; dy_pitch = pl.dy_pitch;
+    } else if (a->rows == 1) dy_pitch = ceil_div(a->n_out, 8) * 16;
+    p.codes = (const uint8_t*)a->x.codes;
+    p.code_pitch = a->n_in;
+    if (pl.move_x) {
+        uint8_t* t = (uint8_t*)a->workspace + pl.x_at;
+        go(repitch_kernel<uint8_t>, repitch_grid(a->rows, pl.x_pitch), 256, p.codes, (long long)a->n_in, a->n_in, pl.x_pitch, a->rows, t);
+        p.codes = t; p.code_pitch = pl.x_pitch;
+    }
+    PFN_cuTensorMapEncodeTiled_v12000 enc = tensor_map_encoder();
+    if (!enc) return err.cuda(cudaErrorNotSupported);
+    const cuuint64_t dims[2] = {(cuuint64_t)a->n_out, (cuuint64_t)a->rows}, strides[1] = {(cuuint64_t)dy_pitch};
+    const cuuint32_t box[2] = {64, kLgRows}, one[2] = {1, 1};
+    if (enc(&p.tmD, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(dy), dims, strides, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+            CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
+        return err.arg("the driver refused the tensor map of dy");
+    p.scales = a->x.scales;
+    p.blocks = (int)ceil_div(a->n_in, 32);
+    p.rows = (int)a->rows; p.n_in = a->n_in; p.n_out = a->n_out;
+    p.BN = pl.BN; p.m_tiles = pl.m_tiles; p.tiles = pl.tiles; p.steps = pl.steps; p.whole = pl.whole; p.splits = pl.splits; p.per = pl.per; p.stages = pl.stages;
+    p.out = a->dw;
+    p.drop = drop;
+    p.partial = (float*)a->workspace;
+    auto* kernel = a->x.format == ALEXNET_CODES_INT8 ? (pl.cg == 2 ? linear_grad_kernel<kSrcInt8, 2> : linear_grad_kernel<kSrcInt8, 1>)
+                                                     : (pl.cg == 2 ? linear_grad_kernel<kSrcE4m3, 2> : linear_grad_kernel<kSrcE4m3, 1>);
+    if (go.e == cudaSuccess) go.e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 227 * 1024);
+    go.smem = pl.smem;
+    go.cluster = pl.cg;
+    const long long rest = pl.tiles - pl.whole;
+    go(kernel, pl.cg * std::min<long long>(kSms / pl.cg, pl.whole + rest * pl.splits), kLgThreads, p);
+    if (rest) {      // four columns at a time where there are enough tiles to fill the device so
+        const int rows = 128 * pl.cg, at_once = 1024 / rows;
+        const bool four = rest * (pl.BN / (4 * at_once)) >= kSms;
+        go(four ? linear_grad_join_kernel<4> : linear_grad_join_kernel<1>, rest * ceil_div(pl.BN, (four ? 4 : 1) * at_once), 256, (const float*)p.partial, p.out, p.n_in, p.n_out, p.m_tiles, p.whole,
+           (int)rest, p.splits, p.BN, rows);
+    }
+    return go.e == cudaSuccess ? ALEXNET_OK : err.cuda(go.e);
+}
 }  // namespace
 
 extern "C" {
@@ -539,62 +595,13 @@ size_t alexnet_linear_weight_grad_workspace_bytes(const alexnet_linear_weight_gr
     return bytes ? bytes + 256 : 256;
 }
 
-int alexnet_linear_weight_grad(const alexnet_linear_weight_grad_t* a, void* stream, char* err_buf, size_t err_len) {
-    const Err err{err_buf, err_len, "linear_weight_grad"};
-    if (!a) return err.arg("NULL arguments");
-    if (const char* m = check_linear(*a)) return err.arg(m);
-    if (!a->dw || (uintptr_t)a->dw % 4) return err.arg("dw is NULL or not aligned");
-    if (a->rows > 0 && (!a->dy || !a->x.codes || !a->x.scales)) return err.arg("NULL pointer");
-    const LinearPlan pl = linear_plan(*a);
-    if (pl.bytes && (!a->workspace || (uintptr_t)a->workspace % 16 || a->workspace_bytes < pl.bytes)) return err.arg("the workspace is too small or not 16-byte aligned");
-    cudaStream_t st = (cudaStream_t)stream;
-    if (a->rows == 0) {
-        const cudaError_t e = cudaMemsetAsync(a->dw, 0, (size_t)a->n_in * a->n_out * sizeof(float), st);
-        return e == cudaSuccess ? ALEXNET_OK : err.cuda(e);
-    }
-    LinearGradParams p{};
-    Launcher go{st};
-    const void* dy = a->dy;
-    long long dy_pitch = a->dy_stride * 2;
-    if (pl.move_dy) {
-        uint8_t* t = (uint8_t*)a->workspace + pl.dy_at;
-        go(repitch_kernel<uint16_t>, repitch_grid(a->rows, pl.dy_pitch), 256, (const uint8_t*)a->dy, a->rows > 1 ? a->dy_stride * 2 : 0ll, a->n_out * 2, pl.dy_pitch, a->rows, t);
-        dy = t; dy_pitch = pl.dy_pitch;
-    } else if (a->rows == 1) dy_pitch = ceil_div(a->n_out, 8) * 16;
-    p.codes = (const uint8_t*)a->x.codes;
-    p.code_pitch = a->n_in;
-    if (pl.move_x) {
-        uint8_t* t = (uint8_t*)a->workspace + pl.x_at;
-        go(repitch_kernel<uint8_t>, repitch_grid(a->rows, pl.x_pitch), 256, p.codes, (long long)a->n_in, a->n_in, pl.x_pitch, a->rows, t);
-        p.codes = t; p.code_pitch = pl.x_pitch;
-    }
-    PFN_cuTensorMapEncodeTiled_v12000 enc = tensor_map_encoder();
-    if (!enc) return err.cuda(cudaErrorNotSupported);
-    const cuuint64_t dims[2] = {(cuuint64_t)a->n_out, (cuuint64_t)a->rows}, strides[1] = {(cuuint64_t)dy_pitch};
-    const cuuint32_t box[2] = {64, kLgRows}, one[2] = {1, 1};
-    if (enc(&p.tmD, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(dy), dims, strides, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
-            CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
-        return err.arg("the driver refused the tensor map of dy");
-    p.scales = a->x.scales;
-    p.blocks = (int)ceil_div(a->n_in, 32);
-    p.rows = (int)a->rows; p.n_in = a->n_in; p.n_out = a->n_out;
-    p.BN = pl.BN; p.m_tiles = pl.m_tiles; p.tiles = pl.tiles; p.steps = pl.steps; p.whole = pl.whole; p.splits = pl.splits; p.per = pl.per; p.stages = pl.stages;
-    p.out = a->dw;
-    p.partial = (float*)a->workspace;
-    auto* kernel = a->x.format == ALEXNET_CODES_INT8 ? (pl.cg == 2 ? linear_grad_kernel<kSrcInt8, 2> : linear_grad_kernel<kSrcInt8, 1>)
-                                                     : (pl.cg == 2 ? linear_grad_kernel<kSrcE4m3, 2> : linear_grad_kernel<kSrcE4m3, 1>);
-    if (go.e == cudaSuccess) go.e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 227 * 1024);
-    go.smem = pl.smem;
-    go.cluster = pl.cg;
-    const long long rest = pl.tiles - pl.whole;
-    go(kernel, pl.cg * std::min<long long>(kSms / pl.cg, pl.whole + rest * pl.splits), kLgThreads, p);
-    if (rest) {      // four columns at a time where there are enough tiles to fill the device so
-        const int rows = 128 * pl.cg, at_once = 1024 / rows;
-        const bool four = rest * (pl.BN / (4 * at_once)) >= kSms;
-        go(four ? linear_grad_join_kernel<4> : linear_grad_join_kernel<1>, rest * ceil_div(pl.BN, (four ? 4 : 1) * at_once), 256, (const float*)p.partial, p.out, p.n_in, p.n_out, p.m_tiles, p.whole,
-           (int)rest, p.splits, p.BN, rows);
-    }
-    return go.e == cudaSuccess ? ALEXNET_OK : err.cuda(go.e);
+int alexnet_linear_weight_grad(const alexnet_linear_weight_grad_t* args, void* stream, char* err, size_t err_len) {
+    return linear_call(args, (cudaStream_t)stream, {err, err_len, "linear_weight_grad"}, -1);
+}
+int alexnet_operators_debug_expire_wait(const alexnet_linear_weight_grad_t* args, int block, void* stream, char* err, size_t err_len) {
+    const Err e{err, err_len, "operators_debug_expire_wait"};
+    if (block < 0 || block > 1) return e.arg("block must be 0 or 1");
+    return linear_call(args, (cudaStream_t)stream, e, block);
 }
 
 int alexnet_operators_check(void) {
