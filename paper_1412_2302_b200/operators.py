@@ -12,6 +12,10 @@ gradients are float32.  Every call queues its work on `stream` (a torch.cuda.Str
 and returns without waiting; tensors that are let go before that stream has passed the call need their record_stream, as with any
 other work on a stream of one's own.  Outputs and workspace come from torch's allocator on that stream unless `out` gives the output.  A wrong
 argument raises AlexNetError with code ERR_ARG before anything is launched.  There is no CPU fallback.
+
+Autograd does not see these calls: gradients come from group_norm_backward and linear_weight_grad, which the caller puts in their places (in the
+backward of a torch.autograd.Function, for instance).  So that none is lost in silence, a y of inputs that require a gradient requires one too, and a
+backward pass that comes to it raises AlexNetError.  (An `out` stays as it is.)
 """
 from __future__ import annotations
 
@@ -186,6 +190,23 @@ def _output(out, shape, dtype, index):
     return out
 
 
+class _NoGradient(torch.autograd.Function):
+    """y as it is, in the place where its gradient would be wanted; `leaf` is there to require it."""
+
+    @staticmethod
+    def forward(ctx, y, leaf):
+        ctx.mark_dirty(y)
+        return y
+
+    @staticmethod
+    def backward(ctx, dy):
+        _refuse("group_norm has no gradient of its own: call group_norm_backward with this dy, for instance in the backward of a torch.autograd.Function")
+
+
+def _without_gradient(y):
+    return _NoGradient.apply(y, torch.empty(0, requires_grad=True))
+
+
 def _new_checkpoint(x, fmt):
     shape = x.shape
     k = Checkpoint.__new__(Checkpoint)
@@ -294,6 +315,8 @@ def group_norm(x, groups, weight=None, bias=None, eps=1e-5, activation="none", k
     _run(_alexnet.load_library().alexnet_group_norm_forward, index, _pack_forward,
          *shape, x.data_ptr(), *xs, y.data_ptr(), *_rows(y, "out")[1], _vector(weight, c, "weight", index), _vector(bias, c, "bias", index), mean.data_ptr(), rstd.data_ptr(),
          *pkx, *pky, 0 if ws is None else ws.data_ptr(), nbytes)
+    if out is None and torch.is_grad_enabled() and (x.requires_grad or (weight is not None and weight.requires_grad) or (bias is not None and bias.requires_grad)):
+        y = _without_gradient(y)
     return GroupNormResult(y, mean, rstd, kx, ky)
 
 

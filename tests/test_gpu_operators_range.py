@@ -8,6 +8,8 @@ come in four chains of at most 64 each, those of warps in chains of at most 32; 
 import pytest
 import torch
 
+from paper_1412_2302_b200 import alexnet as A
+
 pytestmark = pytest.mark.gpu
 
 FP32 = 2.0 ** -17
@@ -168,3 +170,36 @@ def test_check_waits_for_every_stream(ops):
     assert not done.query()
     ops.check()
     assert done.query() and torch.equal(y, want)
+
+
+def test_autograd_is_not_passed_by_in_silence(ops):
+    x, w = torch.randn((2, 4, 4, 64), device="cuda", generator=gen(1)), torch.nn.Parameter(torch.ones(64, device="cuda"))
+    b = torch.zeros(64, device="cuda")
+    plain = ops.group_norm(x, 8, w.detach(), b)
+    assert not plain.y.requires_grad
+    for args in ((x, 8, w, b), (x.clone().requires_grad_(), 8, None, b), (x, 8, None, b.clone().requires_grad_())):
+        r = ops.group_norm(*args)
+        assert torch.equal(r.y, ops.group_norm(args[0].detach(), 8, w.detach(), b).y) and r.y.requires_grad
+        with pytest.raises(A.AlexNetError, match="group_norm_backward"):
+            r.y.square().sum().backward()
+        with torch.no_grad():
+            assert not ops.group_norm(*args).y.requires_grad
+    out = torch.empty_like(x)
+    assert ops.group_norm(x, 8, w, b, out=out).y is out and not out.requires_grad
+
+    class Norm(torch.autograd.Function):        # as a caller puts the two together
+        @staticmethod
+        def forward(ctx, x, weight, bias):
+            r = ops.group_norm(x, 8, weight, bias, activation="silu")
+            ctx.save_for_backward(x, r.mean, r.rstd, weight, bias)
+            return r.y
+
+        @staticmethod
+        def backward(ctx, dy):
+            x, mean, rstd, weight, bias = ctx.saved_tensors
+            return ops.group_norm_backward(dy.contiguous(), x, mean, rstd, weight, bias, activation="silu")
+    leaf = x.clone().requires_grad_()
+    Norm.apply(leaf, w, b).sum().backward()
+    r = ops.group_norm(x, 8, w.detach(), b, activation="silu")
+    dx, dw, _ = ops.group_norm_backward(torch.ones_like(x), x, r.mean, r.rstd, w.detach(), b, activation="silu")
+    assert torch.equal(leaf.grad, dx) and torch.equal(w.grad, dw)

@@ -193,3 +193,14 @@ def test_numbers_that_no_argument_block_holds(lib):
     with pytest.raises(A.AlexNetError) as e:
         ops._run(lib.alexnet_checkpoint_encode, 0, ops._pack_checkpoint, 1, 1, 1 << 31, 1, 0, P, 0, 0, 0, *KEPT)
     assert e.value.code == A.ERR_ARG
+
+
+def test_a_result_without_a_gradient_says_so():
+    y = torch.ones(3)
+    z = ops._without_gradient(y)
+    assert z is y and z.requires_grad and not z.is_leaf
+    with pytest.raises(A.AlexNetError, match="group_norm_backward"):
+        (2 * z).sum().backward()
+    with torch.no_grad():
+        z += 1                                  # its values are anyone's, as before
+    assert torch.equal(z.detach(), torch.full((3,), 2.0))
