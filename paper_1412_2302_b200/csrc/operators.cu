@@ -106,7 +106,7 @@ bool vec_ok(const alexnet_checkpoint_t& k, const Dims& d) { return d.C % 8 == 0 
 // Passes whose blocks end with a reduction: whole rounds of what an SM holds of them (`blocks_per_sm` with vectors of eight, six with single channels), a block being as dear as
 // its positions and ten more, and a thread adds up at most kMostTerms of them, for the sake of the sums' roundings.
 constexpr int kElementwise = 0, kForwardSums = 3, kMostTerms = 192;
-Walk walk_of(const Dims& d, int V, int blocks_per_sm) {
+Walk find_walk(const Dims& d, int V, int blocks_per_sm) {
     Walk w{};
     w.C = d.C; w.HW = d.h * d.w; w.vecs = d.C / V;
     const int q = V == 8 ? 4 : 1, padded = (int)ceil_div(w.vecs, q) * q;
@@ -129,6 +129,18 @@ Walk walk_of(const Dims& d, int V, int blocks_per_sm) {
     w.chunks = ceil_div(w.HW, w.ppc);
     w.dense = dense_of(d.C, w.rows);
     return w;
+}
+// (found once for the sizes of a thread's last calls, three or four walks each: with few large samples the search takes 15 to 60 us)
+const Walk& walk_of(const Dims& d, int V, int blocks_per_sm) {
+    struct Known { long long n = -1; int HW, C, V, blocks_per_sm; Walk walk; };
+    static thread_local Known known[64];
+    static thread_local unsigned next = 0;
+    const int HW = d.h * d.w;
+    for (const Known& q : known)
+        if (q.n == d.n && q.HW == HW && q.C == d.C && q.V == V && q.blocks_per_sm == blocks_per_sm) return q.walk;
+    Known& q = known[next++ % 64];
+    q = {d.n, HW, d.C, V, blocks_per_sm, find_walk(d, V, blocks_per_sm)};
+    return q.walk;
 }
 // the same for rows of any length: a vector is a checkpoint block, taken by a warp
 Walk walk_any(const Dims& d) {
