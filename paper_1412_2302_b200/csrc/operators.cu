@@ -423,7 +423,7 @@ struct LinearPlan {
     long long dy_pitch, x_pitch;        // bytes
     size_t dy_at, x_at, bytes, smem;    // places in the workspace, behind the partial sums
 };
-LinearPlan linear_plan(const alexnet_linear_weight_grad_t& a) {
+LinearPlan find_linear_plan(const alexnet_linear_weight_grad_t& a) {
     LinearPlan b{};
     b.steps = (int)ceil_div(a.rows, kLgRows);
     // The tile's width, pairs or single CTAs and the splits of the last round by a model of the launch in cycles, fitted to measurements (BN 128 to
@@ -453,9 +453,24 @@ LinearPlan linear_plan(const alexnet_linear_weight_grad_t& a) {
     b.smem = tc::own_sm(1024 + (size_t)b.stages * stage + 256);
     b.dy_pitch = ceil_div(a.n_out, 8) * 16;
     b.x_pitch = ceil_div(a.n_in, 16) * 16;
+    b.dy_at = (size_t)b.splits * (b.tiles - b.whole) * b.BN * 128 * b.cg * sizeof(float);
+    return b;
+}
+// (found once for the sizes of a thread's last calls: with few tiles the search takes 10 us; what goes by alignment is added)
+LinearPlan linear_plan(const alexnet_linear_weight_grad_t& a) {
+    struct Known { long long rows = -1; int n_in, n_out; LinearPlan plan; };
+    static thread_local Known known[16];
+    static thread_local unsigned next = 0;
+    const Known* found = nullptr;
+    for (const Known& q : known)
+        if (q.rows == a.rows && q.n_in == a.n_in && q.n_out == a.n_out) found = &q;
+    if (!found) {
+        known[next % 16] = {a.rows, a.n_in, a.n_out, find_linear_plan(a)};
+        found = &known[next++ % 16];
+    }
+    LinearPlan b = found->plan;
     b.move_dy = (uintptr_t)a.dy % 16 != 0 || (a.rows > 1 && (a.dy_stride % 8 != 0 || a.dy_stride < a.n_out));
     b.move_x = (uintptr_t)a.x.codes % 16 != 0 || a.n_in % 16 != 0;
-    b.dy_at = (size_t)b.splits * (b.tiles - b.whole) * b.BN * 128 * b.cg * sizeof(float);
     b.x_at = b.dy_at + (b.move_dy ? ((size_t)a.rows * b.dy_pitch + 255) / 256 * 256 : 0);
     b.bytes = b.x_at + (b.move_x ? ((size_t)a.rows * b.x_pitch + 255) / 256 * 256 : 0);      // 0: none needed
     return b;

@@ -223,3 +223,18 @@ def test_plans_are_found_once_per_size(lib):
             f()
             best = min(best, time.perf_counter() - t)
         assert best < 30e-6, best
+
+
+def test_linear_plans_are_found_once_per_size(lib):
+    """The same for the tiles of a linear layer's gradient (11 us at 16384 x 256 x 256); alignment is looked at in each call."""
+    block = lambda p, stride, q: ops._pack_linear(16384, 256, 256, p, stride, q, P, 1, 0, 0, 0, 0)      # noqa: E731
+    size = lib.alexnet_linear_weight_grad_workspace_bytes
+    best = 1.0
+    for _ in range(200):
+        t = time.perf_counter()
+        size(block(P, 256, P))
+        best = min(best, time.perf_counter() - t)
+    assert best < 5e-6, best
+    plain, copied = size(block(P, 256, P)), 16384 * 256
+    assert size(block(P + 2, 256, P)) == size(block(P, 257, P)) == plain + 2 * copied
+    assert size(block(P, 256, P + 8)) == plain + copied and size(block(P + 2, 256, P + 8)) == plain + 3 * copied
