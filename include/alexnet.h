@@ -491,8 +491,9 @@ typedef struct alexnet_group_norm {
     float eps;
     int32_t reserved;
 } alexnet_group_norm_t;
-/* bytes of workspace of one call, at least 256 (0: invalid shape); 256 means that
- * the call needs none, and workspace may be NULL */
+/* bytes of workspace of one call of this shape, whatever its tensors' alignment and
+ * strides and whatever x is read from, at least 256 (0: invalid shape); 256 means that
+ * no such call needs any, and workspace may be NULL */
 size_t alexnet_group_norm_workspace_bytes(const alexnet_group_norm_t* shape, int backward);
 
 typedef struct alexnet_group_norm_forward_args {
@@ -505,6 +506,9 @@ typedef struct alexnet_group_norm_forward_args {
     void* workspace;                    /* 16-byte aligned */
     size_t workspace_bytes;
 } alexnet_group_norm_forward_t;
+/* the same for a call with these arguments (of pointers the alignment counts; the
+ * workspace need not be set): what vectors need is less */
+size_t alexnet_group_norm_forward_workspace_bytes(const alexnet_group_norm_forward_t* args);
 int alexnet_group_norm_forward(const alexnet_group_norm_forward_t* args, void* stream, char* err, size_t err_len);
 
 /* Gradients of y = act(norm(x) weight + bias) for a given dy and the statistics
@@ -521,6 +525,7 @@ typedef struct alexnet_group_norm_backward_args {
     void* workspace;
     size_t workspace_bytes;
 } alexnet_group_norm_backward_t;
+size_t alexnet_group_norm_backward_workspace_bytes(const alexnet_group_norm_backward_t* args);
 int alexnet_group_norm_backward(const alexnet_group_norm_backward_t* args, void* stream, char* err, size_t err_len);
 
 /* Weight gradient of a linear layer (or of a 1 x 1 convolution, whose rows are the

@@ -41,7 +41,8 @@ EXPORTS = ["alexnet_param_count", "alexnet_workspace_bytes", "alexnet_create", "
            "alexnet_scale_and_refresh", "alexnet_create_error", "alexnet_debug_expire_wait", "alexnet_set_color_augmentation", "alexnet_average_received", "alexnet_param_layout",
            "alexnet_stream_wait_fc_gradients", "alexnet_timeline_read", "alexnet_profile_read_kinds",
            "alexnet_checkpoint_encode", "alexnet_checkpoint_decode", "alexnet_group_norm_workspace_bytes", "alexnet_group_norm_forward",
-           "alexnet_group_norm_backward", "alexnet_linear_weight_grad_workspace_bytes", "alexnet_linear_weight_grad", "alexnet_operators_check", "alexnet_operators_debug_expire_wait"]
+           "alexnet_group_norm_backward", "alexnet_linear_weight_grad_workspace_bytes", "alexnet_linear_weight_grad", "alexnet_operators_check", "alexnet_operators_debug_expire_wait",
+           "alexnet_group_norm_forward_workspace_bytes", "alexnet_group_norm_backward_workspace_bytes"]
 
 
 class Config(ctypes.Structure):
@@ -124,8 +125,9 @@ def load_library():
         getattr(L, "alexnet_" + name).argtypes = [ctypes.c_char_p, vp, ctypes.c_char_p, sz]
     L.alexnet_group_norm_workspace_bytes.restype = sz
     L.alexnet_group_norm_workspace_bytes.argtypes = [ctypes.c_char_p, i32]
-    L.alexnet_linear_weight_grad_workspace_bytes.restype = sz
-    L.alexnet_linear_weight_grad_workspace_bytes.argtypes = [ctypes.c_char_p]
+    for name in ("group_norm_forward", "group_norm_backward", "linear_weight_grad"):
+        getattr(L, "alexnet_" + name + "_workspace_bytes").restype = sz
+        getattr(L, "alexnet_" + name + "_workspace_bytes").argtypes = [ctypes.c_char_p]
     L.alexnet_operators_check.argtypes = []
     L.alexnet_operators_debug_expire_wait.argtypes = [ctypes.c_char_p, i32, vp, ctypes.c_char_p, sz]
     _lib = L

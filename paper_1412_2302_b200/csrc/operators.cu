@@ -309,6 +309,14 @@ size_t backward_ws(const Dims& d, int groups, int dtype, bool kept) {
     const long long chunks = std::max(walk_of(d, V, 2).chunks, walk_of(d, V, 3).chunks);       // (of either source)
     return (size_t)(d.n * groups) * sizeof(float2) + (size_t)(d.n * chunks) * 2 * d.C * sizeof(float);
 }
+size_t reported(size_t bytes) { return bytes ? (bytes + 511) / 256 * 256 : 256; }
+// whether a call reads and writes vectors of eight channels
+bool forward_in_vectors(const alexnet_group_norm_forward_t& a, const Dims& d) {
+    return vec_ok(a.x, d, a.shape.dtype) && vec_ok(a.y, d, a.shape.dtype) && (!a.keep_x.codes || vec_ok(a.keep_x, d)) && (!a.keep_y.codes || vec_ok(a.keep_y, d));
+}
+bool backward_in_vectors(const alexnet_group_norm_backward_t& a, const Dims& d) {
+    return vec_ok(a.dy, d, a.shape.dtype) && vec_ok(a.dx, d, a.shape.dtype) && (a.kept.codes || a.kept.scales ? vec_ok(a.kept, d) : vec_ok(a.x, d, a.shape.dtype));
+}
 template <typename T, int V, int ACT>
 void forward(Launcher& go, const alexnet_group_norm_forward_t* a, const Dims& d) {
     const Walk w = walk_of(d, V, kForwardSums);
@@ -552,7 +560,21 @@ size_t alexnet_group_norm_workspace_bytes(const alexnet_group_norm_t* s, int bac
         if (d.C % 8 == 0) bytes = std::max(bytes, backward ? backward_ws<8>(d, s->groups, s->dtype, kept) : forward_ws<8>(d, s->groups, s->dtype));
         bytes = std::max(bytes, backward ? backward_ws<1>(d, s->groups, s->dtype, kept) : forward_ws<1>(d, s->groups, s->dtype));
     }
-    return bytes ? (bytes + 511) / 256 * 256 : 256;
+    return reported(bytes);
+}
+
+size_t alexnet_group_norm_forward_workspace_bytes(const alexnet_group_norm_forward_t* a) {
+    if (!a || check_shape(a->shape)) return 0;
+    const alexnet_group_norm_t& s = a->shape;
+    const Dims d{s.n, s.h, s.w, s.channels};
+    return reported(forward_in_vectors(*a, d) ? forward_ws<8>(d, s.groups, s.dtype) : forward_ws<1>(d, s.groups, s.dtype));
+}
+size_t alexnet_group_norm_backward_workspace_bytes(const alexnet_group_norm_backward_t* a) {
+    if (!a || check_shape(a->shape)) return 0;
+    const alexnet_group_norm_t& s = a->shape;
+    const Dims d{s.n, s.h, s.w, s.channels};
+    const bool kept = a->kept.codes || a->kept.scales;
+    return reported(backward_in_vectors(*a, d) ? backward_ws<8>(d, s.groups, s.dtype, kept) : backward_ws<1>(d, s.groups, s.dtype, kept));
 }
 
 int alexnet_group_norm_forward(const alexnet_group_norm_forward_t* a, void* stream, char* err_buf, size_t err_len) {
@@ -570,9 +592,7 @@ int alexnet_group_norm_forward(const alexnet_group_norm_forward_t* a, void* stre
     if (!a->mean || !a->rstd) return err.arg("NULL pointer");
     if (a->x.data == a->y.data) return err.arg("y must not share memory with x");
     if (grid_of(walk_of(d, 1, kElementwise), d) > kMaxGrid) return err.arg("the tensor is too large");
-    bool vec = vec_ok(a->x, d, s.dtype) && vec_ok(a->y, d, s.dtype);
-    if (a->keep_x.codes) vec = vec && vec_ok(a->keep_x, d);
-    if (a->keep_y.codes) vec = vec && vec_ok(a->keep_y, d);
+    const bool vec = forward_in_vectors(*a, d);
     const size_t need = vec ? forward_ws<8>(d, s.groups, s.dtype) : forward_ws<1>(d, s.groups, s.dtype);
     if (need && (!a->workspace || (uintptr_t)a->workspace % 16 || a->workspace_bytes < need)) return err.arg("the workspace is too small or not 16-byte aligned");
     Launcher go{(cudaStream_t)stream};
@@ -604,7 +624,7 @@ int alexnet_group_norm_backward(const alexnet_group_norm_backward_t* a, void* st
     if (!a->mean || !a->rstd) return err.arg("NULL pointer");
     if (a->dx.data == a->x.data || a->dx.data == a->dy.data) return err.arg("dx must not share memory with x or dy");
     if (grid_of(walk_of(d, 1, kElementwise), d) > kMaxGrid) return err.arg("the tensor is too large");
-    const bool vec = vec_ok(a->dy, d, s.dtype) && vec_ok(a->dx, d, s.dtype) && (kept ? vec_ok(a->kept, d) : vec_ok(a->x, d, s.dtype));
+    const bool vec = backward_in_vectors(*a, d);
     const size_t need = vec ? backward_ws<8>(d, s.groups, s.dtype, kept) : backward_ws<1>(d, s.groups, s.dtype, kept);
     if (need && (!a->workspace || (uintptr_t)a->workspace % 16 || a->workspace_bytes < need)) return err.arg("the workspace is too small or not 16-byte aligned");
     Launcher go{(cudaStream_t)stream};

@@ -223,13 +223,28 @@ def _kept(k):
     return k.codes.data_ptr(), k.scales.data_ptr(), FORMATS[_FORMAT_OF[k.codes.dtype]], 0
 
 
-@functools.lru_cache(maxsize=1024)
-def _norm_workspace(shape, backward):
-    """bytes of workspace for the sizes (0: the call needs none)"""
-    n = int(_alexnet.load_library().alexnet_group_norm_workspace_bytes(_pack(_pack_shape, *shape), backward))
+def _norm_bytes(n, shape):
     if n == 0:
         raise AlexNetError(ERR_ARG, f"invalid group norm: n, h, w, channels, groups = {tuple(shape[:5])}, eps = {shape[7]}")
     return n if n > 256 else 0
+
+
+def _norm_workspace(shape, backward):
+    """bytes of workspace for the sizes, whatever the tensors (0: no call needs any)"""
+    return _norm_bytes(int(_alexnet.load_library().alexnet_group_norm_workspace_bytes(_pack(_pack_shape, *shape), backward)), shape)
+
+
+# by sizes, strides and alignment: the pointers are given modulo 16
+@functools.lru_cache(maxsize=1024)
+def _forward_workspace(shape, x, xs, y, ys):
+    return _norm_bytes(int(_alexnet.load_library().alexnet_group_norm_forward_workspace_bytes(
+        _pack(_pack_forward, *shape, x, *xs, y, *ys, 0, 0, 0, 0, *_NOT_KEPT, *_NOT_KEPT, 0, 0))), shape)
+
+
+@functools.lru_cache(maxsize=1024)
+def _backward_workspace(shape, dy, ds, x, xs, dx, dxs, codes, fmt):
+    return _norm_bytes(int(_alexnet.load_library().alexnet_group_norm_backward_workspace_bytes(
+        _pack(_pack_backward, *shape, dy, *ds, x, *xs, dx, *dxs, codes, 16 if fmt else 0, fmt, 0, 0, 0, 0, 0, 0, 0, 0, 0))), shape)
 
 
 @functools.lru_cache(maxsize=1024)
@@ -299,8 +314,15 @@ def group_norm(x, groups, weight=None, bias=None, eps=1e-5, activation="none", k
             _refuse(f"groups must be an integer and eps a number, not {groups!r} and {eps!r}")
     (n, h, w, c), xs = _rows(x, "x")
     shape = (n, h, w, c, groups, _name(DTYPES, x.dtype, "dtype"), _name(ACTIVATIONS, activation, "activation"), eps, 0)
-    nbytes = _norm_workspace(shape, 0)
-    y = _dense_like(x) if out is None else _output(out, x.shape, x.dtype, index)
+    px = x.data_ptr()
+    if out is None:                                 # (asked before y is created: a shape may be refused)
+        nbytes = _forward_workspace(shape, px % 16, xs, 0, (h * w * c, w * c, c))
+        y = _dense_like(x)
+        py, ys = y.data_ptr(), _rows(y, "out")[1]
+    else:
+        y = _output(out, x.shape, x.dtype, index)
+        py, ys = y.data_ptr(), _rows(y, "out")[1]
+        nbytes = _forward_workspace(shape, px % 16, xs, py % 16, ys)
     mean = x.new_empty((n, groups), dtype=torch.float32)
     rstd = torch.empty_like(mean)
     kx = ky = None
@@ -313,7 +335,7 @@ def group_norm(x, groups, weight=None, bias=None, eps=1e-5, activation="none", k
         pky = _kept(ky)
     ws = x.new_empty(nbytes, dtype=torch.uint8) if nbytes else None
     _run(_alexnet.load_library().alexnet_group_norm_forward, index, _pack_forward,
-         *shape, x.data_ptr(), *xs, y.data_ptr(), *_rows(y, "out")[1], _vector(weight, c, "weight", index), _vector(bias, c, "bias", index), mean.data_ptr(), rstd.data_ptr(),
+         *shape, px, *xs, py, *ys, _vector(weight, c, "weight", index), _vector(bias, c, "bias", index), mean.data_ptr(), rstd.data_ptr(),
          *pkx, *pky, 0 if ws is None else ws.data_ptr(), nbytes)
     if out is None and torch.is_grad_enabled() and (x.requires_grad or (weight is not None and weight.requires_grad) or (bias is not None and bias.requires_grad)):
         y = _without_gradient(y)
@@ -344,13 +366,20 @@ def group_norm_backward(dy, x, mean, rstd, weight=None, bias=None, activation="n
     if other or mean.get_device() != index or rstd.get_device() != index:
         _other_device()
     shape = (n, h, w, c, mean.shape[1], _name(DTYPES, dy.dtype, "dtype"), _name(ACTIVATIONS, activation, "activation"), 1.0, 0)
-    nbytes = _norm_workspace(shape, 1)
-    dx = _dense_like(dy) if out is None else _output(out, dy.shape, dy.dtype, index)
+    pdy = dy.data_ptr()
+    if out is None:
+        nbytes = _backward_workspace(shape, pdy % 16, ds, xv[0] % 16, xv[1:], 0, (h * w * c, w * c, c), kept[0] % 16, kept[2])
+        dx = _dense_like(dy)
+        pdx, dxs = dx.data_ptr(), _rows(dx, "out")[1]
+    else:
+        dx = _output(out, dy.shape, dy.dtype, index)
+        pdx, dxs = dx.data_ptr(), _rows(dx, "out")[1]
+        nbytes = _backward_workspace(shape, pdy % 16, ds, xv[0] % 16, xv[1:], pdx % 16, dxs, kept[0] % 16, kept[2])
     dweight = dy.new_empty(c, dtype=torch.float32)
     dbias = torch.empty_like(dweight)
     ws = dy.new_empty(nbytes, dtype=torch.uint8) if nbytes else None
     _run(_alexnet.load_library().alexnet_group_norm_backward, index, _pack_backward,
-         *shape, dy.data_ptr(), *ds, *xv, dx.data_ptr(), *_rows(dx, "out")[1], *kept, mean.data_ptr(), rstd.data_ptr(), _vector(weight, c, "weight", index),
+         *shape, pdy, *ds, *xv, pdx, *dxs, *kept, mean.data_ptr(), rstd.data_ptr(), _vector(weight, c, "weight", index),
          _vector(bias, c, "bias", index), dweight.data_ptr(), dbias.data_ptr(), 0 if ws is None else ws.data_ptr(), nbytes)
     return dx, dweight, dbias
 

@@ -203,3 +203,15 @@ def test_autograd_is_not_passed_by_in_silence(ops):
     r = ops.group_norm(x, 8, w.detach(), b, activation="silu")
     dx, dw, _ = ops.group_norm_backward(torch.ones_like(x), x, r.mean, r.rstd, w.detach(), b, activation="silu")
     assert torch.equal(leaf.grad, dx) and torch.equal(w.grad, dw)
+
+
+def test_one_picture_allocates_its_outputs_alone(ops):
+    x = torch.randn((1, 13, 13, 384), device="cuda", generator=gen(1)).to(torch.bfloat16)
+    allocated = lambda: torch.cuda.memory_stats()["allocation.all.allocated"]      # noqa: E731
+    r = ops.group_norm(x, 32)
+    before = allocated()
+    r = ops.group_norm(x, 32)
+    assert allocated() - before == 3                 # y, mean, rstd
+    before = allocated()
+    ops.group_norm_backward(x, x, r.mean, r.rstd)
+    assert allocated() - before == 3                 # dx, dweight, dbias

@@ -238,3 +238,23 @@ def test_linear_plans_are_found_once_per_size(lib):
     plain, copied = size(block(P, 256, P)), 16384 * 256
     assert size(block(P + 2, 256, P)) == size(block(P, 257, P)) == plain + 2 * copied
     assert size(block(P, 256, P + 8)) == plain + copied and size(block(P + 2, 256, P + 8)) == plain + 3 * copied
+
+
+def test_vectors_need_less_workspace(lib):
+    """The queries that know a call's tensors: one picture of 13 x 13 x 384 and a minibatch of 27 x 27 x 256 are kept by blocks where they are read in vectors,
+    and need none; single channels do, and no call needs more than its sizes' query says."""
+    forward, backward = lib.alexnet_group_norm_forward_workspace_bytes, lib.alexnet_group_norm_backward_workspace_bytes
+    for n, h, w, c, groups in ((1, 13, 13, 384, 32), (128, 27, 27, 256, 32)):
+        s, v = shape(n=n, h=h, w=w, c=c, groups=groups), lambda p: VIEW(h, w, c, p)      # noqa: E731
+        most = [lib.alexnet_group_norm_workspace_bytes(ops._pack_shape(*s), b) for b in (0, 1)]
+        f = lambda x, y, kx=NONE: forward(ops._pack_forward(*s, *x, *y, 0, 0, 0, 0, *kx, *NONE, 0, 0))      # noqa: E731
+        b = lambda dy, x, dx, kept=NONE: backward(ops._pack_backward(*s, *dy, *x, *dx, *kept, 0, 0, 0, 0, 0, 0, 0, 0))      # noqa: E731
+        assert f(v(P), v(P)) == f(v(0), v(0), (P, P, 1, 0)) == 256
+        assert f(v(P + 2), v(P)) == f(v(P), v(P + 8)) == f(v(P), v(P), (P + 4, P, 1, 0)) == most[0] > 256
+        assert (b(v(P), v(P), v(P)) == 256) == (n == 1) and b(v(P), v(P), v(P)) <= most[1]
+        assert 256 < b(v(P), NONE, v(P), KEPT) <= most[1] and 256 < b(v(P), v(P), v(P + 8)) <= most[1]
+    for bad in (dict(groups=7), dict(eps=0.0), dict(n=-1)):
+        s, v = shape(**bad), VIEW(3, 4, 64)
+        assert forward(ops._pack_forward(*s, *v, *v, 0, 0, 0, 0, *NONE, *NONE, 0, 0)) == 0
+        assert backward(ops._pack_backward(*s, *v, *v, *v, *NONE, 0, 0, 0, 0, 0, 0, 0, 0)) == 0
+    assert forward(None) == backward(None) == 0
