@@ -159,6 +159,8 @@ def _rows_any(t, what):
     if t.dim() > 4:
         if not t.is_contiguous():
             _refuse(f"{what} has {t.dim()} dimensions and is not dense")
+        if t.shape[-1] == 0:
+            _refuse(f"{what} has no channels")
         t = t.view(-1, t.shape[-1])
     elif t.dim() == 1:
         t = t.view(1, -1)
@@ -398,6 +400,8 @@ def linear_weight_grad(dy, x, out=None, stream=None):
         with _elsewhere(index, stream):
             return linear_weight_grad(dy, x, out)
     n_in, n_out = codes.shape[-1], dy.shape[-1]
+    if n_in == 0 or n_out == 0:
+        _refuse(f"features must be 1 to 1048576, not {n_in} and {n_out}")
     if dy.dim() != 2:
         if not dy.is_contiguous():
             _refuse("dy of other than two dimensions must be dense")

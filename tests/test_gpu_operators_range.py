@@ -215,3 +215,24 @@ def test_one_picture_allocates_its_outputs_alone(ops):
     before = allocated()
     ops.group_norm_backward(x, x, r.mean, r.rstd)
     assert allocated() - before == 3                 # dx, dweight, dbias
+
+
+def test_empty_sizes(ops):
+    """Rows may be none, channels and features may not: an AlexNetError like any wrong argument's."""
+    def refused(word, f, *args, **kw):
+        with pytest.raises(A.AlexNetError, match=word) as e:
+            f(*args, **kw)
+        assert e.value.code == A.ERR_ARG
+    bf16 = dict(dtype=torch.bfloat16, device="cuda")
+    codes = lambda *s: ops.Checkpoint(torch.zeros(s, dtype=torch.int8, device="cuda"), torch.zeros((*s[:-1], (s[-1] + 31) // 32), dtype=torch.uint8, device="cuda"))      # noqa: E731
+    for lead in ((2,), (2, 3), (2, 1, 1, 3), (0, 3)):
+        refused("features", ops.linear_weight_grad, torch.zeros((*lead, 0), **bf16), codes(*lead, 8))
+        refused("features", ops.linear_weight_grad, torch.zeros((*lead, 8), **bf16), codes(*lead, 0))
+        refused("channels", ops.checkpoint_encode, torch.zeros((*lead, 0), **bf16))
+        refused("channels", ops.checkpoint_decode, codes(*lead, 0))
+    refused("channels", ops.checkpoint_encode, torch.zeros((2, 1, 1, 1, 0), **bf16))
+    refused("channels", ops.group_norm, torch.zeros((2, 3, 3, 0), **bf16), 1)
+    refused("at least 1", ops.checkpoint_encode, torch.zeros((2, 0, 3, 8), **bf16))
+    for lead in ((0,), (0, 3), (0, 1, 1, 3)):
+        assert bool((ops.linear_weight_grad(torch.zeros((*lead, 8), **bf16), codes(*lead, 40)) == 0).all())
+        assert ops.checkpoint_decode(ops.checkpoint_encode(torch.zeros((*lead, 8), **bf16))).shape == (*lead, 8)

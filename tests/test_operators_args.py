@@ -196,6 +196,13 @@ def test_numbers_that_no_argument_block_holds(lib):
     assert e.value.code == A.ERR_ARG
 
 
+def test_tensors_without_channels_are_refused():
+    for shape in ((2, 1, 1, 2, 0), (0, 1, 1, 2, 0)):
+        with pytest.raises(A.AlexNetError, match="no channels") as e:
+            ops._rows_any(torch.zeros(shape), "x")
+        assert e.value.code == A.ERR_ARG
+
+
 def test_a_result_without_a_gradient_says_so():
     y = torch.ones(3)
     z = ops._without_gradient(y)
