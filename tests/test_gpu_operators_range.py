@@ -5,6 +5,9 @@ Tolerances.  Where the terms of a sum are alike, an fp32 running sum of k of the
 the running sum, which is half of the last one on average).  A thread of a backward pass sums at most 192 terms so, the sums of its block's rows
 come in four chains of at most 64 each, those of warps in chains of at most 32; everything longer carries the error of its additions along
 (2^-24 in all).  192 + 64 of 2^-25 are 2^-17, FP32 below: that times the sum of the magnitudes."""
+import subprocess
+import sys
+
 import pytest
 import torch
 
@@ -236,3 +239,111 @@ def test_empty_sizes(ops):
     for lead in ((0,), (0, 3), (0, 1, 1, 3)):
         assert bool((ops.linear_weight_grad(torch.zeros((*lead, 8), **bf16), codes(*lead, 40)) == 0).all())
         assert ops.checkpoint_decode(ops.checkpoint_encode(torch.zeros((*lead, 8), **bf16))).shape == (*lead, 8)
+
+
+@pytest.mark.parametrize("fmt", ["int8", "e4m3"])
+@pytest.mark.parametrize("rows,n_in,n_out,width", [(173, 500, 1000, 1008), (64, 64, 64, 72), (300, 1024, 512, 520), (129, 40, 13, 16), (77, 33, 1, 8), (2049, 2080, 2056, 2064), (1000, 4096, 1000, 1024)])
+def test_linear_weight_grad_of_wider_rows(ops, fmt, rows, n_in, n_out, width):
+    """dy as the first columns of rows that are wider and start on 16-byte boundaries: read in place, NaN behind the columns; those before and behind dw stay as
+    they were.  Sums are off by (rows + 16) 2^-24 of their magnitudes at most."""
+    g = gen(rows + n_out)
+    k = ops.checkpoint_encode(torch.randn((rows, n_in), device="cuda", generator=g), fmt)
+    wide = torch.full((rows, width), float("nan"), dtype=torch.bfloat16, device="cuda")
+    dy = wide[:, :n_out]
+    dy.copy_(torch.randn((rows, n_out), device="cuda", generator=g))
+    around = torch.full((n_out * n_in + 64,), 7.0, device="cuda")
+    dw = around[32:32 + n_out * n_in].view(n_out, n_in)
+    assert ops.linear_weight_grad(dy, k, out=dw) is dw
+    value = ops.checkpoint_decode(k, torch.float32).double()
+    want, mag = dy.double().t() @ value, dy.double().abs().t() @ value.abs()
+    assert bool(((dw.double() - want).abs() <= (rows + 16) * 2.0 ** -24 * mag).all())
+    assert bool((around[:32] == 7).all()) and bool((around[-32:] == 7).all())
+    assert torch.equal(dw, ops.linear_weight_grad(dy.contiguous(), k))
+
+
+@pytest.mark.parametrize("fmt", ["int8", "e4m3"])
+def test_linear_weight_grad_at_the_ends_of_the_scales(ops, fmt):
+    """Blocks of every exponent that encode writes, from subnormal values to the largest, and gradients that bring the products back: what is read is the
+    checkpoint's value rounded to bf16 (exact but for e4m3 codes of values below 2^-126)."""
+    rows, n_in, n_out = 96, 64, 24
+    g = gen(3)
+    x = torch.randn((rows, n_in), device="cuda", generator=g) * torch.exp2(torch.linspace(-130, 100, rows, device="cuda").double())[:, None].float()
+    x[::7] *= -1
+    k = ops.checkpoint_encode(x, fmt)
+    value = ops.checkpoint_decode(k, torch.bfloat16).double()
+    dy = torch.zeros((rows, n_out), device="cuda", dtype=torch.bfloat16)
+    for o in range(n_out):                               # each output sees four rows, so that no sum mixes sizes
+        dy[4 * o:4 * o + 4, o] = torch.randn(4, device="cuda", generator=g).bfloat16() * (2.0 ** (100 if o < 4 else 0))
+    dw = ops.linear_weight_grad(dy, k)
+    want, mag = dy.double().t() @ value, dy.double().abs().t() @ value.abs()
+    assert bool(want.abs().amax(1).gt(0).all())
+    assert bool(((dw.double() - want).abs() <= 20 * 2.0 ** -24 * mag + 2.0 ** -149).all())
+
+
+def test_rows_at_any_alignment(ops):
+    """Slices of channels of a wider tensor that start between 16-byte boundaries: statistics against the definition."""
+    n, h, w, c, groups = 4, 6, 5, 64, 8
+    wide = torch.randn((n, h, w, c + 8), device="cuda", generator=gen(41)).to(torch.bfloat16)
+    for off in (1, 3, 5):
+        part = wide[..., off:off + c]
+        r = ops.group_norm(part, groups)
+        v = part.double().reshape(n, h * w, groups, c // groups)
+        mean = v.mean((1, 3))
+        v = v - mean[:, None, :, None]
+        rstd = (v.square().mean((1, 3)) + 1e-5).rsqrt()
+        assert bool(((r.mean.double() - mean).abs() <= FP32 * v.abs().mean((1, 3)) + 2.0 ** -24 * mean.abs()).all())
+        assert bool(((r.rstd.double() - rstd).abs() <= FP32 * rstd).all())
+        y = (v * rstd[:, None, :, None]).view(n, h, w, c)
+        assert bool(((r.y.double() - y).abs() <= 2.0 ** -8 * y.abs() + 3 * FP32 * (y.abs() + 1)).all())
+
+
+def test_more_samples_than_a_grid_of_slices_takes(ops):
+    n, c = (1 << 25) + 77, 4
+    x = torch.randn((n, c), device="cuda", generator=gen(5)).to(torch.float16)
+    r = ops.group_norm(x, 2, activation="none", keep_input="int8")
+    dy = torch.randn((n, c), device="cuda", generator=gen(6)).to(torch.float16)
+    dx, dw, db = ops.group_norm_backward(dy, x, r.mean, r.rstd)
+    for at in (slice(0, 1000), slice(n - 1000, n)):
+        some = ops.group_norm(x[at].clone(), 2, keep_input="int8")
+        assert torch.equal(r.y[at], some.y) and torch.equal(r.mean[at], some.mean) and torch.equal(r.input.codes[at], some.input.codes)
+        assert torch.equal(dx[at], ops.group_norm_backward(dy[at].clone(), x[at].clone(), some.mean, some.rstd)[0])
+    assert bool(((db.double() - dy.double().sum(0)).abs() <= FP32 * dy.double().abs().sum(0)).all())
+
+
+FIRST = r"""
+import torch
+from paper_1412_2302_b200 import operators as ops
+g = torch.Generator(device="cuda").manual_seed(1)
+x = torch.randn((2, 40, 40, 33), device="cuda", generator=g)
+v = torch.randn((4, 13, 13, 64), device="cuda", generator=g).bfloat16()
+dy = torch.randn((200, 72), device="cuda", generator=g).bfloat16()
+codes = torch.randint(-127, 128, (200, 160), device="cuda", generator=g, dtype=torch.int8)
+scales = torch.randint(100, 140, (200, 5), device="cuda", generator=g, dtype=torch.uint8)
+def run():
+    a, b = ops.group_norm(x, 3, activation="silu", keep_input="int8"), ops.group_norm(v, 8, activation="relu", keep_output="e4m3")
+    return [a.y, *ops.group_norm_backward(x, a.input, a.mean, a.rstd, activation="silu"), b.y, *ops.group_norm_backward(v, v, b.mean, b.rstd, activation="relu"),
+            ops.checkpoint_decode(b.output), ops.linear_weight_grad(dy, ops.Checkpoint(codes, scales))]
+graph = torch.cuda.CUDAGraph()
+with torch.cuda.graph(graph):
+    got = run()
+for t in got:
+    t.fill_(5)
+graph.replay()
+torch.cuda.synchronize()
+assert all(torch.equal(a, b) for a, b in zip(got, run()))
+print("same")
+"""
+
+
+def test_the_first_calls_of_a_process_are_captured():
+    """Nothing has to have run before: a kernel's code, its shared memory and its plan are found while the stream is being captured."""
+    r = subprocess.run([sys.executable, "-c", FIRST], capture_output=True, text=True, timeout=300)
+    assert r.returncode == 0 and "same" in r.stdout, r.stdout + r.stderr[-2000:]
+
+
+def test_refusals_name_what_is_wrong(ops):
+    x = torch.zeros((2, 4, 4, 64), device="cuda")
+    for word, kw in (("groups = .2, 4, 4, 64, 7., eps = 1e-05", dict(groups=7)), ("eps = 0.0", dict(groups=8, eps=0.0)), ("eps = -1.0", dict(groups=8, eps=-1.0))):
+        with pytest.raises(A.AlexNetError, match=word) as e:
+            ops.group_norm(x, **kw)
+        assert e.value.code == A.ERR_ARG
