@@ -447,18 +447,18 @@ __device__ __forceinline__ void activation_gradient(int act, const Chan<V>& k, c
     }
 }
 // Positions whose loads a thread of the two kernels below has under way, of two tensors each, and blocks per SM (two with 128 registers, three with 80).
-// 512 x 55 x 55 x 96 bf16, ReLU, both kernels: four and two from x 289 us, from int8 codes 315; three and two 297 and 325; two and three 314 and 396.  From e4m3
-// codes, SiLU: two and three 351, three and two 393, four and two 406.  In fp32 (a quarter of the samples, from x): three and two 131, four and two 147.
-template <typename T, int V, int SRC> constexpr int kBackwardBlocks = V == 8 && (sizeof(T) == 4 || SRC != kSrcE4m3) ? 2 : 3;
-template <typename T, int V, int SRC> constexpr int kBackwardLoads = V == 8 ? (sizeof(T) == 4 ? 3 : SRC == kSrcE4m3 ? 2 : 4) : 4;
+// 512 x 55 x 55 x 96 bf16, ReLU, both kernels: four and two from x 275 us, from int8 codes 303, from e4m3 301; three and two 297, 327 and 324; two and three
+// 322, 389 and 376.  In fp32 (a quarter of the samples, from x): three and two 131, four and two 143.
+template <int V> constexpr int kBackwardBlocks = V == 8 ? 2 : 3;
+template <typename T, int V> constexpr int kBackwardLoads = V == 8 && sizeof(T) == 4 ? 3 : 4;
 template <typename T, int V, int SRC, int ACT>
-__global__ void __launch_bounds__(256, kBackwardBlocks<T, V, SRC>) gn_backward_sums_kernel(const T* __restrict__ dy, const Geo gdy, const Source src, const Geo gx, const Walk w, const NormShape sh,
+__global__ void __launch_bounds__(256, kBackwardBlocks<V>) gn_backward_sums_kernel(const T* __restrict__ dy, const Geo gdy, const Source src, const Geo gx, const Walk w, const NormShape sh,
                                                                const BackwardArgs A, float* __restrict__ partial) {
     kn::pdl_sync();
     __shared__ float sums[2 * V * 260];
     const Table<V> table{sums, 260};
     const Spot s = spot(w);
-    constexpr int U = kBackwardLoads<T, V, SRC>;
+    constexpr int U = kBackwardLoads<T, V>;
     float S1[V], S2[V];
     #pragma unroll
     for (int i = 0; i < V; ++i) S1[i] = S2[i] = 0.f;
@@ -578,7 +578,7 @@ __global__ void __launch_bounds__(1024) gn_parameter_gradient_kernel(const float
     parameter_gradient<32>(partial, C, n, blockIdx.x, red, dweight, dbias);
 }
 template <typename T, int V, int SRC, int ACT>
-__global__ void __launch_bounds__(256, kBackwardBlocks<T, V, SRC>) gn_backward_apply_kernel(const T* __restrict__ dy, const Geo gdy, const Source src, const Geo gx, const Walk w, const NormShape sh,
+__global__ void __launch_bounds__(256, kBackwardBlocks<V>) gn_backward_apply_kernel(const T* __restrict__ dy, const Geo gdy, const Source src, const Geo gx, const Walk w, const NormShape sh,
                                                                 const BackwardArgs A, const float2* __restrict__ c12, T* __restrict__ dx, const Geo gdx, const float* __restrict__ partial,
                                                                 long long partials, int extra, float* __restrict__ dweight, float* __restrict__ dbias) {
     kn::pdl_sync();
@@ -600,7 +600,7 @@ __global__ void __launch_bounds__(256, kBackwardBlocks<T, V, SRC>) gn_backward_a
     }
     const T* dp = dy + s.n * gdy.sn + V * s.v;
     T* op = dx + s.n * gdx.sn + V * s.v;
-    constexpr int U = kBackwardLoads<T, V, SRC>;
+    constexpr int U = kBackwardLoads<T, V>;
     Cursor c(gdy, s.p0 + s.row), co(gdx, s.p0 + s.row);
     SourceCursor<T, V, SRC> cx(src, gx, w, s.n, s.p0 + s.row, s.v);
     for (int p = s.p0 + s.row; p < s.p1; p += U * w.rows) {
@@ -837,7 +837,7 @@ __global__ void __launch_bounds__(kSlThreads, 2) gn_slice_forward_kernel(const T
         #pragma unroll 1
         for (int bt = 0; bt < kSlBatches; ++bt) {
             const int e = min(cnt, (bt + 1) * batch);
-            #pragma unroll 2
+            #pragma unroll 1
             for (int it = bt * batch; it < e; ++it) {
                 const R r = has ? slots[it * w.threads] : R{};
                 float f[V], z[V];

@@ -306,8 +306,7 @@ size_t backward_ws(const Dims& d, int groups, int dtype, bool kept) {
     const SliceWalk& s = backward_slices<V>(d, groups, elem, kept);
     // (never more blocks of a slice than 32 per SM; slice_sums grows with them by less than their number)
     if (s.threads) return d.n == 1 ? 0 : (size_t)(std::min<long long>(d.n, 32 * kSms) + d.n / kSlSamples) * 2 * d.C * sizeof(float);
-    const long long chunks = std::max(walk_of(d, V, 2).chunks, walk_of(d, V, 3).chunks);       // (of either source)
-    return (size_t)(d.n * groups) * sizeof(float2) + (size_t)(d.n * chunks) * 2 * d.C * sizeof(float);
+    return (size_t)(d.n * groups) * sizeof(float2) + (size_t)(d.n * walk_of(d, V, kBackwardBlocks<V>).chunks) * 2 * d.C * sizeof(float);
 }
 size_t reported(size_t bytes) { return bytes ? (bytes + 511) / 256 * 256 : 256; }
 // whether a call reads and writes vectors of eight channels
@@ -356,7 +355,7 @@ void forward(Launcher& go, const alexnet_group_norm_forward_t* a, const Dims& d)
 }
 template <typename T, int V, int SRC, int ACT>
 void backward(Launcher& go, const alexnet_group_norm_backward_t* a, const Dims& d) {
-    const Walk w = walk_of(d, V, kBackwardBlocks<T, V, SRC>);
+    const Walk w = walk_of(d, V, kBackwardBlocks<V>);
     const NormShape s = norm_shape(a->shape);
     float2* c12 = (float2*)a->workspace;
     float* partial = (float*)(c12 + d.n * s.groups);
