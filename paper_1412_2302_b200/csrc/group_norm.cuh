@@ -87,7 +87,7 @@ struct NormShape {
 };
 
 // per-channel constants of a thread's vector
-template <int V> struct Chan { float nm[V], a[V], b[V]; uint32_t negative; };      // negative: (backward) not 0 where an a is
+template <int V> struct Chan { float nm[V], a[V], b[V]; uint32_t negative; };      // negative: (backward) the sign bit where an a is
 template <int V>
 __device__ __forceinline__ void load_chan(Chan<V>& k, const NormShape& s, const float* mean, const float* rstd, const float* weight, const float* bias, long long n, int c0) {
     #pragma unroll
@@ -428,7 +428,8 @@ __device__ __forceinline__ void activation_gradient(int act, const Chan<V>& k, c
             for (int i = 0; i < V; ++i) x[i] *= sc;
         }
         v_add<V>(x, k.b, z);
-        if (k.negative) {
+        if constexpr (V == 1) z[0] = __uint_as_float(__float_as_uint(z[0]) ^ k.negative);
+        else if (k.negative) {
             #pragma unroll
             for (int i = 0; i < V; ++i) z[i] = __uint_as_float(__float_as_uint(z[i]) ^ (__float_as_uint(k.a[i]) & 0x80000000u));
         }
