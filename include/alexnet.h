@@ -462,7 +462,9 @@ typedef struct alexnet_view {
  * magnitude is at most 127 (int8) or 448 (e4m3) in codes; codes are rounded to
  * nearest even.  A block with an infinity or NaN has E = 255 and codes 0 and
  * stands for NaN.  (Magnitudes within a code's half step of 2^128 round up to it,
- * which is an infinity in fp32 and bf16; fp16 has them beyond 65504.) */
+ * which is an infinity in fp32 and bf16; fp16 has them beyond 65504.  A value is
+ * exact in fp32, and in bf16 but for e4m3 blocks with E below 3, all of whose values
+ * are below 2^-116: their steps are finer than bf16's last, 2^-133.) */
 typedef struct alexnet_checkpoint {
     void* codes;
     uint8_t* scales;
@@ -483,7 +485,10 @@ int alexnet_checkpoint_decode(const alexnet_checkpoint_args_t* args, void* strea
  * channels / groups channels of a group of one sample: mean and (biased)
  * variance, rstd = 1 / sqrt(var + eps); z = (x - mean) rstd weight + bias;
  * y = act(z) with act the identity, max(z, 0) or z / (1 + e^-z).  Statistics and
- * sums are fp32 or wider; squared deviations must stay within fp32's range. */
+ * sums are fp32 or wider; squared deviations must stay within fp32's range, and
+ * the values below 2^76 in magnitude (means are formed to 2^-23 of them, and what
+ * is left over is squared).  A group with an infinity or a NaN has statistics and
+ * results of NaN. */
 typedef struct alexnet_group_norm {
     int64_t n;
     int32_t h, w, channels, groups;
@@ -530,7 +535,7 @@ int alexnet_group_norm_backward(const alexnet_group_norm_backward_t* args, void*
 
 /* Weight gradient of a linear layer (or of a 1 x 1 convolution, whose rows are the
  * positions) whose input was kept as a checkpoint: dw[o][i] = sum over rows of
- * dy[row][o] x[row][i], products of bf16 dy and decoded x, sums in fp32. */
+ * dy[row][o] x[row][i], products of bf16 dy and x decoded to bf16, sums in fp32. */
 typedef struct alexnet_linear_weight_grad_args {
     int64_t rows;
     int32_t n_in, n_out;

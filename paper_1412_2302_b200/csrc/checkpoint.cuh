@@ -4,7 +4,7 @@
 // and one byte E per block, value = code * 2^(E - 127).  E is the smallest exponent with which the block's largest magnitude stays
 // within 127 (int8) or 448 (e4m3); the codes are rounded to nearest even.  The scale is a power of two, so dividing by it is exact, a code
 // follows from the values alone (no reciprocal whose last bit decides a tie), and a decoded value is exact in bf16 (both codes have at
-// most seven significant bits).  A block with an infinity or a NaN gets E = 255 and codes 0 and stands for NaN throughout.
+// most seven significant bits; only e4m3 blocks with E below 3, values below 2^-116, have steps finer than bf16's last).  A block with an infinity or a NaN gets E = 255 and codes 0 and stands for NaN throughout.
 #pragma once
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>

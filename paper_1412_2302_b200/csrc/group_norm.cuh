@@ -7,8 +7,8 @@
 //
 // Written with d = x - mean and a = rstd w as  z = d a + b  and  dx = dz a + (d (-rstd^2 c2) - rstd c1): two packed instructions per pair
 // of channels each.  Both directions are HBM-bound: x in and y out; dy and x in and dx out.  Measured, bf16 (at the copy rate): 128 x 27 x 27 x 256, a launch per
-// direction, forward 27 us (14.6), SiLU 33, backward 44 (21.9), SiLU 65; 512 x 55 x 55 x 96, read twice, forward 164 (91), backward 258 (136), ReLU 275, SiLU 320.
-// Small calls are bound by their launches and a chain of sums and barriers: 1 x 13 x 13 x 384 7.5 us.
+// direction, forward 27 us (14.6), SiLU 32, backward 44 (21.9), SiLU 63; 512 x 55 x 55 x 96, read twice from memory, forward 164 (91), backward 255 (136), ReLU 274, SiLU 316.
+// Small calls are bound by their launches and a chain of sums and barriers: 1 x 13 x 13 x 384 7.4 us.
 //
 // Sums.  Where a block keeps its values, it goes over them twice, the second time with the first's mean as the shift.  Elsewhere a thread sums, for
 // each of its channels, the differences from the first value and their squares, in fp32; after 8 values, 40, 72 and so on it moves to those from the mean
@@ -315,7 +315,7 @@ __global__ void __launch_bounds__(256, V == 8 && !KEEP ? 4 : 3) gn_apply_kernel(
     T* yp = y + s.n * gy.sn + V * s.v;
     Cursor cx(gx, p0), cy(gy, p0);
     CodesCursor ckx(kx.codes, kx.scales, s.n * w.HW + p0, s.v, w.dense), cky(ky.codes, ky.scales, s.n * w.HW + p0, s.v, w.dense);
-    constexpr int U = 4;                       // vectors in flight: bound by their number (two: 155 us for 512 x 55 x 55 x 96, 3.8 TB/s)
+    constexpr int U = 4;                       // vectors in flight: bound by their number (two: 155 us for 512 x 55 x 55 x 96, 3.8 TB/s; four: 96)
     for (int p = p0; p < s.p1; p += U * w.rows) {
         Raw<T, V> r[U] = {};
         #pragma unroll

@@ -15,7 +15,7 @@
 // bounded; a CTA whose wait runs out writes NaN from there on and raises g_expired.  It arrives on no barrier any more, so that the other CTA of a pair comes to
 // the same end instead of working on tiles and sums that are not there.
 //
-// Measured: 8192 rows, 4096 x 4096: 215 us, 1280 TFLOP/s; the library's product alone, with x in bf16 already, 181 us, and the decoding and
+// Measured: 8192 rows, 4096 x 4096: 225 us, 1220 TFLOP/s; the library's product alone, with x in bf16 already, 181 us, and the decoding and
 // writing of x before it another 25.  128 rows, 9216 x 4096: 29.5 us, 5.2 TB/s, all but 11 % of them the fp32 stores of dw.  173 rows, 4096 x 1000:
 // 7.5 us, of which the first loads, one chain of steps and the stores are the most: a latency.  Long products are bound by the shared memory
 // (the decoded tile's stores and the operands' reads), then by the power limit; short ones by the stores of dw.

@@ -259,7 +259,8 @@ const SliceWalk& slice_walk(const Dims& d, int groups, int slot, int elem, bool 
     return q.walk;
 }
 // Forward passes: samples of more than 64 positions are kept by blocks where they are read in vectors of eight.  (With single channels the three launches are
-// faster or alike: 1 x 13 x 13 x 75 6.4 us against 18, 512 samples of it 23.6 both; 512 x 7 x 7 x 75 takes 13.2 against 11.3.)
+// faster or alike: 1 x 13 x 13 x 75 6.2 us against 17, 512 x 9 x 9 x 75 15.4 against 18.9, 512 x 13 x 13 x 75 24 against 22.5; 512 x 7 x 7 x 75 takes 12.9
+// against 10.7.)
 template <int V>
 const SliceWalk& forward_slices(const Dims& d, int groups, int elem) {
     static const SliceWalk none{};
@@ -267,8 +268,9 @@ const SliceWalk& forward_slices(const Dims& d, int groups, int elem) {
     return slice_walk<V>(d, groups, elem * V, elem, false);
 }
 // Backward passes: samples of more than 64 positions are kept by blocks where x is read as it is, in vectors of eight.  (From int8 codes, or with single
-// channels, the three launches are faster, SiLU: 128 x 27 x 27 x 256 60 us against 79, 512 x 13 x 13 x 384 92 against 108, 256 x 13 x 13 x 75 bf16 from x 23
-// against 37; with fewer positions they are not: 2048 x 7 x 7 x 512 154 against 139; nor from x: 512 x 27 x 27 x 256 without an activation 167 against 134.)
+// channels, the three launches are faster, SiLU: 128 x 27 x 27 x 256 61 us against 71, 512 x 13 x 13 x 384 93 against 99, 512 x 11 x 11 x 256 47 against 50,
+// 512 x 9 x 9 x 75 from x 25 against 30; with fewer positions they are not: 512 x 9 x 9 x 256 36 against 34, 2048 x 7 x 7 x 512 159 against 133; nor from x:
+// 512 x 27 x 27 x 256 without an activation 168 against 139.)
 template <int V>
 const SliceWalk& backward_slices(const Dims& d, int groups, int elem, bool kept) {
     static const SliceWalk none{};

@@ -347,3 +347,23 @@ def test_refusals_name_what_is_wrong(ops):
         with pytest.raises(A.AlexNetError, match=word) as e:
             ops.group_norm(x, **kw)
         assert e.value.code == A.ERR_ARG
+
+
+@pytest.mark.parametrize("value", [2.0 ** 75 * 1.1, -2.0 ** 70])
+@pytest.mark.parametrize("shape", [(2, 8, 8, 64), (2, 8, 8, 33), (300, 27, 27, 64), (1, 150, 150, 64)])
+def test_alike_values_of_any_size(ops, shape, value):
+    """Up to 2^76: no sum or square of what is left over passes fp32, the mean is the value and y the bias."""
+    for dtype in (torch.float32, torch.bfloat16):
+        x = torch.full(shape, value, device="cuda", dtype=dtype)
+        bias = torch.arange(shape[-1], device="cuda", dtype=torch.float32)
+        r = ops.group_norm(x, 1, None, bias)
+        assert torch.equal(r.mean, x[:, 0, 0, :1].float()) and torch.equal(r.y, bias.to(dtype).expand(shape)) and bool(r.rstd.isfinite().all() and (r.rstd > 0).all())
+
+
+def test_a_group_with_an_infinity_is_nan(ops):
+    for shape in ((2, 8, 8, 64), (2, 8, 8, 33), (2, 150, 150, 64)):
+        for at in (0, 5, -1):
+            x = torch.randn(shape, device="cuda", generator=gen(2))
+            x[1, at, at, 0] = float("-inf")
+            r = ops.group_norm(x, 1)
+            assert bool(r.mean[1].isnan().all() and r.rstd[1].isnan().all() and r.y[1].isnan().all() and r.y[0].isfinite().all())
