@@ -1,8 +1,9 @@
 """The operators on caller-owned tensors (paper_1412_2302_b200.operators) against their definitions in 64 bits.
 
 Tolerances.  An output is rounded once to its type: half a step, finfo.eps / 2 of the value (below the smallest normal number, half of a
-subnormal step).  What is in front of that is fp32: a thread sums at most 128 terms one after another (each addition off by 2^-24 of
-the running sum), everything behind is fp64, so a sum is off by at most 2^-17 of the sum of the magnitudes, a mean of deviations by 2^-17 of their
+subnormal step).  What is in front of that is fp32: a thread sums at most 192 terms one after another, a block's rows are added in chains of at
+most 64 (k alike terms are off by k 2^-25 of their sum: half a step, at most 2^-24 of the running sum, which is half the last one on average), and what is
+longer carries the errors of its additions along, so a sum is off by at most 2^-17 of the sum of the magnitudes, a mean of deviations by 2^-17 of their
 mean magnitude and a root of a mean square by 2^-17 relative (half of 2^-17 from the root, the rest from the 2^-24s around it).  `FP32`
 below is that 2^-17; it multiplies the magnitudes that an expression adds up, not its value.  Codes, exponents and decoded values are whole
 numbers of steps by definition and must be equal."""
