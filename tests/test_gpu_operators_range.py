@@ -7,6 +7,7 @@ come in four chains of at most 64 each, those of warps in chains of at most 32; 
 (2^-24 in all).  192 + 64 of 2^-25 are 2^-17, FP32 below: that times the sum of the magnitudes."""
 import subprocess
 import sys
+import threading
 
 import pytest
 import torch
@@ -367,3 +368,60 @@ def test_a_group_with_an_infinity_is_nan(ops):
             x[1, at, at, 0] = float("-inf")
             r = ops.group_norm(x, 1)
             assert bool(r.mean[1].isnan().all() and r.rstd[1].isnan().all() and r.y[1].isnan().all() and r.y[0].isfinite().all())
+
+
+@pytest.mark.parametrize("c,groups", [(72, 9), (73, 1)])
+def test_tensors_of_more_than_2_to_the_32_values(ops, c, groups):
+    """The last sample of a dense tensor of 4.8e9 values against the definition, and its codes against those of the sample alone."""
+    n, h, w = 64, 1024, 1024
+    g = gen(9)
+    x = torch.empty((n, h, w, c), dtype=torch.bfloat16, device="cuda")
+    dy = torch.empty_like(x)
+    for t in (x, dy):
+        t[:-1] = 1.0
+        t[-1] = torch.randn((h, w, c), device="cuda", generator=g).to(torch.bfloat16) + 0.5
+    r = ops.group_norm(x, groups, activation="silu", keep_input="int8")
+    alone = ops.checkpoint_encode(x[-1:], "int8")
+    assert torch.equal(r.input.codes[-1:], alone.codes) and torch.equal(r.input.scales[-1:], alone.scales)
+    v = x[-1].double().view(h * w, groups, c // groups)
+    mean = v.mean((0, 2), keepdim=True)
+    rstd = ((v - mean).square().mean((0, 2), keepdim=True) + 1e-5).rsqrt()
+    z = ((v - mean) * rstd).view(h, w, c)
+    assert bool(((r.y[-1].double() - z * torch.sigmoid(z)).abs() <= 2.0 ** -8 * z.abs() + 3 * FP32 * (z.abs() + 1)).all())
+    del v, z
+    dx, dw, db = ops.group_norm_backward(dy, r.input, r.mean, r.rstd, activation="silu")
+    one = ops.group_norm_backward(dy[-1:], alone, r.mean[-1:], r.rstd[-1:], activation="silu")
+    assert bool(((dx[-1:].float() - one[0].float()).abs() <= 2.0 ** -7 * one[0].float().abs() + 2 * FP32).all())
+    assert bool(dx[:-1].float().abs().max() < 1e-3 * 316 + 1)              # (no variance: rstd is 316 and dy alike)
+
+
+def test_threads_call_side_by_side(ops):
+    """Four threads with streams of their own, each with its own sizes: plans and messages belong to a thread."""
+    def work(i, out):
+        s = torch.cuda.Stream()
+        with torch.cuda.stream(s):
+            g = torch.Generator(device="cuda").manual_seed(i)
+            for k in range(30):
+                c = 32 * (1 + (i + k) % 5)
+                x = torch.randn((2 + i, 9, 9 + k, c), device="cuda", generator=g).to(torch.bfloat16)
+                r = ops.group_norm(x, 4, activation="silu", keep_input="int8")
+                d = ops.group_norm_backward(x, r.input, r.mean, r.rstd, activation="silu")
+                dw = ops.linear_weight_grad(x, r.input)
+                out.append((x, r, d, dw))
+                try:
+                    ops.group_norm(x, 5 + i)
+                except A.AlexNetError as e:
+                    assert f", {5 + i})" in str(e)
+        s.synchronize()
+    results = [[] for _ in range(4)]
+    threads = [threading.Thread(target=work, args=(i, results[i])) for i in range(4)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    for out in results:
+        assert len(out) == 30
+        for x, r, d, dw in out:
+            again = ops.group_norm(x, 4, activation="silu", keep_input="int8")
+            assert torch.equal(again.y, r.y) and torch.equal(again.input.codes, r.input.codes) and torch.equal(dw, ops.linear_weight_grad(x, r.input))
+            assert all(torch.equal(a, b) for a, b in zip(d, ops.group_norm_backward(x, r.input, r.mean, r.rstd, activation="silu")))
