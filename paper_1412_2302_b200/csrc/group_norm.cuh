@@ -920,116 +920,116 @@ __global__ void __launch_bounds__(kSlThreads, 2) gn_slice_backward_kernel(const 
     }
     #pragma unroll 1
     for (long long n = b.n0, out = b.n0; n < samples; out += b.step) {
-    const long long end = min(samples, n + kSlSamples * b.step);
-    #pragma unroll 1
-    for (; n < end; n += b.step) {
-        const long long gb = n * sh.groups + b.g0;              // this block's first group
-        for (int g = tid; g < w.groups; g += w.threads) m.rstd[g] = A.rstd[gb + g];
-        Chan<V> k;
-        if (has) load_backward_chan<V, ACT>(k, sh, A, n, V * cv);
-        // d and dz of the thread's position `it`
-        auto values = [&](int it, float* f, float* q) {
-            Fetch<T, V, SRC> fx;
-            fx.r = xslots[it * w.threads];
-            if constexpr (SRC != kSrcSame) fx.e = eslots[it * w.threads];
-            unpack<T, V>(slots[it * w.threads], q);
-            activation_gradient<T, V, SRC, ACT>(sh.act, k, fx, f, q);
-        };
-        float S1[V], S2[V];
-        #pragma unroll
-        for (int i = 0; i < V; ++i) S1[i] = S2[i] = 0.f;
+        const long long end = min(samples, n + kSlSamples * b.step);
         #pragma unroll 1
-        for (int bt = 0; bt < kSlBatches; ++bt) {
-            copies_wait(kSlBatches - 1 - bt);
-            const int e = min(cnt, (bt + 1) * batch);
-            #pragma unroll 1
-            for (int it = bt * batch; it < e; ++it) {
-                float f[V], q[V];
-                values(it, f, q);
-                v_add<V>(S1, q, S1);
-                v_fma<V>(f, q, S2, S2);
-            }
-        }
-        #pragma unroll
-        for (int i = 0; i < V; ++i) { m.part.at(0, i, tid) = S1[i]; m.part.at(1, i, tid) = S2[i]; }
-        __syncthreads();
-        for (uint32_t c = tid; c < (uint32_t)w.Cs; c += w.threads) {
-            const float* p = m.part.p + (c % V) * m.part.pitch + c / V;
-            float2 t = make_float2(0.f, 0.f);
-            #pragma unroll 8
-            for (int r = 0; r < w.rows; ++r, p += w.cols) { t.x += p[0]; t.y += p[V * m.part.pitch]; }
-            t.y *= m.rstd[sh.group(c)];                         // of xhat
-            m.chan[c] = t.x;
-            m.chan[w.Cs + c] = t.y;
-            m.acc[c] += t.x;
-            m.acc[w.Cs + c] += t.y;
-        }
-        __syncthreads();
-        const float per = __frcp_rn((float)sh.HW * (float)sh.cg);
-        for (int g0 = warp * (32 / w.lanes); g0 < w.groups; g0 += warps * (32 / w.lanes)) {
-            const int g = g0 + lane / w.lanes;
-            float2 t = make_float2(0.f, 0.f);
-            if (g < w.groups)
-                #pragma unroll 2
-                for (int c = g * sh.cg + lane % w.lanes; c < (g + 1) * sh.cg; c += w.lanes) {
-                    t.x = fmaf(m.weight[c], m.chan[c], t.x);
-                    t.y = fmaf(m.weight[c], m.chan[w.Cs + c], t.y);
-                }
-            t.x = lanes_sum(t.x, w.lanes);
-            t.y = lanes_sum(t.y, w.lanes);
-            if (g < w.groups && lane % w.lanes == 0) m.res[g] = make_float2(t.x * per, t.y * per);
-        }
-        __syncthreads();
-        float B[V], D[V];
-        if (has) {
+        for (; n < end; n += b.step) {
+            const long long gb = n * sh.groups + b.g0;              // this block's first group
+            for (int g = tid; g < w.groups; g += w.threads) m.rstd[g] = A.rstd[gb + g];
+            Chan<V> k;
+            if (has) load_backward_chan<V, ACT>(k, sh, A, n, V * cv);
+            // d and dz of the thread's position `it`
+            auto values = [&](int it, float* f, float* q) {
+                Fetch<T, V, SRC> fx;
+                fx.r = xslots[it * w.threads];
+                if constexpr (SRC != kSrcSame) fx.e = eslots[it * w.threads];
+                unpack<T, V>(slots[it * w.threads], q);
+                activation_gradient<T, V, SRC, ACT>(sh.act, k, fx, f, q);
+            };
+            float S1[V], S2[V];
             #pragma unroll
-            for (int i = 0; i < V; ++i) {
-                const int g = sh.group(V * v + i);
-                const float2 c = m.res[g];
-                const float r = m.rstd[g];
-                B[i] = -r * (r * c.y);
-                D[i] = -r * c.x;
-            }
-        }
-        const bool more = n + b.step < samples;
-        const long long n1 = n + b.step;
-        const T* dn = dy + n1 * gdy.sn + V * cv;
-        T* op = dx + n * gdx.sn + V * cv;
-        Cursor c(gdx, row), cdy(gdy, row);
-        SourceCursor<T, V, SRC> cx(src, gx, w, n1, row, cv);
-        uint8_t e_next = 0;                                     // the exponent of the next sample's copies, stored a position after it was asked for
-        #pragma unroll 1
-        for (int bt = 0; bt < kSlBatches; ++bt) {
-            const int e = min(cnt, (bt + 1) * batch);
+            for (int i = 0; i < V; ++i) S1[i] = S2[i] = 0.f;
             #pragma unroll 1
-            for (int it = bt * batch; it < e; ++it) {
-                float f[V], q[V];
-                values(it, f, q);
-                if (SRC != kSrcSame && more) {
-                    if (it > 0) eslots[(it - 1) * w.threads] = e_next;
-                    e_next = *cx.scales;
-                }
-                v_fma<V>(f, B, D, f);
-                v_fma<V>(q, k.a, f, q);
-                *(R*)(op + c.off) = pack<T, V>(q);
-                c.next(gdx);
-                if (more) {
-                    fill_slot(slots + it * w.threads, dn + cdy.off);
-                    cdy.next(gdy);
-                    fill_slot(xslots + it * w.threads, cx.place());
-                    cx.next(gx, w);
+            for (int bt = 0; bt < kSlBatches; ++bt) {
+                copies_wait(kSlBatches - 1 - bt);
+                const int e = min(cnt, (bt + 1) * batch);
+                #pragma unroll 1
+                for (int it = bt * batch; it < e; ++it) {
+                    float f[V], q[V];
+                    values(it, f, q);
+                    v_add<V>(S1, q, S1);
+                    v_fma<V>(f, q, S2, S2);
                 }
             }
-            copies_commit();
+            #pragma unroll
+            for (int i = 0; i < V; ++i) { m.part.at(0, i, tid) = S1[i]; m.part.at(1, i, tid) = S2[i]; }
+            __syncthreads();
+            for (uint32_t c = tid; c < (uint32_t)w.Cs; c += w.threads) {
+                const float* p = m.part.p + (c % V) * m.part.pitch + c / V;
+                float2 t = make_float2(0.f, 0.f);
+                #pragma unroll 8
+                for (int r = 0; r < w.rows; ++r, p += w.cols) { t.x += p[0]; t.y += p[V * m.part.pitch]; }
+                t.y *= m.rstd[sh.group(c)];                         // of xhat
+                m.chan[c] = t.x;
+                m.chan[w.Cs + c] = t.y;
+                m.acc[c] += t.x;
+                m.acc[w.Cs + c] += t.y;
+            }
+            __syncthreads();
+            const float per = __frcp_rn((float)sh.HW * (float)sh.cg);
+            for (int g0 = warp * (32 / w.lanes); g0 < w.groups; g0 += warps * (32 / w.lanes)) {
+                const int g = g0 + lane / w.lanes;
+                float2 t = make_float2(0.f, 0.f);
+                if (g < w.groups)
+                    #pragma unroll 2
+                    for (int c = g * sh.cg + lane % w.lanes; c < (g + 1) * sh.cg; c += w.lanes) {
+                        t.x = fmaf(m.weight[c], m.chan[c], t.x);
+                        t.y = fmaf(m.weight[c], m.chan[w.Cs + c], t.y);
+                    }
+                t.x = lanes_sum(t.x, w.lanes);
+                t.y = lanes_sum(t.y, w.lanes);
+                if (g < w.groups && lane % w.lanes == 0) m.res[g] = make_float2(t.x * per, t.y * per);
+            }
+            __syncthreads();
+            float B[V], D[V];
+            if (has) {
+                #pragma unroll
+                for (int i = 0; i < V; ++i) {
+                    const int g = sh.group(V * v + i);
+                    const float2 c = m.res[g];
+                    const float r = m.rstd[g];
+                    B[i] = -r * (r * c.y);
+                    D[i] = -r * c.x;
+                }
+            }
+            const bool more = n + b.step < samples;
+            const long long n1 = n + b.step;
+            const T* dn = dy + n1 * gdy.sn + V * cv;
+            T* op = dx + n * gdx.sn + V * cv;
+            Cursor c(gdx, row), cdy(gdy, row);
+            SourceCursor<T, V, SRC> cx(src, gx, w, n1, row, cv);
+            uint8_t e_next = 0;                                     // the exponent of the next sample's copies, stored a position after it was asked for
+            #pragma unroll 1
+            for (int bt = 0; bt < kSlBatches; ++bt) {
+                const int e = min(cnt, (bt + 1) * batch);
+                #pragma unroll 1
+                for (int it = bt * batch; it < e; ++it) {
+                    float f[V], q[V];
+                    values(it, f, q);
+                    if (SRC != kSrcSame && more) {
+                        if (it > 0) eslots[(it - 1) * w.threads] = e_next;
+                        e_next = *cx.scales;
+                    }
+                    v_fma<V>(f, B, D, f);
+                    v_fma<V>(q, k.a, f, q);
+                    *(R*)(op + c.off) = pack<T, V>(q);
+                    c.next(gdx);
+                    if (more) {
+                        fill_slot(slots + it * w.threads, dn + cdy.off);
+                        cdy.next(gdy);
+                        fill_slot(xslots + it * w.threads, cx.place());
+                        cx.next(gx, w);
+                    }
+                }
+                copies_commit();
+            }
+            if (SRC != kSrcSame && more && cnt > 0) eslots[(cnt - 1) * w.threads] = e_next;
+            __syncthreads();                                        // (the groups' rstd and results are free for the next sample)
         }
-        if (SRC != kSrcSame && more && cnt > 0) eslots[(cnt - 1) * w.threads] = e_next;
-        __syncthreads();                                        // (the groups' rstd and results are free for the next sample)
-    }
-    for (int c = tid; c < w.Cs; c += w.threads) {               // (this thread's sums)
-        if (sum1) sum1[out * sum_pitch + b.c0 + c] = m.acc[c];
-        if (sum2) sum2[out * sum_pitch + b.c0 + c] = m.acc[w.Cs + c];
-        m.acc[c] = m.acc[w.Cs + c] = 0.f;
-    }
+        for (int c = tid; c < w.Cs; c += w.threads) {               // (this thread's sums)
+            if (sum1) sum1[out * sum_pitch + b.c0 + c] = m.acc[c];
+            if (sum2) sum2[out * sum_pitch + b.c0 + c] = m.acc[w.Cs + c];
+            m.acc[c] = m.acc[w.Cs + c] = 0.f;
+        }
     }
 }
 
